@@ -133,6 +133,19 @@ int sim_family(const hx_grid* grid, const hx::ClusterK& ck, bool record, bool fo
 
 }  // namespace
 
+namespace hx {
+
+// For the library's other translation units: the message of hx_last_error.
+int report(int code, const char* msg) noexcept {
+  try {
+    g_err = msg;
+  } catch (...) {
+  }
+  return code;
+}
+
+}  // namespace hx
+
 struct hx_sim {
   int32_t n_traces = 0, n_points = 0;
   int64_t n_sims = 0, n_q = 0, n_c = 0;

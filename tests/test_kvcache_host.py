@@ -1,0 +1,158 @@
+"""The cache operators without a GPU: struct layouts, refusals before any launch,
+and the tests' own plain implementations."""
+import ctypes
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_05286_gb300 import build as B_
+from paper_2505_05286_gb300 import hxsim as H
+from paper_2505_05286_gb300 import kvcache as KV
+from tests import kv_cases as P
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+STRUCTS = (KV.hx_kv_map_args, KV.hx_kv_cache, KV.hx_kv_new, KV.hx_kv_query)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    B_.build()
+    return KV.load()
+
+
+def test_both_builds_export_what_the_header_declares(lib):
+    text = open(os.path.join(ROOT, "include", "hxkv.h")).read()
+    names = sorted(set(re.findall(r"^\s*(?:int|int64_t)\s+(hx_kv_\w+)\s*\(", text, re.M)))
+    assert names == ["hx_kv_append", "hx_kv_attend", "hx_kv_attend_workspace", "hx_kv_map", "hx_kv_max_runs"]
+    for n in names:
+        assert hasattr(lib, n) and hasattr(H.load_checked(), n)
+
+
+def test_struct_layout_matches_binding(tmp_path):
+    lines = "".join(f'printf("{s.__name__} %zu\\n", sizeof({s.__name__}));\n' + "".join(
+        f'printf("{s.__name__}.{f} %zu\\n", offsetof({s.__name__}, {f}));\n' for f, _ in s._fields_) for s in STRUCTS)
+    src = tmp_path / "probe.c"
+    src.write_text('#include <stdio.h>\n#include "hxkv.h"\nint main(void) {\n' + lines + "return 0;\n}\n")
+    exe = tmp_path / "probe"
+    subprocess.check_call(["gcc", "-std=c11", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)])
+    by = {s.__name__: s for s in STRUCTS}
+    for line in subprocess.check_output([str(exe)], text=True).splitlines():
+        name, size = line.split()
+        s, _, f = name.partition(".")
+        assert (getattr(by[s], f).offset if f else ctypes.sizeof(by[s])) == int(size), name
+
+
+def _set(struct, **kw):
+    s = type(struct)()
+    ctypes.pointer(s)[0] = struct
+    for k, v in kw.items():
+        setattr(s, k, v)
+    return s
+
+
+FAKE = 1 << 20  # an aligned address; nothing is launched with it
+
+
+def _cache(**kw):
+    return _set(KV.hx_kv_cache(FAKE, FAKE, FAKE, FAKE, 4 * 32 * 64, 4, 10, 4, 32, 64), **kw)
+
+
+def _refused(lib, rc, msg):
+    err = lib.hx_last_error().decode()
+    assert rc == H.HX_ERR_INVALID and msg in err, (rc, err)
+
+
+CACHE_BAD = [(dict(k=None), "NULL"), (dict(v_scale=None), "NULL"), (dict(n_blocks=0), "n_blocks"),
+             (dict(n_kv_heads=0), "n_kv_heads"), (dict(block_tokens=48), "block_tokens"), (dict(head_dim=96), "head_dim"),
+             (dict(k=FAKE + 8), "aligned"), (dict(k_scale=FAKE + 2), "aligned"), (dict(block_stride=4 * 32 * 64 - 16), "block_stride"),
+             (dict(block_stride=4 * 32 * 64 + 8), "block_stride"), (dict(scale_stride=3), "scale_stride")]
+
+
+def test_map_refusals(lib):
+    good = KV.hx_kv_map_args(3, 10, 32, 8, 4, 6, 4, *[FAKE] * 10, FAKE + 64)
+    for kw, msg in [(dict(n_rows=0), "n_rows"), (dict(n_rows=65537), "n_rows"), (dict(n_tokens=-1), "n_tokens"),
+                    (dict(n_tokens=2 ** 30 + 1), "n_tokens"), (dict(block_tokens=0), "block_tokens"),
+                    (dict(n_blocks=0), "n_blocks"), (dict(table_width=0), "table_width"),
+                    (dict(table_width=2 ** 23 + 1, table_stride=2 ** 24), "table_width"),
+                    (dict(table_stride=3), "table_stride"), (dict(n_runs=5), "n_runs"), (dict(held=None), "NULL"),
+                    (dict(slots=None), "NULL"), (dict(ring_state_out=FAKE), "ring_state_out"),
+                    (dict(runs=FAKE + 4), "aligned")]:
+        a = _set(good, **kw)
+        _refused(lib, lib.hx_kv_map(ctypes.byref(a), None), msg)
+    _refused(lib, lib.hx_kv_map(None, None), "NULL")
+
+
+def test_append_refusals(lib):
+    good = KV.hx_kv_new(FAKE, FAKE, 256, 64, 256, 64, 10, KV.HX_BF16, FAKE, 3)
+    for kw, msg in CACHE_BAD:
+        c = _cache(**kw)
+        _refused(lib, lib.hx_kv_append(ctypes.byref(c), ctypes.byref(good), None), msg)
+    c = _cache()
+    for kw, msg in [(dict(n_tokens=-1), "n_tokens"), (dict(n_runs=-1), "n_runs"), (dict(dtype=3), "dtype"),
+                    (dict(k=None), "NULL"), (dict(runs=None), "NULL"), (dict(v=FAKE + 2), "aligned"),
+                    (dict(k_token_stride=260), "strides"), (dict(v_head_stride=4), "strides"),
+                    (dict(dtype=KV.HX_F32, v_head_stride=2), "strides"), (dict(n_runs=2 ** 28), "n_runs")]:
+        a = _set(good, **kw)
+        _refused(lib, lib.hx_kv_append(ctypes.byref(c), ctypes.byref(a), None), msg)
+    _refused(lib, lib.hx_kv_append(None, ctypes.byref(good), None), "NULL")
+    _refused(lib, lib.hx_kv_append(ctypes.byref(c), None, None), "NULL")
+    for kw in (dict(n_tokens=0), dict(n_runs=0)):  # nothing to do
+        a = _set(good, **kw)
+        assert lib.hx_kv_append(ctypes.byref(c), ctypes.byref(a), None) == H.HX_OK
+
+
+def test_attend_refusals(lib):
+    good = KV.hx_kv_query(FAKE, FAKE, None, 512, 64, 512, 64, 10, 8, KV.HX_F16, 3, FAKE, FAKE, FAKE, 4, 4, 1, 1, 0, 0.125,
+                          FAKE, 1 << 40)
+    for kw, msg in CACHE_BAD:
+        c = _cache(**kw)
+        _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(good), None), msg)
+    c = _cache()
+    for kw, msg in [(dict(n_tokens=-1), "n_tokens"), (dict(n_rows=0), "n_rows"), (dict(n_rows=65537), "n_rows"),
+                    (dict(n_heads=6), "n_heads"), (dict(n_heads=0), "n_heads"), (dict(n_heads=4 * 129), "n_heads"),
+                    (dict(dtype=KV.HX_F32), "dtype"), (dict(max_q=-1), "max_q"), (dict(causal=2), "causal"),
+                    (dict(window=-1), "window"), (dict(sm_scale=float("nan")), "sm_scale"), (dict(q=None), "NULL"),
+                    (dict(kv_len=None), "NULL"), (dict(block_table=None), "NULL"), (dict(table_width=0), "table_width"),
+                    (dict(table_stride=3), "table_stride"), (dict(q=FAKE + 2), "aligned"), (dict(out=FAKE + 8), "aligned"),
+                    (dict(q_head_stride=4), "strides"), (dict(out_token_stride=514), "strides")]:
+        a = _set(good, **kw)
+        _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(a), None), msg)
+    need = ctypes.c_int64()
+    assert lib.hx_kv_attend_workspace(ctypes.byref(c), ctypes.byref(good), ctypes.byref(need)) == H.HX_OK
+    if need.value:
+        a = _set(good, workspace_bytes=need.value - 1)
+        _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(a), None), "workspace")
+        a = _set(good, workspace=None)
+        _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(a), None), "workspace")
+    a = _set(good, n_tokens=0)
+    assert lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(a), None) == H.HX_OK
+
+
+def test_binding_refuses_host_tensors():
+    z = torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(H.HxError) as e:
+        KV.map_step(z, z, z[None], z, z.long(), 1, 16)
+    assert e.value.code == H.HX_ERR_INVALID and "CUDA" in str(e.value)
+    f = torch.zeros((2, 1, 16, 64), dtype=torch.uint8)
+    with pytest.raises(H.HxError):
+        KV.Cache(f.view(torch.float8_e4m3fn), f.view(torch.float8_e4m3fn), torch.ones(2, 1), torch.ones(2, 1))
+
+
+def test_max_runs_agrees(lib):
+    for n, t, b in ((1, 0, 16), (1, 1, 16), (5, 3, 64), (3, 1000, 32), (65536, 1 << 30, 16)):
+        assert lib.hx_kv_max_runs(n, t, b) == KV.max_runs(n, t, b)
+
+
+def test_plain_e4m3_agrees_with_the_type():
+    bits = np.arange(256, dtype=np.uint8)
+    want = torch.from_numpy(bits).view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(P.GRID, want, equal_nan=True)
+    x = np.concatenate([np.random.default_rng(0).normal(0, 2.0 ** e, 4000) for e in range(-12, 9)])
+    mid = (P._POS[1:] + P._POS[:-1]) / 2
+    x = np.concatenate([x, mid, -mid, P._POS]).astype(np.float32)
+    t = torch.from_numpy(x).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    assert np.array_equal(P.to_e4m3(x), t)
