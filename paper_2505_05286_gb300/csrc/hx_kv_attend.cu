@@ -1,12 +1,649 @@
-// hx_kv_attend.cu -- attention of a step's tokens over the paged 8-bit cache.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
+// hx_kv_attend.cu -- attention of a step's tokens over the paged 8-bit cache:
+// requests of few rows (a row: one token and query head of a kv head's group),
+// which is every request that decodes.
+#include <algorithm>
+
 #include <cuda_fp8.h>
 
-#include "hx_kv.cuh"
+#include "hx_kv_attend.cuh"
 
 namespace hx {
 namespace {
+
+// out = softmax(c q k^T) v for up to 16 rows that share their keys: bound by
+// reading the cache once.  An item is one request and kv head; its tokens are cut
+// into tiles of kTokens, and all items' tiles, laid end to end, are dealt out to the blocks in
+// equal stretches, whatever the lengths.  One warp of a block fetches (tile copies
+// into a ring of kStages), four compute, each on its own tiles with its own running
+// maximum, sum and 16 x D sums, joined where an item ends.  An item that
+// several blocks share leaves partial results, joined by a second kernel in a fixed order, so
+// that a result never depends on the order in which blocks run.
+constexpr int kRows = 16;
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kStageBytes = 8192;
+constexpr int kTileBytes = kStageBytes / 2;
+
+template <int D>
+struct Shape {
+  static constexpr int kTokens = kTileBytes / D;   // of a tile: 32 or 64
+  static constexpr int kGroups = kTokens / 16;     // 16 tokens lie in one block of the cache
+  static constexpr int kStages = D == 128 ? 11 : 12;
+  static constexpr int kMergeBytes = 2 * kRows * D * 4;
+  static constexpr int kSmem = kStages * kStageBytes + kMergeBytes + 1024;
+};
+
+// What a tile's scales are, and which of its groups of 16 tokens were fetched.
+struct Meta {
+  float ks[4], vs[4];
+  uint32_t valid;
+};
+
+// The tiles of an item, 0: it is not this kernel's.  An item that sees nothing,
+// with any number of rows, counts as one, so that its zeros are written.
+template <int D>
+__device__ __forceinline__ int tiles_of(const AttendArgs& a, const Request& q, int* first_tile) {
+  constexpr int NT = Shape<D>::kTokens;
+  *first_tile = 0;
+  if (q.n == 0) return 0;
+  if (q.kv == 0) return 1;
+  if ((int64_t)q.n * a.group > kRows) return 0;
+  *first_tile = see_from(a, q, 0) / NT;
+  return (q.kv + NT - 1) / NT - *first_tile;
+}
+
+// A place in the sequence of all tiles.
+template <int D>
+struct Place {
+  int r, h, t, tiles, first_tile;
+  Request q;
+  __device__ void load(const AttendArgs& a) {
+    q = request(a, r);
+    tiles = tiles_of<D>(a, q, &first_tile);
+  }
+  // Steps by d tiles; false past the last request.
+  __device__ bool step(const AttendArgs& a, int d) {
+    t += d;
+    while (t >= tiles) {
+      t -= tiles;
+      if (tiles && ++h < a.n_kv_heads) continue;
+      h = 0;
+      do {
+        if (++r >= a.n_rows) return false;
+        load(a);
+      } while (!tiles);
+    }
+    return true;
+  }
+};
+
+__device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
+
+template <class T>
+__device__ __forceinline__ float2 to_float2(uint32_t u);
+template <>
+__device__ __forceinline__ float2 to_float2<__half>(uint32_t u) {
+  return __half22float2(*(const __half2*)&u);
+}
+template <>
+__device__ __forceinline__ float2 to_float2<__nv_bfloat16>(uint32_t u) {
+  return __bfloat1622float2(*(const __nv_bfloat162*)&u);
+}
+template <class T>
+__device__ __forceinline__ uint32_t from_float2(float x, float y);
+template <>
+__device__ __forceinline__ uint32_t from_float2<__half>(float x, float y) {
+  return pack_half(x, y);
+}
+template <>
+__device__ __forceinline__ uint32_t from_float2<__nv_bfloat16>(float x, float y) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *(const uint32_t*)&h;
+}
+
+// Writes zeros and -inf for `rows` rows of an item (all of them: any number).
+template <class T>
+__device__ void write_empty(const AttendArgs& a, int D, const Request& q, int h, int tid, int threads) {
+  const int64_t rows = (int64_t)q.n * a.group;
+  const int units = D / 8;
+  for (int64_t i = tid; i < rows * units; i += threads) {
+    const int64_t x = i / units;
+    const int token = q.first + (int)(x / a.group), head = h * a.group + (int)(x % a.group);
+    *(uint4*)((T*)a.out + token * a.out_token_stride + head * a.out_head_stride + (i % units) * 8) = uint4{0, 0, 0, 0};
+    if (i % units == 0 && a.lse) a.lse[(int64_t)token * a.n_heads + head] = -INFINITY;
+  }
+}
+
+// Row x of an item: its output of D / 4 contiguous values held by one thread.
+template <class T, int N>
+__device__ __forceinline__ void store_row(const AttendArgs& a, const Request& q, int h, int x, int col, const float* o,
+                                          float inv) {
+  const int token = q.first + x / a.group, head = h * a.group + x % a.group;
+  T* p = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + col;
+#pragma unroll
+  for (int i = 0; i < N; i += 8)
+    *(uint4*)(p + i) = uint4{from_float2<T>(o[i] * inv, o[i + 1] * inv), from_float2<T>(o[i + 2] * inv, o[i + 3] * inv),
+                             from_float2<T>(o[i + 4] * inv, o[i + 5] * inv), from_float2<T>(o[i + 6] * inv, o[i + 7] * inv)};
+}
+
+template <int D>
+__device__ void produce(const AttendArgs& a, const CUtensorMap* km, const CUtensorMap* vm, Place<D> at, int count,
+                        int skip, uint8_t* ring, Meta* meta, uint64_t* full, uint64_t* empty, volatile int* dead) {
+  using S = Shape<D>;
+  const int lane = threadIdx.x & 31;
+  const int block = 1 << a.block_shift;
+  const int box = min(block, S::kTokens), pieces = S::kTokens / box;
+  int stage = 0;
+  uint32_t phase = 1;
+  bool more = at.step(a, skip + lane);
+  for (int base = 0; base < count; base += 32) {
+    // each lane looks up one of the next 32 tiles
+    int id[4];
+    Meta m = {};
+    bool tile = more && base + lane < count && at.q.kv > 0;
+    uint32_t bytes = 0;
+    int y = 0;
+    if (tile) {
+      const int pos = (at.first_tile + at.t) * S::kTokens;
+      const int32_t* row = a.block_table + at.r * a.table_stride + (pos >> a.block_shift);
+      y = at.h * block + (pos & (block - 1));
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        id[p] = -1;
+        if (p < pieces && pos + p * box < at.q.kv) id[p] = row[p];
+      }
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        if (p >= pieces) break;
+        float ks = 0.f, vs = 0.f;
+        if ((unsigned)id[p] < (unsigned)a.n_blocks) {
+          ks = a.k_scale[id[p] * a.scale_stride + at.h];
+          vs = a.v_scale[id[p] * a.scale_stride + at.h];
+          bytes += 2 * box * D;
+        } else {
+          id[p] = -1;
+        }
+#pragma unroll
+        for (int g = 0; g < S::kGroups; ++g)
+          if (g * 16 / box == p) {
+            m.ks[g] = ks, m.vs[g] = vs;
+            if (id[p] >= 0) m.valid |= 1u << g;
+          }
+      }
+    }
+    for (int j = 0; j < 32 && base + j < count; ++j) {
+      if (!__shfl_sync(~0u, tile, j)) continue;
+      if (!__all_sync(~0u, bar_wait(&empty[stage], phase, dead))) return;
+      if (lane == j) {
+        uint8_t* dst = ring + stage * kStageBytes;
+        meta[stage] = m;
+        bar_expect(&full[stage], bytes);
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+          if (p < pieces && id[p] >= 0) {
+            tile_load(dst + p * box * D, km, &full[stage], 0, y, id[p]);
+            tile_load(dst + kTileBytes + p * box * D, vm, &full[stage], 0, y, id[p]);
+          }
+      }
+      __syncwarp();
+      if (++stage == S::kStages) stage = 0, phase ^= 1;
+    }
+    if (more) more = at.step(a, 32);
+  }
+}
+
+// Where the four threads of a row find their values in a tile.  Rows of D
+// bytes lie in shared memory with their 16-byte units permuted by the tile copy
+// (by the row's low bits); column n of a matrix instruction is token order(n) of eight, so that
+// both the keys' 16-byte reads and the values' fall on different banks.
+template <int D>
+__device__ __forceinline__ int order(int n) {
+  return ((D == 128 ? 0x37156240u : 0x67542310u) >> (4 * n)) & 7;
+}
+
+template <int D, class T>
+__device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, const uint8_t* ring, const Meta* meta,
+                        uint64_t* full, uint64_t* empty, volatile int* dead, float* merge, float (*s_ml)[kRows][2]) {
+  using S = Shape<D>;
+  constexpr int NT = S::kTokens, KJ = D / 64, ND = D / 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q4 = lane & 3;
+  const int tn = order<D>(n), ta = order<D>(2 * q4), tb = order<D>(2 * q4 + 1);
+  // the four values rows' and the key row's permutation of 16-byte units
+  const int swk = D == 128 ? tn : (tn >> 1) & 3;
+  const int swa = D == 128 ? ta : (ta >> 1) & 3, swb = D == 128 ? tb : (tb >> 1) & 3;
+
+  int it = 0;  // tiles fetched so far, over all items
+  bool more = at.step(a, skip);
+  while (more && count > 0) {
+    const int seg = min(count, at.tiles - at.t);
+    const Request q = at.q;
+    const int rows = q.n * a.group;
+    if (q.kv == 0) {
+      write_empty<T>(a, D, q, at.h, threadIdx.x, 32 * kWarps);
+      count -= seg;
+      more = at.step(a, seg);
+      continue;
+    }
+
+    // rows n and n + 8: what they see, and their q in f16, scaled by a power of two so
+    // that no value leaves f16's range
+    int lo[2], hi[2];
+    float c[2];
+    uint32_t aq[KJ * 4][4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int row = n + 8 * x, token = row / a.group;
+      const bool real = row < rows;
+      lo[x] = real ? see_from(a, q, token) : 0;
+      hi[x] = real ? see_to(a, q, token) : 0;
+      const T* p = (const T*)a.q + (q.first + token) * a.q_token_stride + (at.h * a.group + row % a.group) * a.q_head_stride;
+      uint4 raw[KJ][2];
+#pragma unroll
+      for (int j = 0; j < KJ; ++j)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          raw[j][u] = real ? *(const uint4*)(p + 16 * (q4 + 4 * j) + 8 * u) : uint4{0, 0, 0, 0};
+      float amax = 0;
+#pragma unroll
+      for (int j = 0; j < KJ; ++j)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float2 f = to_float2<T>(((const uint32_t*)raw[j])[u]);
+          amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+        }
+      amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
+      int e = 0;
+      if (sizeof(T) == 2 && !(amax == 0) && amax < INFINITY) e = max((int)(__float_as_uint(amax) >> 23) - 127, -126);
+      const float down = __uint_as_float((unsigned)(127 - e) << 23);
+      c[x] = a.sm_scale_log2 * __uint_as_float((unsigned)(127 + e) << 23);
+#pragma unroll
+      for (int j = 0; j < KJ; ++j)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float2 f = to_float2<T>(((const uint32_t*)raw[j])[u]);
+          aq[4 * j + (u >> 1)][x + 2 * (u & 1)] = pack_half(f.x * down, f.y * down);
+        }
+    }
+    // where every row sees everything: [all_lo, all_hi); where any sees something: [any_lo, any_hi)
+    const int any_lo = see_from(a, q, 0), any_hi = q.kv;
+    const int all_lo = see_from(a, q, q.n - 1), all_hi = see_to(a, q, 0);
+
+    float acc[ND][4];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0, 0};
+    // sums are kept in units of the values' scale, so that scales far apart lose nothing in 16 bits
+    float unit = 1.f, unit_top = 0.f;
+
+    for (int i = (warp - it) & (kWarps - 1); i < seg; i += kWarps) {
+      const int stage = (it + i) % S::kStages;
+      const uint32_t phase = ((it + i) / S::kStages) & 1;
+      if (!bar_wait(&full[stage], phase, dead)) l[0] = l[1] = NAN;
+      const uint8_t* kt = ring + stage * kStageBytes;
+      const uint8_t* vt = kt + kTileBytes;
+      const Meta& mt = meta[stage];
+      const int pos = (at.first_tile + at.t + i) * NT;
+      const uint32_t valid = mt.valid;
+      const bool whole = valid == (1u << S::kGroups) - 1 && pos >= all_lo && pos + NT <= all_hi;
+
+      float s[NT / 8][4];
+#pragma unroll
+      for (int half = 0; half < NT / 32; ++half) {
+#pragma unroll
+        for (int x = 4 * half; x < 4 * half + 4; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0;
+#pragma unroll
+        for (int j = 0; j < KJ; ++j) {
+          uint4 kw[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            kw[x] = *(const uint4*)(kt + (tn + 8 * (4 * half + x)) * D + (((q4 + 4 * j) ^ swk) << 4));
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t u = ((const uint32_t*)&kw[x])[w];
+              mma16816(s[4 * half + x], aq[4 * j + w], cvt2(u), cvt2_hi(u));
+            }
+        }
+      }
+      float top[2] = {m[0], m[1]};
+#pragma unroll
+      for (int x = 0; x < NT / 8; ++x) {
+        const float ks = mt.ks[x >> 1];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          s[x][y] *= ks * c[y >> 1];
+          if (!whole) {
+            const int p = pos + 8 * x + (y & 1 ? tb : ta);
+            if (p < lo[y >> 1] || p >= hi[y >> 1] || !(valid >> (x >> 1) & 1)) s[x][y] = -INFINITY;
+          }
+          top[y >> 1] = fmaxf(top[y >> 1], s[x][y]);
+        }
+      }
+      float keep[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
+        top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
+        const float base = top[x] == -INFINITY ? 0.f : top[x];
+        keep[x] = ex2(m[x] - base);
+        m[x] = top[x];
+        top[x] = base;
+        l[x] *= keep[x];
+      }
+#pragma unroll
+      for (int x = 0; x < NT / 8; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          s[x][y] = ex2(s[x][y] - top[y >> 1]);
+          l[y >> 1] += s[x][y];
+        }
+
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g) {
+        // the unit follows the values' scale, at most 2^60 below the largest so far
+        const float vs = valid >> g & 1 ? mt.vs[g] : unit;
+        unit_top = fmaxf(unit_top, vs);
+        const float next = fmaxf(fmaxf(vs, unit_top * 0x1p-60f), 0x1p-110f);
+        const float to = unit / next, pf = vs / next;
+        unit = next;
+        float f0 = to, f1 = to;
+        if (g == 0) f0 *= keep[0], f1 *= keep[1];
+        if (__any_sync(~0u, f0 != 1.f || f1 != 1.f)) {
+#pragma unroll
+          for (int d = 0; d < ND; ++d) acc[d][0] *= f0, acc[d][1] *= f0, acc[d][2] *= f1, acc[d][3] *= f1;
+        }
+        if (pf != 1.f) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) s[2 * g][y] *= pf, s[2 * g + 1][y] *= pf;
+        }
+        uint32_t ap[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float* p = s[2 * g + (y >> 1)] + 2 * (y & 1);
+          ap[y] = pack_half(p[0], p[1]);
+        }
+        // values of tokens ta, tb, ta + 8, tb + 8 of the group, D / 8 columns each
+        uint32_t vw[4][ND / 4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const uint8_t* p = vt + (16 * g + 8 * (y >> 1) + (y & 1 ? tb : ta)) * D;
+          const int sw = y & 1 ? swb : swa;
+          if constexpr (D == 128) {
+            *(uint4*)vw[y] = *(const uint4*)(p + ((n ^ sw) << 4));
+          } else {
+            *(uint2*)vw[y] = *(const uint2*)(p + (((n >> 1) ^ sw) << 4) + ((n & 1) << 3));
+          }
+        }
+        bool nan = false;
+        if (!whole) {
+          // a masked position's values must not count, not even as 0 * NaN
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int p = pos + 16 * g + 8 * (y >> 1) + (y & 1 ? tb : ta);
+            const bool in = p >= any_lo && p < any_hi && (valid >> g & 1);
+#pragma unroll
+            for (int w = 0; w < ND / 4; ++w) {
+              if (!in) vw[y][w] = 0;
+              nan |= (((vw[y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            }
+          }
+          nan = __any_sync(~0u, nan);
+        }
+        if (nan) {
+          // rows that do not see a NaN must not get it: count what each row sees of them, then take them out
+          uint32_t as[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int p = pos + 16 * g + 8 * (y >> 1);
+            const bool s0 = p + ta >= lo[y & 1] && p + ta < hi[y & 1], s1 = p + tb >= lo[y & 1] && p + tb < hi[y & 1];
+            as[y] = (s0 ? 0x3c00u : 0) | (s1 ? 0x3c000000u : 0);
+          }
+#pragma unroll
+          for (int w = 0; w < ND / 4; ++w) {
+            uint32_t f[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              f[y] = (((vw[y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+              vw[y][w] &= ~(f[y] * 0xffu);
+              f[y] *= 0x38u;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t b0 = __byte_perm(f[0], f[1], e < 2 ? 0x5140 : 0x7362);
+              const uint32_t b1 = __byte_perm(f[2], f[3], e < 2 ? 0x5140 : 0x7362);
+              float seen[4] = {0, 0, 0, 0};
+              mma16816(seen, as, e & 1 ? cvt2_hi(b0) : cvt2(b0), e & 1 ? cvt2_hi(b1) : cvt2(b1));
+#pragma unroll
+              for (int y = 0; y < 4; ++y)
+                if (seen[y] > 0) acc[4 * w + e][y] = NAN;
+            }
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < ND / 4; ++w) {
+          const uint32_t a01 = __byte_perm(vw[0][w], vw[1][w], 0x5140), a23 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
+          const uint32_t b01 = __byte_perm(vw[2][w], vw[3][w], 0x5140), b23 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
+          mma16816(acc[4 * w], ap, cvt2(a01), cvt2(b01));
+          mma16816(acc[4 * w + 1], ap, cvt2_hi(a01), cvt2_hi(b01));
+          mma16816(acc[4 * w + 2], ap, cvt2(a23), cvt2(b23));
+          mma16816(acc[4 * w + 3], ap, cvt2_hi(a23), cvt2_hi(b23));
+        }
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(&empty[stage]);
+    }
+
+    // the four warps' results as one, in warp 0
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      l[x] += __shfl_xor_sync(~0u, l[x], 1);
+      l[x] += __shfl_xor_sync(~0u, l[x], 2);
+      if (q4 == 0) s_ml[warp][n + 8 * x][0] = m[x], s_ml[warp][n + 8 * x][1] = l[x];
+    }
+    sync_consumers();
+    float mt[2], lt[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      mt[x] = -INFINITY, lt[x] = 0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) mt[x] = fmaxf(mt[x], s_ml[w][n + 8 * x][0]);
+      const float base = mt[x] == -INFINITY ? 0.f : mt[x];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) lt[x] += s_ml[w][n + 8 * x][1] * ex2(s_ml[w][n + 8 * x][0] - base);
+      const float f = ex2(m[x] - base) * unit;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc[d][2 * x] *= f, acc[d][2 * x + 1] *= f;
+    }
+    float4* buf = (float4*)merge + (warp & 1) * (ND * 32) + lane;
+    if (warp >= 2) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) buf[d * 32] = *(float4*)acc[d];
+    }
+    sync_consumers();
+    if (warp < 2) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const float4 o = buf[d * 32];
+        acc[d][0] += o.x, acc[d][1] += o.y, acc[d][2] += o.z, acc[d][3] += o.w;
+      }
+      if (warp == 1) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) buf[d * 32] = *(float4*)acc[d];
+      }
+    }
+    sync_consumers();
+    if (warp == 0) {
+      buf += ND * 32;
+      const bool done = seg == at.tiles;
+      const int slot = 2 * blockIdx.x + (at.t == 0);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const float4 o = buf[d * 32];
+        acc[d][0] += o.x, acc[d][1] += o.y, acc[d][2] += o.z, acc[d][3] += o.w;
+      }
+      // this thread's columns: c0 of the ND column tiles are D / 8 values in a row, c1 the next D / 8
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int row = n + 8 * x;
+        if (row >= rows) continue;
+        float o[D / 4];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] = acc[d][2 * x], o[ND + d] = acc[d][2 * x + 1];
+        const int col = q4 * (D / 4);
+        if (done) {
+          const bool none = lt[x] == 0;
+          store_row<T, D / 4>(a, q, at.h, row, col, o, none ? 0.f : 1.f / lt[x]);
+          if (q4 == 0 && a.lse)
+            a.lse[(int64_t)(q.first + row / a.group) * a.n_heads + at.h * a.group + row % a.group] =
+                none ? -INFINITY : (mt[x] + log2f(lt[x])) * 0.6931471805599453f;
+        } else {
+          float* p = a.part + ((int64_t)slot * kRows + row) * D + col;
+#pragma unroll
+          for (int d = 0; d < D / 4; d += 4) *(float4*)(p + d) = *(float4*)(o + d);
+          if (q4 == 0) *(float2*)(a.part_ml + ((int64_t)slot * kRows + row) * 2) = float2{mt[x], lt[x]};
+        }
+      }
+    }
+    it += seg;
+    count -= seg;
+    more = at.step(a, seg);
+  }
+}
+
+template <int D, class T>
+__global__ void __launch_bounds__(kThreads, 2)
+    hx_kv_attend_rows(const __grid_constant__ CUtensorMap km, const __grid_constant__ CUtensorMap vm,
+                      const __grid_constant__ AttendArgs a) {
+  using S = Shape<D>;
+  extern __shared__ uint8_t s_raw[];
+  __shared__ uint64_t s_full[S::kStages], s_empty[S::kStages];
+  __shared__ Meta s_meta[S::kStages];
+  __shared__ float s_ml[kWarps][kRows][2];
+  __shared__ long long s_sum[kThreads / 32], s_skip;
+  __shared__ int s_row, s_dead;
+  uint8_t* ring = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+  float* merge = (float*)(ring + S::kStages * kStageBytes);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("griddepcontrol.launch_dependents;");
+
+  if (tid == 0) {
+    for (int i = 0; i < S::kStages; ++i) bar_init(&s_full[i], 1), bar_init(&s_empty[i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    s_dead = 0;
+    s_row = -1;
+  }
+
+  // how many tiles there are before each thread's rows, and in all
+  const int per = (a.n_rows + kThreads - 1) / kThreads;
+  const int r0 = min(a.n_rows, tid * per), r1 = min(a.n_rows, r0 + per);
+  long long mine = 0;
+  int ft;
+  for (int r = r0; r < r1; ++r) mine += (long long)tiles_of<D>(a, request(a, r), &ft) * a.n_kv_heads;
+  long long upto = mine;
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long o = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 31) s_sum[warp] = upto;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += s_sum[w];
+    total += s_sum[w];
+  }
+  before += upto - mine;
+  // this block's stretch of the tiles: none of the first G is empty
+  const long long G = max(1LL, min((long long)gridDim.x, total)), b = blockIdx.x;
+  const long long n0 = b < G ? total * b / G : 0, n1 = b < G ? total * (b + 1) / G : 0;
+  if (n0 < n1 && before <= n0 && n0 < before + mine) {
+    int r = r0;
+    for (;; ++r) {
+      const long long x = (long long)tiles_of<D>(a, request(a, r), &ft) * a.n_kv_heads;
+      if (n0 < before + x) break;
+      before += x;
+    }
+    s_row = r;
+    s_skip = n0 - before;
+  }
+  __syncthreads();
+
+  // tokens that no row owns
+  const int owned = min(max(a.row_start[a.n_rows], 0), a.n_tokens);
+  for (int t = owned + blockIdx.x; t < a.n_tokens; t += gridDim.x) {
+    const Request q = {t, 1, 0};
+    for (int h = 0; h < a.n_kv_heads; ++h) write_empty<T>(a, D, q, h, tid, kThreads);
+  }
+
+  Place<D> at;
+  const int count = (int)(n1 - n0);
+  int skip = 0;
+  if (s_row >= 0) {
+    at.r = s_row;
+    at.load(a);
+    at.h = (int)(s_skip / at.tiles);
+    at.t = 0;
+    skip = (int)(s_skip % at.tiles);
+  }
+  if (tid == 0) {
+    // an item that began in an earlier block and ends in this one is joined here
+    int4 join = {0, 0, -1, 0};
+    if (s_row >= 0 && skip > 0 && skip + (long long)count >= at.tiles) {
+      const long long f0 = n0 - skip;
+      long long c = f0 * G / total;
+      while (total * (c + 1) / G <= f0) ++c;
+      while (total * c / G > f0) --c;
+      join = int4{at.r, at.h, (int)c, 0};
+    }
+    a.joins[b] = join;
+  }
+  if (s_row < 0) return;
+  if (warp == kWarps)
+    produce<D>(a, &km, &vm, at, count, skip, ring, s_meta, s_full, s_empty, &s_dead);
+  else
+    consume<D, T>(a, at, count, skip, ring, s_meta, s_full, s_empty, &s_dead, merge, s_ml);
+  drain(&s_dead);
+}
+
+// Joins an item's partial results: block e those of the item that ends in stretch e.
+template <int D, class T>
+__global__ void __launch_bounds__(256) hx_kv_attend_join(const __grid_constant__ AttendArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int4 join = a.joins[blockIdx.x];
+  if (join.z < 0) return;
+  const Request q = request(a, join.x);
+  const int parts = blockIdx.x - join.z + 1;
+  const int x0 = threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4;
+  for (int row = x0; row < q.n * a.group; row += 256 / (D / 4)) {
+    float m = -INFINITY;
+    for (int i = 0; i < parts; ++i) {
+      const int64_t slot = 2 * (int64_t)(join.z + i) + (i == 0);
+      m = fmaxf(m, a.part_ml[(slot * kRows + row) * 2]);
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0;
+    float4 o = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) {
+      const int64_t slot = 2 * (int64_t)(join.z + i) + (i == 0);
+      const float2 ml = *(const float2*)(a.part_ml + (slot * kRows + row) * 2);
+      const float4 p = *(const float4*)(a.part + (slot * kRows + row) * D + col);
+      const float f = ex2(ml.x - base);
+      l += ml.y * f;
+      o.x += p.x * f, o.y += p.y * f, o.z += p.z * f, o.w += p.w * f;
+    }
+    const float inv = l == 0 ? 0.f : 1.f / l;
+    const int token = q.first + row / a.group, head = join.y * a.group + row % a.group;
+    T* to = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + col;
+    *(uint2*)to = uint2{from_float2<T>(o.x * inv, o.y * inv), from_float2<T>(o.z * inv, o.w * inv)};
+    if (col == 0 && a.lse)
+      a.lse[(int64_t)token * a.n_heads + head] = l == 0 ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  }
+}
+
+// ------------------------------------------------- many rows, simplest form
 
 constexpr int kTile = 128;
 
@@ -48,6 +685,7 @@ __global__ void __launch_bounds__(kTile) hx_kv_attend_kernel(const hx_kv_cache c
   const int p = kv - n + (t - first);
   int j1 = a.causal ? min(kv, p + 1) : kv, j0 = a.window ? max(0, p - a.window + 1) : 0;
   if (a.max_q && n > a.max_q) j1 = 0;
+  if ((int64_t)n * (a.n_heads / c.n_kv_heads) <= kRows) return;
 
   const T* q = (const T*)a.q + t * a.q_token_stride + hq * a.q_head_stride;
   if (tid < D) s_q[tid] = (float)q[tid];
@@ -92,13 +730,117 @@ __global__ void __launch_bounds__(kTile) hx_kv_attend_kernel(const hx_kv_cache c
 
 }  // namespace
 
-int64_t kv_attend_workspace(const hx_kv_cache&, const hx_kv_query&) { return 0; }
+namespace {
 
-cudaError_t launch_kv_attend(const hx_kv_cache& c, const hx_kv_query& a, cudaStream_t s) {
-  const int64_t grid = (int64_t)a.n_tokens * a.n_heads;
+int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 152;
+  return sms;
+}
+
+// Two blocks fill an SM's shared memory.
+int row_blocks() { return 2 * sm_count(); }
+
+struct Work {
+  int64_t part, ml, joins, bytes;
+};
+
+Work workspace(int head_dim, int blocks) {
+  Work w;
+  w.part = 0;
+  w.ml = w.part + 2 * (int64_t)blocks * kRows * head_dim * 4;
+  w.joins = w.ml + 2 * (int64_t)blocks * kRows * 8;
+  w.bytes = w.joins + (int64_t)blocks * 16;
+  return w;
+}
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+Encode encoder() {
+  static const Encode f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return (Encode)p;
+  }();
+  return f;
+}
+
+// k or v as [blocks][heads * block_tokens][head_dim] bytes, fetched `rows` tokens at a time.
+bool tile_map(CUtensorMap* m, const void* base, const hx_kv_cache& c, int rows) {
+  const Encode f = encoder();
+  if (!f) return false;
+  const cuuint64_t dim[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.n_kv_heads * c.block_tokens, (cuuint64_t)c.n_blocks};
+  const cuuint64_t stride[2] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.block_stride};
+  const cuuint32_t box[3] = {(cuuint32_t)c.head_dim, (cuuint32_t)rows, 1}, one[3] = {1, 1, 1};
+  return f(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, (void*)base, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+           c.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+AttendArgs args_of(const hx_kv_cache& c, const hx_kv_query& q) {
+  AttendArgs a = {};
+  a.k = (const uint8_t*)c.k, a.v = (const uint8_t*)c.v, a.k_scale = c.k_scale, a.v_scale = c.v_scale;
+  a.block_stride = c.block_stride, a.scale_stride = c.scale_stride;
+  a.q = q.q, a.out = q.out, a.lse = q.lse;
+  a.q_token_stride = q.q_token_stride, a.q_head_stride = q.q_head_stride;
+  a.out_token_stride = q.out_token_stride, a.out_head_stride = q.out_head_stride;
+  a.row_start = q.row_start, a.kv_len = q.kv_len, a.block_table = q.block_table, a.table_stride = q.table_stride;
+  a.table_width = q.table_width, a.n_blocks = c.n_blocks, a.n_tokens = q.n_tokens, a.n_rows = q.n_rows;
+  a.n_heads = q.n_heads, a.n_kv_heads = c.n_kv_heads, a.group = q.n_heads / c.n_kv_heads;
+  while ((1 << a.block_shift) < c.block_tokens) ++a.block_shift;
+  a.max_q = q.max_q, a.causal = q.causal;
+  a.window = q.window >= (1 << 30) ? 0 : q.window;  // no request holds so many tokens
+  a.sm_scale_log2 = q.sm_scale * kLog2e;
+  return a;
+}
+
+template <int D, class T>
+cudaError_t launch_rows(const hx_kv_cache& c, const AttendArgs& a, cudaStream_t s) {
+  CUtensorMap km, vm;
+  const int box = std::min(c.block_tokens, Shape<D>::kTokens);
+  if (!tile_map(&km, c.k, c, box) || !tile_map(&vm, c.v, c, box)) return cudaErrorInvalidValue;
+  const auto kernel = hx_kv_attend_rows<D, T>;
+  if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem)) return e;
+  const int blocks = row_blocks();
+  kernel<<<blocks, kThreads, Shape<D>::kSmem, s>>>(km, vm, a);
+  if (cudaError_t e = cudaGetLastError()) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = blocks;
+  cfg.blockDim = 256;
+  cfg.stream = s;
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, hx_kv_attend_join<D, T>, a);
+}
+
+}  // namespace
+
+int64_t kv_attend_workspace(const hx_kv_cache& c, const hx_kv_query&) { return workspace(c.head_dim, row_blocks()).bytes; }
+
+cudaError_t launch_kv_attend(const hx_kv_cache& c, const hx_kv_query& q, cudaStream_t s) {
+  AttendArgs a = args_of(c, q);
+  const Work w = workspace(c.head_dim, row_blocks());
+  a.part = (float*)((uint8_t*)q.workspace + w.part);
+  a.part_ml = (float*)((uint8_t*)q.workspace + w.ml);
+  a.joins = (int4*)((uint8_t*)q.workspace + w.joins);
+  const bool bf = q.dtype == HX_BF16;
+  cudaError_t e;
+  if (c.head_dim == 128) e = bf ? launch_rows<128, __nv_bfloat16>(c, a, s) : launch_rows<128, __half>(c, a, s);
+  else e = bf ? launch_rows<64, __nv_bfloat16>(c, a, s) : launch_rows<64, __half>(c, a, s);
+  if (e || (q.max_q && (int64_t)q.max_q * a.group <= kRows)) return e;
+  const int64_t grid = (int64_t)q.n_tokens * q.n_heads;
   if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-  if (a.dtype == HX_BF16) hx_kv_attend_kernel<__nv_bfloat16><<<(unsigned)grid, kTile, 0, s>>>(c, a);
-  else hx_kv_attend_kernel<__half><<<(unsigned)grid, kTile, 0, s>>>(c, a);
+  if (bf) hx_kv_attend_kernel<__nv_bfloat16><<<(unsigned)grid, kTile, 0, s>>>(c, q);
+  else hx_kv_attend_kernel<__half><<<(unsigned)grid, kTile, 0, s>>>(c, q);
   return cudaGetLastError();
 }
 

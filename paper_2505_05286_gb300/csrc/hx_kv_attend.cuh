@@ -1,0 +1,140 @@
+// hx_kv_attend.cuh -- device helpers of the attention kernels: barriers and tile
+// copies with bounded waits, e4m3 to f16, the rows of a request.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "hx_kv.cuh"
+
+namespace hx {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// What the kernels read of hx_kv_cache and hx_kv_query.
+struct AttendArgs {
+  const uint8_t* k;
+  const uint8_t* v;
+  const float* k_scale;
+  const float* v_scale;
+  int64_t block_stride, scale_stride;
+  const void* q;
+  void* out;
+  float* lse;
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+  const int32_t* row_start;
+  const int32_t* kv_len;
+  const int32_t* block_table;
+  int64_t table_stride;
+  int32_t table_width, n_blocks, n_tokens, n_rows, n_heads, n_kv_heads, group;
+  int32_t block_shift, max_q, causal, window;
+  float sm_scale_log2;  // sm_scale * log2(e): scores are exponents of two
+  float* part;          // partial results of items that several blocks share
+  float* part_ml;
+  int4* joins;          // [blocks]
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bar_init(uint64_t* b, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(smem_addr(b)), "r"(parity)
+      : "memory");
+  return ok;
+}
+// Waits for a phase, but not for ever: after kWaitCycles (about two seconds) it gives up, says
+// so in *dead, and from then on no wait of the block waits.
+constexpr long long kWaitCycles = 4000000000LL;
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead) {
+  if (bar_try(b, parity)) return true;
+  const long long t0 = clock64();
+  do {
+    for (int i = 0; i < 32; ++i)
+      if (bar_try(b, parity)) return true;
+  } while (!*dead && clock64() - t0 < kWaitCycles);
+  *dead = 1;
+  return false;
+}
+// Before a block that gave up ends: time for its own copies in flight to land.
+__device__ __forceinline__ void drain(volatile int* dead) {
+  if (!*dead) return;
+  const long long t0 = clock64();
+  while (clock64() - t0 < 20000000LL) __nanosleep(1000);
+}
+
+__device__ __forceinline__ void tile_load(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+          smem_addr(dst)),
+      "l"(map), "r"(smem_addr(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Two e4m3 bytes to two f16 (exact).
+__device__ __forceinline__ uint32_t cvt2(uint32_t two) {
+  uint32_t h;
+  asm("{\n.reg .b16 l;\ncvt.u16.u32 l, %1;\ncvt.rn.f16x2.e4m3x2 %0, l;\n}\n" : "=r"(h) : "r"(two));
+  return h;
+}
+__device__ __forceinline__ uint32_t cvt2_hi(uint32_t four) {
+  uint32_t h;
+  asm("{\n.reg .b16 l, u;\nmov.b32 {l, u}, %1;\ncvt.rn.f16x2.e4m3x2 %0, u;\n}\n" : "=r"(h) : "r"(four));
+  return h;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(hi), "f"(lo));
+  return h;
+}
+
+// d += a b, 16 x 8 x 16, f16 with 32-bit sums.
+__device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// One request's part in the step, its lengths brought into range.
+struct Request {
+  int first, n, kv;  // its first token, its tokens in the step, the tokens it holds
+};
+__device__ __forceinline__ Request request(const AttendArgs& a, int r) {
+  Request q;
+  q.first = min(max(a.row_start[r], 0), a.n_tokens);
+  q.n = min(max(a.row_start[r + 1], q.first), a.n_tokens) - q.first;
+  const int64_t room = (int64_t)a.table_width << a.block_shift;
+  q.kv = (int)min((int64_t)max(a.kv_len[r], 0), room);
+  if (a.max_q && q.n > a.max_q) q.kv = 0;
+  return q;
+}
+
+// [lo, hi) of token i of a request.
+__device__ __forceinline__ int see_from(const AttendArgs& a, const Request& q, int i) {
+  return a.window ? max(0, q.kv - q.n + i - a.window + 1) : 0;
+}
+__device__ __forceinline__ int see_to(const AttendArgs& a, const Request& q, int i) {
+  return a.causal ? min(q.kv, max(0, q.kv - q.n + i + 1)) : q.kv;
+}
+
+}  // namespace hx
