@@ -10,26 +10,32 @@
 namespace hx {
 namespace {
 
-// out = softmax(c q k^T) v for up to 16 rows that share their keys: bound by
+// out = softmax(c q k^T) v for up to 8 or 16 rows that share their keys: bound by
 // reading the cache once.  An item is one request and kv head; its tokens are cut
 // into tiles of kTokens, and all items' tiles, laid end to end, are dealt out to the blocks in
 // equal stretches, whatever the lengths.  One warp of a block fetches (tile copies
-// into a ring of kStages), four compute, each on its own tiles with its own running
-// maximum, sum and 16 x D sums, joined where an item ends.  An item that
+// into a ring of kStages), the others compute, each on its own tiles with its own running
+// maximum, sum and rows x D sums, joined where an item ends.  An item that
 // several blocks share leaves partial results, joined by a second kernel in a fixed order, so
 // that a result never depends on the order in which blocks run.
-constexpr int kRows = 16;
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * (kWarps + 1);
+//
+// Tokens are the matrix instructions' 16 rows and the few rows their 8 columns:
+// S^T = K Q^T, O^T = V^T P^T.  So eight rows waste nothing (16 x 8 x 16 the other way round would
+// compute 16), and the sums take half the registers, which lets 14 computing warps reside on an SM.
+constexpr int kRows = 16;  // most rows of an item
 constexpr int kStageBytes = 8192;
 constexpr int kTileBytes = kStageBytes / 2;
 
-template <int D>
+// D: head dim, NR: rows in eights.
+template <int D, int NR>
 struct Shape {
-  static constexpr int kTokens = kTileBytes / D;   // of a tile: 32 or 64
-  static constexpr int kGroups = kTokens / 16;     // 16 tokens lie in one block of the cache
-  static constexpr int kStages = D == 128 ? 11 : 12;
-  static constexpr int kMergeBytes = 2 * kRows * D * 4;
+  static constexpr int kTokens = kTileBytes / D;  // of a tile: 32 or 64
+  static constexpr int kGroups = kTokens / 16;    // 16 tokens lie in one block of the cache
+  static constexpr int kWarps = NR * D <= 128 ? 7 : 5;  // computing warps, by the registers of their sums
+  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr int kMergeRow = D + 4;         // floats; padded against bank conflicts
+  static constexpr int kMergeBytes = 4 * 8 * NR * kMergeRow * 4;
+  static constexpr int kStages = (110 * 1024 - kMergeBytes) / kStageBytes;
   static constexpr int kSmem = kStages * kStageBytes + kMergeBytes + 1024;
 };
 
@@ -43,11 +49,11 @@ struct Meta {
 // with any number of rows, counts as one, so that its zeros are written.
 template <int D>
 __device__ __forceinline__ int tiles_of(const AttendArgs& a, const Request& q, int* first_tile) {
-  constexpr int NT = Shape<D>::kTokens;
+  constexpr int NT = kTileBytes / D;
   *first_tile = 0;
   if (q.n == 0) return 0;
   if (q.kv == 0) return 1;
-  if ((int64_t)q.n * a.group > kRows) return 0;
+  if ((int64_t)q.n * a.group > a.few_rows) return 0;
   *first_tile = see_from(a, q, 0) / NT;
   return (q.kv + NT - 1) / NT - *first_tile;
 }
@@ -77,7 +83,17 @@ struct Place {
   }
 };
 
-__device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
+template <int kThreads>
+__device__ __forceinline__ void sync_consumers() {
+  asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+}
+
+// The 8 x 8 matrix of 16-bit values that a warp holds, transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
 
 template <class T>
 __device__ __forceinline__ float2 to_float2(uint32_t u);
@@ -114,22 +130,10 @@ __device__ void write_empty(const AttendArgs& a, int D, const Request& q, int h,
   }
 }
 
-// Row x of an item: its output of D / 4 contiguous values held by one thread.
-template <class T, int N>
-__device__ __forceinline__ void store_row(const AttendArgs& a, const Request& q, int h, int x, int col, const float* o,
-                                          float inv) {
-  const int token = q.first + x / a.group, head = h * a.group + x % a.group;
-  T* p = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + col;
-#pragma unroll
-  for (int i = 0; i < N; i += 8)
-    *(uint4*)(p + i) = uint4{from_float2<T>(o[i] * inv, o[i + 1] * inv), from_float2<T>(o[i + 2] * inv, o[i + 3] * inv),
-                             from_float2<T>(o[i + 4] * inv, o[i + 5] * inv), from_float2<T>(o[i + 6] * inv, o[i + 7] * inv)};
-}
-
-template <int D>
+template <int D, int NR>
 __device__ void produce(const AttendArgs& a, const CUtensorMap* km, const CUtensorMap* vm, Place<D> at, int count,
                         int skip, uint8_t* ring, Meta* meta, uint64_t* full, uint64_t* empty, volatile int* dead) {
-  using S = Shape<D>;
+  using S = Shape<D, NR>;
   const int lane = threadIdx.x & 31;
   const int block = 1 << a.block_shift;
   const int box = min(block, S::kTokens), pieces = S::kTokens / box;
@@ -201,41 +205,43 @@ __device__ __forceinline__ int order(int n) {
   return ((D == 128 ? 0x37156240u : 0x67542310u) >> (4 * n)) & 7;
 }
 
-template <int D, class T>
+template <int D, int NR, class T>
 __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, const uint8_t* ring, const Meta* meta,
                         uint64_t* full, uint64_t* empty, volatile int* dead, float* merge, float (*s_ml)[kRows][2]) {
-  using S = Shape<D>;
-  constexpr int NT = S::kTokens, KJ = D / 64, ND = D / 8;
+  using S = Shape<D, NR>;
+  constexpr int NT = S::kTokens, KJ = D / 64, ND = D / 16, W = S::kWarps;
+  // a maximum may lag by this factor of two: the weights then reach 2^8, far from f16's limit, and
+  // most tiles need neither the maximum over the warp nor new factors
+  constexpr float kLag = 8.f;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q4 = lane & 3;
   const int tn = order<D>(n), ta = order<D>(2 * q4), tb = order<D>(2 * q4 + 1);
-  // the four values rows' and the key row's permutation of 16-byte units
+  // the permutation of 16-byte units in the rows of this thread's key and two values
   const int swk = D == 128 ? tn : (tn >> 1) & 3;
   const int swa = D == 128 ? ta : (ta >> 1) & 3, swb = D == 128 ? tb : (tb >> 1) & 3;
 
   int it = 0;  // tiles fetched so far, over all items
+  int stage = warp, left = warp;  // this warp's next: its place in the ring, and its number less `it`
+  uint32_t phase = 0;
   bool more = at.step(a, skip);
   while (more && count > 0) {
     const int seg = min(count, at.tiles - at.t);
     const Request q = at.q;
     const int rows = q.n * a.group;
     if (q.kv == 0) {
-      write_empty<T>(a, D, q, at.h, threadIdx.x, 32 * kWarps);
+      write_empty<T>(a, D, q, at.h, threadIdx.x, 32 * W);
       count -= seg;
       more = at.step(a, seg);
       continue;
     }
 
-    // rows n and n + 8: what they see, and their q in f16, scaled by a power of two so
-    // that no value leaves f16's range
-    int lo[2], hi[2];
-    float c[2];
-    uint32_t aq[KJ * 4][4];
+    // q of row n (of each eight) in f16, scaled by a power of two so that no value leaves f16's range
+    uint32_t bq[NR][KJ * 4][2];
+    float c[NR][2];  // factors of the scores of rows 2 q4 and 2 q4 + 1, and what those rows see
+    int lo[NR][2], hi[NR][2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int row = n + 8 * x, token = row / a.group;
+    for (int r = 0; r < NR; ++r) {
+      const int row = n + 8 * r, token = row / a.group;
       const bool real = row < rows;
-      lo[x] = real ? see_from(a, q, token) : 0;
-      hi[x] = real ? see_to(a, q, token) : 0;
       const T* p = (const T*)a.q + (q.first + token) * a.q_token_stride + (at.h * a.group + row % a.group) * a.q_head_stride;
       uint4 raw[KJ][2];
 #pragma unroll
@@ -254,273 +260,322 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
       amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
       amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
       int e = 0;
-      if (sizeof(T) == 2 && !(amax == 0) && amax < INFINITY) e = max((int)(__float_as_uint(amax) >> 23) - 127, -126);
+      if (amax > 0 && amax < INFINITY) e = max((int)(__float_as_uint(amax) >> 23) - 127, -126);
       const float down = __uint_as_float((unsigned)(127 - e) << 23);
-      c[x] = a.sm_scale_log2 * __uint_as_float((unsigned)(127 + e) << 23);
 #pragma unroll
       for (int j = 0; j < KJ; ++j)
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           const float2 f = to_float2<T>(((const uint32_t*)raw[j])[u]);
-          aq[4 * j + (u >> 1)][x + 2 * (u & 1)] = pack_half(f.x * down, f.y * down);
+          bq[r][4 * j + (u >> 1)][u & 1] = pack_half(f.x * down, f.y * down);
         }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int col = 2 * q4 + x, i = (col + 8 * r) / a.group;
+        c[r][x] = a.sm_scale_log2 * __uint_as_float((unsigned)(127 + __shfl_sync(~0u, e, 4 * col)) << 23);
+        lo[r][x] = col + 8 * r < rows ? see_from(a, q, i) : 0;
+        hi[r][x] = col + 8 * r < rows ? see_to(a, q, i) : 0;
+      }
     }
     // where every row sees everything: [all_lo, all_hi); where any sees something: [any_lo, any_hi)
     const int any_lo = see_from(a, q, 0), any_hi = q.kv;
     const int all_lo = see_from(a, q, q.n - 1), all_hi = see_to(a, q, 0);
 
-    float acc[ND][4];
+    float acc[NR][ND][4];  // column tiles of 16 values by 8 rows
+    float m[NR][2], l[NR][2];
 #pragma unroll
-    for (int i = 0; i < ND; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0, 0};
+    for (int r = 0; r < NR; ++r) {
+#pragma unroll
+      for (int i = 0; i < ND; ++i) acc[r][i][0] = acc[r][i][1] = acc[r][i][2] = acc[r][i][3] = 0;
+      m[r][0] = m[r][1] = -INFINITY, l[r][0] = l[r][1] = 0;
+    }
     // sums are kept in units of the values' scale, so that scales far apart lose nothing in 16 bits
     float unit = 1.f, unit_top = 0.f;
 
-    for (int i = (warp - it) & (kWarps - 1); i < seg; i += kWarps) {
-      const int stage = (it + i) % S::kStages;
-      const uint32_t phase = ((it + i) / S::kStages) & 1;
-      if (!bar_wait(&full[stage], phase, dead)) l[0] = l[1] = NAN;
+    for (; left < seg; left += W) {
+      if (!bar_wait(&full[stage], phase, dead)) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
       const uint8_t* kt = ring + stage * kStageBytes;
       const uint8_t* vt = kt + kTileBytes;
       const Meta& mt = meta[stage];
-      const int pos = (at.first_tile + at.t + i) * NT;
+      const int pos = (at.first_tile + at.t + left) * NT;
       const uint32_t valid = mt.valid;
       const bool whole = valid == (1u << S::kGroups) - 1 && pos >= all_lo && pos + NT <= all_hi;
 
-      float s[NT / 8][4];
+      // scores: of group g, tokens tn and tn + 8 by rows 2 q4 and 2 q4 + 1
+      float s[S::kGroups][NR][4];
+      float top[NR][2];
 #pragma unroll
-      for (int half = 0; half < NT / 32; ++half) {
+      for (int r = 0; r < NR; ++r) top[r][0] = top[r][1] = -INFINITY;
 #pragma unroll
-        for (int x = 4 * half; x < 4 * half + 4; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0;
+      for (int g = 0; g < S::kGroups; ++g) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) s[g][r][0] = s[g][r][1] = s[g][r][2] = s[g][r][3] = 0;
 #pragma unroll
         for (int j = 0; j < KJ; ++j) {
-          uint4 kw[4];
+          const uint8_t* p = kt + (16 * g + tn) * D + (((q4 + 4 * j) ^ swk) << 4);
+          const uint4 k0 = *(const uint4*)p, k1 = *(const uint4*)(p + 8 * D);
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            kw[x] = *(const uint4*)(kt + (tn + 8 * (4 * half + x)) * D + (((q4 + 4 * j) ^ swk) << 4));
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t u0 = ((const uint32_t*)&k0)[w], u1 = ((const uint32_t*)&k1)[w];
+            const uint32_t ak[4] = {cvt2(u0), cvt2(u1), cvt2_hi(u0), cvt2_hi(u1)};
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const uint32_t u = ((const uint32_t*)&kw[x])[w];
-              mma16816(s[4 * half + x], aq[4 * j + w], cvt2(u), cvt2_hi(u));
-            }
-        }
-      }
-      float top[2] = {m[0], m[1]};
-#pragma unroll
-      for (int x = 0; x < NT / 8; ++x) {
-        const float ks = mt.ks[x >> 1];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          s[x][y] *= ks * c[y >> 1];
-          if (!whole) {
-            const int p = pos + 8 * x + (y & 1 ? tb : ta);
-            if (p < lo[y >> 1] || p >= hi[y >> 1] || !(valid >> (x >> 1) & 1)) s[x][y] = -INFINITY;
+            for (int r = 0; r < NR; ++r) mma16816(s[g][r], ak, bq[r][4 * j + w][0], bq[r][4 * j + w][1]);
           }
-          top[y >> 1] = fmaxf(top[y >> 1], s[x][y]);
         }
+        const float ks = mt.ks[g];
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            s[g][r][y] *= ks * c[r][y & 1];
+            if (!whole) {
+              const int p = pos + 16 * g + tn + 4 * (y & 2);
+              if (p < lo[r][y & 1] || p >= hi[r][y & 1] || !(valid >> g & 1)) s[g][r][y] = -INFINITY;
+            }
+            top[r][y & 1] = fmaxf(top[r][y & 1], s[g][r][y]);
+          }
       }
-      float keep[2];
+      bool late = false;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
-        top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
-        const float base = top[x] == -INFINITY ? 0.f : top[x];
-        keep[x] = ex2(m[x] - base);
-        m[x] = top[x];
-        top[x] = base;
-        l[x] *= keep[x];
+      for (int r = 0; r < NR; ++r) late |= top[r][0] > m[r][0] + kLag || top[r][1] > m[r][1] + kLag;
+      float keep[NR][2];
+      const bool moved = __any_sync(~0u, late);
+      if (moved) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float z = fmaxf(m[r][x], top[r][x]);
+            z = fmaxf(z, __shfl_xor_sync(~0u, z, 4));
+            z = fmaxf(z, __shfl_xor_sync(~0u, z, 8));
+            z = fmaxf(z, __shfl_xor_sync(~0u, z, 16));
+            keep[r][x] = z == -INFINITY ? 1.f : ex2(m[r][x] - z);
+            m[r][x] = z;
+            l[r][x] *= keep[r][x];
+          }
       }
 #pragma unroll
-      for (int x = 0; x < NT / 8; ++x)
+      for (int r = 0; r < NR; ++r)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          s[x][y] = ex2(s[x][y] - top[y >> 1]);
-          l[y >> 1] += s[x][y];
+        for (int x = 0; x < 2; ++x) {
+          const float base = m[r][x] == -INFINITY ? 0.f : m[r][x];
+#pragma unroll
+          for (int g = 0; g < S::kGroups; ++g)
+#pragma unroll
+            for (int y = x; y < 4; y += 2) {
+              s[g][r][y] = ex2(s[g][r][y] - base);
+              l[r][x] += s[g][r][y];
+            }
         }
 
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g) {
         // the unit follows the values' scale, at most 2^60 below the largest so far
         const float vs = valid >> g & 1 ? mt.vs[g] : unit;
-        unit_top = fmaxf(unit_top, vs);
-        const float next = fmaxf(fmaxf(vs, unit_top * 0x1p-60f), 0x1p-110f);
-        const float to = unit / next, pf = vs / next;
-        unit = next;
-        float f0 = to, f1 = to;
-        if (g == 0) f0 *= keep[0], f1 *= keep[1];
-        if (__any_sync(~0u, f0 != 1.f || f1 != 1.f)) {
-#pragma unroll
-          for (int d = 0; d < ND; ++d) acc[d][0] *= f0, acc[d][1] *= f0, acc[d][2] *= f1, acc[d][3] *= f1;
+        const bool other = vs != unit;
+        float to = 1.f, pf = 1.f;
+        if (other) {
+          unit_top = fmaxf(unit_top, vs);
+          const float next = fmaxf(fmaxf(vs, unit_top * 0x1p-60f), 0x1p-110f);
+          to = unit / next, pf = vs / next;
+          unit = next;
         }
-        if (pf != 1.f) {
+        if (other || (g == 0 && moved)) {
 #pragma unroll
-          for (int y = 0; y < 4; ++y) s[2 * g][y] *= pf, s[2 * g + 1][y] *= pf;
+          for (int r = 0; r < NR; ++r) {
+            const float f0 = g == 0 && moved ? to * keep[r][0] : to, f1 = g == 0 && moved ? to * keep[r][1] : to;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) acc[r][d][0] *= f0, acc[r][d][1] *= f1, acc[r][d][2] *= f0, acc[r][d][3] *= f1;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) s[g][r][y] *= pf;
+          }
         }
-        uint32_t ap[4];
+        uint32_t bp[NR][2];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const float* p = s[2 * g + (y >> 1)] + 2 * (y & 1);
-          ap[y] = pack_half(p[0], p[1]);
+        for (int r = 0; r < NR; ++r) {
+          bp[r][0] = transpose8(pack_half(s[g][r][0], s[g][r][1]));
+          bp[r][1] = transpose8(pack_half(s[g][r][2], s[g][r][3]));
         }
         // values of tokens ta, tb, ta + 8, tb + 8 of the group, D / 8 columns each
-        uint32_t vw[4][ND / 4];
+        uint32_t vw[4][D / 32];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const uint8_t* p = vt + (16 * g + 8 * (y >> 1) + (y & 1 ? tb : ta)) * D;
           const int sw = y & 1 ? swb : swa;
-          if constexpr (D == 128) {
-            *(uint4*)vw[y] = *(const uint4*)(p + ((n ^ sw) << 4));
-          } else {
-            *(uint2*)vw[y] = *(const uint2*)(p + (((n >> 1) ^ sw) << 4) + ((n & 1) << 3));
-          }
+          if constexpr (D == 128) *(uint4*)vw[y] = *(const uint4*)(p + ((n ^ sw) << 4));
+          else *(uint2*)vw[y] = *(const uint2*)(p + (((n >> 1) ^ sw) << 4) + ((n & 1) << 3));
         }
-        bool nan = false;
         if (!whole) {
           // a masked position's values must not count, not even as 0 * NaN
+          bool nan = false;
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const int p = pos + 16 * g + 8 * (y >> 1) + (y & 1 ? tb : ta);
             const bool in = p >= any_lo && p < any_hi && (valid >> g & 1);
 #pragma unroll
-            for (int w = 0; w < ND / 4; ++w) {
+            for (int w = 0; w < D / 32; ++w) {
               if (!in) vw[y][w] = 0;
               nan |= (((vw[y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
             }
           }
-          nan = __any_sync(~0u, nan);
-        }
-        if (nan) {
-          // rows that do not see a NaN must not get it: count what each row sees of them, then take them out
-          uint32_t as[4];
+          if (__any_sync(~0u, nan)) {
+            // rows that do not see a NaN must not get it: count what each row sees of them, then take them out
+            uint32_t bs[NR][2];
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int p = pos + 16 * g + 8 * (y >> 1);
-            const bool s0 = p + ta >= lo[y & 1] && p + ta < hi[y & 1], s1 = p + tb >= lo[y & 1] && p + tb < hi[y & 1];
-            as[y] = (s0 ? 0x3c00u : 0) | (s1 ? 0x3c000000u : 0);
-          }
+            for (int r = 0; r < NR; ++r) {
+              const int row = n + 8 * r, i = row / a.group;
+              const int l0 = row < rows ? see_from(a, q, i) : 0, h0 = row < rows ? see_to(a, q, i) : 0;
 #pragma unroll
-          for (int w = 0; w < ND / 4; ++w) {
-            uint32_t f[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              f[y] = (((vw[y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-              vw[y][w] &= ~(f[y] * 0xffu);
-              f[y] *= 0x38u;
+              for (int y = 0; y < 2; ++y) {
+                const int p = pos + 16 * g + 8 * y;
+                bs[r][y] = (p + ta >= l0 && p + ta < h0 ? 0x3c00u : 0) | (p + tb >= l0 && p + tb < h0 ? 0x3c000000u : 0);
+              }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t b0 = __byte_perm(f[0], f[1], e < 2 ? 0x5140 : 0x7362);
-              const uint32_t b1 = __byte_perm(f[2], f[3], e < 2 ? 0x5140 : 0x7362);
-              float seen[4] = {0, 0, 0, 0};
-              mma16816(seen, as, e & 1 ? cvt2_hi(b0) : cvt2(b0), e & 1 ? cvt2_hi(b1) : cvt2(b1));
+            for (int w = 0; w < D / 32; ++w) {
+              uint32_t f[4];
 #pragma unroll
-              for (int y = 0; y < 4; ++y)
-                if (seen[y] > 0) acc[4 * w + e][y] = NAN;
+              for (int y = 0; y < 4; ++y) {
+                f[y] = (((vw[y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+                vw[y][w] &= ~(f[y] * 0xffu);
+                f[y] *= 0x38u;
+              }
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const uint32_t x = __byte_perm(f[0], f[1], e ? 0x7362 : 0x5140), y = __byte_perm(f[2], f[3], e ? 0x7362 : 0x5140);
+                const uint32_t av[4] = {cvt2(x), cvt2_hi(x), cvt2(y), cvt2_hi(y)};
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                  float seen[4] = {0, 0, 0, 0};
+                  mma16816(seen, av, bs[r][0], bs[r][1]);
+#pragma unroll
+                  for (int z = 0; z < 4; ++z)
+                    if (seen[z] > 0) acc[r][2 * w + e][z] = NAN;
+                }
+              }
             }
           }
         }
 #pragma unroll
-        for (int w = 0; w < ND / 4; ++w) {
-          const uint32_t a01 = __byte_perm(vw[0][w], vw[1][w], 0x5140), a23 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
-          const uint32_t b01 = __byte_perm(vw[2][w], vw[3][w], 0x5140), b23 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
-          mma16816(acc[4 * w], ap, cvt2(a01), cvt2(b01));
-          mma16816(acc[4 * w + 1], ap, cvt2_hi(a01), cvt2_hi(b01));
-          mma16816(acc[4 * w + 2], ap, cvt2(a23), cvt2(b23));
-          mma16816(acc[4 * w + 3], ap, cvt2_hi(a23), cvt2_hi(b23));
-        }
+        for (int w = 0; w < D / 32; ++w)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t x = __byte_perm(vw[0][w], vw[1][w], e ? 0x7362 : 0x5140);
+            const uint32_t y = __byte_perm(vw[2][w], vw[3][w], e ? 0x7362 : 0x5140);
+            const uint32_t av[4] = {cvt2(x), cvt2_hi(x), cvt2(y), cvt2_hi(y)};
+#pragma unroll
+            for (int r = 0; r < NR; ++r) mma16816(acc[r][2 * w + e], av, bp[r][0], bp[r][1]);
+          }
       }
       __syncwarp();
       if (lane == 0) bar_arrive(&empty[stage]);
+      stage += W;
+      if (stage >= S::kStages) stage -= S::kStages, phase ^= 1;
     }
+    left -= seg;
 
-    // the four warps' results as one, in warp 0
+    // the warps' results as one
+    float part[NR][2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      l[x] += __shfl_xor_sync(~0u, l[x], 1);
-      l[x] += __shfl_xor_sync(~0u, l[x], 2);
-      if (q4 == 0) s_ml[warp][n + 8 * x][0] = m[x], s_ml[warp][n + 8 * x][1] = l[x];
-    }
-    sync_consumers();
-    float mt[2], lt[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      mt[x] = -INFINITY, lt[x] = 0;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) mt[x] = fmaxf(mt[x], s_ml[w][n + 8 * x][0]);
-      const float base = mt[x] == -INFINITY ? 0.f : mt[x];
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) lt[x] += s_ml[w][n + 8 * x][1] * ex2(s_ml[w][n + 8 * x][0] - base);
-      const float f = ex2(m[x] - base) * unit;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) acc[d][2 * x] *= f, acc[d][2 * x + 1] *= f;
-    }
-    float4* buf = (float4*)merge + (warp & 1) * (ND * 32) + lane;
-    if (warp >= 2) {
-#pragma unroll
-      for (int d = 0; d < ND; ++d) buf[d * 32] = *(float4*)acc[d];
-    }
-    sync_consumers();
-    if (warp < 2) {
-#pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        const float4 o = buf[d * 32];
-        acc[d][0] += o.x, acc[d][1] += o.y, acc[d][2] += o.z, acc[d][3] += o.w;
-      }
-      if (warp == 1) {
-#pragma unroll
-        for (int d = 0; d < ND; ++d) buf[d * 32] = *(float4*)acc[d];
-      }
-    }
-    sync_consumers();
-    if (warp == 0) {
-      buf += ND * 32;
-      const bool done = seg == at.tiles;
-      const int slot = 2 * blockIdx.x + (at.t == 0);
-#pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        const float4 o = buf[d * 32];
-        acc[d][0] += o.x, acc[d][1] += o.y, acc[d][2] += o.z, acc[d][3] += o.w;
-      }
-      // this thread's columns: c0 of the ND column tiles are D / 8 values in a row, c1 the next D / 8
+    for (int r = 0; r < NR; ++r)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int row = n + 8 * x;
-        if (row >= rows) continue;
-        float o[D / 4];
+        float z = l[r][x];
+        z += __shfl_xor_sync(~0u, z, 4);
+        z += __shfl_xor_sync(~0u, z, 8);
+        z += __shfl_xor_sync(~0u, z, 16);
+        if (n == 0) *(float2*)s_ml[warp][2 * q4 + x + 8 * r] = float2{m[r][x], z};
+      }
+    sync_consumers<32 * W>();
 #pragma unroll
-        for (int d = 0; d < ND; ++d) o[d] = acc[d][2 * x], o[ND + d] = acc[d][2 * x + 1];
-        const int col = q4 * (D / 4);
-        if (done) {
-          const bool none = lt[x] == 0;
-          store_row<T, D / 4>(a, q, at.h, row, col, o, none ? 0.f : 1.f / lt[x]);
-          if (q4 == 0 && a.lse)
-            a.lse[(int64_t)(q.first + row / a.group) * a.n_heads + at.h * a.group + row % a.group] =
-                none ? -INFINITY : (mt[x] + log2f(lt[x])) * 0.6931471805599453f;
-        } else {
-          float* p = a.part + ((int64_t)slot * kRows + row) * D + col;
+    for (int r = 0; r < NR; ++r)
 #pragma unroll
-          for (int d = 0; d < D / 4; d += 4) *(float4*)(p + d) = *(float4*)(o + d);
-          if (q4 == 0) *(float2*)(a.part_ml + ((int64_t)slot * kRows + row) * 2) = float2{mt[x], lt[x]};
-        }
+      for (int x = 0; x < 2; ++x) {
+        float z = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) z = fmaxf(z, s_ml[w][2 * q4 + x + 8 * r][0]);
+        part[r][x] = (z == -INFINITY ? 0.f : ex2(m[r][x] - z)) * unit;
+      }
+    // this thread's columns are D / 8 in a row from n * D / 8, for rows 2 q4 and 2 q4 + 1
+    const auto place = [&](int buf, int r, int x) {
+      return (float4*)(merge + ((buf * NR + r) * 8 + 2 * q4 + x) * S::kMergeRow + n * (D / 8));
+    };
+    if (warp >= 4) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (2 * q4 + x + 8 * r < rows) {
+#pragma unroll
+            for (int d = 0; d < ND; d += 2)
+              place(warp - 4, r, x)[d / 2] =
+                  float4{acc[r][d][x] * part[r][x], acc[r][d][2 + x] * part[r][x], acc[r][d + 1][x] * part[r][x],
+                         acc[r][d + 1][2 + x] * part[r][x]};
+          }
+    }
+    sync_consumers<32 * W>();
+    if (warp < 4) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (2 * q4 + x + 8 * r < rows) {
+#pragma unroll
+            for (int d = 0; d < ND; d += 2) {
+              float4 o = {0, 0, 0, 0};
+              if (warp < W - 4) o = place(warp, r, x)[d / 2];
+              o.x += acc[r][d][x] * part[r][x], o.y += acc[r][d][2 + x] * part[r][x];
+              o.z += acc[r][d + 1][x] * part[r][x], o.w += acc[r][d + 1][2 + x] * part[r][x];
+              place(warp, r, x)[d / 2] = o;
+            }
+          }
+    }
+    sync_consumers<32 * W>();
+    const bool done = seg == at.tiles;
+    const int64_t slot = 2 * blockIdx.x + (at.t == 0);
+    for (int i = threadIdx.x; i < rows * (D / 4); i += 32 * W) {
+      const int row = i / (D / 4), col = i % (D / 4) * 4;
+      float mt = -INFINITY, lt = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) mt = fmaxf(mt, s_ml[w][row][0]);
+      const float base = mt == -INFINITY ? 0.f : mt;
+#pragma unroll
+      for (int w = 0; w < W; ++w) lt += s_ml[w][row][1] * ex2(s_ml[w][row][0] - base);
+      float4 o = {0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float4 p = *(const float4*)(merge + (w * 8 * NR + row) * S::kMergeRow + col);
+        o.x += p.x, o.y += p.y, o.z += p.z, o.w += p.w;
+      }
+      if (done) {
+        const float inv = lt == 0 ? 0.f : 1.f / lt;
+        const int token = q.first + row / a.group, head = at.h * a.group + row % a.group;
+        *(uint2*)((T*)a.out + token * a.out_token_stride + head * a.out_head_stride + col) =
+            uint2{from_float2<T>(o.x * inv, o.y * inv), from_float2<T>(o.z * inv, o.w * inv)};
+        if (col == 0 && a.lse)
+          a.lse[(int64_t)token * a.n_heads + head] = lt == 0 ? -INFINITY : (mt + log2f(lt)) * 0.6931471805599453f;
+      } else {
+        *(float4*)(a.part + (slot * kRows + row) * D + col) = o;
+        if (col == 0) *(float2*)(a.part_ml + (slot * kRows + row) * 2) = float2{mt, lt};
       }
     }
     it += seg;
     count -= seg;
     more = at.step(a, seg);
+    if (more && count > 0) sync_consumers<32 * W>();  // s_ml and the sums have been read
   }
 }
 
-template <int D, class T>
-__global__ void __launch_bounds__(kThreads, 2)
+template <int D, int NR, class T>
+__global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
     hx_kv_attend_rows(const __grid_constant__ CUtensorMap km, const __grid_constant__ CUtensorMap vm,
                       const __grid_constant__ AttendArgs a) {
-  using S = Shape<D>;
+  using S = Shape<D, NR>;
+  constexpr int kThreads = S::kThreads, kWarps = S::kWarps;
   extern __shared__ uint8_t s_raw[];
   __shared__ uint64_t s_full[S::kStages], s_empty[S::kStages];
   __shared__ Meta s_meta[S::kStages];
-  __shared__ float s_ml[kWarps][kRows][2];
+  __shared__ __align__(16) float s_ml[kWarps][kRows][2];
   __shared__ long long s_sum[kThreads / 32], s_skip;
   __shared__ int s_row, s_dead;
   uint8_t* ring = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
@@ -601,9 +656,9 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
   if (s_row < 0) return;
   if (warp == kWarps)
-    produce<D>(a, &km, &vm, at, count, skip, ring, s_meta, s_full, s_empty, &s_dead);
+    produce<D, NR>(a, &km, &vm, at, count, skip, ring, s_meta, s_full, s_empty, &s_dead);
   else
-    consume<D, T>(a, at, count, skip, ring, s_meta, s_full, s_empty, &s_dead, merge, s_ml);
+    consume<D, NR, T>(a, at, count, skip, ring, s_meta, s_full, s_empty, &s_dead, merge, s_ml);
   drain(&s_dead);
 }
 
@@ -667,7 +722,7 @@ __device__ float block_reduce(float x, bool sum, float* s) {
 // scores of a tile, then a thread per column for the weighted values, with
 // the running maximum and sum of the softmax.
 template <class T>
-__global__ void __launch_bounds__(kTile) hx_kv_attend_kernel(const hx_kv_cache c, const hx_kv_query a) {
+__global__ void __launch_bounds__(kTile) hx_kv_attend_kernel(const hx_kv_cache c, const hx_kv_query a, int few_rows) {
   __shared__ float s_q[128], s_p[kTile], s_red[4], s_o[kTile];
   __shared__ int64_t s_at[kTile];
   __shared__ float s_vs[kTile];
@@ -685,7 +740,7 @@ __global__ void __launch_bounds__(kTile) hx_kv_attend_kernel(const hx_kv_cache c
   const int p = kv - n + (t - first);
   int j1 = a.causal ? min(kv, p + 1) : kv, j0 = a.window ? max(0, p - a.window + 1) : 0;
   if (a.max_q && n > a.max_q) j1 = 0;
-  if ((int64_t)n * (a.n_heads / c.n_kv_heads) <= kRows) return;
+  if ((int64_t)n * (a.n_heads / c.n_kv_heads) <= few_rows) return;
 
   const T* q = (const T*)a.q + t * a.q_token_stride + hq * a.q_head_stride;
   if (tid < D) s_q[tid] = (float)q[tid];
@@ -800,15 +855,15 @@ AttendArgs args_of(const hx_kv_cache& c, const hx_kv_query& q) {
   return a;
 }
 
-template <int D, class T>
+template <int D, int NR, class T>
 cudaError_t launch_rows(const hx_kv_cache& c, const AttendArgs& a, cudaStream_t s) {
   CUtensorMap km, vm;
-  const int box = std::min(c.block_tokens, Shape<D>::kTokens);
+  const int box = std::min(c.block_tokens, Shape<D, NR>::kTokens);
   if (!tile_map(&km, c.k, c, box) || !tile_map(&vm, c.v, c, box)) return cudaErrorInvalidValue;
-  const auto kernel = hx_kv_attend_rows<D, T>;
-  if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem)) return e;
+  const auto kernel = hx_kv_attend_rows<D, NR, T>;
+  if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D, NR>::kSmem)) return e;
   const int blocks = row_blocks();
-  kernel<<<blocks, kThreads, Shape<D>::kSmem, s>>>(km, vm, a);
+  kernel<<<blocks, Shape<D, NR>::kThreads, Shape<D, NR>::kSmem, s>>>(km, vm, a);
   if (cudaError_t e = cudaGetLastError()) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = blocks;
@@ -833,14 +888,24 @@ cudaError_t launch_kv_attend(const hx_kv_cache& c, const hx_kv_query& q, cudaStr
   a.part_ml = (float*)((uint8_t*)q.workspace + w.ml);
   a.joins = (int4*)((uint8_t*)q.workspace + w.joins);
   const bool bf = q.dtype == HX_BF16;
+  // Up to 8 rows in the leaner form; up to 16 in the other where a step has no longer requests
+  // (max_q) or a single token of a group needs them.
+  const bool all_few = q.max_q && (int64_t)q.max_q * a.group <= kRows;
+  const int most = all_few ? q.max_q * a.group : a.group;
+  a.few_rows = most <= 8 ? 8 : kRows;
   cudaError_t e;
-  if (c.head_dim == 128) e = bf ? launch_rows<128, __nv_bfloat16>(c, a, s) : launch_rows<128, __half>(c, a, s);
-  else e = bf ? launch_rows<64, __nv_bfloat16>(c, a, s) : launch_rows<64, __half>(c, a, s);
-  if (e || (q.max_q && (int64_t)q.max_q * a.group <= kRows)) return e;
+  if (c.head_dim == 128) {
+    if (a.few_rows == 8) e = bf ? launch_rows<128, 1, __nv_bfloat16>(c, a, s) : launch_rows<128, 1, __half>(c, a, s);
+    else e = bf ? launch_rows<128, 2, __nv_bfloat16>(c, a, s) : launch_rows<128, 2, __half>(c, a, s);
+  } else {
+    if (a.few_rows == 8) e = bf ? launch_rows<64, 1, __nv_bfloat16>(c, a, s) : launch_rows<64, 1, __half>(c, a, s);
+    else e = bf ? launch_rows<64, 2, __nv_bfloat16>(c, a, s) : launch_rows<64, 2, __half>(c, a, s);
+  }
+  if (e || all_few) return e;
   const int64_t grid = (int64_t)q.n_tokens * q.n_heads;
   if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-  if (bf) hx_kv_attend_kernel<__nv_bfloat16><<<(unsigned)grid, kTile, 0, s>>>(c, q);
-  else hx_kv_attend_kernel<__half><<<(unsigned)grid, kTile, 0, s>>>(c, q);
+  if (bf) hx_kv_attend_kernel<__nv_bfloat16><<<(unsigned)grid, kTile, 0, s>>>(c, q, a.few_rows);
+  else hx_kv_attend_kernel<__half><<<(unsigned)grid, kTile, 0, s>>>(c, q, a.few_rows);
   return cudaGetLastError();
 }
 

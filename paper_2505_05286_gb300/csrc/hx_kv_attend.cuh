@@ -30,6 +30,7 @@ struct AttendArgs {
   int64_t table_stride;
   int32_t table_width, n_blocks, n_tokens, n_rows, n_heads, n_kv_heads, group;
   int32_t block_shift, max_q, causal, window;
+  int32_t few_rows;     // requests of so many rows at most are the few-rows kernel's
   float sm_scale_log2;  // sm_scale * log2(e): scores are exponents of two
   float* part;          // partial results of items that several blocks share
   float* part_ml;
