@@ -35,15 +35,19 @@ struct Shape {
   static constexpr int kThreads = 32 * (kWarps + 1);
   static constexpr int kMergeRow = D + 4;         // floats; padded against bank conflicts
   static constexpr int kMergeBytes = 4 * 8 * NR * kMergeRow * 4;
-  static constexpr int kStages = (110 * 1024 - kMergeBytes) / kStageBytes;
+  static constexpr int kStages = (106 * 1024 - kMergeBytes) / kStageBytes;
   static constexpr int kSmem = kStages * kStageBytes + kMergeBytes + 1024;
 };
 
-// What a tile's scales are, and which of its groups of 16 tokens were fetched.
-struct Meta {
+// Where a tile lies, its scales, and which of its groups of 16 tokens are fetched.
+struct __align__(16) Tile {
   float ks[4], vs[4];
-  uint32_t valid;
+  int id[4];  // blocks of the cache, -1: not fetched
+  int y;      // row in the tile map
+  uint32_t bytes, valid;
 };
+// Tiles are looked up 32 at a time, and a tile is read no later than kStages after it: 64 places.
+constexpr int kTiles = 64;
 
 // The tiles of an item, 0: it is not this kernel's.  An item that sees nothing,
 // with any number of rows, counts as one, so that its zeros are written.
@@ -130,69 +134,97 @@ __device__ void write_empty(const AttendArgs& a, int D, const Request& q, int h,
   }
 }
 
+// The fetching warp: looks tiles up, a lane each, one batch ahead of the copies that
+// lane 0 issues.  A look-up is two loads that depend on one another (block number, its scales);
+// they are placed before and halfway through the copies of the batch before, which hide them.
 template <int D, int NR>
 __device__ void produce(const AttendArgs& a, const CUtensorMap* km, const CUtensorMap* vm, Place<D> at, int count,
-                        int skip, uint8_t* ring, Meta* meta, uint64_t* full, uint64_t* empty, volatile int* dead) {
+                        int skip, uint8_t* ring, Tile* tiles, uint64_t* full, uint64_t* empty, volatile int* dead) {
   using S = Shape<D, NR>;
   const int lane = threadIdx.x & 31;
   const int block = 1 << a.block_shift;
   const int box = min(block, S::kTokens), pieces = S::kTokens / box;
   int stage = 0;
   uint32_t phase = 1;
-  bool more = at.step(a, skip + lane);
-  for (int base = 0; base < count; base += 32) {
-    // each lane looks up one of the next 32 tiles
-    int id[4];
-    Meta m = {};
-    bool tile = more && base + lane < count && at.q.kv > 0;
-    uint32_t bytes = 0;
-    int y = 0;
+  bool more = at.step(a, skip + lane), tile = false, alive = true;
+  Tile x;
+  int h = 0;
+
+  const auto look_up = [&](int base) {
+    tile = more && base + lane < count && at.q.kv > 0;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) x.id[p] = -1;
     if (tile) {
       const int pos = (at.first_tile + at.t) * S::kTokens;
       const int32_t* row = a.block_table + at.r * a.table_stride + (pos >> a.block_shift);
-      y = at.h * block + (pos & (block - 1));
+      h = at.h;
+      x.y = h * block + (pos & (block - 1));
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        id[p] = -1;
-        if (p < pieces && pos + p * box < at.q.kv) id[p] = row[p];
-      }
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        if (p >= pieces) break;
-        float ks = 0.f, vs = 0.f;
-        if ((unsigned)id[p] < (unsigned)a.n_blocks) {
-          ks = a.k_scale[id[p] * a.scale_stride + at.h];
-          vs = a.v_scale[id[p] * a.scale_stride + at.h];
-          bytes += 2 * box * D;
-        } else {
-          id[p] = -1;
-        }
-#pragma unroll
-        for (int g = 0; g < S::kGroups; ++g)
-          if (g * 16 / box == p) {
-            m.ks[g] = ks, m.vs[g] = vs;
-            if (id[p] >= 0) m.valid |= 1u << g;
-          }
-      }
-    }
-    for (int j = 0; j < 32 && base + j < count; ++j) {
-      if (!__shfl_sync(~0u, tile, j)) continue;
-      if (!__all_sync(~0u, bar_wait(&empty[stage], phase, dead))) return;
-      if (lane == j) {
-        uint8_t* dst = ring + stage * kStageBytes;
-        meta[stage] = m;
-        bar_expect(&full[stage], bytes);
-#pragma unroll
-        for (int p = 0; p < 4; ++p)
-          if (p < pieces && id[p] >= 0) {
-            tile_load(dst + p * box * D, km, &full[stage], 0, y, id[p]);
-            tile_load(dst + kTileBytes + p * box * D, vm, &full[stage], 0, y, id[p]);
-          }
-      }
-      __syncwarp();
-      if (++stage == S::kStages) stage = 0, phase ^= 1;
+      for (int p = 0; p < 4; ++p)
+        if (p < pieces && pos + p * box < at.q.kv) x.id[p] = row[p];
     }
     if (more) more = at.step(a, 32);
+  };
+  const auto scales = [&] {
+    x.bytes = x.valid = 0;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      float ks = 0.f, vs = 0.f;
+      if ((unsigned)x.id[p] < (unsigned)a.n_blocks) {
+        ks = a.k_scale[x.id[p] * a.scale_stride + h];
+        vs = a.v_scale[x.id[p] * a.scale_stride + h];
+        x.bytes += 2 * box * D;
+      } else {
+        x.id[p] = -1;
+      }
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g)
+        if (g * 16 / box == p) {
+          x.ks[g] = ks, x.vs[g] = vs;
+          if (x.id[p] >= 0) x.valid |= 1u << g;
+        }
+    }
+  };
+  // Tiles are numbered without those of items that see nothing: `number` is the next batch's first.
+  int number = 0;
+  const auto store = [&]() -> int {
+    const unsigned who = __ballot_sync(~0u, tile);
+    if (tile) tiles[(number + __popc(who & ((1u << lane) - 1))) & (kTiles - 1)] = x;
+    __syncwarp();
+    return __popc(who);
+  };
+  const auto issue = [&](int from, int to) {
+    if (lane == 0 && alive)
+      for (int k = from; k < to; ++k) {
+        const Tile& y = tiles[k & (kTiles - 1)];
+        uint8_t* dst = ring + stage * kStageBytes;
+        if (!bar_wait(&empty[stage], phase, dead)) {
+          alive = false;
+          break;
+        }
+        bar_expect(&full[stage], y.bytes);
+        for (int p = 0; p < pieces; ++p) {
+          const int id = y.id[p];
+          if (id < 0) continue;
+          tile_load(dst + p * box * D, km, &full[stage], 0, y.y, id);
+          tile_load(dst + kTileBytes + p * box * D, vm, &full[stage], 0, y.y, id);
+        }
+        if (++stage == S::kStages) stage = 0, phase ^= 1;
+      }
+    __syncwarp();
+  };
+
+  look_up(0);
+  scales();
+  for (int base = 0; base < count;) {
+    const int have = store();
+    base += 32;
+    const bool next = base < count;
+    if (next) look_up(base);
+    issue(number, number + have / 2);
+    if (next) scales();
+    issue(number + have / 2, number + have);
+    number += have;
   }
 }
 
@@ -206,7 +238,7 @@ __device__ __forceinline__ int order(int n) {
 }
 
 template <int D, int NR, class T>
-__device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, const uint8_t* ring, const Meta* meta,
+__device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, const uint8_t* ring, const Tile* tiles,
                         uint64_t* full, uint64_t* empty, volatile int* dead, float* merge, float (*s_ml)[kRows][2]) {
   using S = Shape<D, NR>;
   constexpr int NT = S::kTokens, KJ = D / 64, ND = D / 16, W = S::kWarps;
@@ -293,10 +325,12 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
     float unit = 1.f, unit_top = 0.f;
 
     for (; left < seg; left += W) {
-      if (!bar_wait(&full[stage], phase, dead)) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
+      // Tiles land in any order, and the tile before this one in its place is another warp's: a
+      // barrier tells a phase from the one before it only, so that one's end is waited for first.
+      if (!bar_wait(&empty[stage], phase ^ 1, dead) || !bar_wait(&full[stage], phase, dead)) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
       const uint8_t* kt = ring + stage * kStageBytes;
       const uint8_t* vt = kt + kTileBytes;
-      const Meta& mt = meta[stage];
+      const Tile& mt = tiles[(it + left) & (kTiles - 1)];
       const int pos = (at.first_tile + at.t + left) * NT;
       const uint32_t valid = mt.valid;
       const bool whole = valid == (1u << S::kGroups) - 1 && pos >= all_lo && pos + NT <= all_hi;
@@ -574,7 +608,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   constexpr int kThreads = S::kThreads, kWarps = S::kWarps;
   extern __shared__ uint8_t s_raw[];
   __shared__ uint64_t s_full[S::kStages], s_empty[S::kStages];
-  __shared__ Meta s_meta[S::kStages];
+  __shared__ Tile s_tiles[kTiles];
   __shared__ __align__(16) float s_ml[kWarps][kRows][2];
   __shared__ long long s_sum[kThreads / 32], s_skip;
   __shared__ int s_row, s_dead;
@@ -656,9 +690,9 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   }
   if (s_row < 0) return;
   if (warp == kWarps)
-    produce<D, NR>(a, &km, &vm, at, count, skip, ring, s_meta, s_full, s_empty, &s_dead);
+    produce<D, NR>(a, &km, &vm, at, count, skip, ring, s_tiles, s_full, s_empty, &s_dead);
   else
-    consume<D, NR, T>(a, at, count, skip, ring, s_meta, s_full, s_empty, &s_dead, merge, s_ml);
+    consume<D, NR, T>(a, at, count, skip, ring, s_tiles, s_full, s_empty, &s_dead, merge, s_ml);
   drain(&s_dead);
 }
 
