@@ -194,23 +194,21 @@ __device__ void produce(const AttendArgs& a, const CUtensorMap* km, const CUtens
     return __popc(who);
   };
   const auto issue = [&](int from, int to) {
-    if (lane == 0 && alive)
-      for (int k = from; k < to; ++k) {
-        const Tile& y = tiles[k & (kTiles - 1)];
-        uint8_t* dst = ring + stage * kStageBytes;
-        if (!bar_wait(&empty[stage], phase, dead)) {
-          alive = false;
-          break;
-        }
-        bar_expect(&full[stage], y.bytes);
-        for (int p = 0; p < pieces; ++p) {
-          const int id = y.id[p];
-          if (id < 0) continue;
-          tile_load(dst + p * box * D, km, &full[stage], 0, y.y, id);
-          tile_load(dst + kTileBytes + p * box * D, vm, &full[stage], 0, y.y, id);
-        }
-        if (++stage == S::kStages) stage = 0, phase ^= 1;
+    for (int k = from; k < to && alive; ++k) {
+      const Tile& y = tiles[k & (kTiles - 1)];
+      const int id = y.id[lane & 3], at_y = y.y;
+      const uint32_t bytes = y.bytes / 2;
+      uint8_t* dst = ring + stage * kStageBytes + lane * box * D;
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        alive &= __all_sync(~0u, bar_wait(&empty[2 * stage + v], phase, dead));
+        if (!alive) break;
+        if (lane == 0) bar_expect(&full[2 * stage + v], bytes);
+        __syncwarp();
+        if (lane < pieces && id >= 0) tile_load(dst + v * kTileBytes, v ? vm : km, &full[2 * stage + v], 0, at_y, id);
       }
+      if (++stage == S::kStages) stage = 0, phase ^= 1;
+    }
     __syncwarp();
   };
 
@@ -254,6 +252,9 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
   int it = 0;  // tiles fetched so far, over all items
   int stage = warp, left = warp;  // this warp's next: its place in the ring, and its number less `it`
   uint32_t phase = 0;
+  // Tiles land in any order, and the tile before this one in its place is another warp's: a
+  // barrier tells a phase from the one before it only, so that one's end is waited for first.
+  const auto landed = [&](int x) { return bar_wait(&empty[x], phase ^ 1, dead) && bar_wait(&full[x], phase, dead); };
   bool more = at.step(a, skip);
   while (more && count > 0) {
     const int seg = min(count, at.tiles - at.t);
@@ -325,9 +326,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
     float unit = 1.f, unit_top = 0.f;
 
     for (; left < seg; left += W) {
-      // Tiles land in any order, and the tile before this one in its place is another warp's: a
-      // barrier tells a phase from the one before it only, so that one's end is waited for first.
-      if (!bar_wait(&empty[stage], phase ^ 1, dead) || !bar_wait(&full[stage], phase, dead)) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
+      if (!landed(2 * stage)) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
       const uint8_t* kt = ring + stage * kStageBytes;
       const uint8_t* vt = kt + kTileBytes;
       const Tile& mt = tiles[(it + left) & (kTiles - 1)];
@@ -369,6 +368,8 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
             top[r][y & 1] = fmaxf(top[r][y & 1], s[g][r][y]);
           }
       }
+      __syncwarp();
+      if (lane == 0) bar_arrive(&empty[2 * stage]);
       bool late = false;
 #pragma unroll
       for (int r = 0; r < NR; ++r) late |= top[r][0] > m[r][0] + kLag || top[r][1] > m[r][1] + kLag;
@@ -402,6 +403,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
             }
         }
 
+      if (!landed(2 * stage + 1)) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g) {
         // the unit follows the values' scale, at most 2^60 below the largest so far
@@ -502,7 +504,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
           }
       }
       __syncwarp();
-      if (lane == 0) bar_arrive(&empty[stage]);
+      if (lane == 0) bar_arrive(&empty[2 * stage + 1]);
       stage += W;
       if (stage >= S::kStages) stage -= S::kStages, phase ^= 1;
     }
@@ -607,7 +609,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   using S = Shape<D, NR>;
   constexpr int kThreads = S::kThreads, kWarps = S::kWarps;
   extern __shared__ uint8_t s_raw[];
-  __shared__ uint64_t s_full[S::kStages], s_empty[S::kStages];
+  __shared__ uint64_t s_full[2 * S::kStages], s_empty[2 * S::kStages];  // of a place: keys, values
   __shared__ Tile s_tiles[kTiles];
   __shared__ __align__(16) float s_ml[kWarps][kRows][2];
   __shared__ long long s_sum[kThreads / 32], s_skip;
@@ -618,7 +620,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   asm volatile("griddepcontrol.launch_dependents;");
 
   if (tid == 0) {
-    for (int i = 0; i < S::kStages; ++i) bar_init(&s_full[i], 1), bar_init(&s_empty[i], 1);
+    for (int i = 0; i < 2 * S::kStages; ++i) bar_init(&s_full[i], 1), bar_init(&s_empty[i], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s_dead = 0;
     s_row = -1;
