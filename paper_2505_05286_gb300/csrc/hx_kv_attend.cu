@@ -699,38 +699,82 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
 }
 
 // Joins an item's partial results: block e those of the item that ends in stretch e.
+// Each warp turns its rows' maxima and sums into a weight for every part; then D / 4 threads
+// take a row's sums (or an equal share of its parts, where there are fewer rows than
+// that), with eight loads in flight: what counts is the latency of few dependent loads.
+constexpr int kJoinThreads = 256;
+constexpr int kMaxBlocks = 512;  // and so of an item's parts
+
 template <int D, class T>
-__global__ void __launch_bounds__(256) hx_kv_attend_join(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_constant__ AttendArgs a) {
+  constexpr int kCols = D / 4, kTeams = kJoinThreads / kCols;
+  __shared__ float s_w[kRows][kMaxBlocks];
+  __shared__ float2 s_ml[kRows];
+  __shared__ float4 s_o[kTeams][kCols];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int4 join = a.joins[blockIdx.x];
   if (join.z < 0) return;
   const Request q = request(a, join.x);
-  const int parts = blockIdx.x - join.z + 1;
-  const int x0 = threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4;
-  for (int row = x0; row < q.n * a.group; row += 256 / (D / 4)) {
-    float m = -INFINITY;
-    for (int i = 0; i < parts; ++i) {
-      const int64_t slot = 2 * (int64_t)(join.z + i) + (i == 0);
-      m = fmaxf(m, a.part_ml[(slot * kRows + row) * 2]);
-    }
+  const int rows = q.n * a.group, parts = blockIdx.x - join.z + 1;
+  const auto slot = [&](int i) { return 2 * (int64_t)(join.z + i) + (i == 0); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int row = warp; row < rows; row += kJoinThreads / 32) {
+    float m = -INFINITY, l = 0;
+    for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[(slot(i) * kRows + row) * 2]);
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
     const float base = m == -INFINITY ? 0.f : m;
-    float l = 0;
-    float4 o = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int i = 0; i < parts; ++i) {
-      const int64_t slot = 2 * (int64_t)(join.z + i) + (i == 0);
-      const float2 ml = *(const float2*)(a.part_ml + (slot * kRows + row) * 2);
-      const float4 p = *(const float4*)(a.part + (slot * kRows + row) * D + col);
-      const float f = ex2(ml.x - base);
-      l += ml.y * f;
-      o.x += p.x * f, o.y += p.y * f, o.z += p.z * f, o.w += p.w * f;
+    for (int i = lane; i < parts; i += 32) {
+      const float2 ml = *(const float2*)(a.part_ml + (slot(i) * kRows + row) * 2);
+      const float w = ex2(ml.x - base);
+      s_w[row][i] = w;
+      l += ml.y * w;
     }
-    const float inv = l == 0 ? 0.f : 1.f / l;
-    const int token = q.first + row / a.group, head = join.y * a.group + row % a.group;
-    T* to = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + col;
-    *(uint2*)to = uint2{from_float2<T>(o.x * inv, o.y * inv), from_float2<T>(o.z * inv, o.w * inv)};
-    if (col == 0 && a.lse)
-      a.lse[(int64_t)token * a.n_heads + head] = l == 0 ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
+    if (lane == 0) s_ml[row] = float2{m, l};
+  }
+  __syncthreads();
+  const int team = threadIdx.x / kCols, col = threadIdx.x % kCols;
+  const int share = max(1, kTeams / rows);  // teams of a row
+  for (int r0 = 0; r0 < rows; r0 += kTeams / share) {
+    const int row = r0 + team / share, sub = team % share;
+    float4 o = {0, 0, 0, 0};
+    if (row < rows && team / share < kTeams / share) {
+      int i = sub;
+      for (; i + 7 * share < parts; i += 8 * share) {
+        float4 p[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) p[u] = *(const float4*)(a.part + (slot(i + u * share) * kRows + row) * D + 4 * col);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float w = s_w[row][i + u * share];
+          o.x += p[u].x * w, o.y += p[u].y * w, o.z += p[u].z * w, o.w += p[u].w * w;
+        }
+      }
+      for (; i < parts; i += share) {
+        const float4 p = *(const float4*)(a.part + (slot(i) * kRows + row) * D + 4 * col);
+        const float w = s_w[row][i];
+        o.x += p.x * w, o.y += p.y * w, o.z += p.z * w, o.w += p.w * w;
+      }
+    }
+    if (share > 1) {
+      s_o[team][col] = o;
+      __syncthreads();
+      if (sub == 0)
+        for (int i = 1; i < share && team + i < kTeams; ++i) {
+          const float4 p = s_o[team + i][col];
+          o.x += p.x, o.y += p.y, o.z += p.z, o.w += p.w;
+        }
+      __syncthreads();
+    }
+    if (sub == 0 && row < rows && team / share < kTeams / share) {
+      const float2 ml = s_ml[row];
+      const float inv = ml.y == 0 ? 0.f : 1.f / ml.y;
+      const int token = q.first + row / a.group, head = join.y * a.group + row % a.group;
+      T* to = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + 4 * col;
+      *(uint2*)to = uint2{from_float2<T>(o.x * inv, o.y * inv), from_float2<T>(o.z * inv, o.w * inv)};
+      if (col == 0 && a.lse)
+        a.lse[(int64_t)token * a.n_heads + head] = ml.y == 0 ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
+    }
   }
 }
 
@@ -831,7 +875,7 @@ int sm_count() {
 }
 
 // Two blocks fill an SM's shared memory.
-int row_blocks() { return 2 * sm_count(); }
+int row_blocks() { return std::min(2 * sm_count(), kMaxBlocks); }
 
 struct Work {
   int64_t part, ml, joins, bytes;
@@ -903,7 +947,7 @@ cudaError_t launch_rows(const hx_kv_cache& c, const AttendArgs& a, cudaStream_t 
   if (cudaError_t e = cudaGetLastError()) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = blocks;
-  cfg.blockDim = 256;
+  cfg.blockDim = kJoinThreads;
   cfg.stream = s;
   cudaLaunchAttribute at = {};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
