@@ -17,7 +17,8 @@ LIB = os.path.join(PKG, "libhxsim.so")
 # the bounds-checked build (-DHX_CHECKED): every index the simulation kernel
 # forms is range-checked, a failure is a per-simulation status (HX_ERR_BOUNDS)
 LIB_CHECKED = os.path.join(PKG, "libhxsim_checked.so")
-SOURCES = ["hx_kernels.cu", "hx_api.cu", "hx_kv_api.cu", "hx_kv_step.cu", "hx_kv_attend.cu"]
+SOURCES = ["hx_kernels.cu", "hx_api.cu", "hx_kv_api.cu", "hx_kv_step.cu", "hx_kv_attend.cu",
+           "hx_kv_attend_many.cu"]
 NVCC = os.environ.get("NVCC", "nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]

@@ -2,8 +2,7 @@
 // requests of few rows (a row: one token and query head of a kv head's group),
 // which is every request that decodes.
 #include <algorithm>
-
-#include <cuda_fp8.h>
+#include <type_traits>
 
 #include "hx_kv_attend.cuh"
 
@@ -698,14 +697,14 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   drain(&s_dead);
 }
 
-// Joins an item's partial results: block e those of the item that ends in stretch e.
+// Joins an item's partial results: block (e, y) rows 16 y and on of the item that ends in stretch e.
 // Each warp turns its rows' maxima and sums into a weight for every part; then D / 4 threads
 // take a row's sums (or an equal share of its parts, where there are fewer rows than
 // that), with eight loads in flight: what counts is the latency of few dependent loads.
 constexpr int kJoinThreads = 256;
 constexpr int kMaxBlocks = 512;  // and so of an item's parts
 
-template <int D, class T>
+template <int D, int kSlotRows, class T>
 __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_constant__ AttendArgs a) {
   constexpr int kCols = D / 4, kTeams = kJoinThreads / kCols;
   __shared__ float s_w[kRows][kMaxBlocks];
@@ -715,16 +714,20 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
   const int4 join = a.joins[blockIdx.x];
   if (join.z < 0) return;
   const Request q = request(a, join.x);
-  const int rows = q.n * a.group, parts = blockIdx.x - join.z + 1;
-  const auto slot = [&](int i) { return 2 * (int64_t)(join.z + i) + (i == 0); };
+  const int64_t item = (int64_t)join.w * kSlotRows;  // the item's first row of its request
+  const int y0 = blockIdx.y * kRows;
+  const int rows = min(kRows, (int)min((int64_t)kSlotRows, (int64_t)q.n * a.group - item) - y0);
+  const int parts = blockIdx.x - join.z + 1;
+  if (rows <= 0) return;
+  const auto slot = [&](int i) { return (2 * (int64_t)(join.z + i) + (i == 0)) * kSlotRows + y0; };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int row = warp; row < rows; row += kJoinThreads / 32) {
     float m = -INFINITY, l = 0;
-    for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[(slot(i) * kRows + row) * 2]);
+    for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[(slot(i) + row) * 2]);
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
     const float base = m == -INFINITY ? 0.f : m;
     for (int i = lane; i < parts; i += 32) {
-      const float2 ml = *(const float2*)(a.part_ml + (slot(i) * kRows + row) * 2);
+      const float2 ml = *(const float2*)(a.part_ml + (slot(i) + row) * 2);
       const float w = ex2(ml.x - base);
       s_w[row][i] = w;
       l += ml.y * w;
@@ -743,7 +746,7 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
       for (; i + 7 * share < parts; i += 8 * share) {
         float4 p[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) p[u] = *(const float4*)(a.part + (slot(i + u * share) * kRows + row) * D + 4 * col);
+        for (int u = 0; u < 8; ++u) p[u] = *(const float4*)(a.part + (slot(i + u * share) + row) * D + 4 * col);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           const float w = s_w[row][i + u * share];
@@ -751,7 +754,7 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
         }
       }
       for (; i < parts; i += share) {
-        const float4 p = *(const float4*)(a.part + (slot(i) * kRows + row) * D + 4 * col);
+        const float4 p = *(const float4*)(a.part + (slot(i) + row) * D + 4 * col);
         const float w = s_w[row][i];
         o.x += p.x * w, o.y += p.y * w, o.z += p.z * w, o.w += p.w * w;
       }
@@ -769,103 +772,14 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
     if (sub == 0 && row < rows && team / share < kTeams / share) {
       const float2 ml = s_ml[row];
       const float inv = ml.y == 0 ? 0.f : 1.f / ml.y;
-      const int token = q.first + row / a.group, head = join.y * a.group + row % a.group;
+      const int64_t x = item + y0 + row, token = q.first + x / a.group, head = join.y * a.group + x % a.group;
       T* to = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + 4 * col;
       *(uint2*)to = uint2{from_float2<T>(o.x * inv, o.y * inv), from_float2<T>(o.z * inv, o.w * inv)};
       if (col == 0 && a.lse)
-        a.lse[(int64_t)token * a.n_heads + head] = ml.y == 0 ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
+        a.lse[token * a.n_heads + head] = ml.y == 0 ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
     }
   }
 }
-
-// ------------------------------------------------- many rows, simplest form
-
-constexpr int kTile = 128;
-
-__device__ float value_of(uint8_t b) {
-  const __half_raw h = __nv_cvt_fp8_to_halfraw(b, __NV_E4M3);
-  return __half2float(*(const __half*)&h);
-}
-
-__device__ float block_reduce(float x, bool sum, float* s) {
-  for (int d = 16; d; d >>= 1) {
-    const float o = __shfl_xor_sync(~0u, x, d);
-    x = sum ? x + o : fmaxf(x, o);
-  }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
-  __syncthreads();
-  return sum ? s[0] + s[1] + s[2] + s[3] : fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-}
-
-// One block of threads per token and head: a thread per position for the
-// scores of a tile, then a thread per column for the weighted values, with
-// the running maximum and sum of the softmax.
-template <class T>
-__global__ void __launch_bounds__(kTile) hx_kv_attend_kernel(const hx_kv_cache c, const hx_kv_query a, int few_rows) {
-  __shared__ float s_q[128], s_p[kTile], s_red[4], s_o[kTile];
-  __shared__ int64_t s_at[kTile];
-  __shared__ float s_vs[kTile];
-  const int tid = threadIdx.x, D = c.head_dim, B = c.block_tokens;
-  const int t = blockIdx.x / a.n_heads, hq = blockIdx.x % a.n_heads, h = hq / (a.n_heads / c.n_kv_heads);
-
-  int lo = 0, hi = a.n_rows;  // the last row that starts at or before t
-  while (lo + 1 < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (a.row_start[mid] <= t) lo = mid;
-    else hi = mid;
-  }
-  const int r = lo, first = a.row_start[r], end = a.row_start[r + 1], n = end - first;
-  int kv = t >= first && t < end ? min(max(a.kv_len[r], 0), (int)min((int64_t)a.table_width * B, (int64_t)0x7fffffff)) : 0;
-  const int p = kv - n + (t - first);
-  int j1 = a.causal ? min(kv, p + 1) : kv, j0 = a.window ? max(0, p - a.window + 1) : 0;
-  if (a.max_q && n > a.max_q) j1 = 0;
-  if ((int64_t)n * (a.n_heads / c.n_kv_heads) <= few_rows) return;
-
-  const T* q = (const T*)a.q + t * a.q_token_stride + hq * a.q_head_stride;
-  if (tid < D) s_q[tid] = (float)q[tid];
-  float m = -INFINITY, l = 0, o = 0;
-  const int d = tid % D, part = tid / D, parts = kTile / D;
-  __syncthreads();
-  for (int base = j0; base < j1; base += kTile) {
-    const int j = base + tid;
-    float s = -INFINITY;
-    int64_t at = -1;
-    if (j < j1) {
-      const int blk = a.block_table[r * a.table_stride + j / B];
-      if ((unsigned)blk < (unsigned)c.n_blocks) {
-        at = blk * c.block_stride + ((int64_t)h * B + j % B) * D;
-        const uint8_t* k = (const uint8_t*)c.k + at;
-        float x = 0;
-        for (int e = 0; e < D; ++e) x += s_q[e] * value_of(k[e]);
-        s = x * c.k_scale[blk * c.scale_stride + h] * a.sm_scale;
-        s_vs[tid] = c.v_scale[blk * c.scale_stride + h];
-      }
-    }
-    s_at[tid] = at;
-    const float top = fmaxf(m, block_reduce(s, false, s_red));
-    const float e = at >= 0 && top > -INFINITY ? expf(s - top) : 0.f;
-    s_p[tid] = e;
-    const float keep = top > -INFINITY ? expf(m - top) : 1.f;
-    l = l * keep + block_reduce(e, true, s_red);
-    o *= keep;
-    m = top;
-    for (int i = part; i < min(kTile, j1 - base); i += parts)
-      if (s_at[i] >= 0) o += s_p[i] * (value_of(((const uint8_t*)c.v)[s_at[i] + d]) * s_vs[i]);
-    __syncthreads();
-  }
-  s_o[tid] = o;
-  __syncthreads();
-  if (tid < D) {
-    for (int i = 1; i < parts; ++i) o += s_o[tid + i * D];
-    ((T*)a.out)[t * a.out_token_stride + hq * a.out_head_stride + tid] = (T)(l > 0 ? o / l : isnan(l) ? l : 0.f);
-  }
-  if (tid == 0 && a.lse) a.lse[(int64_t)t * a.n_heads + hq] = l > 0 || isnan(l) ? m + logf(l) : -INFINITY;
-}
-
-}  // namespace
-
-namespace {
 
 int sm_count() {
   int dev = 0, sms = 0;
@@ -881,13 +795,26 @@ struct Work {
   int64_t part, ml, joins, bytes;
 };
 
-Work workspace(int head_dim, int blocks) {
+// Two partial results of a block at most, and what it joins.
+Work workspace(int head_dim, int blocks, int slot_rows) {
   Work w;
   w.part = 0;
-  w.ml = w.part + 2 * (int64_t)blocks * kRows * head_dim * 4;
-  w.joins = w.ml + 2 * (int64_t)blocks * kRows * 8;
+  w.ml = w.part + 2 * (int64_t)blocks * slot_rows * head_dim * 4;
+  w.joins = w.ml + 2 * (int64_t)blocks * slot_rows * 8;
   w.bytes = w.joins + (int64_t)blocks * 16;
   return w;
+}
+
+AttendArgs with(AttendArgs a, void* workspace, const Work& w) {
+  a.part = (float*)((uint8_t*)workspace + w.part);
+  a.part_ml = (float*)((uint8_t*)workspace + w.ml);
+  a.joins = (int4*)((uint8_t*)workspace + w.joins);
+  return a;
+}
+
+// Whether no request of the step has more rows than the few-rows kernel takes.
+bool all_few(const hx_kv_cache& c, const hx_kv_query& q) {
+  return q.max_q && (int64_t)q.max_q * (q.n_heads / c.n_kv_heads) <= kRows;
 }
 
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -935,6 +862,21 @@ AttendArgs args_of(const hx_kv_cache& c, const hx_kv_query& q) {
   return a;
 }
 
+// Its blocks are launched while the kernel before still runs, and wait for its end.
+template <int D, int kSlotRows, class T>
+cudaError_t launch_join(const AttendArgs& a, int blocks, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks, kSlotRows / kRows);
+  cfg.blockDim = kJoinThreads;
+  cfg.stream = s;
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, hx_kv_attend_join<D, kSlotRows, T>, a);
+}
+
 template <int D, int NR, class T>
 cudaError_t launch_rows(const hx_kv_cache& c, const AttendArgs& a, cudaStream_t s) {
   CUtensorMap km, vm;
@@ -945,48 +887,36 @@ cudaError_t launch_rows(const hx_kv_cache& c, const AttendArgs& a, cudaStream_t 
   const int blocks = row_blocks();
   kernel<<<blocks, Shape<D, NR>::kThreads, Shape<D, NR>::kSmem, s>>>(km, vm, a);
   if (cudaError_t e = cudaGetLastError()) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = blocks;
-  cfg.blockDim = kJoinThreads;
-  cfg.stream = s;
-  cudaLaunchAttribute at = {};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, hx_kv_attend_join<D, T>, a);
+  return launch_join<D, kRows, T>(a, blocks, s);
+}
+
+template <int D, class T>
+cudaError_t launch_typed(const hx_kv_cache& c, const hx_kv_query& q, AttendArgs a, cudaStream_t s) {
+  const bool few = all_few(c, q);
+  // Up to 8 rows in the leaner form; up to 16 in the other where a step has no longer requests
+  // (max_q) or a single token of a group needs them.
+  a.few_rows = (few ? q.max_q * a.group : a.group) <= 8 ? 8 : kRows;
+  const AttendArgs rows = with(a, q.workspace, workspace(D, row_blocks(), kRows));
+  if (cudaError_t e = a.few_rows == 8 ? launch_rows<D, 1, T>(c, rows, s) : launch_rows<D, 2, T>(c, rows, s)) return e;
+  if (few) return cudaSuccess;
+  const int blocks = sm_count();
+  const AttendArgs many = with(a, q.workspace, workspace(D, blocks, kItemRows));
+  if (cudaError_t e = launch_attend_many(many, D, std::is_same<T, __nv_bfloat16>::value, blocks, s)) return e;
+  return launch_join<D, kItemRows, T>(many, blocks, s);
 }
 
 }  // namespace
 
-int64_t kv_attend_workspace(const hx_kv_cache& c, const hx_kv_query&) { return workspace(c.head_dim, row_blocks()).bytes; }
+int64_t kv_attend_workspace(const hx_kv_cache& c, const hx_kv_query& q) {
+  const int64_t rows = workspace(c.head_dim, row_blocks(), kRows).bytes;
+  return all_few(c, q) ? rows : std::max(rows, workspace(c.head_dim, sm_count(), kItemRows).bytes);
+}
 
 cudaError_t launch_kv_attend(const hx_kv_cache& c, const hx_kv_query& q, cudaStream_t s) {
-  AttendArgs a = args_of(c, q);
-  const Work w = workspace(c.head_dim, row_blocks());
-  a.part = (float*)((uint8_t*)q.workspace + w.part);
-  a.part_ml = (float*)((uint8_t*)q.workspace + w.ml);
-  a.joins = (int4*)((uint8_t*)q.workspace + w.joins);
+  const AttendArgs a = args_of(c, q);
   const bool bf = q.dtype == HX_BF16;
-  // Up to 8 rows in the leaner form; up to 16 in the other where a step has no longer requests
-  // (max_q) or a single token of a group needs them.
-  const bool all_few = q.max_q && (int64_t)q.max_q * a.group <= kRows;
-  const int most = all_few ? q.max_q * a.group : a.group;
-  a.few_rows = most <= 8 ? 8 : kRows;
-  cudaError_t e;
-  if (c.head_dim == 128) {
-    if (a.few_rows == 8) e = bf ? launch_rows<128, 1, __nv_bfloat16>(c, a, s) : launch_rows<128, 1, __half>(c, a, s);
-    else e = bf ? launch_rows<128, 2, __nv_bfloat16>(c, a, s) : launch_rows<128, 2, __half>(c, a, s);
-  } else {
-    if (a.few_rows == 8) e = bf ? launch_rows<64, 1, __nv_bfloat16>(c, a, s) : launch_rows<64, 1, __half>(c, a, s);
-    else e = bf ? launch_rows<64, 2, __nv_bfloat16>(c, a, s) : launch_rows<64, 2, __half>(c, a, s);
-  }
-  if (e || all_few) return e;
-  const int64_t grid = (int64_t)q.n_tokens * q.n_heads;
-  if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-  if (bf) hx_kv_attend_kernel<__nv_bfloat16><<<(unsigned)grid, kTile, 0, s>>>(c, q, a.few_rows);
-  else hx_kv_attend_kernel<__half><<<(unsigned)grid, kTile, 0, s>>>(c, q, a.few_rows);
-  return cudaGetLastError();
+  if (c.head_dim == 128) return bf ? launch_typed<128, __nv_bfloat16>(c, q, a, s) : launch_typed<128, __half>(c, q, a, s);
+  return bf ? launch_typed<64, __nv_bfloat16>(c, q, a, s) : launch_typed<64, __half>(c, q, a, s);
 }
 
 }  // namespace hx

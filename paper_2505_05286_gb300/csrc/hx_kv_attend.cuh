@@ -12,6 +12,7 @@
 namespace hx {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kItemRows = 256;  // rows of an item of the many-rows kernel
 
 // What the kernels read of hx_kv_cache and hx_kv_query.
 struct AttendArgs {
@@ -34,8 +35,11 @@ struct AttendArgs {
   float sm_scale_log2;  // sm_scale * log2(e): scores are exponents of two
   float* part;          // partial results of items that several blocks share
   float* part_ml;
-  int4* joins;          // [blocks]
+  int4* joins;          // [blocks] {request, kv head, first block of the item, which rows} or -1 in third place
 };
+
+// Launches the many-rows kernel (hx_kv_attend_many.cu) on `blocks` blocks.
+cudaError_t launch_attend_many(const AttendArgs& a, int head_dim, bool bf16, int blocks, cudaStream_t s);
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 

@@ -1,0 +1,713 @@
+// hx_kv_attend_many.cu -- attention of a step's tokens over the paged 8-bit cache:
+// requests of many rows (a row: one token and query head of a kv head's group), which
+// is a prompt or a chunk of one.
+#include <algorithm>
+#include <type_traits>
+
+#include "hx_kv_attend.cuh"
+
+namespace hx {
+namespace {
+
+// Bound by the tensor cores: 4 D operations per row and visible token.  An item is 256 rows of
+// one request and kv head, in two halves of 128, the height of a tcgen05
+// accumulator; its tokens come in tiles of 128, and all items' tiles, laid end to end, are
+// dealt out to one block per SM in equal stretches (items that blocks share are joined by a
+// second kernel).  In a block,
+//   4 warps turn the tiles' e4m3 into f16 in shared memory, in the layout that tcgen05 reads
+//     (both halves use each: the conversion is paid once for 256 rows),
+//   1 thread issues the products: S = Q K^T into tensor memory, O += P V with P read from
+//     tensor memory, the halves alternating, so that one half's products run while the other's
+//     softmax does,
+//   2 x 4 warps do a half's softmax, a row to a thread, and write P over S.
+// Tensor memory (512 columns): S, P of the halves at 0 and 128, O at 256 and 256 + D.
+//
+// Scales: a score is s * ks * c, and a value's scale vs goes into the weight, P = exp2(s ks c +
+// log2(vs) - M) with M the largest of those exponents so far (or up to 2^8 less: O is
+// rescaled only when it has moved by more).  So P in f16 is accurate
+// relative to the row's largest weight times scale, however far apart scales lie, and the
+// softmax's sum is that of P / vs.
+constexpr int kHalf = 128;
+constexpr int kKv = 128;       // tokens of a tile
+constexpr int kGroups = kKv / 16;
+constexpr int kConvWarp = 8, kMmaWarp = 12;
+constexpr int kManyThreads = 32 * 13;
+constexpr int kNanList = 64;
+
+template <int D>
+struct Many {
+  static constexpr int kQBytes = kHalf * D * 2;   // one half's q
+  static constexpr int kTile = kKv * D * 2;       // K or V in f16
+  static constexpr int kSmem = 2 * kQBytes + 4 * kTile + 1024;
+};
+
+struct Segment {  // a stretch of one item's tiles
+  int r, h, mt;           // request, kv head, which 256 rows
+  int t, tiles;           // the next tile, and how many the item has
+  int first_tile;
+  Request q;
+  int rows;               // of this item
+  int lo[2], hi[2];       // tokens that any row of a half sees
+  bool empty;             // nothing visible, or not to be computed: zeros
+};
+
+__device__ __forceinline__ bool many(const AttendArgs& a, const Request& q) {
+  return q.kv > 0 && (int64_t)q.n * a.group > a.few_rows;
+}
+__device__ __forceinline__ int items_of(const AttendArgs& a, const Request& q) {
+  return (int)(((int64_t)q.n * a.group + kItemRows - 1) / kItemRows);
+}
+// First and end tile of item mt of a request (at least one, to write its zeros).
+__device__ __forceinline__ void item_span(const AttendArgs& a, const Request& q, int mt, int* t0, int* t1, bool* empty) {
+  const int64_t x0 = (int64_t)mt * kItemRows, x1 = min(x0 + kItemRows, (int64_t)q.n * a.group);
+  const int lo = see_from(a, q, (int)(x0 / a.group)), hi = see_to(a, q, (int)((x1 - 1) / a.group));
+  *empty = hi <= lo;
+  *t0 = *empty ? 0 : lo / kKv;
+  *t1 = *empty ? 1 : (hi + kKv - 1) / kKv;
+}
+__device__ __forceinline__ long long tiles_per_head(const AttendArgs& a, const Request& q) {
+  long long sum = 0;
+  if (!many(a, q)) return 0;
+  const int items = items_of(a, q);
+  for (int mt = 0; mt < items; ++mt) {
+    int t0, t1;
+    bool e;
+    item_span(a, q, mt, &t0, &t1, &e);
+    sum += t1 - t0;
+  }
+  return sum;
+}
+
+__device__ __forceinline__ void load_item(const AttendArgs& a, Segment& s) {
+  int t0, t1;
+  item_span(a, s.q, s.mt, &t0, &t1, &s.empty);
+  s.first_tile = t0;
+  s.tiles = t1 - t0;
+  const int64_t x0 = (int64_t)s.mt * kItemRows, all = (int64_t)s.q.n * a.group;
+  s.rows = (int)min((int64_t)kItemRows, all - x0);
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const int64_t b = x0 + y * kHalf, e = min(b + kHalf, all);
+    s.lo[y] = s.hi[y] = 0;
+    if (b < all) s.lo[y] = see_from(a, s.q, (int)(b / a.group)), s.hi[y] = see_to(a, s.q, (int)((e - 1) / a.group));
+  }
+}
+// To the next item; false past the last.
+__device__ __forceinline__ bool next_item(const AttendArgs& a, Segment& s) {
+  s.t = 0;
+  if (++s.mt < items_of(a, s.q)) {
+    load_item(a, s);
+    return true;
+  }
+  s.mt = 0;
+  if (++s.h < a.n_kv_heads) {
+    load_item(a, s);
+    return true;
+  }
+  s.h = 0;
+  do {
+    if (++s.r >= a.n_rows) return false;
+    s.q = request(a, s.r);
+  } while (!many(a, s.q));
+  load_item(a, s);
+  return true;
+}
+__device__ __forceinline__ bool active(const Segment& s, int half, int tile) {
+  return tile * kKv < s.hi[half] && (tile + 1) * kKv > s.lo[half];
+}
+
+// ---- tcgen05
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+// A 64-bit descriptor of an operand in shared memory, 128-byte rows permuted in 16-byte units by the
+// row's low three bits; lead: bytes between panels of 64 columns (rows of values only).
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)2 << 61;
+}
+// f16 x f16 with 32-bit sums, M = 128; b_rows: B is stored with its N side contiguous.
+__host__ __device__ constexpr uint32_t instruction(int n, bool b_rows) {
+  return 1u << 4 | (b_rows ? 1u << 16 : 0) | (uint32_t)(n / 8) << 17 | (uint32_t)(128 / 16) << 24;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a),
+      "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d), "r"(a),
+      "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void tm_load(uint32_t addr, uint32_t* r) {  // 32 columns
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+      "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+      "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// What a tile's groups of 16 tokens are scaled by: {ks, log2 vs, 1 / vs, -}, and which of them exist.
+struct TileInfo {
+  float4 g[kGroups];
+  uint32_t valid;
+};
+
+// The barriers and small shared state of a block.
+struct Shared {
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t q_full[2], s_full[2], p_full[2], o_full[2], go;
+  TileInfo info[4];
+  int nan_count[4];
+  int nan_pos[4][kNanList];
+  long long sum[kManyThreads / 32];
+  long long skip;
+  int row, dead;
+  uint32_t tmem;
+};
+
+// The end of a stretch: `count` tiles from s.t on that lie in s's item.
+#define HX_SEGMENTS(s, count)                                                                       \
+  for (int seg = min((count), (s).tiles - (s).t); (count) > 0;                                      \
+       (count) -= seg, (s).t += seg, seg = (count) > 0 && next_item(a, (s)) ? min((count), (s).tiles - (s).t) : (count))
+
+// ---- the converting warps
+
+template <int D>
+__device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* kbuf, uint8_t* vbuf) {
+  constexpr int kLanes = D / 16;           // lanes of a token, 16 bytes each
+  constexpr int kPer = 32 / kLanes;        // tokens of a warp's load
+  constexpr int kLoads = 32 / kPer;        // loads of a warp's 32 tokens
+  const int tid = threadIdx.x - 32 * kConvWarp, warp = tid >> 5, lane = tid & 31;
+  const int unit = lane % kLanes, sub = lane / kLanes;
+  const int block = 1 << a.block_shift;
+  int it = 0, seg_no = 0;
+  HX_SEGMENTS(s, count) {
+    if (s.empty) continue;
+    const int list = seg_no & 3;
+    if (tid == 0) sh->nan_count[list] = 0;
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    const int end = max(s.hi[0], s.hi[1]);
+    for (int i = 0; i < seg; ++i, ++it) {
+      const int st = it & 1;
+      const uint32_t phase = (it >> 1) & 1;
+      const int pos = (s.first_tile + s.t + i) * kKv;
+      // this warp's 32 tokens lie in one block of the cache, or in two of 16
+      int64_t at[2];
+      bool ok[2];
+      float ks[2] = {0, 0}, vs[2] = {0, 0};
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int p = pos + 32 * warp + 16 * x;
+        const int id = p < end ? a.block_table[s.r * a.table_stride + (p >> a.block_shift)] : -1;
+        ok[x] = (unsigned)id < (unsigned)a.n_blocks;
+        at[x] = 0;
+        if (ok[x]) {
+          at[x] = id * a.block_stride + ((int64_t)s.h * block + (p & (block - 1))) * D;
+          ks[x] = a.k_scale[id * a.scale_stride + s.h];
+          vs[x] = a.v_scale[id * a.scale_stride + s.h];
+        }
+      }
+      uint4 kr[kLoads], vr[kLoads];
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int tok = j * kPer + sub, x = tok >> 4;
+        const bool in = ok[x] && pos + 32 * warp + tok < end;
+        const int64_t o = at[x] + (tok & 15) * D + unit * 16;
+        kr[j] = in ? *(const uint4*)(a.k + o) : uint4{0, 0, 0, 0};
+        vr[j] = in ? *(const uint4*)(a.v + o) : uint4{0, 0, 0, 0};
+      }
+      // the tile's f16 rows: panels of 64 columns, 128-byte rows, 16-byte units permuted
+      const auto put = [&](uint8_t* buf, const uint4& u, int tok) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        uint8_t* row = buf + (unit >> 2) * (kKv * 128) + tok * 128;
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const int y = z ^ (unit >> 2 & 1);
+          const uint4 h = y ? uint4{cvt2(w[2]), cvt2_hi(w[2]), cvt2(w[3]), cvt2_hi(w[3])}
+                            : uint4{cvt2(w[0]), cvt2_hi(w[0]), cvt2(w[1]), cvt2_hi(w[1])};
+          *(uint4*)(row + (((2 * (unit & 3) + y) ^ (tok & 7)) << 4)) = h;
+        }
+      };
+      bar_wait(&sh->k_empty[st], phase ^ 1, &sh->dead);
+      if (lane < 2) {
+        const float r = fmaxf(lane ? vs[1] : vs[0], 0x1p-100f);
+        sh->info[it & 3].g[2 * warp + lane] = float4{lane ? ks[1] : ks[0], log2f(r), 1.f / r, 0.f};
+      }
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) put(kbuf + st * Many<D>::kTile, kr[j], 32 * warp + j * kPer + sub);
+      const uint32_t valid = (ok[0] ? 1u : 0u) | (ok[1] ? 2u : 0u);
+      if (lane == 0) ((uint8_t*)&sh->info[it & 3].valid)[warp] = (uint8_t)valid;
+      fence_async();
+      bar_arrive(&sh->k_full[st]);
+      bar_wait(&sh->v_empty[st], phase ^ 1, &sh->dead);
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        uint32_t* w = (uint32_t*)&vr[j];
+        uint32_t nan = 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) nan |= ((w[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+        if (nan) {
+          // a NaN would reach rows that do not see it (0 * NaN): taken out here, and put
+          // into the rows that see it at their end
+#pragma unroll
+          for (int x = 0; x < 4; ++x) w[x] &= ~(((((w[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
+          const int n = atomicAdd(&sh->nan_count[list], 1);
+          if (n < kNanList) sh->nan_pos[list][n] = pos + 32 * warp + j * kPer + sub;
+        }
+        put(vbuf + st * Many<D>::kTile, vr[j], 32 * warp + j * kPer + sub);
+      }
+      fence_async();
+      bar_arrive(&sh->v_full[st]);
+    }
+    ++seg_no;
+  }
+}
+
+// ---- the issuing thread
+
+template <int D>
+__device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, const uint8_t* qbuf, const uint8_t* kbuf,
+                      const uint8_t* vbuf) {
+  const uint32_t tm = sh->tmem;
+  uint32_t n_s[2] = {0, 0}, n_q = 0;  // products issued per half; items
+  int it = 0;
+  volatile int* dead = &sh->dead;
+  HX_SEGMENTS(s, count) {
+    if (s.empty) continue;
+    const auto scores = [&](int half, int st) {
+      // S's columns hold the last P: its product must have ended
+      if (n_s[half]) bar_wait(&sh->o_full[half], (n_s[half] - 1) & 1, dead);
+      tc_fence_after();
+      const uint32_t q = smem_addr(qbuf + half * Many<D>::kQBytes), k = smem_addr(kbuf + st * Many<D>::kTile);
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) {
+        const uint32_t o = (x >> 2) * (128 * 128) + (x & 3) * 32;
+        mma_ss(tm + half * kKv, operand(q + o, 16), operand(k + o, 16), instruction(kKv, false), x > 0);
+      }
+      tc_commit(&sh->s_full[half]);
+    };
+    bool has[2] = {false, false};  // a half's O holds something
+    const auto values = [&](int half, int st) {
+      bar_wait(&sh->p_full[half], n_s[half] & 1, dead);
+      tc_fence_after();
+      const uint32_t v = smem_addr(vbuf + st * Many<D>::kTile);
+#pragma unroll
+      for (int x = 0; x < kKv / 16; ++x)
+        mma_ts(tm + 256 + half * D, tm + half * kKv + 8 * x, operand(v + x * 2048, kKv * 128), instruction(D, true),
+               has[half] || x > 0);
+      has[half] = true;
+      tc_commit(&sh->o_full[half]);
+      ++n_s[half];
+    };
+    const int tile0 = s.first_tile + s.t;
+    bar_wait(&sh->q_full[0], n_q & 1, dead);
+    bar_wait(&sh->q_full[1], n_q & 1, dead);
+    ++n_q;
+    bar_arrive(&sh->go);  // no half's softmax is more than one item ahead of the other's
+    bar_wait(&sh->k_full[it & 1], (it >> 1) & 1, dead);
+    if (active(s, 0, tile0)) scores(0, it & 1);
+    if (active(s, 1, tile0)) scores(1, it & 1);
+    tc_commit(&sh->k_empty[it & 1]);
+    for (int i = 0; i < seg && !*dead; ++i, ++it) {
+      const int tile = tile0 + i, st = it & 1;
+      const uint32_t phase = (it >> 1) & 1;
+      const bool more = i + 1 < seg;
+      bar_wait(&sh->v_full[st], phase, dead);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (active(s, half, tile)) values(half, st);
+        if (half == 1) tc_commit(&sh->v_empty[st]);
+        if (more && half == 0) bar_wait(&sh->k_full[st ^ 1], ((it + 1) >> 1) & 1, dead);
+        if (more && active(s, half, tile + 1)) scores(half, st ^ 1);
+      }
+      if (more) tc_commit(&sh->k_empty[st ^ 1]);
+    }
+  }
+}
+
+// ---- the softmax warps
+
+template <class T>
+__device__ __forceinline__ float2 two(uint32_t u) {
+  if constexpr (std::is_same<T, __half>::value) return __half22float2(*(const __half2*)&u);
+  else return __bfloat1622float2(*(const __nv_bfloat162*)&u);
+}
+template <class T>
+__device__ __forceinline__ uint32_t pack(float x, float y) {
+  if constexpr (std::is_same<T, __half>::value) return pack_half(x, y);
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *(const uint32_t*)&h;
+}
+
+// The row's q in f16 times a power of two (so that no value leaves f16's range) to shared memory; the power.
+template <int D, class T>
+__device__ float put_q(const T* p, bool real, uint8_t* buf, int row) {
+  float amax = 0;
+  uint4 u[D / 8];
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) {
+    u[x] = real ? *(const uint4*)(p + 8 * x) : uint4{0, 0, 0, 0};
+    const uint32_t* w = (const uint32_t*)&u[x];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const float2 f = two<T>(w[y]);
+      amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+    }
+  }
+  int e = 0;
+  if (amax > 0 && amax < INFINITY) e = max((int)(__float_as_uint(amax) >> 23) - 127, -126);
+  const float down = __uint_as_float((unsigned)(127 - e) << 23);
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) {
+    const uint32_t* w = (const uint32_t*)&u[x];
+    uint32_t h[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const float2 f = two<T>(w[y]);
+      h[y] = pack_half(f.x * down, f.y * down);
+    }
+    *(uint4*)(buf + (x >> 3) * (kHalf * 128) + row * 128 + (((x & 7) ^ (row & 7)) << 4)) = uint4{h[0], h[1], h[2], h[3]};
+  }
+  return __uint_as_float((unsigned)(127 + e) << 23);
+}
+
+template <int D, class T>
+__device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* qbuf) {
+  constexpr float kLag = 8.f;
+  const int half = threadIdx.x >> 7, row = threadIdx.x & 127;
+  const uint32_t lanes = (threadIdx.x & 96) << 16;
+  const uint32_t ts = sh->tmem + lanes + half * kKv, to = sh->tmem + lanes + 256 + half * D;
+  int it = 0, seg_no = 0;
+  uint32_t n_s = 0;
+  volatile int* dead = &sh->dead;
+  HX_SEGMENTS(s, count) {
+    const int64_t x = (int64_t)s.mt * kItemRows + half * kHalf + row;
+    const bool real = half * kHalf + row < s.rows;
+    const int i = (int)(x / a.group), head = s.h * a.group + (int)(x % a.group);
+    const int64_t token = s.q.first + i;
+    T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
+    if (s.empty) {
+      if (real) {
+#pragma unroll
+        for (int y = 0; y < D / 8; ++y) *(uint4*)(out + 8 * y) = uint4{0, 0, 0, 0};
+        if (a.lse) a.lse[token * a.n_heads + head] = -INFINITY;
+      }
+      continue;
+    }
+    const float c = a.sm_scale_log2 * put_q<D, T>((const T*)a.q + token * a.q_token_stride + head * a.q_head_stride, real,
+                                                  qbuf + half * Many<D>::kQBytes, row);
+    fence_async();
+    bar_arrive(&sh->q_full[half]);
+    if (!__all_sync(~0u, bar_wait(&sh->go, seg_no & 1, dead))) break;
+    const int lo = real ? see_from(a, s.q, i) : 0, hi = real ? see_to(a, s.q, i) : 0;
+    // what all rows of the half see: [all_lo, all_hi)
+    const int64_t xb = (int64_t)s.mt * kItemRows + half * kHalf, xe = min(xb + kHalf, (int64_t)s.q.n * a.group);
+    const bool full_half = xb + kHalf <= (int64_t)s.q.n * a.group;
+    const int all_lo = full_half ? see_from(a, s.q, (int)((xe - 1) / a.group)) : 0x7fffffff;
+    const int all_hi = full_half ? see_to(a, s.q, (int)(xb / a.group)) : 0;
+
+    float m = -INFINITY, l = 0;
+    bool has = false;
+    for (int j = 0; j < seg && !__any_sync(~0u, *dead); ++j, ++it) {
+      const int tile = s.first_tile + s.t + j;
+      if (!active(s, half, tile)) continue;
+      const int pos = tile * kKv;
+      const TileInfo& info = sh->info[it & 3];
+      if (!bar_wait(&sh->s_full[half], n_s & 1, dead)) l = NAN;
+      tc_fence_after();
+      const uint32_t valid = info.valid;
+      const bool whole = valid == 0x03030303u && pos >= all_lo && pos + kKv <= all_hi;
+      // bit g of `exists`: group g has a block
+      const auto exists = [&](int g) { return (valid >> (8 * (g >> 1) + (g & 1))) & 1; };
+      float top = -INFINITY;
+#pragma unroll
+      for (int ch = 0; ch < 4; ++ch) {
+        uint32_t u[32];
+        tm_load(ts + 32 * ch, u);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const float4 z = info.g[2 * ch + g];
+          const float f = z.x * c;
+#pragma unroll
+          for (int y = 0; y < 16; ++y) {
+            float v = fmaf(__uint_as_float(u[16 * g + y]), f, z.y);
+            if (!whole) {
+              const int p = pos + 32 * ch + 16 * g + y;
+              if (p < lo || p >= hi || !exists(2 * ch + g)) v = -INFINITY;
+            }
+            top = fmaxf(top, v);
+          }
+        }
+      }
+      if (__any_sync(~0u, top > m + kLag)) {
+        const float z = fmaxf(m, top);
+        const float keep = z == -INFINITY ? 1.f : ex2(m - z);
+        m = z;
+        l *= keep;
+        if (has) {
+#pragma unroll
+          for (int ch = 0; ch < D / 32; ++ch) {
+            uint32_t u[32];
+            tm_load(to + 32 * ch, u);
+#pragma unroll
+            for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * keep);
+            tm_store32(to + 32 * ch, u);
+          }
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int ch = 0; ch < 4; ++ch) {
+        uint32_t u[32], w[16];
+        tm_load(ts + 32 * ch, u);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const float4 z = info.g[2 * ch + g];
+          const float f = z.x * c, b = z.y - base;
+          float sum = 0;
+#pragma unroll
+          for (int y = 0; y < 16; ++y) {
+            float v = fmaf(__uint_as_float(u[16 * g + y]), f, b);
+            if (!whole) {
+              const int p = pos + 32 * ch + 16 * g + y;
+              if (p < lo || p >= hi || !exists(2 * ch + g)) v = -INFINITY;
+            }
+            v = ex2(v);
+            sum += v;
+            u[16 * g + y] = __float_as_uint(v);
+          }
+          l = fmaf(sum, z.z, l);
+        }
+#pragma unroll
+        for (int y = 0; y < 16; ++y) w[y] = pack_half(__uint_as_float(u[2 * y]), __uint_as_float(u[2 * y + 1]));
+        tm_store16(ts + 16 * ch, w);
+      }
+      tm_stored();
+      tc_fence_before();
+      bar_arrive(&sh->p_full[half]);
+      has = true;
+      ++n_s;
+    }
+
+    if (has) {
+      if (!bar_wait(&sh->o_full[half], (n_s - 1) & 1, dead)) l = NAN;
+      tc_fence_after();
+    }
+    const bool done = seg == s.tiles;
+    const int64_t slot = 2 * blockIdx.x + (s.t == 0);
+    float* part = a.part + (slot * kItemRows + half * kHalf + row) * D;
+    const bool none = l == 0;
+    const float inv = done ? (none ? 0.f : 1.f / l) : 1.f;
+    // NaN among the values that this row sees
+    const int list = seg_no & 3;
+    int nans = 0;
+    if (has) nans = sh->nan_count[list];
+    uint32_t nan_cols[D / 32] = {};
+    if (nans && real) {
+      const int p0 = max(lo, (s.first_tile + s.t) * kKv), p1 = min(hi, (s.first_tile + s.t + seg) * kKv);
+      const bool listed = nans <= kNanList;
+      for (int e = listed ? 0 : p0; e < (listed ? nans : p1); ++e) {
+        const int p = listed ? sh->nan_pos[list][e] : e;
+        if (p < p0 || p >= p1) continue;
+        const int id = a.block_table[s.r * a.table_stride + (p >> a.block_shift)];
+        if ((unsigned)id >= (unsigned)a.n_blocks) continue;
+        const int block = 1 << a.block_shift;
+        const uint32_t* v = (const uint32_t*)(a.v + id * a.block_stride + ((int64_t)s.h * block + (p & (block - 1))) * D);
+#pragma unroll
+        for (int y = 0; y < D / 4; ++y) {
+          const uint32_t f = (((v[y] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+          nan_cols[y >> 3] |= ((f & 1) | (f >> 7 & 2) | (f >> 14 & 4) | (f >> 21 & 8)) << (4 * (y & 7));
+        }
+      }
+    }
+#pragma unroll
+    for (int ch = 0; ch < D / 32; ++ch) {
+      uint32_t u[32];
+      if (has) tm_load(to + 32 * ch, u);
+#pragma unroll
+      for (int y = 0; y < 32; ++y) {
+        float o = has && !none ? __uint_as_float(u[y]) * inv : 0.f;
+        if (nan_cols[ch] >> y & 1) o = NAN;
+        u[y] = __float_as_uint(o);
+      }
+      if (!real) continue;
+      if (done) {
+#pragma unroll
+        for (int y = 0; y < 32; y += 8) {
+          uint4 w;
+          w.x = pack<T>(__uint_as_float(u[y]), __uint_as_float(u[y + 1]));
+          w.y = pack<T>(__uint_as_float(u[y + 2]), __uint_as_float(u[y + 3]));
+          w.z = pack<T>(__uint_as_float(u[y + 4]), __uint_as_float(u[y + 5]));
+          w.w = pack<T>(__uint_as_float(u[y + 6]), __uint_as_float(u[y + 7]));
+          *(uint4*)(out + 32 * ch + y) = w;
+        }
+      } else {
+#pragma unroll
+        for (int y = 0; y < 32; y += 4) *(uint4*)(part + 32 * ch + y) = uint4{u[y], u[y + 1], u[y + 2], u[y + 3]};
+      }
+    }
+    if (real) {
+      if (!done) *(float2*)(a.part_ml + (slot * kItemRows + half * kHalf + row) * 2) = float2{m, l};
+      else if (a.lse) a.lse[token * a.n_heads + head] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    }
+    tc_fence_before();
+    ++seg_no;
+  }
+}
+
+template <int D, class T>
+__global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __grid_constant__ AttendArgs a) {
+  extern __shared__ uint8_t s_raw[];
+  __shared__ __align__(16) Shared sh;
+  uint8_t* qbuf = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* kbuf = qbuf + 2 * Many<D>::kQBytes;
+  uint8_t* vbuf = kbuf + 2 * Many<D>::kTile;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("griddepcontrol.launch_dependents;");
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      bar_init(&sh.k_full[i], 128), bar_init(&sh.v_full[i], 128);
+      bar_init(&sh.k_empty[i], 1), bar_init(&sh.v_empty[i], 1);
+      bar_init(&sh.q_full[i], 128), bar_init(&sh.s_full[i], 1), bar_init(&sh.p_full[i], 128), bar_init(&sh.o_full[i], 1);
+    }
+    bar_init(&sh.go, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    sh.dead = 0;
+    sh.row = -1;
+  }
+
+  // this block's stretch of all tiles
+  const int per = (a.n_rows + kManyThreads - 1) / kManyThreads;
+  const int r0 = min(a.n_rows, tid * per), r1 = min(a.n_rows, r0 + per);
+  long long mine = 0;
+  for (int r = r0; r < r1; ++r) mine += tiles_per_head(a, request(a, r)) * a.n_kv_heads;
+  long long upto = mine;
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long o = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 31) sh.sum[warp] = upto;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kManyThreads / 32; ++w) {
+    if (w < warp) before += sh.sum[w];
+    total += sh.sum[w];
+  }
+  before += upto - mine;
+  const long long G = max(1LL, min((long long)gridDim.x, total)), b = blockIdx.x;
+  const long long n0 = b < G ? total * b / G : 0, n1 = b < G ? total * (b + 1) / G : 0;
+  if (n0 < n1 && before <= n0 && n0 < before + mine) {
+    int r = r0;
+    for (;; ++r) {
+      const long long x = tiles_per_head(a, request(a, r)) * a.n_kv_heads;
+      if (n0 < before + x) break;
+      before += x;
+    }
+    sh.row = r;
+    sh.skip = n0 - before;
+  }
+  __syncthreads();
+  if (sh.row < 0) {
+    if (tid == 0) a.joins[b] = int4{0, 0, -1, 0};
+    return;
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sh.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  Segment s;
+  s.r = sh.row;
+  s.q = request(a, s.r);
+  long long skip = sh.skip;
+  {
+    const long long head = tiles_per_head(a, s.q);
+    s.h = (int)(skip / head);
+    skip %= head;
+    for (s.mt = 0;; ++s.mt) {
+      int t0, t1;
+      bool e;
+      item_span(a, s.q, s.mt, &t0, &t1, &e);
+      if (skip < t1 - t0) break;
+      skip -= t1 - t0;
+    }
+  }
+  load_item(a, s);
+  s.t = (int)skip;
+  int count = (int)(n1 - n0);
+  if (tid == 0) {
+    // an item that began in an earlier block and ends in this one is joined here
+    int4 join = {0, 0, -1, 0};
+    if (skip > 0 && skip + count >= s.tiles) {
+      const long long f0 = n0 - skip;
+      long long c = f0 * G / total;
+      while (total * (c + 1) / G <= f0) ++c;
+      while (total * c / G > f0) --c;
+      join = int4{s.r, s.h, (int)c, s.mt};
+    }
+    a.joins[b] = join;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp < kConvWarp) softmax<D, T>(a, s, count, &sh, qbuf);
+  else if (warp < kMmaWarp) convert<D>(a, s, count, &sh, kbuf, vbuf);
+  else if (lane == 0) issue<D>(a, s, count, &sh, qbuf, kbuf, vbuf);
+  __syncwarp();
+  drain(&sh.dead);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem) : "memory");
+}
+
+template <int D, class T>
+cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t s) {
+  const auto kernel = hx_kv_attend_many<D, T>;
+  if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Many<D>::kSmem)) return e;
+  kernel<<<blocks, kManyThreads, Many<D>::kSmem, s>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attend_many(const AttendArgs& a, int head_dim, bool bf16, int blocks, cudaStream_t s) {
+  if (head_dim == 128) return bf16 ? launch<128, __nv_bfloat16>(a, blocks, s) : launch<128, __half>(a, blocks, s);
+  return bf16 ? launch<64, __nv_bfloat16>(a, blocks, s) : launch<64, __half>(a, blocks, s);
+}
+
+}  // namespace hx
