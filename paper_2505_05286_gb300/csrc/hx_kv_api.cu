@@ -41,6 +41,8 @@ int check_query(const hx_kv_cache* c, const hx_kv_query* a) {
   if (a->n_rows < 1 || a->n_rows > HX_KV_MAX_ROWS) return bad("queries: n_rows must be 1..65536");
   if (a->n_heads < 1 || a->n_heads % c->n_kv_heads || a->n_heads / c->n_kv_heads > 128)
     return bad("queries: n_heads must be a multiple of n_kv_heads, at most 128 times it");
+  if ((int64_t)a->n_tokens * (a->n_heads / c->n_kv_heads) > HX_KV_MAX_TOKENS)
+    return bad("queries: n_tokens * (n_heads / n_kv_heads) must be at most 2^30");
   if (a->dtype != HX_BF16 && a->dtype != HX_F16) return bad("queries: dtype must be bf16 or f16");
   if (a->max_q < 0) return bad("queries: max_q is negative");
   if (a->causal != 0 && a->causal != 1) return bad("queries: causal must be 0 or 1");

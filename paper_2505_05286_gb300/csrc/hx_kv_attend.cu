@@ -56,7 +56,7 @@ __device__ __forceinline__ int tiles_of(const AttendArgs& a, const Request& q, i
   *first_tile = 0;
   if (q.n == 0) return 0;
   if (q.kv == 0) return 1;
-  if ((int64_t)q.n * a.group > a.few_rows) return 0;
+  if (q.n * a.group > a.few_rows) return 0;
   *first_tile = see_from(a, q, 0) / NT;
   return (q.kv + NT - 1) / NT - *first_tile;
 }
@@ -856,6 +856,7 @@ AttendArgs args_of(const hx_kv_cache& c, const hx_kv_query& q) {
   a.table_width = q.table_width, a.n_blocks = c.n_blocks, a.n_tokens = q.n_tokens, a.n_rows = q.n_rows;
   a.n_heads = q.n_heads, a.n_kv_heads = c.n_kv_heads, a.group = q.n_heads / c.n_kv_heads;
   while ((1 << a.block_shift) < c.block_tokens) ++a.block_shift;
+  a.by_group = divisor(a.group);
   a.max_q = q.max_q, a.causal = q.causal;
   a.window = q.window >= (1 << 30) ? 0 : q.window;  // no request holds so many tokens
   a.sm_scale_log2 = q.sm_scale * kLog2e;

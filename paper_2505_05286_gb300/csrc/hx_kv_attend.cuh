@@ -14,6 +14,22 @@ namespace hx {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kItemRows = 256;  // rows of an item of the many-rows kernel
 
+// Division by a divisor known on the host (Granlund and Montgomery's invariant
+// division): x / d for 0 <= x < 2^31.
+struct Divisor {
+  uint32_t mul, shift;
+  int32_t d;
+#ifdef __CUDACC__
+  __device__ __forceinline__ int of(int x) const { return (int)((__umulhi((uint32_t)x, mul) + (uint32_t)x) >> shift); }
+  __device__ __forceinline__ int rest(int x) const { return x - of(x) * d; }
+#endif
+};
+inline Divisor divisor(int32_t d) {
+  uint32_t s = 0;
+  while ((1u << s) < (uint32_t)d) ++s;
+  return {(uint32_t)((((1ull << s) - (uint32_t)d) << 32) / (uint32_t)d + 1), s, d};
+}
+
 // What the kernels read of hx_kv_cache and hx_kv_query.
 struct AttendArgs {
   const uint8_t* k;
@@ -32,6 +48,7 @@ struct AttendArgs {
   int32_t table_width, n_blocks, n_tokens, n_rows, n_heads, n_kv_heads, group;
   int32_t block_shift, max_q, causal, window;
   int32_t few_rows;     // requests of so many rows at most are the few-rows kernel's
+  Divisor by_group;     // rows to tokens
   float sm_scale_log2;  // sm_scale * log2(e): scores are exponents of two
   float* part;          // partial results of items that several blocks share
   float* part_ml;

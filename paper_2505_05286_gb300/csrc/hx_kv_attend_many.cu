@@ -16,7 +16,8 @@ namespace {
 // second kernel).  In a block,
 //   4 warps turn the tiles' e4m3 into f16 in shared memory, in the layout that tcgen05 reads
 //     (both halves use each: the conversion is paid once for 256 rows),
-//   1 thread issues the products: S = Q K^T into tensor memory, O += P V with P read from
+//   3 warps put the item's q beside them,
+//   1 warp issues the products: S = Q K^T into tensor memory, O += P V with P read from
 //     tensor memory, the halves alternating, so that one half's products run while the other's
 //     softmax does,
 //   2 x 4 warps do a half's softmax, a row to a thread, and write P over S.
@@ -30,8 +31,9 @@ namespace {
 constexpr int kHalf = 128;
 constexpr int kKv = 128;       // tokens of a tile
 constexpr int kGroups = kKv / 16;
-constexpr int kConvWarp = 8, kMmaWarp = 12;
-constexpr int kManyThreads = 32 * 13;
+constexpr int kConvWarp = 8, kMmaWarp = 12, kQueryWarp = 13;
+constexpr int kQueryWarps = 3;
+constexpr int kManyThreads = 32 * (kQueryWarp + kQueryWarps);
 constexpr int kNanList = 64;
 
 template <int D>
@@ -52,28 +54,44 @@ struct Segment {  // a stretch of one item's tiles
 };
 
 __device__ __forceinline__ bool many(const AttendArgs& a, const Request& q) {
-  return q.kv > 0 && (int64_t)q.n * a.group > a.few_rows;
+  return q.kv > 0 && q.n * a.group > a.few_rows;
 }
 __device__ __forceinline__ int items_of(const AttendArgs& a, const Request& q) {
-  return (int)(((int64_t)q.n * a.group + kItemRows - 1) / kItemRows);
+  return (q.n * a.group + kItemRows - 1) / kItemRows;
 }
 // First and end tile of item mt of a request (at least one, to write its zeros).
 __device__ __forceinline__ void item_span(const AttendArgs& a, const Request& q, int mt, int* t0, int* t1, bool* empty) {
-  const int64_t x0 = (int64_t)mt * kItemRows, x1 = min(x0 + kItemRows, (int64_t)q.n * a.group);
-  const int lo = see_from(a, q, (int)(x0 / a.group)), hi = see_to(a, q, (int)((x1 - 1) / a.group));
+  const int x0 = mt * kItemRows, x1 = min(x0 + kItemRows, q.n * a.group);
+  const int lo = see_from(a, q, a.by_group.of(x0)), hi = see_to(a, q, a.by_group.of(x1 - 1));
   *empty = hi <= lo;
   *t0 = *empty ? 0 : lo / kKv;
   *t1 = *empty ? 1 : (hi + kKv - 1) / kKv;
 }
-__device__ __forceinline__ long long tiles_per_head(const AttendArgs& a, const Request& q) {
+__device__ __forceinline__ int item_tiles(const AttendArgs& a, const Request& q, int mt) {
+  int t0, t1;
+  bool e;
+  item_span(a, q, mt, &t0, &t1, &e);
+  return t1 - t0;
+}
+__device__ __forceinline__ long long warp_sum(long long x) {
+  for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+  return x;
+}
+// Tiles of a request's items for one kv head, for the 32 rows of a warp's lanes: a request of few
+// items by its lane, one of many by all lanes together.
+__device__ long long tiles_per_head(const AttendArgs& a, const Request& q, bool real) {
+  const int lane = threadIdx.x & 31, items = real && many(a, q) ? items_of(a, q) : 0;
   long long sum = 0;
-  if (!many(a, q)) return 0;
-  const int items = items_of(a, q);
-  for (int mt = 0; mt < items; ++mt) {
-    int t0, t1;
-    bool e;
-    item_span(a, q, mt, &t0, &t1, &e);
-    sum += t1 - t0;
+  if (items <= 8)
+    for (int mt = 0; mt < items; ++mt) sum += item_tiles(a, q, mt);
+  for (unsigned big = __ballot_sync(~0u, items > 8); big; big &= big - 1) {
+    const int src = __ffs(big) - 1;
+    const Request o = {__shfl_sync(~0u, q.first, src), __shfl_sync(~0u, q.n, src), __shfl_sync(~0u, q.kv, src)};
+    const int n = items_of(a, o);
+    long long part = 0;
+    for (int mt = lane; mt < n; mt += 32) part += item_tiles(a, o, mt);
+    part = warp_sum(part);
+    if (lane == src) sum = part;
   }
   return sum;
 }
@@ -83,13 +101,13 @@ __device__ __forceinline__ void load_item(const AttendArgs& a, Segment& s) {
   item_span(a, s.q, s.mt, &t0, &t1, &s.empty);
   s.first_tile = t0;
   s.tiles = t1 - t0;
-  const int64_t x0 = (int64_t)s.mt * kItemRows, all = (int64_t)s.q.n * a.group;
-  s.rows = (int)min((int64_t)kItemRows, all - x0);
+  const int x0 = s.mt * kItemRows, all = s.q.n * a.group;
+  s.rows = min(kItemRows, all - x0);
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
-    const int64_t b = x0 + y * kHalf, e = min(b + kHalf, all);
+    const int b = x0 + y * kHalf, e = min(b + kHalf, all);
     s.lo[y] = s.hi[y] = 0;
-    if (b < all) s.lo[y] = see_from(a, s.q, (int)(b / a.group)), s.hi[y] = see_to(a, s.q, (int)((e - 1) / a.group));
+    if (b < all) s.lo[y] = see_from(a, s.q, a.by_group.of(b)), s.hi[y] = see_to(a, s.q, a.by_group.of(e - 1));
   }
 }
 // To the next item; false past the last.
@@ -180,6 +198,21 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t* r) {
 }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Two 32-bit values at once.
+__device__ __forceinline__ float2 both(float x) { return float2{x, x}; }
+__device__ __forceinline__ float2 pair(uint32_t x, uint32_t y) { return float2{__uint_as_float(x), __uint_as_float(y)}; }
+__device__ __forceinline__ uint64_t bits(float2 x) { return (uint64_t)__float_as_uint(x.y) << 32 | __float_as_uint(x.x); }
+__device__ __forceinline__ float2 floats(uint64_t x) { return pair((uint32_t)x, (uint32_t)(x >> 32)); }
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(x)), "l"(bits(y)), "l"(bits(z)));
+  return floats(r);
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(x)), "l"(bits(y)));
+  return floats(r);
+}
 // What a tile's groups of 16 tokens are scaled by: {ks, log2 vs, 1 / vs, -}, and which of them exist.
 struct TileInfo {
   float4 g[kGroups];
@@ -189,13 +222,14 @@ struct TileInfo {
 // The barriers and small shared state of a block.
 struct Shared {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t q_full[2], s_full[2], p_full[2], o_full[2], go;
+  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], go[2], ended[2][2];  // go and ended: of even and odd items
+  float q_scale[2][kItemRows];
   TileInfo info[4];
   int nan_count[4];
   int nan_pos[4][kNanList];
   long long sum[kManyThreads / 32];
-  long long skip;
-  int row, dead;
+  long long skip;  // tiles of the item before this block's stretch
+  int row, head, mt, dead;
   uint32_t tmem;
 };
 
@@ -203,163 +237,6 @@ struct Shared {
 #define HX_SEGMENTS(s, count)                                                                       \
   for (int seg = min((count), (s).tiles - (s).t); (count) > 0;                                      \
        (count) -= seg, (s).t += seg, seg = (count) > 0 && next_item(a, (s)) ? min((count), (s).tiles - (s).t) : (count))
-
-// ---- the converting warps
-
-template <int D>
-__device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* kbuf, uint8_t* vbuf) {
-  constexpr int kLanes = D / 16;           // lanes of a token, 16 bytes each
-  constexpr int kPer = 32 / kLanes;        // tokens of a warp's load
-  constexpr int kLoads = 32 / kPer;        // loads of a warp's 32 tokens
-  const int tid = threadIdx.x - 32 * kConvWarp, warp = tid >> 5, lane = tid & 31;
-  const int unit = lane % kLanes, sub = lane / kLanes;
-  const int block = 1 << a.block_shift;
-  int it = 0, seg_no = 0;
-  HX_SEGMENTS(s, count) {
-    if (s.empty) continue;
-    const int list = seg_no & 3;
-    if (tid == 0) sh->nan_count[list] = 0;
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    const int end = max(s.hi[0], s.hi[1]);
-    for (int i = 0; i < seg; ++i, ++it) {
-      const int st = it & 1;
-      const uint32_t phase = (it >> 1) & 1;
-      const int pos = (s.first_tile + s.t + i) * kKv;
-      // this warp's 32 tokens lie in one block of the cache, or in two of 16
-      int64_t at[2];
-      bool ok[2];
-      float ks[2] = {0, 0}, vs[2] = {0, 0};
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int p = pos + 32 * warp + 16 * x;
-        const int id = p < end ? a.block_table[s.r * a.table_stride + (p >> a.block_shift)] : -1;
-        ok[x] = (unsigned)id < (unsigned)a.n_blocks;
-        at[x] = 0;
-        if (ok[x]) {
-          at[x] = id * a.block_stride + ((int64_t)s.h * block + (p & (block - 1))) * D;
-          ks[x] = a.k_scale[id * a.scale_stride + s.h];
-          vs[x] = a.v_scale[id * a.scale_stride + s.h];
-        }
-      }
-      uint4 kr[kLoads], vr[kLoads];
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int tok = j * kPer + sub, x = tok >> 4;
-        const bool in = ok[x] && pos + 32 * warp + tok < end;
-        const int64_t o = at[x] + (tok & 15) * D + unit * 16;
-        kr[j] = in ? *(const uint4*)(a.k + o) : uint4{0, 0, 0, 0};
-        vr[j] = in ? *(const uint4*)(a.v + o) : uint4{0, 0, 0, 0};
-      }
-      // the tile's f16 rows: panels of 64 columns, 128-byte rows, 16-byte units permuted
-      const auto put = [&](uint8_t* buf, const uint4& u, int tok) {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        uint8_t* row = buf + (unit >> 2) * (kKv * 128) + tok * 128;
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const int y = z ^ (unit >> 2 & 1);
-          const uint4 h = y ? uint4{cvt2(w[2]), cvt2_hi(w[2]), cvt2(w[3]), cvt2_hi(w[3])}
-                            : uint4{cvt2(w[0]), cvt2_hi(w[0]), cvt2(w[1]), cvt2_hi(w[1])};
-          *(uint4*)(row + (((2 * (unit & 3) + y) ^ (tok & 7)) << 4)) = h;
-        }
-      };
-      bar_wait(&sh->k_empty[st], phase ^ 1, &sh->dead);
-      if (lane < 2) {
-        const float r = fmaxf(lane ? vs[1] : vs[0], 0x1p-100f);
-        sh->info[it & 3].g[2 * warp + lane] = float4{lane ? ks[1] : ks[0], log2f(r), 1.f / r, 0.f};
-      }
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) put(kbuf + st * Many<D>::kTile, kr[j], 32 * warp + j * kPer + sub);
-      const uint32_t valid = (ok[0] ? 1u : 0u) | (ok[1] ? 2u : 0u);
-      if (lane == 0) ((uint8_t*)&sh->info[it & 3].valid)[warp] = (uint8_t)valid;
-      fence_async();
-      bar_arrive(&sh->k_full[st]);
-      bar_wait(&sh->v_empty[st], phase ^ 1, &sh->dead);
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        uint32_t* w = (uint32_t*)&vr[j];
-        uint32_t nan = 0;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) nan |= ((w[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-        if (nan) {
-          // a NaN would reach rows that do not see it (0 * NaN): taken out here, and put
-          // into the rows that see it at their end
-#pragma unroll
-          for (int x = 0; x < 4; ++x) w[x] &= ~(((((w[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
-          const int n = atomicAdd(&sh->nan_count[list], 1);
-          if (n < kNanList) sh->nan_pos[list][n] = pos + 32 * warp + j * kPer + sub;
-        }
-        put(vbuf + st * Many<D>::kTile, vr[j], 32 * warp + j * kPer + sub);
-      }
-      fence_async();
-      bar_arrive(&sh->v_full[st]);
-    }
-    ++seg_no;
-  }
-}
-
-// ---- the issuing thread
-
-template <int D>
-__device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, const uint8_t* qbuf, const uint8_t* kbuf,
-                      const uint8_t* vbuf) {
-  const uint32_t tm = sh->tmem;
-  uint32_t n_s[2] = {0, 0}, n_q = 0;  // products issued per half; items
-  int it = 0;
-  volatile int* dead = &sh->dead;
-  HX_SEGMENTS(s, count) {
-    if (s.empty) continue;
-    const auto scores = [&](int half, int st) {
-      // S's columns hold the last P: its product must have ended
-      if (n_s[half]) bar_wait(&sh->o_full[half], (n_s[half] - 1) & 1, dead);
-      tc_fence_after();
-      const uint32_t q = smem_addr(qbuf + half * Many<D>::kQBytes), k = smem_addr(kbuf + st * Many<D>::kTile);
-#pragma unroll
-      for (int x = 0; x < D / 16; ++x) {
-        const uint32_t o = (x >> 2) * (128 * 128) + (x & 3) * 32;
-        mma_ss(tm + half * kKv, operand(q + o, 16), operand(k + o, 16), instruction(kKv, false), x > 0);
-      }
-      tc_commit(&sh->s_full[half]);
-    };
-    bool has[2] = {false, false};  // a half's O holds something
-    const auto values = [&](int half, int st) {
-      bar_wait(&sh->p_full[half], n_s[half] & 1, dead);
-      tc_fence_after();
-      const uint32_t v = smem_addr(vbuf + st * Many<D>::kTile);
-#pragma unroll
-      for (int x = 0; x < kKv / 16; ++x)
-        mma_ts(tm + 256 + half * D, tm + half * kKv + 8 * x, operand(v + x * 2048, kKv * 128), instruction(D, true),
-               has[half] || x > 0);
-      has[half] = true;
-      tc_commit(&sh->o_full[half]);
-      ++n_s[half];
-    };
-    const int tile0 = s.first_tile + s.t;
-    bar_wait(&sh->q_full[0], n_q & 1, dead);
-    bar_wait(&sh->q_full[1], n_q & 1, dead);
-    ++n_q;
-    bar_arrive(&sh->go);  // no half's softmax is more than one item ahead of the other's
-    bar_wait(&sh->k_full[it & 1], (it >> 1) & 1, dead);
-    if (active(s, 0, tile0)) scores(0, it & 1);
-    if (active(s, 1, tile0)) scores(1, it & 1);
-    tc_commit(&sh->k_empty[it & 1]);
-    for (int i = 0; i < seg && !*dead; ++i, ++it) {
-      const int tile = tile0 + i, st = it & 1;
-      const uint32_t phase = (it >> 1) & 1;
-      const bool more = i + 1 < seg;
-      bar_wait(&sh->v_full[st], phase, dead);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (active(s, half, tile)) values(half, st);
-        if (half == 1) tc_commit(&sh->v_empty[st]);
-        if (more && half == 0) bar_wait(&sh->k_full[st ^ 1], ((it + 1) >> 1) & 1, dead);
-        if (more && active(s, half, tile + 1)) scores(half, st ^ 1);
-      }
-      if (more) tc_commit(&sh->k_empty[st ^ 1]);
-    }
-  }
-}
-
-// ---- the softmax warps
 
 template <class T>
 __device__ __forceinline__ float2 two(uint32_t u) {
@@ -373,40 +250,287 @@ __device__ __forceinline__ uint32_t pack(float x, float y) {
   return *(const uint32_t*)&h;
 }
 
-// The row's q in f16 times a power of two (so that no value leaves f16's range) to shared memory; the power.
-template <int D, class T>
-__device__ float put_q(const T* p, bool real, uint8_t* buf, int row) {
-  float amax = 0;
-  uint4 u[D / 8];
+// ---- the converting warps
+
+// Loads run ahead of the conversion: a tile's keys are asked for as soon as the registers of the one
+// before are written out, its block numbers a tile earlier.
+template <int D>
+__device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* kbuf, uint8_t* vbuf) {
+  constexpr int kLanes = D / 16;           // lanes of a token, 16 bytes each
+  constexpr int kPer = 32 / kLanes;        // tokens of a warp's load
+  constexpr int kLoads = 32 / kPer;        // loads of a warp's 32 tokens
+  const int tid = threadIdx.x - 32 * kConvWarp, warp = tid >> 5, lane = tid & 31;
+  const int unit = lane % kLanes, sub = lane / kLanes;
+  const int block = 1 << a.block_shift;
+  int seg_no = 0;
+
+  // this warp's 32 tokens of a tile lie in one block of the cache, or in two of 16
+  int pos, end, id[2];
+  int64_t at[2];
+  float ks[2], vs[2];
+  uint4 kr[kLoads], vr[kLoads];
+  const auto numbers = [&] {
+    pos = (s.first_tile + s.t) * kKv + 32 * warp;
+    end = max(s.hi[0], s.hi[1]);
 #pragma unroll
-  for (int x = 0; x < D / 8; ++x) {
-    u[x] = real ? *(const uint4*)(p + 8 * x) : uint4{0, 0, 0, 0};
-    const uint32_t* w = (const uint32_t*)&u[x];
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const float2 f = two<T>(w[y]);
-      amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+    for (int x = 0; x < 2; ++x) {
+      const int p = pos + 16 * x;
+      id[x] = p < end ? a.block_table[s.r * a.table_stride + (p >> a.block_shift)] : -1;
     }
-  }
-  int e = 0;
-  if (amax > 0 && amax < INFINITY) e = max((int)(__float_as_uint(amax) >> 23) - 127, -126);
-  const float down = __uint_as_float((unsigned)(127 - e) << 23);
+  };
+  const auto places = [&] {
 #pragma unroll
-  for (int x = 0; x < D / 8; ++x) {
-    const uint32_t* w = (const uint32_t*)&u[x];
-    uint32_t h[4];
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const float2 f = two<T>(w[y]);
-      h[y] = pack_half(f.x * down, f.y * down);
+    for (int x = 0; x < 2; ++x) {
+      ks[x] = vs[x] = 0;
+      at[x] = -1;
+      if ((unsigned)id[x] < (unsigned)a.n_blocks) {
+        at[x] = id[x] * a.block_stride + ((int64_t)s.h * block + ((pos + 16 * x) & (block - 1))) * D + unit * 16;
+        ks[x] = a.k_scale[id[x] * a.scale_stride + s.h];
+        vs[x] = a.v_scale[id[x] * a.scale_stride + s.h];
+      }
     }
-    *(uint4*)(buf + (x >> 3) * (kHalf * 128) + row * 128 + (((x & 7) ^ (row & 7)) << 4)) = uint4{h[0], h[1], h[2], h[3]};
+  };
+  const auto fetch = [&](const uint8_t* from, uint4* to) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int tok = j * kPer + sub;
+      const int64_t o = (j * kPer) >> 4 ? at[1] : at[0];
+      to[j] = o >= 0 && pos + tok < end ? *(const uint4*)(from + o + (tok & 15) * D) : uint4{0, 0, 0, 0};
+    }
+  };
+  // the tile's f16 rows: panels of 64 columns, 128-byte rows, 16-byte units permuted
+  const auto put = [&](uint8_t* buf, const uint4& u, int tok) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint8_t* row = buf + (unit >> 2) * (kKv * 128) + tok * 128;
+    const bool odd = unit >> 2 & 1;
+    uint4 h[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) h[y] = uint4{cvt2(w[2 * y]), cvt2_hi(w[2 * y]), cvt2(w[2 * y + 1]), cvt2_hi(w[2 * y + 1])};
+    // the two halves of the lanes take their two units in opposite order: all on different banks
+    *(uint4*)(row + (((2 * (unit & 3) + odd) ^ (tok & 7)) << 4)) = odd ? h[1] : h[0];
+    *(uint4*)(row + (((2 * (unit & 3) + !odd) ^ (tok & 7)) << 4)) = odd ? h[0] : h[1];
+  };
+  // items that see nothing have one tile, and nothing in it
+  const auto skip_empty = [&] {
+    while (count > 0 && s.empty)
+      if (--count > 0) next_item(a, s);
+  };
+
+  skip_empty();
+  if (count <= 0) return;
+  numbers();
+  places();
+  fetch(a.k, kr);
+  fetch(a.v, vr);
+  bool first = true;
+  for (int it = 0;; ++it) {
+    const int st = it & 1, here = pos;
+    const uint32_t phase = (it >> 1) & 1;
+    bar_wait(&sh->k_empty[st], phase ^ 1, &sh->dead);
+    TileInfo& info = sh->info[it & 3];
+    if (lane < 2) {
+      const float r = fmaxf(lane ? vs[1] : vs[0], 0x1p-100f);
+      info.g[2 * warp + lane] = float4{lane ? ks[1] : ks[0], log2f(r), 1.f / r, 0.f};
+    }
+    if (lane == 0) ((uint8_t*)&info.valid)[warp] = (uint8_t)((at[0] >= 0 ? 1 : 0) | (at[1] >= 0 ? 2 : 0));
+    const int list = seg_no & 3;
+    if (first) {
+      if (tid == 0) sh->nan_count[list] = 0;
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
+    // the next tile
+    --count;
+    first = false;
+    if (count > 0 && ++s.t == s.tiles) {
+      next_item(a, s);
+      skip_empty();
+      first = true;
+      ++seg_no;
+    }
+    const bool more = count > 0;
+    if (more) numbers();
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) put(kbuf + st * Many<D>::kTile, kr[j], 32 * warp + j * kPer + sub);
+    fence_async();
+    bar_arrive(&sh->k_full[st]);
+    if (more) {
+      places();
+      fetch(a.k, kr);
+    }
+    bar_wait(&sh->v_empty[st], phase ^ 1, &sh->dead);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      uint32_t* w = (uint32_t*)&vr[j];
+      uint32_t nan = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) nan |= (w[x] & 0x7f7f7f7fu) + 0x01010101u;
+      if (nan & 0x80808080u) {
+        // a NaN would reach rows that do not see it (0 * NaN): taken out here, and put
+        // into the rows that see it at their end
+#pragma unroll
+        for (int x = 0; x < 4; ++x) w[x] &= ~(((((w[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
+        const int n = atomicAdd(&sh->nan_count[list], 1);
+        if (n < kNanList) sh->nan_pos[list][n] = here + j * kPer + sub;
+      }
+      put(vbuf + st * Many<D>::kTile, vr[j], 32 * warp + j * kPer + sub);
+    }
+    fence_async();
+    bar_arrive(&sh->v_full[st]);
+    if (!more) break;
+    fetch(a.v, vr);
   }
-  return __uint_as_float((unsigned)(127 + e) << 23);
 }
 
+// ---- the query warps
+
+// Both halves' q in f16 times a power of two for each row (so that no value leaves f16's range), as soon as
+// the last item's products have read theirs.
 template <int D, class T>
-__device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* qbuf) {
+__device__ void queries(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* qbuf) {
+  constexpr int kLanes = D / 8, kPer = 32 / kLanes;  // lanes of a row, rows of a warp's load
+  constexpr int kStep = kPer * kQueryWarps, kLoads = (kHalf + kStep - 1) / kStep;
+  const int warp = (threadIdx.x >> 5) - kQueryWarp, lane = threadIdx.x & 31;
+  const int unit = lane % kLanes, sub = warp * kPer + lane / kLanes;
+  int seg_no = 0;
+  HX_SEGMENTS(s, count) {
+    if (s.empty) continue;
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      uint4 u[kLoads];
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int row = j * kStep + sub, x = s.mt * kItemRows + half * kHalf + row;
+        const int i = a.by_group.of(x), head = s.h * a.group + a.by_group.rest(x);
+        const bool real = row < kHalf && half * kHalf + row < s.rows;
+        u[j] = real ? *(const uint4*)((const T*)a.q + (int64_t)(s.q.first + i) * a.q_token_stride + head * a.q_head_stride + 8 * unit)
+                    : uint4{0, 0, 0, 0};
+      }
+      bar_wait(&sh->q_empty[half], (seg_no & 1) ^ 1, &sh->dead);
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int row = j * kStep + sub;
+        const uint32_t* w = (const uint32_t*)&u[j];
+        float2 f[4];
+        float amax = 0;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          f[y] = two<T>(w[y]);
+          amax = fmaxf(amax, fmaxf(fabsf(f[y].x), fabsf(f[y].y)));
+        }
+#pragma unroll
+        for (int d = kLanes / 2; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
+        int e = 0;
+        if (amax > 0 && amax < INFINITY) e = max((int)(__float_as_uint(amax) >> 23) - 127, -126);
+        const float down = __uint_as_float((unsigned)(127 - e) << 23);
+        uint32_t h[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) h[y] = pack_half(f[y].x * down, f[y].y * down);
+        if (row < kHalf) {
+          *(uint4*)(qbuf + half * Many<D>::kQBytes + (unit >> 3) * (kHalf * 128) + row * 128 + (((unit & 7) ^ (row & 7)) << 4)) =
+              uint4{h[0], h[1], h[2], h[3]};
+          if (unit == 0) sh->q_scale[seg_no & 1][half * kHalf + row] = __uint_as_float((unsigned)(127 + e) << 23);
+        }
+      }
+      fence_async();
+      bar_arrive(&sh->q_full[half]);
+    }
+    ++seg_no;
+  }
+}
+
+// ---- the issuing warp
+
+// One thread of the warp, the same each time; what it does, the hardware takes from uniform registers.
+__device__ __forceinline__ bool elected() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p;
+}
+
+template <int D>
+__device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, const uint8_t* qbuf, const uint8_t* kbuf,
+                      const uint8_t* vbuf) {
+  const uint32_t tm = sh->tmem;
+  const uint64_t q0 = operand(smem_addr(qbuf), 16), k0 = operand(smem_addr(kbuf), 16), v0 = operand(smem_addr(vbuf), kKv * 128);
+  uint32_t n_s[2] = {0, 0};  // products P V issued per half
+  int it = 0, seg_no = 0;
+  volatile int* dead = &sh->dead;
+  const auto scores = [&](int half, int st) {
+    // S's columns hold the last P: its product must have ended
+    if (n_s[half]) bar_wait(&sh->o_full[half], (n_s[half] - 1) & 1, dead);
+    tc_fence_after();
+    if (elected()) {
+      const uint64_t q = q0 + half * (Many<D>::kQBytes >> 4), k = k0 + st * (Many<D>::kTile >> 4);
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) {
+        const uint32_t o = ((x >> 2) * (128 * 128) + (x & 3) * 32) >> 4;
+        mma_ss(tm + half * kKv, q + o, k + o, instruction(kKv, false), x > 0);
+      }
+      tc_commit(&sh->s_full[half]);
+    }
+    __syncwarp();
+  };
+  const auto values = [&](int half, int st, bool add) {
+    bar_wait(&sh->p_full[half], n_s[half] & 1, dead);
+    tc_fence_after();
+    if (elected()) {
+      const uint64_t v = v0 + st * (Many<D>::kTile >> 4);
+#pragma unroll
+      for (int x = 0; x < kKv / 16; ++x)
+        mma_ts(tm + 256 + half * D, tm + half * kKv + 8 * x, v + x * (2048 >> 4), instruction(D, true), add || x > 0);
+      tc_commit(&sh->o_full[half]);
+    }
+    __syncwarp();
+    ++n_s[half];
+  };
+  const auto commit = [&](uint64_t* bar) {
+    if (elected()) tc_commit(bar);
+    __syncwarp();
+  };
+  HX_SEGMENTS(s, count) {
+    if (s.empty) continue;
+    const int tile0 = s.first_tile + s.t;
+    // the item before the last has been written out, and this one may begin
+    if (seg_no >= 2) {
+      bar_wait(&sh->ended[0][seg_no & 1], ((seg_no - 2) >> 1) & 1, dead);
+      bar_wait(&sh->ended[1][seg_no & 1], ((seg_no - 2) >> 1) & 1, dead);
+    }
+    if ((threadIdx.x & 31) == 0) bar_arrive(&sh->go[seg_no & 1]);
+    bool has[2] = {false, false};  // a half's O holds something
+    bar_wait(&sh->k_full[it & 1], (it >> 1) & 1, dead);
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      bar_wait(&sh->q_full[half], seg_no & 1, dead);
+      if (active(s, half, tile0)) scores(half, it & 1);
+      if (seg == 1) commit(&sh->q_empty[half]);
+    }
+    commit(&sh->k_empty[it & 1]);
+    for (int i = 0; i < seg && !__any_sync(~0u, *dead); ++i, ++it) {
+      const int tile = tile0 + i, st = it & 1;
+      const bool more = i + 1 < seg;
+      bar_wait(&sh->v_full[st], (it >> 1) & 1, dead);
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        if (active(s, half, tile)) {
+          values(half, st, has[half]);
+          has[half] = true;
+        }
+        if (half == 1) commit(&sh->v_empty[st]);
+        if (!more) continue;
+        if (half == 0) bar_wait(&sh->k_full[st ^ 1], ((it + 1) >> 1) & 1, dead);
+        if (active(s, half, tile + 1)) scores(half, st ^ 1);
+        if (i + 2 == seg) commit(&sh->q_empty[half]);
+      }
+      if (more) commit(&sh->k_empty[st ^ 1]);
+    }
+    ++seg_no;
+  }
+}
+
+// ---- the softmax warps
+
+template <int D, class T>
+__device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
   constexpr float kLag = 8.f;
   const int half = threadIdx.x >> 7, row = threadIdx.x & 127;
   const uint32_t lanes = (threadIdx.x & 96) << 16;
@@ -415,9 +539,9 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh, u
   uint32_t n_s = 0;
   volatile int* dead = &sh->dead;
   HX_SEGMENTS(s, count) {
-    const int64_t x = (int64_t)s.mt * kItemRows + half * kHalf + row;
+    const int x = s.mt * kItemRows + half * kHalf + row;
     const bool real = half * kHalf + row < s.rows;
-    const int i = (int)(x / a.group), head = s.h * a.group + (int)(x % a.group);
+    const int i = a.by_group.of(x), head = s.h * a.group + a.by_group.rest(x);
     const int64_t token = s.q.first + i;
     T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
     if (s.empty) {
@@ -428,18 +552,15 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh, u
       }
       continue;
     }
-    const float c = a.sm_scale_log2 * put_q<D, T>((const T*)a.q + token * a.q_token_stride + head * a.q_head_stride, real,
-                                                  qbuf + half * Many<D>::kQBytes, row);
-    fence_async();
-    bar_arrive(&sh->q_full[half]);
-    if (!__all_sync(~0u, bar_wait(&sh->go, seg_no & 1, dead))) break;
+    __all_sync(~0u, bar_wait(&sh->go[seg_no & 1], (seg_no >> 1) & 1, dead));
     const int lo = real ? see_from(a, s.q, i) : 0, hi = real ? see_to(a, s.q, i) : 0;
     // what all rows of the half see: [all_lo, all_hi)
-    const int64_t xb = (int64_t)s.mt * kItemRows + half * kHalf, xe = min(xb + kHalf, (int64_t)s.q.n * a.group);
-    const bool full_half = xb + kHalf <= (int64_t)s.q.n * a.group;
-    const int all_lo = full_half ? see_from(a, s.q, (int)((xe - 1) / a.group)) : 0x7fffffff;
-    const int all_hi = full_half ? see_to(a, s.q, (int)(xb / a.group)) : 0;
+    const int xb = s.mt * kItemRows + half * kHalf;
+    const bool full_half = xb + kHalf <= s.q.n * a.group;
+    const int all_lo = full_half ? see_from(a, s.q, a.by_group.of(xb + kHalf - 1)) : 0x7fffffff;
+    const int all_hi = full_half ? see_to(a, s.q, a.by_group.of(xb)) : 0;
 
+    float c = 0;
     float m = -INFINITY, l = 0;
     bool has = false;
     for (int j = 0; j < seg && !__any_sync(~0u, *dead); ++j, ++it) {
@@ -449,37 +570,48 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh, u
       const TileInfo& info = sh->info[it & 3];
       if (!bar_wait(&sh->s_full[half], n_s & 1, dead)) l = NAN;
       tc_fence_after();
+      if (!has) c = a.sm_scale_log2 * sh->q_scale[seg_no & 1][half * kHalf + row];
       const uint32_t valid = info.valid;
       const bool whole = valid == 0x03030303u && pos >= all_lo && pos + kKv <= all_hi;
-      // bit g of `exists`: group g has a block
-      const auto exists = [&](int g) { return (valid >> (8 * (g >> 1) + (g & 1))) & 1; };
+      // what this row sees of 32 tokens
+      const auto sees = [&](int ch) -> uint32_t {
+        const int p = pos + 32 * ch, f = min(max(lo - p, 0), 32), e = min(max(hi - p, 0), 32);
+        if (f >= e) return 0;
+        const uint32_t range = (0xffffffffu >> (32 - (e - f))) << f;
+        const uint32_t have = valid >> (8 * ch);
+        return range & ((have & 1 ? 0xffffu : 0) | (have & 2 ? 0xffff0000u : 0));
+      };
       float top = -INFINITY;
+      const auto find_top = [&](auto kind) {
+        constexpr bool masked = decltype(kind)::value;
+#pragma unroll 1
+        for (int ch = 0; ch < 4; ++ch) {
+          uint32_t u[32];
+          tm_load(ts + 32 * ch, u);
+          const uint32_t see = masked ? sees(ch) : 0;
 #pragma unroll
-      for (int ch = 0; ch < 4; ++ch) {
-        uint32_t u[32];
-        tm_load(ts + 32 * ch, u);
+          for (int g = 0; g < 2; ++g) {
+            const float4 z = info.g[2 * ch + g];
+            const float2 f = both(z.x * c), b = both(z.y);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const float4 z = info.g[2 * ch + g];
-          const float f = z.x * c;
-#pragma unroll
-          for (int y = 0; y < 16; ++y) {
-            float v = fmaf(__uint_as_float(u[16 * g + y]), f, z.y);
-            if (!whole) {
-              const int p = pos + 32 * ch + 16 * g + y;
-              if (p < lo || p >= hi || !exists(2 * ch + g)) v = -INFINITY;
+            for (int y = 0; y < 16; y += 2) {
+              float2 v = fma2(pair(u[16 * g + y], u[16 * g + y + 1]), f, b);
+              if (masked && !(see >> (16 * g + y) & 1)) v.x = -INFINITY;
+              if (masked && !(see >> (16 * g + y + 1) & 1)) v.y = -INFINITY;
+              top = fmaxf(top, fmaxf(v.x, v.y));
             }
-            top = fmaxf(top, v);
           }
         }
-      }
+      };
+      if (whole) find_top(std::false_type{});
+      else find_top(std::true_type{});
       if (__any_sync(~0u, top > m + kLag)) {
         const float z = fmaxf(m, top);
         const float keep = z == -INFINITY ? 1.f : ex2(m - z);
         m = z;
         l *= keep;
         if (has) {
-#pragma unroll
+#pragma unroll 1
           for (int ch = 0; ch < D / 32; ++ch) {
             uint32_t u[32];
             tm_load(to + 32 * ch, u);
@@ -490,32 +622,34 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh, u
         }
       }
       const float base = m == -INFINITY ? 0.f : m;
+      const auto weigh = [&](auto kind) {
+        constexpr bool masked = decltype(kind)::value;
+#pragma unroll 1
+        for (int ch = 0; ch < 4; ++ch) {
+          uint32_t u[32], w[16];
+          tm_load(ts + 32 * ch, u);
+          const uint32_t see = masked ? sees(ch) : 0;
 #pragma unroll
-      for (int ch = 0; ch < 4; ++ch) {
-        uint32_t u[32], w[16];
-        tm_load(ts + 32 * ch, u);
+          for (int g = 0; g < 2; ++g) {
+            const float4 z = info.g[2 * ch + g];
+            const float2 f = both(z.x * c), b = both(z.y - base);
+            float2 sum = {0, 0};
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const float4 z = info.g[2 * ch + g];
-          const float f = z.x * c, b = z.y - base;
-          float sum = 0;
-#pragma unroll
-          for (int y = 0; y < 16; ++y) {
-            float v = fmaf(__uint_as_float(u[16 * g + y]), f, b);
-            if (!whole) {
-              const int p = pos + 32 * ch + 16 * g + y;
-              if (p < lo || p >= hi || !exists(2 * ch + g)) v = -INFINITY;
+            for (int y = 0; y < 16; y += 2) {
+              float2 v = fma2(pair(u[16 * g + y], u[16 * g + y + 1]), f, b);
+              v.x = ex2(v.x), v.y = ex2(v.y);
+              if (masked && !(see >> (16 * g + y) & 1)) v.x = 0;
+              if (masked && !(see >> (16 * g + y + 1) & 1)) v.y = 0;
+              sum = add2(sum, v);
+              w[8 * g + y / 2] = pack_half(v.x, v.y);
             }
-            v = ex2(v);
-            sum += v;
-            u[16 * g + y] = __float_as_uint(v);
+            l = fmaf(sum.x + sum.y, z.z, l);
           }
-          l = fmaf(sum, z.z, l);
+          tm_store16(ts + 16 * ch, w);
         }
-#pragma unroll
-        for (int y = 0; y < 16; ++y) w[y] = pack_half(__uint_as_float(u[2 * y]), __uint_as_float(u[2 * y + 1]));
-        tm_store16(ts + 16 * ch, w);
-      }
+      };
+      if (whole) weigh(std::false_type{});
+      else weigh(std::true_type{});
       tm_stored();
       tc_fence_before();
       bar_arrive(&sh->p_full[half]);
@@ -585,6 +719,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh, u
       else if (a.lse) a.lse[token * a.n_heads + head] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
     }
     tc_fence_before();
+    bar_arrive(&sh->ended[half][seg_no & 1]);
     ++seg_no;
   }
 }
@@ -602,25 +737,29 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __gri
     for (int i = 0; i < 2; ++i) {
       bar_init(&sh.k_full[i], 128), bar_init(&sh.v_full[i], 128);
       bar_init(&sh.k_empty[i], 1), bar_init(&sh.v_empty[i], 1);
-      bar_init(&sh.q_full[i], 128), bar_init(&sh.s_full[i], 1), bar_init(&sh.p_full[i], 128), bar_init(&sh.o_full[i], 1);
+      bar_init(&sh.q_full[i], 32 * kQueryWarps), bar_init(&sh.q_empty[i], 1), bar_init(&sh.s_full[i], 1);
+      bar_init(&sh.ended[i][0], 128), bar_init(&sh.ended[i][1], 128);
+      bar_init(&sh.p_full[i], 128), bar_init(&sh.o_full[i], 1);
     }
-    bar_init(&sh.go, 1);
+    bar_init(&sh.go[0], 1), bar_init(&sh.go[1], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.dead = 0;
     sh.row = -1;
   }
 
-  // this block's stretch of all tiles
-  const int per = (a.n_rows + kManyThreads - 1) / kManyThreads;
-  const int r0 = min(a.n_rows, tid * per), r1 = min(a.n_rows, r0 + per);
+  // this block's stretch of all tiles: each warp adds up its rows', and the one that holds the
+  // stretch's first looks it up
+  const int per = ((a.n_rows + kManyThreads - 1) / kManyThreads) * 32;  // rows of a warp
+  const int w0 = warp * per, w1 = min(a.n_rows, w0 + per);
+  const auto row_tiles = [&](int r) {
+    const bool real = r < w1;
+    const Request q = real ? request(a, r) : Request{0, 0, 0};
+    return tiles_per_head(a, q, real);
+  };
   long long mine = 0;
-  for (int r = r0; r < r1; ++r) mine += tiles_per_head(a, request(a, r)) * a.n_kv_heads;
-  long long upto = mine;
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long o = __shfl_up_sync(~0u, upto, d);
-    if (lane >= d) upto += o;
-  }
-  if (lane == 31) sh.sum[warp] = upto;
+  for (int r = w0; r < w1; r += 32) mine += row_tiles(r + lane);
+  mine = warp_sum(mine) * a.n_kv_heads;
+  if (lane == 0) sh.sum[warp] = mine;
   __syncthreads();
   long long before = 0, total = 0;
 #pragma unroll
@@ -628,18 +767,47 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __gri
     if (w < warp) before += sh.sum[w];
     total += sh.sum[w];
   }
-  before += upto - mine;
   const long long G = max(1LL, min((long long)gridDim.x, total)), b = blockIdx.x;
   const long long n0 = b < G ? total * b / G : 0, n1 = b < G ? total * (b + 1) / G : 0;
   if (n0 < n1 && before <= n0 && n0 < before + mine) {
-    int r = r0;
-    for (;; ++r) {
-      const long long x = tiles_per_head(a, request(a, r)) * a.n_kv_heads;
-      if (n0 < before + x) break;
-      before += x;
+    for (int r = w0; r < w1; r += 32) {
+      const long long head = row_tiles(r + lane), x = head * a.n_kv_heads;
+      long long upto = x;
+      for (int d = 1; d < 32; d <<= 1) {
+        const long long o = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += o;
+      }
+      const unsigned past = __ballot_sync(~0u, n0 < before + upto);
+      if (!past) {
+        before += __shfl_sync(~0u, upto, 31);
+        continue;
+      }
+      const int src = __ffs(past) - 1;
+      const long long per_head = __shfl_sync(~0u, head, src);
+      long long skip = n0 - before - __shfl_sync(~0u, upto - x, src);
+      const int h = (int)(skip / per_head);
+      skip -= h * per_head;
+      const Request q = request(a, r + src);
+      const int items = items_of(a, q);
+      for (int mt = 0; mt < items; mt += 32) {
+        const int tiles = mt + lane < items ? item_tiles(a, q, mt + lane) : 0;
+        int sum = tiles;
+        for (int d = 1; d < 32; d <<= 1) {
+          const int o = __shfl_up_sync(~0u, sum, d);
+          if (lane >= d) sum += o;
+        }
+        const unsigned in = __ballot_sync(~0u, skip < sum);
+        if (!in) {
+          skip -= __shfl_sync(~0u, sum, 31);
+          continue;
+        }
+        const int y = __ffs(in) - 1;
+        skip -= __shfl_sync(~0u, sum - tiles, y);
+        if (lane == 0) sh.row = r + src, sh.head = h, sh.mt = mt + y, sh.skip = skip;
+        break;
+      }
+      break;
     }
-    sh.row = r;
-    sh.skip = n0 - before;
   }
   __syncthreads();
   if (sh.row < 0) {
@@ -653,19 +821,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __gri
   Segment s;
   s.r = sh.row;
   s.q = request(a, s.r);
-  long long skip = sh.skip;
-  {
-    const long long head = tiles_per_head(a, s.q);
-    s.h = (int)(skip / head);
-    skip %= head;
-    for (s.mt = 0;; ++s.mt) {
-      int t0, t1;
-      bool e;
-      item_span(a, s.q, s.mt, &t0, &t1, &e);
-      if (skip < t1 - t0) break;
-      skip -= t1 - t0;
-    }
-  }
+  s.h = sh.head;
+  s.mt = sh.mt;
+  const long long skip = sh.skip;
   load_item(a, s);
   s.t = (int)skip;
   int count = (int)(n1 - n0);
@@ -684,9 +842,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __gri
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp < kConvWarp) softmax<D, T>(a, s, count, &sh, qbuf);
+  if (warp < kConvWarp) softmax<D, T>(a, s, count, &sh);
   else if (warp < kMmaWarp) convert<D>(a, s, count, &sh, kbuf, vbuf);
-  else if (lane == 0) issue<D>(a, s, count, &sh, qbuf, kbuf, vbuf);
+  else if (warp == kMmaWarp) issue<D>(a, s, count, &sh, qbuf, kbuf, vbuf);
+  else queries<D, T>(a, s, count, &sh, qbuf);
   __syncwarp();
   drain(&sh.dead);
   tc_fence_before();
