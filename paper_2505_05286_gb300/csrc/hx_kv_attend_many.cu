@@ -49,7 +49,8 @@ struct Segment {  // a stretch of one item's tiles
   int first_tile;
   Request q;
   int rows;               // of this item
-  int lo[2], hi[2];       // tokens that any row of a half sees
+  int lo0, hi0, lo1, hi1; // tokens that any row of a half sees (no arrays: an index that is not
+                          // constant would put them into local memory)
   bool empty;             // nothing visible, or not to be computed: zeros
 };
 
@@ -103,11 +104,12 @@ __device__ __forceinline__ void load_item(const AttendArgs& a, Segment& s) {
   s.tiles = t1 - t0;
   const int x0 = s.mt * kItemRows, all = s.q.n * a.group;
   s.rows = min(kItemRows, all - x0);
-#pragma unroll
-  for (int y = 0; y < 2; ++y) {
-    const int b = x0 + y * kHalf, e = min(b + kHalf, all);
-    s.lo[y] = s.hi[y] = 0;
-    if (b < all) s.lo[y] = see_from(a, s.q, a.by_group.of(b)), s.hi[y] = see_to(a, s.q, a.by_group.of(e - 1));
+  s.lo0 = see_from(a, s.q, a.by_group.of(x0));
+  s.hi0 = see_to(a, s.q, a.by_group.of(min(x0 + kHalf, all) - 1));
+  s.lo1 = s.hi1 = 0;
+  if (x0 + kHalf < all) {
+    s.lo1 = see_from(a, s.q, a.by_group.of(x0 + kHalf));
+    s.hi1 = see_to(a, s.q, a.by_group.of(min(x0 + kItemRows, all) - 1));
   }
 }
 // To the next item; false past the last.
@@ -131,7 +133,7 @@ __device__ __forceinline__ bool next_item(const AttendArgs& a, Segment& s) {
   return true;
 }
 __device__ __forceinline__ bool active(const Segment& s, int half, int tile) {
-  return tile * kKv < s.hi[half] && (tile + 1) * kKv > s.lo[half];
+  return tile * kKv < (half ? s.hi1 : s.hi0) && (tile + 1) * kKv > (half ? s.lo1 : s.lo0);
 }
 
 // ---- tcgen05
@@ -177,23 +179,20 @@ __device__ __forceinline__ void tm_load(uint32_t addr, uint32_t* r) {  // 32 col
       : "r"(addr)
       : "memory");
 }
-__device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t* r) {
+__device__ __forceinline__ void tm_load16(uint32_t addr, uint32_t* r) {  // 16 columns
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
-      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-      "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
-      "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr)
       : "memory");
 }
 __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
-      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+      "r"(addr)
       : "memory");
 }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -255,8 +254,9 @@ __device__ __forceinline__ uint32_t pack(float x, float y) {
 // Loads run ahead of the conversion: a tile's keys are asked for as soon as the registers of the one
 // before are written out, its block numbers a tile earlier.
 template <int D>
-__device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* kbuf, uint8_t* vbuf) {
-  constexpr int kLanes = D / 16;           // lanes of a token, 16 bytes each
+__device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* kbuf) {
+  // 8 bytes a lane: a lane's 8 f16 are one 16-byte unit, and eight lanes' units lie on different banks
+  constexpr int kLanes = D / 8;            // lanes of a token
   constexpr int kPer = 32 / kLanes;        // tokens of a warp's load
   constexpr int kLoads = 32 / kPer;        // loads of a warp's 32 tokens
   const int tid = threadIdx.x - 32 * kConvWarp, warp = tid >> 5, lane = tid & 31;
@@ -268,10 +268,10 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, u
   int pos, end, id[2];
   int64_t at[2];
   float ks[2], vs[2];
-  uint4 kr[kLoads], vr[kLoads];
+  uint2 kr[kLoads], vr[kLoads];
   const auto numbers = [&] {
     pos = (s.first_tile + s.t) * kKv + 32 * warp;
-    end = max(s.hi[0], s.hi[1]);
+    end = max(s.hi0, s.hi1);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int p = pos + 16 * x;
@@ -284,31 +284,26 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, u
       ks[x] = vs[x] = 0;
       at[x] = -1;
       if ((unsigned)id[x] < (unsigned)a.n_blocks) {
-        at[x] = id[x] * a.block_stride + ((int64_t)s.h * block + ((pos + 16 * x) & (block - 1))) * D + unit * 16;
+        at[x] = id[x] * a.block_stride + ((int64_t)s.h * block + ((pos + 16 * x) & (block - 1))) * D + unit * 8;
         ks[x] = a.k_scale[id[x] * a.scale_stride + s.h];
         vs[x] = a.v_scale[id[x] * a.scale_stride + s.h];
       }
     }
   };
-  const auto fetch = [&](const uint8_t* from, uint4* to) {
+  const auto fetch = [&](const uint8_t* from, uint2* to) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       const int tok = j * kPer + sub;
       const int64_t o = (j * kPer) >> 4 ? at[1] : at[0];
-      to[j] = o >= 0 && pos + tok < end ? *(const uint4*)(from + o + (tok & 15) * D) : uint4{0, 0, 0, 0};
+      to[j] = o >= 0 && pos + tok < end ? *(const uint2*)(from + o + (tok & 15) * D) : uint2{0, 0};
     }
   };
   // the tile's f16 rows: panels of 64 columns, 128-byte rows, 16-byte units permuted
-  const auto put = [&](uint8_t* buf, const uint4& u, int tok) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    uint8_t* row = buf + (unit >> 2) * (kKv * 128) + tok * 128;
-    const bool odd = unit >> 2 & 1;
-    uint4 h[2];
-#pragma unroll
-    for (int y = 0; y < 2; ++y) h[y] = uint4{cvt2(w[2 * y]), cvt2_hi(w[2 * y]), cvt2(w[2 * y + 1]), cvt2_hi(w[2 * y + 1])};
-    // the two halves of the lanes take their two units in opposite order: all on different banks
-    *(uint4*)(row + (((2 * (unit & 3) + odd) ^ (tok & 7)) << 4)) = odd ? h[1] : h[0];
-    *(uint4*)(row + (((2 * (unit & 3) + !odd) ^ (tok & 7)) << 4)) = odd ? h[0] : h[1];
+  uint8_t* const row0 = kbuf + (unit >> 3) * (kKv * 128) + (32 * warp + sub) * 128;
+  const auto put = [&](int offset, const uint2& u, int j) {
+    const int tok = j * kPer;  // of this lane's first; kPer <= 4 leaves bits of the row number apart
+    *(uint4*)(row0 + offset + tok * 128 + (((unit & 7) ^ ((tok + sub) & 7)) << 4)) =
+        uint4{cvt2(u.x), cvt2_hi(u.x), cvt2(u.y), cvt2_hi(u.y)};
   };
   // items that see nothing have one tile, and nothing in it
   const auto skip_empty = [&] {
@@ -350,7 +345,7 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, u
     const bool more = count > 0;
     if (more) numbers();
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) put(kbuf + st * Many<D>::kTile, kr[j], 32 * warp + j * kPer + sub);
+    for (int j = 0; j < kLoads; ++j) put(st * Many<D>::kTile, kr[j], j);
     fence_async();
     bar_arrive(&sh->k_full[st]);
     if (more) {
@@ -360,19 +355,16 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, u
     bar_wait(&sh->v_empty[st], phase ^ 1, &sh->dead);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      uint32_t* w = (uint32_t*)&vr[j];
-      uint32_t nan = 0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) nan |= (w[x] & 0x7f7f7f7fu) + 0x01010101u;
-      if (nan & 0x80808080u) {
+      const auto nans = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };
+      if (nans(vr[j].x) | nans(vr[j].y)) {
         // a NaN would reach rows that do not see it (0 * NaN): taken out here, and put
         // into the rows that see it at their end
-#pragma unroll
-        for (int x = 0; x < 4; ++x) w[x] &= ~(((((w[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
+        vr[j].x &= ~((nans(vr[j].x) >> 7) * 0xffu);
+        vr[j].y &= ~((nans(vr[j].y) >> 7) * 0xffu);
         const int n = atomicAdd(&sh->nan_count[list], 1);
         if (n < kNanList) sh->nan_pos[list][n] = here + j * kPer + sub;
       }
-      put(vbuf + st * Many<D>::kTile, vr[j], 32 * warp + j * kPer + sub);
+      put((2 + st) * Many<D>::kTile, vr[j], j);
     }
     fence_async();
     bar_arrive(&sh->v_full[st]);
@@ -383,10 +375,12 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, u
 
 // ---- the query warps
 
-// Both halves' q in f16 times a power of two for each row (so that no value leaves f16's range), as soon as
-// the last item's products have read theirs.
+// Both halves' q in f16.  bf16 rows are scaled by a power of two so that no value leaves f16's
+// range; those are found while the item before is still computed, when these warps have
+// time.  The first half is then held ready in registers until the last item's products have read theirs.
 template <int D, class T>
 __device__ void queries(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* qbuf) {
+  constexpr bool kScaled = std::is_same<T, __nv_bfloat16>::value;
   constexpr int kLanes = D / 8, kPer = 32 / kLanes;  // lanes of a row, rows of a warp's load
   constexpr int kStep = kPer * kQueryWarps, kLoads = (kHalf + kStep - 1) / kStep;
   const int warp = (threadIdx.x >> 5) - kQueryWarp, lane = threadIdx.x & 31;
@@ -394,45 +388,81 @@ __device__ void queries(const AttendArgs& a, Segment s, int count, Shared* sh, u
   int seg_no = 0;
   HX_SEGMENTS(s, count) {
     if (s.empty) continue;
+    const auto load = [&](int half, int j) {
+      const int row = j * kStep + sub, x = s.mt * kItemRows + half * kHalf + row;
+      const int i = a.by_group.of(x), head = s.h * a.group + a.by_group.rest(x);
+      const bool real = row < kHalf && half * kHalf + row < s.rows;
+      return real ? *(const uint4*)((const T*)a.q + (int64_t)(s.q.first + i) * a.q_token_stride + head * a.q_head_stride + 8 * unit)
+                  : uint4{0, 0, 0, 0};
+    };
+    float* scale = sh->q_scale[seg_no & 1];
+    if constexpr (kScaled) {
+      constexpr int kMost = 4;
 #pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
-      uint4 u[kLoads];
+      for (int j0 = 0; j0 < 2 * kLoads; j0 += kMost) {
+        uint4 u[kMost];
+        float amax[kMost];
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int row = j * kStep + sub, x = s.mt * kItemRows + half * kHalf + row;
-        const int i = a.by_group.of(x), head = s.h * a.group + a.by_group.rest(x);
-        const bool real = row < kHalf && half * kHalf + row < s.rows;
-        u[j] = real ? *(const uint4*)((const T*)a.q + (int64_t)(s.q.first + i) * a.q_token_stride + head * a.q_head_stride + 8 * unit)
-                    : uint4{0, 0, 0, 0};
-      }
-      bar_wait(&sh->q_empty[half], (seg_no & 1) ^ 1, &sh->dead);
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int row = j * kStep + sub;
-        const uint32_t* w = (const uint32_t*)&u[j];
-        float2 f[4];
-        float amax = 0;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          f[y] = two<T>(w[y]);
-          amax = fmaxf(amax, fmaxf(fabsf(f[y].x), fabsf(f[y].y)));
+        for (int y = 0; y < kMost; ++y) {
+          const int j = j0 + y;
+          u[y] = j < 2 * kLoads ? load(j >= kLoads, j >= kLoads ? j - kLoads : j) : uint4{0, 0, 0, 0};
         }
 #pragma unroll
-        for (int d = kLanes / 2; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
-        int e = 0;
-        if (amax > 0 && amax < INFINITY) e = max((int)(__float_as_uint(amax) >> 23) - 127, -126);
-        const float down = __uint_as_float((unsigned)(127 - e) << 23);
-        uint32_t h[4];
+        for (int y = 0; y < kMost; ++y) {
+          // the largest size, as 16 bits without a sign: bf16 values order as integers
+          const uint32_t w[4] = {u[y].x & 0x7fff7fffu, u[y].y & 0x7fff7fffu, u[y].z & 0x7fff7fffu, u[y].w & 0x7fff7fffu};
+          const uint32_t m = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
+          amax[y] = __uint_as_float(max(m >> 16, m & 0xffff) << 16);
+        }
 #pragma unroll
-        for (int y = 0; y < 4; ++y) h[y] = pack_half(f[y].x * down, f[y].y * down);
-        if (row < kHalf) {
-          *(uint4*)(qbuf + half * Many<D>::kQBytes + (unit >> 3) * (kHalf * 128) + row * 128 + (((unit & 7) ^ (row & 7)) << 4)) =
-              uint4{h[0], h[1], h[2], h[3]};
-          if (unit == 0) sh->q_scale[seg_no & 1][half * kHalf + row] = __uint_as_float((unsigned)(127 + e) << 23);
+        for (int d = kLanes / 2; d; d >>= 1)
+#pragma unroll
+          for (int y = 0; y < kMost; ++y) {
+            const float o = __shfl_xor_sync(~0u, amax[y], d);
+            amax[y] = __float_as_uint(o) > __float_as_uint(amax[y]) ? o : amax[y];
+          }
+#pragma unroll
+        for (int y = 0; y < kMost; ++y) {
+          const int j = j0 + y, half = j >= kLoads, row = (half ? j - kLoads : j) * kStep + sub;
+          int e = 0;
+          if (amax[y] > 0 && amax[y] < INFINITY) e = max((int)(__float_as_uint(amax[y]) >> 23) - 127, -126);
+          if (unit == 0 && j < 2 * kLoads && row < kHalf) scale[half * kHalf + row] = __uint_as_float((unsigned)(127 + e) << 23);
         }
       }
-      fence_async();
-      bar_arrive(&sh->q_full[half]);
+      __syncwarp();  // a warp writes and reads its own rows' scales
+    }
+#pragma unroll 1
+    for (int part = 0; part < 4; ++part) {  // half a half at a time: what registers hold
+      constexpr int kSome = (kLoads + 1) / 2;
+      const int half = part >> 1, j0 = part & 1 ? kSome : 0;
+      uint4 u[kSome];
+#pragma unroll
+      for (int j = 0; j < kSome; ++j) u[j] = load(half, j0 + j);
+      if constexpr (kScaled) {
+#pragma unroll
+        for (int j = 0; j < kSome; ++j) {
+          const int row = (j0 + j) * kStep + sub;
+          // 2^-e from 2^e: the exponents' sum is 254
+          const float down = __uint_as_float(0x7f000000u - __float_as_uint(row < kHalf ? scale[half * kHalf + row] : 1.f));
+          uint32_t* w = (uint32_t*)&u[j];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const float2 f = two<T>(w[y]);
+            w[y] = pack_half(f.x * down, f.y * down);
+          }
+        }
+      }
+      if (!(part & 1)) bar_wait(&sh->q_empty[half], (seg_no & 1) ^ 1, &sh->dead);
+#pragma unroll
+      for (int j = 0; j < kSome; ++j) {
+        const int row = (j0 + j) * kStep + sub;
+        if (row < kHalf)
+          *(uint4*)(qbuf + half * Many<D>::kQBytes + (unit >> 3) * (kHalf * 128) + row * 128 + (((unit & 7) ^ (row & 7)) << 4)) = u[j];
+      }
+      if (part & 1) {
+        fence_async();
+        bar_arrive(&sh->q_full[half]);
+      }
     }
     ++seg_no;
   }
@@ -498,7 +528,7 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
     if ((threadIdx.x & 31) == 0) bar_arrive(&sh->go[seg_no & 1]);
     bool has[2] = {false, false};  // a half's O holds something
     bar_wait(&sh->k_full[it & 1], (it >> 1) & 1, dead);
-#pragma unroll 1
+#pragma unroll
     for (int half = 0; half < 2; ++half) {
       bar_wait(&sh->q_full[half], seg_no & 1, dead);
       if (active(s, half, tile0)) scores(half, it & 1);
@@ -509,17 +539,18 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
       const int tile = tile0 + i, st = it & 1;
       const bool more = i + 1 < seg;
       bar_wait(&sh->v_full[st], (it >> 1) & 1, dead);
-#pragma unroll 1
+#pragma unroll
       for (int half = 0; half < 2; ++half) {
         if (active(s, half, tile)) {
           values(half, st, has[half]);
           has[half] = true;
         }
         if (half == 1) commit(&sh->v_empty[st]);
-        if (!more) continue;
-        if (half == 0) bar_wait(&sh->k_full[st ^ 1], ((it + 1) >> 1) & 1, dead);
-        if (active(s, half, tile + 1)) scores(half, st ^ 1);
-        if (i + 2 == seg) commit(&sh->q_empty[half]);
+        if (more) {
+          if (half == 0) bar_wait(&sh->k_full[st ^ 1], ((it + 1) >> 1) & 1, dead);
+          if (active(s, half, tile + 1)) scores(half, st ^ 1);
+          if (i + 2 == seg) commit(&sh->q_empty[half]);
+        }
       }
       if (more) commit(&sh->k_empty[st ^ 1]);
     }
@@ -531,7 +562,7 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
 
 template <int D, class T>
 __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
-  constexpr float kLag = 8.f;
+  constexpr float kLag = 10.f;  // of f16's 2^16
   const int half = threadIdx.x >> 7, row = threadIdx.x & 127;
   const uint32_t lanes = (threadIdx.x & 96) << 16;
   const uint32_t ts = sh->tmem + lanes + half * kKv, to = sh->tmem + lanes + 256 + half * D;
@@ -541,11 +572,11 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
   HX_SEGMENTS(s, count) {
     const int x = s.mt * kItemRows + half * kHalf + row;
     const bool real = half * kHalf + row < s.rows;
-    const int i = a.by_group.of(x), head = s.h * a.group + a.by_group.rest(x);
-    const int64_t token = s.q.first + i;
-    T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
     if (s.empty) {
       if (real) {
+        const int64_t token = s.q.first + a.by_group.of(x);
+        const int head = s.h * a.group + a.by_group.rest(x);
+        T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
 #pragma unroll
         for (int y = 0; y < D / 8; ++y) *(uint4*)(out + 8 * y) = uint4{0, 0, 0, 0};
         if (a.lse) a.lse[token * a.n_heads + head] = -INFINITY;
@@ -553,7 +584,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       continue;
     }
     __all_sync(~0u, bar_wait(&sh->go[seg_no & 1], (seg_no >> 1) & 1, dead));
-    const int lo = real ? see_from(a, s.q, i) : 0, hi = real ? see_to(a, s.q, i) : 0;
+    const int lo = real ? see_from(a, s.q, a.by_group.of(x)) : 0, hi = real ? see_to(a, s.q, a.by_group.of(x)) : 0;
     // what all rows of the half see: [all_lo, all_hi)
     const int xb = s.mt * kItemRows + half * kHalf;
     const bool full_half = xb + kHalf <= s.q.n * a.group;
@@ -561,8 +592,8 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     const int all_hi = full_half ? see_to(a, s.q, a.by_group.of(xb)) : 0;
 
     float c = 0;
-    float m = -INFINITY, l = 0;
-    bool has = false;
+    float m = 0, l = 0;
+    bool has = false, fresh = true;  // fresh: the row has seen nothing yet
     for (int j = 0; j < seg && !__any_sync(~0u, *dead); ++j, ++it) {
       const int tile = s.first_tile + s.t + j;
       if (!active(s, half, tile)) continue;
@@ -570,7 +601,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       const TileInfo& info = sh->info[it & 3];
       if (!bar_wait(&sh->s_full[half], n_s & 1, dead)) l = NAN;
       tc_fence_after();
-      if (!has) c = a.sm_scale_log2 * sh->q_scale[seg_no & 1][half * kHalf + row];
+      if (!has) c = std::is_same<T, __half>::value ? a.sm_scale_log2 : a.sm_scale_log2 * sh->q_scale[seg_no & 1][half * kHalf + row];
       const uint32_t valid = info.valid;
       const bool whole = valid == 0x03030303u && pos >= all_lo && pos + kKv <= all_hi;
       // what this row sees of 32 tokens
@@ -581,47 +612,9 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
         const uint32_t have = valid >> (8 * ch);
         return range & ((have & 1 ? 0xffffu : 0) | (have & 2 ? 0xffff0000u : 0));
       };
-      float top = -INFINITY;
-      const auto find_top = [&](auto kind) {
-        constexpr bool masked = decltype(kind)::value;
-#pragma unroll 1
-        for (int ch = 0; ch < 4; ++ch) {
-          uint32_t u[32];
-          tm_load(ts + 32 * ch, u);
-          const uint32_t see = masked ? sees(ch) : 0;
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float4 z = info.g[2 * ch + g];
-            const float2 f = both(z.x * c), b = both(z.y);
-#pragma unroll
-            for (int y = 0; y < 16; y += 2) {
-              float2 v = fma2(pair(u[16 * g + y], u[16 * g + y + 1]), f, b);
-              if (masked && !(see >> (16 * g + y) & 1)) v.x = -INFINITY;
-              if (masked && !(see >> (16 * g + y + 1) & 1)) v.y = -INFINITY;
-              top = fmaxf(top, fmaxf(v.x, v.y));
-            }
-          }
-        }
-      };
-      if (whole) find_top(std::false_type{});
-      else find_top(std::true_type{});
-      if (__any_sync(~0u, top > m + kLag)) {
-        const float z = fmaxf(m, top);
-        const float keep = z == -INFINITY ? 1.f : ex2(m - z);
-        m = z;
-        l *= keep;
-        if (has) {
-#pragma unroll 1
-          for (int ch = 0; ch < D / 32; ++ch) {
-            uint32_t u[32];
-            tm_load(to + 32 * ch, u);
-#pragma unroll
-            for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * keep);
-            tm_store32(to + 32 * ch, u);
-          }
-        }
-      }
-      const float base = m == -INFINITY ? 0.f : m;
+      // 32 tokens at a time, P over the S that has been read.  m need not be the maximum: a row moves its m
+      // (by a whole number) only when a weight would pass 2^kLag, and then what it has written of this tile
+      // and O follow.
       const auto weigh = [&](auto kind) {
         constexpr bool masked = decltype(kind)::value;
 #pragma unroll 1
@@ -629,21 +622,61 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
           uint32_t u[32], w[16];
           tm_load(ts + 32 * ch, u);
           const uint32_t see = masked ? sees(ch) : 0;
+          float top = -INFINITY;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             const float4 z = info.g[2 * ch + g];
-            const float2 f = both(z.x * c), b = both(z.y - base);
-            float2 sum = {0, 0};
+            const float2 f = both(z.x * c), b = both(z.y - m);
 #pragma unroll
-            for (int y = 0; y < 16; y += 2) {
-              float2 v = fma2(pair(u[16 * g + y], u[16 * g + y + 1]), f, b);
-              v.x = ex2(v.x), v.y = ex2(v.y);
-              if (masked && !(see >> (16 * g + y) & 1)) v.x = 0;
-              if (masked && !(see >> (16 * g + y + 1) & 1)) v.y = 0;
-              sum = add2(sum, v);
-              w[8 * g + y / 2] = pack_half(v.x, v.y);
+            for (int y = 16 * g; y < 16 * g + 16; y += 2) {
+              float2 v = fma2(pair(u[y], u[y + 1]), f, b);
+              if (masked && !(see >> y & 1)) v.x = -INFINITY;
+              if (masked && !(see >> (y + 1) & 1)) v.y = -INFINITY;
+              top = fmaxf(top, fmaxf(v.x, v.y));
+              u[y] = __float_as_uint(v.x), u[y + 1] = __float_as_uint(v.y);
             }
-            l = fmaf(sum.x + sum.y, z.z, l);
+          }
+          const bool late = fresh ? top > -INFINITY : top > kLag;
+          if (__any_sync(~0u, late)) {
+            const float by = late && top < INFINITY ? ceilf(top) : 0.f;
+            const float keep = fresh ? 1.f : ex2(-by);  // nothing has been kept while nothing was seen
+            fresh &= !late;
+            m += by;
+            l *= keep;
+#pragma unroll
+            for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) - by);
+            tm_stored();
+#pragma unroll 1
+            for (int o = 0; o < 16 * ch; o += 16) {
+              const __half2 k2 = __float2half2_rn(keep);
+              tm_load16(ts + o, w);
+#pragma unroll
+              for (int y = 0; y < 16; ++y) {
+                const __half2 h = __hmul2(*(const __half2*)&w[y], k2);
+                w[y] = *(const uint32_t*)&h;
+              }
+              tm_store16(ts + o, w);
+            }
+            if (has) {
+#pragma unroll 1
+              for (int o = 0; o < D; o += 16) {
+                tm_load16(to + o, w);
+#pragma unroll
+                for (int y = 0; y < 16; ++y) w[y] = __float_as_uint(__uint_as_float(w[y]) * keep);
+                tm_store16(to + o, w);
+              }
+            }
+          }
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            float2 part = {0, 0};
+#pragma unroll
+            for (int y = 16 * g; y < 16 * g + 16; y += 2) {
+              const float2 v = {ex2(__uint_as_float(u[y])), ex2(__uint_as_float(u[y + 1]))};
+              part = add2(part, v);
+              w[y / 2] = pack_half(v.x, v.y);
+            }
+            l = fmaf(part.x + part.y, info.g[2 * ch + g].z, l);
           }
           tm_store16(ts + 16 * ch, w);
         }
@@ -661,6 +694,10 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       if (!bar_wait(&sh->o_full[half], (n_s - 1) & 1, dead)) l = NAN;
       tc_fence_after();
     }
+    const int64_t token = s.q.first + a.by_group.of(x);
+    const int head = s.h * a.group + a.by_group.rest(x);
+    T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
+    if (fresh) m = -INFINITY;
     const bool done = seg == s.tiles;
     const int64_t slot = 2 * blockIdx.x + (s.t == 0);
     float* part = a.part + (slot * kItemRows + half * kHalf + row) * D;
@@ -843,7 +880,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __gri
   __syncthreads();
   tc_fence_after();
   if (warp < kConvWarp) softmax<D, T>(a, s, count, &sh);
-  else if (warp < kMmaWarp) convert<D>(a, s, count, &sh, kbuf, vbuf);
+  else if (warp < kMmaWarp) convert<D>(a, s, count, &sh, kbuf);
   else if (warp == kMmaWarp) issue<D>(a, s, count, &sh, qbuf, kbuf, vbuf);
   else queries<D, T>(a, s, count, &sh, qbuf);
   __syncwarp();
