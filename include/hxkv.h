@@ -124,7 +124,7 @@ typedef struct hx_kv_query {
   const void* q;              /* 16-byte aligned */
   void* out;                  /* 16-byte aligned, same type as q; may not overlap it */
   float* lse;                 /* [n_tokens][n_heads] log of the sum of exponentials (-inf: nothing visible), or NULL */
-  int64_t q_token_stride, q_head_stride;      /* elements, multiples of 8 */
+  int64_t q_token_stride, q_head_stride;      /* elements, multiples of 8, 0..2^38 */
   int64_t out_token_stride, out_head_stride;  /* elements, multiples of 8 */
   int32_t n_tokens;           /* 0.., and n_tokens * n_heads / n_kv_heads at most HX_KV_MAX_TOKENS */
   int32_t n_heads;            /* a multiple of n_kv_heads, at most 128 * n_kv_heads */

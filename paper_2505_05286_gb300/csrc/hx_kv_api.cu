@@ -110,6 +110,8 @@ int hx_kv_attend(const hx_kv_cache* c, const hx_kv_query* a, void* stream) {
   if (!aligned(a->q) || !aligned(a->out)) return bad("queries: q and out must be 16-byte aligned");
   if (a->q_token_stride % 8 || a->q_head_stride % 8 || a->out_token_stride % 8 || a->out_head_stride % 8)
     return bad("queries: strides must be multiples of 8 elements");
+  if (a->q_token_stride < 0 || a->q_head_stride < 0 || a->q_token_stride >= (int64_t)1 << 38 || a->q_head_stride >= (int64_t)1 << 38)
+    return bad("queries: q's strides must be 0..2^38");
   const int64_t need = hx::kv_attend_workspace(*c, *a);
   if (a->workspace_bytes < need || (need && !a->workspace)) return bad("queries: workspace is too small");
   if (need && !aligned(a->workspace)) return bad("queries: workspace must be 16-byte aligned");

@@ -714,9 +714,12 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
   const int4 join = a.joins[blockIdx.x];
   if (join.z < 0) return;
   const Request q = request(a, join.x);
-  const int64_t item = (int64_t)join.w * kSlotRows;  // the item's first row of its request
+  // the token and head of this block's rows; a half's rows of the many-rows kernel begin at 0 and 128
   const int y0 = blockIdx.y * kRows;
-  const int rows = min(kRows, (int)min((int64_t)kSlotRows, (int64_t)q.n * a.group - item) - y0);
+  constexpr int kHalf = kSlotRows / 2;
+  const bool halves = kSlotRows == kItemRows;
+  const int i0 = halves ? (join.w * 2 + y0 / kHalf) * a.half_tokens : 0, x0 = halves ? y0 % kHalf : y0;
+  const int rows = min(kRows, (halves ? min(a.half_tokens, q.n - i0) : q.n) * a.group - x0);
   const int parts = blockIdx.x - join.z + 1;
   if (rows <= 0) return;
   const auto slot = [&](int i) { return (2 * (int64_t)(join.z + i) + (i == 0)) * kSlotRows + y0; };
@@ -772,7 +775,8 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
     if (sub == 0 && row < rows && team / share < kTeams / share) {
       const float2 ml = s_ml[row];
       const float inv = ml.y == 0 ? 0.f : 1.f / ml.y;
-      const int64_t x = item + y0 + row, token = q.first + x / a.group, head = join.y * a.group + x % a.group;
+      const int64_t token = q.first + i0 + a.by_group.of(x0 + row);
+      const int head = join.y * a.group + a.by_group.rest(x0 + row);
       T* to = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + 4 * col;
       *(uint2*)to = uint2{from_float2<T>(o.x * inv, o.y * inv), from_float2<T>(o.z * inv, o.w * inv)};
       if (col == 0 && a.lse)
@@ -845,6 +849,21 @@ bool tile_map(CUtensorMap* m, const void* base, const hx_kv_cache& c, int rows) 
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// q as [tokens][heads][head_dim], fetched a half's tokens of one group and 64 columns at a time.
+bool query_map(CUtensorMap* m, const hx_kv_cache& c, const hx_kv_query& q, int tokens) {
+  const Encode f = encoder();
+  if (!f) return false;
+  const int group = q.n_heads / c.n_kv_heads;
+  const cuuint64_t dim[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)q.n_heads, (cuuint64_t)q.n_tokens};
+  // the stride of a dimension of one is of no matter, but has to be one that a map can have
+  const cuuint64_t stride[2] = {2 * (cuuint64_t)(q.n_heads > 1 ? q.q_head_stride : c.head_dim),
+                                2 * (cuuint64_t)(q.n_tokens > 1 ? q.q_token_stride : c.head_dim)};
+  const cuuint32_t box[3] = {64, (cuuint32_t)group, (cuuint32_t)tokens}, one[3] = {1, 1, 1};
+  return f(m, q.dtype == HX_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)q.q, dim, stride, box,
+           one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 AttendArgs args_of(const hx_kv_cache& c, const hx_kv_query& q) {
   AttendArgs a = {};
   a.k = (const uint8_t*)c.k, a.v = (const uint8_t*)c.v, a.k_scale = c.k_scale, a.v_scale = c.v_scale;
@@ -857,6 +876,7 @@ AttendArgs args_of(const hx_kv_cache& c, const hx_kv_query& q) {
   a.n_heads = q.n_heads, a.n_kv_heads = c.n_kv_heads, a.group = q.n_heads / c.n_kv_heads;
   while ((1 << a.block_shift) < c.block_tokens) ++a.block_shift;
   a.by_group = divisor(a.group);
+  a.half_tokens = kItemRows / 2 / a.group;
   a.max_q = q.max_q, a.causal = q.causal;
   a.window = q.window >= (1 << 30) ? 0 : q.window;  // no request holds so many tokens
   a.sm_scale_log2 = q.sm_scale * kLog2e;
@@ -902,7 +922,9 @@ cudaError_t launch_typed(const hx_kv_cache& c, const hx_kv_query& q, AttendArgs 
   if (few) return cudaSuccess;
   const int blocks = sm_count();
   const AttendArgs many = with(a, q.workspace, workspace(D, blocks, kItemRows));
-  if (cudaError_t e = launch_attend_many(many, D, std::is_same<T, __nv_bfloat16>::value, blocks, s)) return e;
+  CUtensorMap qm;
+  if (!query_map(&qm, c, q, a.half_tokens)) return cudaErrorInvalidValue;
+  if (cudaError_t e = launch_attend_many(qm, many, D, std::is_same<T, __nv_bfloat16>::value, blocks, s)) return e;
   return launch_join<D, kItemRows, T>(many, blocks, s);
 }
 

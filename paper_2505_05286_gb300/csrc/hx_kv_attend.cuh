@@ -12,7 +12,7 @@
 namespace hx {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kItemRows = 256;  // rows of an item of the many-rows kernel
+constexpr int kItemRows = 256;  // places for rows of an item of the many-rows kernel: two halves of 128
 
 // Division by a divisor known on the host (Granlund and Montgomery's invariant
 // division): x / d for 0 <= x < 2^31.
@@ -49,6 +49,7 @@ struct AttendArgs {
   int32_t block_shift, max_q, causal, window;
   int32_t few_rows;     // requests of so many rows at most are the few-rows kernel's
   Divisor by_group;     // rows to tokens
+  int32_t half_tokens;  // of an item's half in the many-rows kernel: 128 / group
   float sm_scale_log2;  // sm_scale * log2(e): scores are exponents of two
   float* part;          // partial results of items that several blocks share
   float* part_ml;
@@ -56,7 +57,7 @@ struct AttendArgs {
 };
 
 // Launches the many-rows kernel (hx_kv_attend_many.cu) on `blocks` blocks.
-cudaError_t launch_attend_many(const AttendArgs& a, int head_dim, bool bf16, int blocks, cudaStream_t s);
+cudaError_t launch_attend_many(const CUtensorMap& qm, const AttendArgs& a, int head_dim, bool bf16, int blocks, cudaStream_t s);
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -104,6 +105,18 @@ __device__ __forceinline__ void tile_load(void* dst, const CUtensorMap* map, uin
           smem_addr(dst)),
       "l"(map), "r"(smem_addr(bar)), "r"(x), "r"(y), "r"(z)
       : "memory");
+}
+
+__device__ __forceinline__ void tile_prefetch(const CUtensorMap* map, int x, int y, int z) {  // into L2
+  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+
+// `bytes` (a multiple of 16) in a row, both sides 16-byte aligned.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(dst)),
+               "l"(src), "r"(bytes), "r"(smem_addr(bar))
+               : "memory");
 }
 
 __device__ __forceinline__ float ex2(float x) {

@@ -9,46 +9,46 @@
 namespace hx {
 namespace {
 
-// Bound by the tensor cores: 4 D operations per row and visible token.  An item is 256 rows of
-// one request and kv head, in two halves of 128, the height of a tcgen05
-// accumulator; its tokens come in tiles of 128, and all items' tiles, laid end to end, are
+// Bound by the tensor cores: 4 D operations per row and visible token.  An item is two halves of
+// one request and kv head, each as many whole tokens as give 128 rows at most (the height of
+// a tcgen05 accumulator); the tokens it sees come in tiles of 128, and all items' tiles, laid end to end, are
 // dealt out to one block per SM in equal stretches (items that blocks share are joined by a
 // second kernel).  In a block,
-//   4 warps turn the tiles' e4m3 into f16 in shared memory, in the layout that tcgen05 reads
-//     (both halves use each: the conversion is paid once for 256 rows),
-//   3 warps put the item's q beside them,
-//   1 warp issues the products: S = Q K^T into tensor memory, O += P V with P read from
+//   1 warp looks the tiles up and has them copied to shared memory as they are,
+//   4 warps turn their e4m3 into 16 bits in the layout that tcgen05 reads: keys into q's type, values
+//     into f16, both exact (both halves use each: the conversion is paid once for 256 rows),
+//   1 thread has an item's q copied as soon as the last item's products have read theirs,
+//   1 thread issues the products: S = Q K^T into tensor memory, O += P V with P read from
 //     tensor memory, the halves alternating, so that one half's products run while the other's
 //     softmax does,
 //   2 x 4 warps do a half's softmax, a row to a thread, and write P over S.
 // Tensor memory (512 columns): S, P of the halves at 0 and 128, O at 256 and 256 + D.
 //
 // Scales: a score is s * ks * c, and a value's scale vs goes into the weight, P = exp2(s ks c +
-// log2(vs) - M) with M the largest of those exponents so far (or up to 2^8 less: O is
-// rescaled only when it has moved by more).  So P in f16 is accurate
+// log2(vs) - m) with m within kLag of the largest of those exponents so far.  So P in f16 is accurate
 // relative to the row's largest weight times scale, however far apart scales lie, and the
 // softmax's sum is that of P / vs.
 constexpr int kHalf = 128;
 constexpr int kKv = 128;       // tokens of a tile
 constexpr int kGroups = kKv / 16;
-constexpr int kConvWarp = 8, kMmaWarp = 12, kQueryWarp = 13;
-constexpr int kQueryWarps = 3;
-constexpr int kManyThreads = 32 * (kQueryWarp + kQueryWarps);
-constexpr int kNanList = 64;
+constexpr int kConvWarp = 8, kMmaWarp = 12, kFetchWarp = 13, kQueryWarp = 14;
+constexpr int kManyThreads = 32 * (kQueryWarp + 1);
+constexpr int kNanList = 16;
 
 template <int D>
 struct Many {
   static constexpr int kQBytes = kHalf * D * 2;   // one half's q
   static constexpr int kTile = kKv * D * 2;       // K or V in f16
-  static constexpr int kSmem = 2 * kQBytes + 4 * kTile + 1024;
+  static constexpr int kRaw = kKv * D;            // K or V as it is in the cache
+  static constexpr int kTiles = 2 * kQBytes + 4 * kTile + 2 * kRaw;
 };
 
 struct Segment {  // a stretch of one item's tiles
-  int r, h, mt;           // request, kv head, which 256 rows
+  int r, h, mt;           // request, kv head, which tokens
   int t, tiles;           // the next tile, and how many the item has
   int first_tile;
   Request q;
-  int rows;               // of this item
+  int i0;                 // its first token in the request
   int lo0, hi0, lo1, hi1; // tokens that any row of a half sees (no arrays: an index that is not
                           // constant would put them into local memory)
   bool empty;             // nothing visible, or not to be computed: zeros
@@ -58,12 +58,12 @@ __device__ __forceinline__ bool many(const AttendArgs& a, const Request& q) {
   return q.kv > 0 && q.n * a.group > a.few_rows;
 }
 __device__ __forceinline__ int items_of(const AttendArgs& a, const Request& q) {
-  return (q.n * a.group + kItemRows - 1) / kItemRows;
+  return (q.n + 2 * a.half_tokens - 1) / (2 * a.half_tokens);
 }
 // First and end tile of item mt of a request (at least one, to write its zeros).
 __device__ __forceinline__ void item_span(const AttendArgs& a, const Request& q, int mt, int* t0, int* t1, bool* empty) {
-  const int x0 = mt * kItemRows, x1 = min(x0 + kItemRows, q.n * a.group);
-  const int lo = see_from(a, q, a.by_group.of(x0)), hi = see_to(a, q, a.by_group.of(x1 - 1));
+  const int i0 = mt * 2 * a.half_tokens, i1 = min(i0 + 2 * a.half_tokens, q.n);
+  const int lo = see_from(a, q, i0), hi = see_to(a, q, i1 - 1);
   *empty = hi <= lo;
   *t0 = *empty ? 0 : lo / kKv;
   *t1 = *empty ? 1 : (hi + kKv - 1) / kKv;
@@ -102,14 +102,13 @@ __device__ __forceinline__ void load_item(const AttendArgs& a, Segment& s) {
   item_span(a, s.q, s.mt, &t0, &t1, &s.empty);
   s.first_tile = t0;
   s.tiles = t1 - t0;
-  const int x0 = s.mt * kItemRows, all = s.q.n * a.group;
-  s.rows = min(kItemRows, all - x0);
-  s.lo0 = see_from(a, s.q, a.by_group.of(x0));
-  s.hi0 = see_to(a, s.q, a.by_group.of(min(x0 + kHalf, all) - 1));
+  s.i0 = s.mt * 2 * a.half_tokens;
+  s.lo0 = see_from(a, s.q, s.i0);
+  s.hi0 = see_to(a, s.q, min(s.i0 + a.half_tokens, s.q.n) - 1);
   s.lo1 = s.hi1 = 0;
-  if (x0 + kHalf < all) {
-    s.lo1 = see_from(a, s.q, a.by_group.of(x0 + kHalf));
-    s.hi1 = see_to(a, s.q, a.by_group.of(min(x0 + kItemRows, all) - 1));
+  if (s.i0 + a.half_tokens < s.q.n) {
+    s.lo1 = see_from(a, s.q, s.i0 + a.half_tokens);
+    s.hi1 = see_to(a, s.q, min(s.i0 + 2 * a.half_tokens, s.q.n) - 1);
   }
 }
 // To the next item; false past the last.
@@ -150,9 +149,9 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
   return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
          (uint64_t)2 << 61;
 }
-// f16 x f16 with 32-bit sums, M = 128; b_rows: B is stored with its N side contiguous.
-__host__ __device__ constexpr uint32_t instruction(int n, bool b_rows) {
-  return 1u << 4 | (b_rows ? 1u << 16 : 0) | (uint32_t)(n / 8) << 17 | (uint32_t)(128 / 16) << 24;
+// f16 x f16 or bf16 x bf16 with 32-bit sums, M = 128; b_rows: B is stored with its N side contiguous.
+__host__ __device__ constexpr uint32_t instruction(int n, bool b_rows, bool bf16) {
+  return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0) | (b_rows ? 1u << 16 : 0) | (uint32_t)(n / 8) << 17 | (uint32_t)(128 / 16) << 24;
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
   asm volatile(
@@ -220,10 +219,10 @@ struct TileInfo {
 
 // The barriers and small shared state of a block.
 struct Shared {
+  uint64_t raw_full[2], raw_empty[2];  // of keys and values as they come
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], go[2], ended[2][2];  // go and ended: of even and odd items
-  float q_scale[2][kItemRows];
-  TileInfo info[4];
+  TileInfo info[8];
   int nan_count[4];
   int nan_pos[4][kNanList];
   long long sum[kManyThreads / 32];
@@ -249,220 +248,166 @@ __device__ __forceinline__ uint32_t pack(float x, float y) {
   return *(const uint32_t*)&h;
 }
 
+// ---- the fetching warp
+
+// Lane g looks up the block of a tile's 16 tokens g, a tile ahead; the lanes whose block begins
+// there (or is the tile's first) have it copied.
+template <int D>
+__device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* raw) {
+  const int lane = threadIdx.x & 31, block = 1 << a.block_shift;
+  const int tokens = min(block, kKv);  // of a copy
+  const bool copies = lane < kGroups && (16 * lane & (tokens - 1)) == 0;
+  volatile int* dead = &sh->dead;
+  int id = -1, pos = 0, h = 0;
+  const auto look_up = [&] {
+    pos = (s.first_tile + s.t) * kKv + 16 * lane;
+    h = s.h;
+    id = lane < kGroups && pos < max(s.hi0, s.hi1) ? a.block_table[s.r * a.table_stride + (pos >> a.block_shift)] : -1;
+  };
+  const auto skip_empty = [&] {  // items that see nothing have one tile, and nothing in it
+    while (count > 0 && s.empty)
+      if (--count > 0) next_item(a, s);
+  };
+  skip_empty();
+  if (count > 0) look_up();
+  for (int it = 0; count > 0; ++it) {
+    const bool ok = (unsigned)id < (unsigned)a.n_blocks;
+    const uint32_t valid = __ballot_sync(~0u, ok);
+    const int64_t at = id * a.block_stride + ((int64_t)h * block + (pos & (block - 1))) * D;
+    float ks = 0, vs = 0;
+    if (ok) ks = a.k_scale[id * a.scale_stride + h], vs = a.v_scale[id * a.scale_stride + h];
+    --count;
+    if (count > 0 && ++s.t == s.tiles) {
+      next_item(a, s);
+      skip_empty();
+    }
+    if (count > 0) look_up();
+    const uint32_t bytes = (uint32_t)__popc(__ballot_sync(~0u, ok && copies)) * tokens * D;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      if (!__all_sync(~0u, bar_wait(&sh->raw_empty[v], (it & 1) ^ 1, dead))) return;
+      if (v == 0) {
+        TileInfo& info = sh->info[it & 7];
+        const float r = fmaxf(vs, 0x1p-100f);
+        if (lane < kGroups) info.g[lane] = float4{ks, log2f(r), 1.f / r, 0.f};
+        if (lane == 0) info.valid = valid;
+        __syncwarp();
+      }
+      if (lane == 0) bar_expect(&sh->raw_full[v], bytes);
+      __syncwarp();
+      if (ok && copies) bulk_load(raw + v * Many<D>::kRaw + 16 * lane * D, (v ? a.v : a.k) + at, tokens * D, &sh->raw_full[v]);
+    }
+  }
+}
+
 // ---- the converting warps
 
-// Loads run ahead of the conversion: a tile's keys are asked for as soon as the registers of the one
-// before are written out, its block numbers a tile earlier.
-template <int D>
-__device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* kbuf) {
+// What has not been copied (no such block) is converted as it lies there: its scores are masked, and its
+// values are numbers times weights of zero.
+template <int D, class T>
+__device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, const uint8_t* raw, uint8_t* kbuf) {
   // 8 bytes a lane: a lane's 8 f16 are one 16-byte unit, and eight lanes' units lie on different banks
   constexpr int kLanes = D / 8;            // lanes of a token
   constexpr int kPer = 32 / kLanes;        // tokens of a warp's load
   constexpr int kLoads = 32 / kPer;        // loads of a warp's 32 tokens
   const int tid = threadIdx.x - 32 * kConvWarp, warp = tid >> 5, lane = tid & 31;
   const int unit = lane % kLanes, sub = lane / kLanes;
-  const int block = 1 << a.block_shift;
-  int seg_no = 0;
-
-  // this warp's 32 tokens of a tile lie in one block of the cache, or in two of 16
-  int pos, end, id[2];
-  int64_t at[2];
-  float ks[2], vs[2];
-  uint2 kr[kLoads], vr[kLoads];
-  const auto numbers = [&] {
-    pos = (s.first_tile + s.t) * kKv + 32 * warp;
-    end = max(s.hi0, s.hi1);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int p = pos + 16 * x;
-      id[x] = p < end ? a.block_table[s.r * a.table_stride + (p >> a.block_shift)] : -1;
-    }
+  volatile int* dead = &sh->dead;
+  int seg_no = 0, it = 0;
+  // a tile's f16 rows: panels of 64 columns, 128-byte rows, 16-byte units permuted
+  uint8_t* const row0 = kbuf + (unit >> 3) * (kKv * 128) + (32 * warp + sub) * 128;
+  const auto put = [&](int offset, uint4 h, int j) {
+    const int tok = j * kPer;
+    *(uint4*)(row0 + offset + tok * 128 + (((unit & 7) ^ ((tok + sub) & 7)) << 4)) = h;
   };
-  const auto places = [&] {
+  const auto halves = [](const uint2& u) { return uint4{cvt2(u.x), cvt2_hi(u.x), cvt2(u.y), cvt2_hi(u.y)}; };
+  const auto key = [&](const uint2& u) {
+    uint4 h = halves(u);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+      uint32_t* w = (uint32_t*)&h;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      ks[x] = vs[x] = 0;
-      at[x] = -1;
-      if ((unsigned)id[x] < (unsigned)a.n_blocks) {
-        at[x] = id[x] * a.block_stride + ((int64_t)s.h * block + ((pos + 16 * x) & (block - 1))) * D + unit * 8;
-        ks[x] = a.k_scale[id[x] * a.scale_stride + s.h];
-        vs[x] = a.v_scale[id[x] * a.scale_stride + s.h];
+      for (int y = 0; y < 4; ++y) {
+        const float2 f = two<__half>(w[y]);
+        w[y] = pack<__nv_bfloat16>(f.x, f.y);
       }
     }
+    return h;
   };
-  const auto fetch = [&](const uint8_t* from, uint2* to) {
+  const auto take = [&](int v, uint2* u) {
+    bar_wait(&sh->raw_full[v], it & 1, dead);
+    const uint8_t* from = raw + v * Many<D>::kRaw + (32 * warp + sub) * D + unit * 8;
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const int tok = j * kPer + sub;
-      const int64_t o = (j * kPer) >> 4 ? at[1] : at[0];
-      to[j] = o >= 0 && pos + tok < end ? *(const uint2*)(from + o + (tok & 15) * D) : uint2{0, 0};
-    }
+    for (int j = 0; j < kLoads; ++j) u[j] = *(const uint2*)(from + j * kPer * D);
+    __syncwarp();
+    if (lane == 0) bar_arrive(&sh->raw_empty[v]);
   };
-  // the tile's f16 rows: panels of 64 columns, 128-byte rows, 16-byte units permuted
-  uint8_t* const row0 = kbuf + (unit >> 3) * (kKv * 128) + (32 * warp + sub) * 128;
-  const auto put = [&](int offset, const uint2& u, int j) {
-    const int tok = j * kPer;  // of this lane's first; kPer <= 4 leaves bits of the row number apart
-    *(uint4*)(row0 + offset + tok * 128 + (((unit & 7) ^ ((tok + sub) & 7)) << 4)) =
-        uint4{cvt2(u.x), cvt2_hi(u.x), cvt2(u.y), cvt2_hi(u.y)};
-  };
-  // items that see nothing have one tile, and nothing in it
-  const auto skip_empty = [&] {
-    while (count > 0 && s.empty)
-      if (--count > 0) next_item(a, s);
-  };
-
-  skip_empty();
-  if (count <= 0) return;
-  numbers();
-  places();
-  fetch(a.k, kr);
-  fetch(a.v, vr);
-  bool first = true;
-  for (int it = 0;; ++it) {
-    const int st = it & 1, here = pos;
-    const uint32_t phase = (it >> 1) & 1;
-    bar_wait(&sh->k_empty[st], phase ^ 1, &sh->dead);
-    TileInfo& info = sh->info[it & 3];
-    if (lane < 2) {
-      const float r = fmaxf(lane ? vs[1] : vs[0], 0x1p-100f);
-      info.g[2 * warp + lane] = float4{lane ? ks[1] : ks[0], log2f(r), 1.f / r, 0.f};
-    }
-    if (lane == 0) ((uint8_t*)&info.valid)[warp] = (uint8_t)((at[0] >= 0 ? 1 : 0) | (at[1] >= 0 ? 2 : 0));
+  HX_SEGMENTS(s, count) {
+    if (s.empty) continue;
     const int list = seg_no & 3;
-    if (first) {
-      if (tid == 0) sh->nan_count[list] = 0;
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-    }
-    // the next tile
-    --count;
-    first = false;
-    if (count > 0 && ++s.t == s.tiles) {
-      next_item(a, s);
-      skip_empty();
-      first = true;
-      ++seg_no;
-    }
-    const bool more = count > 0;
-    if (more) numbers();
+    if (tid == 0) sh->nan_count[list] = 0;
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    for (int i = 0; i < seg && !__any_sync(~0u, *dead); ++i, ++it) {
+      const int st = it & 1;
+      const uint32_t phase = (it >> 1) & 1;
+      uint2 u[kLoads];
+      take(0, u);
+      bar_wait(&sh->k_empty[st], phase ^ 1, dead);
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) put(st * Many<D>::kTile, kr[j], j);
-    fence_async();
-    bar_arrive(&sh->k_full[st]);
-    if (more) {
-      places();
-      fetch(a.k, kr);
-    }
-    bar_wait(&sh->v_empty[st], phase ^ 1, &sh->dead);
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
+      for (int j = 0; j < kLoads; ++j) put(st * Many<D>::kTile, key(u[j]), j);
+      fence_async();
+      bar_arrive(&sh->k_full[st]);
+      take(1, u);
+      bar_wait(&sh->v_empty[st], phase ^ 1, dead);
       const auto nans = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };
-      if (nans(vr[j].x) | nans(vr[j].y)) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) any |= ((u[j].x & 0x7f7f7f7fu) + 0x01010101u) | ((u[j].y & 0x7f7f7f7fu) + 0x01010101u);
+      if (any & 0x80808080u) {
         // a NaN would reach rows that do not see it (0 * NaN): taken out here, and put
         // into the rows that see it at their end
-        vr[j].x &= ~((nans(vr[j].x) >> 7) * 0xffu);
-        vr[j].y &= ~((nans(vr[j].y) >> 7) * 0xffu);
-        const int n = atomicAdd(&sh->nan_count[list], 1);
-        if (n < kNanList) sh->nan_pos[list][n] = here + j * kPer + sub;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          if (!(nans(u[j].x) | nans(u[j].y))) continue;
+          u[j].x &= ~((nans(u[j].x) >> 7) * 0xffu);
+          u[j].y &= ~((nans(u[j].y) >> 7) * 0xffu);
+          const int tok = 32 * warp + j * kPer + sub, p = (s.first_tile + s.t + i) * kKv + tok;
+          if (p < max(s.hi0, s.hi1) && (sh->info[it & 7].valid >> (tok >> 4) & 1)) {
+            const int n = atomicAdd(&sh->nan_count[list], 1);
+            if (n < kNanList) sh->nan_pos[list][n] = p;
+          }
+        }
       }
-      put((2 + st) * Many<D>::kTile, vr[j], j);
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) put((2 + st) * Many<D>::kTile, halves(u[j]), j);
+      fence_async();
+      bar_arrive(&sh->v_full[st]);
     }
-    fence_async();
-    bar_arrive(&sh->v_full[st]);
-    if (!more) break;
-    fetch(a.v, vr);
+    ++seg_no;
   }
 }
 
-// ---- the query warps
+// ---- the query warp
 
-// Both halves' q in f16.  bf16 rows are scaled by a power of two so that no value leaves f16's
-// range; those are found while the item before is still computed, when these warps have
-// time.  The first half is then held ready in registers until the last item's products have read theirs.
-template <int D, class T>
-__device__ void queries(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* qbuf) {
-  constexpr bool kScaled = std::is_same<T, __nv_bfloat16>::value;
-  constexpr int kLanes = D / 8, kPer = 32 / kLanes;  // lanes of a row, rows of a warp's load
-  constexpr int kStep = kPer * kQueryWarps, kLoads = (kHalf + kStep - 1) / kStep;
-  const int warp = (threadIdx.x >> 5) - kQueryWarp, lane = threadIdx.x & 31;
-  const int unit = lane % kLanes, sub = warp * kPer + lane / kLanes;
+// A half's q: rows of token and head of the group, as they lie in q; what lies past the request
+// or past q is not used.
+template <int D>
+__device__ void queries(const AttendArgs& a, const CUtensorMap* qm, Segment s, int count, Shared* sh, uint8_t* qbuf) {
+  const uint32_t bytes = (uint32_t)(a.half_tokens * a.group) * D * 2;
   int seg_no = 0;
   HX_SEGMENTS(s, count) {
     if (s.empty) continue;
-    const auto load = [&](int half, int j) {
-      const int row = j * kStep + sub, x = s.mt * kItemRows + half * kHalf + row;
-      const int i = a.by_group.of(x), head = s.h * a.group + a.by_group.rest(x);
-      const bool real = row < kHalf && half * kHalf + row < s.rows;
-      return real ? *(const uint4*)((const T*)a.q + (int64_t)(s.q.first + i) * a.q_token_stride + head * a.q_head_stride + 8 * unit)
-                  : uint4{0, 0, 0, 0};
-    };
-    float* scale = sh->q_scale[seg_no & 1];
-    if constexpr (kScaled) {
-      constexpr int kMost = 4;
-#pragma unroll 1
-      for (int j0 = 0; j0 < 2 * kLoads; j0 += kMost) {
-        uint4 u[kMost];
-        float amax[kMost];
+    for (int half = 0; half < 2; ++half) {
+      const int token = s.q.first + s.i0 + half * a.half_tokens;
 #pragma unroll
-        for (int y = 0; y < kMost; ++y) {
-          const int j = j0 + y;
-          u[y] = j < 2 * kLoads ? load(j >= kLoads, j >= kLoads ? j - kLoads : j) : uint4{0, 0, 0, 0};
-        }
-#pragma unroll
-        for (int y = 0; y < kMost; ++y) {
-          // the largest size, as 16 bits without a sign: bf16 values order as integers
-          const uint32_t w[4] = {u[y].x & 0x7fff7fffu, u[y].y & 0x7fff7fffu, u[y].z & 0x7fff7fffu, u[y].w & 0x7fff7fffu};
-          const uint32_t m = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
-          amax[y] = __uint_as_float(max(m >> 16, m & 0xffff) << 16);
-        }
-#pragma unroll
-        for (int d = kLanes / 2; d; d >>= 1)
-#pragma unroll
-          for (int y = 0; y < kMost; ++y) {
-            const float o = __shfl_xor_sync(~0u, amax[y], d);
-            amax[y] = __float_as_uint(o) > __float_as_uint(amax[y]) ? o : amax[y];
-          }
-#pragma unroll
-        for (int y = 0; y < kMost; ++y) {
-          const int j = j0 + y, half = j >= kLoads, row = (half ? j - kLoads : j) * kStep + sub;
-          int e = 0;
-          if (amax[y] > 0 && amax[y] < INFINITY) e = max((int)(__float_as_uint(amax[y]) >> 23) - 127, -126);
-          if (unit == 0 && j < 2 * kLoads && row < kHalf) scale[half * kHalf + row] = __uint_as_float((unsigned)(127 + e) << 23);
-        }
-      }
-      __syncwarp();  // a warp writes and reads its own rows' scales
+      for (int x = 0; x < D; x += 64) tile_prefetch(qm, x, s.h * a.group, token);
     }
-#pragma unroll 1
-    for (int part = 0; part < 4; ++part) {  // half a half at a time: what registers hold
-      constexpr int kSome = (kLoads + 1) / 2;
-      const int half = part >> 1, j0 = part & 1 ? kSome : 0;
-      uint4 u[kSome];
+    for (int half = 0; half < 2; ++half) {
+      const int token = s.q.first + s.i0 + half * a.half_tokens;
+      if (!bar_wait(&sh->q_empty[half], (seg_no & 1) ^ 1, &sh->dead)) return;
+      bar_expect(&sh->q_full[half], bytes);
 #pragma unroll
-      for (int j = 0; j < kSome; ++j) u[j] = load(half, j0 + j);
-      if constexpr (kScaled) {
-#pragma unroll
-        for (int j = 0; j < kSome; ++j) {
-          const int row = (j0 + j) * kStep + sub;
-          // 2^-e from 2^e: the exponents' sum is 254
-          const float down = __uint_as_float(0x7f000000u - __float_as_uint(row < kHalf ? scale[half * kHalf + row] : 1.f));
-          uint32_t* w = (uint32_t*)&u[j];
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const float2 f = two<T>(w[y]);
-            w[y] = pack_half(f.x * down, f.y * down);
-          }
-        }
-      }
-      if (!(part & 1)) bar_wait(&sh->q_empty[half], (seg_no & 1) ^ 1, &sh->dead);
-#pragma unroll
-      for (int j = 0; j < kSome; ++j) {
-        const int row = (j0 + j) * kStep + sub;
-        if (row < kHalf)
-          *(uint4*)(qbuf + half * Many<D>::kQBytes + (unit >> 3) * (kHalf * 128) + row * 128 + (((unit & 7) ^ (row & 7)) << 4)) = u[j];
-      }
-      if (part & 1) {
-        fence_async();
-        bar_arrive(&sh->q_full[half]);
-      }
+      for (int x = 0; x < D; x += 64)
+        tile_load(qbuf + half * Many<D>::kQBytes + x / 64 * (kHalf * 128), qm, &sh->q_full[half], x, s.h * a.group, token);
     }
     ++seg_no;
   }
@@ -477,7 +422,7 @@ __device__ __forceinline__ bool elected() {
   return p;
 }
 
-template <int D>
+template <int D, class T>
 __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, const uint8_t* qbuf, const uint8_t* kbuf,
                       const uint8_t* vbuf) {
   const uint32_t tm = sh->tmem;
@@ -492,7 +437,7 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) {
         const uint32_t o = ((x >> 2) * (128 * 128) + (x & 3) * 32) >> 4;
-        mma_ss(tm + half * kKv, q + o, k + o, instruction(kKv, false), x > 0);
+        mma_ss(tm + half * kKv, q + o, k + o, instruction(kKv, false, std::is_same<T, __nv_bfloat16>::value), x > 0);
       }
       tc_commit(&sh->s_full[half]);
     }
@@ -505,7 +450,7 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
       const uint64_t v = v0 + st * (Many<D>::kTile >> 4);
 #pragma unroll
       for (int x = 0; x < kKv / 16; ++x)
-        mma_ts(tm + 256 + half * D, tm + half * kKv + 8 * x, v + x * (2048 >> 4), instruction(D, true), add || x > 0);
+        mma_ts(tm + 256 + half * D, tm + half * kKv + 8 * x, v + x * (2048 >> 4), instruction(D, true, false), add || x > 0);
       tc_commit(&sh->o_full[half]);
     }
     __syncwarp();
@@ -568,12 +513,12 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
   uint32_t n_s = 0;
   volatile int* dead = &sh->dead;
   HX_SEGMENTS(s, count) {
-    const int x = s.mt * kItemRows + half * kHalf + row;
-    const bool real = half * kHalf + row < s.rows;
+    const int i = s.i0 + half * a.half_tokens + a.by_group.of(row);  // the row's token in its request
+    const bool real = row < a.half_tokens * a.group && i < s.q.n;
     if (s.empty) {
       if (real) {
-        const int64_t token = s.q.first + a.by_group.of(x);
-        const int head = s.h * a.group + a.by_group.rest(x);
+        const int64_t token = s.q.first + i;
+        const int head = s.h * a.group + a.by_group.rest(row);
         T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
 #pragma unroll
         for (int y = 0; y < D / 8; ++y) *(uint4*)(out + 8 * y) = uint4{0, 0, 0, 0};
@@ -582,32 +527,28 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       continue;
     }
     __all_sync(~0u, bar_wait(&sh->go[seg_no & 1], (seg_no >> 1) & 1, dead));
-    const int lo = real ? see_from(a, s.q, a.by_group.of(x)) : 0, hi = real ? see_to(a, s.q, a.by_group.of(x)) : 0;
-    // what all rows of the half see: [all_lo, all_hi)
-    const int xb = s.mt * kItemRows + half * kHalf;
-    const bool full_half = xb + kHalf <= s.q.n * a.group;
-    const int all_lo = full_half ? see_from(a, s.q, a.by_group.of(xb + kHalf - 1)) : 0x7fffffff;
-    const int all_hi = full_half ? see_to(a, s.q, a.by_group.of(xb)) : 0;
-
-    float c = 0;
+    const int lo = real ? see_from(a, s.q, i) : 0, hi = real ? see_to(a, s.q, i) : 0;
+    // what all rows of the half see: [all_lo, all_hi); rows without a token do not matter
+    const int first = s.i0 + half * a.half_tokens, last = min(first + a.half_tokens, s.q.n) - 1;
+    const int all_lo = last < first ? 0 : see_from(a, s.q, last), all_hi = last < first ? 0 : see_to(a, s.q, first);
+    const float c = a.sm_scale_log2;
     float m = 0, l = 0;
     bool has = false, fresh = true;  // fresh: the row has seen nothing yet
     for (int j = 0; j < seg && !__any_sync(~0u, *dead); ++j, ++it) {
       const int tile = s.first_tile + s.t + j;
       if (!active(s, half, tile)) continue;
       const int pos = tile * kKv;
-      const TileInfo& info = sh->info[it & 3];
+      const TileInfo& info = sh->info[it & 7];
       if (!bar_wait(&sh->s_full[half], n_s & 1, dead)) l = NAN;
       tc_fence_after();
-      if (!has) c = std::is_same<T, __half>::value ? a.sm_scale_log2 : a.sm_scale_log2 * sh->q_scale[seg_no & 1][half * kHalf + row];
       const uint32_t valid = info.valid;
-      const bool whole = valid == 0x03030303u && pos >= all_lo && pos + kKv <= all_hi;
+      const bool whole = valid == (1u << kGroups) - 1 && pos >= all_lo && pos + kKv <= all_hi;
       // what this row sees of 32 tokens
       const auto sees = [&](int ch) -> uint32_t {
         const int p = pos + 32 * ch, f = min(max(lo - p, 0), 32), e = min(max(hi - p, 0), 32);
         if (f >= e) return 0;
         const uint32_t range = (0xffffffffu >> (32 - (e - f))) << f;
-        const uint32_t have = valid >> (8 * ch);
+        const uint32_t have = valid >> (2 * ch);
         return range & ((have & 1 ? 0xffffu : 0) | (have & 2 ? 0xffff0000u : 0));
       };
       // 32 tokens at a time, P over the S that has been read.  m need not be the maximum: a row moves its m
@@ -634,7 +575,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
               u[y] = __float_as_uint(v.x), u[y + 1] = __float_as_uint(v.y);
             }
           }
-          const bool late = fresh ? top > -INFINITY : top > kLag;
+          const bool late = real && (fresh ? top > -INFINITY : top > kLag);
           if (__any_sync(~0u, late)) {
             const float by = late && top < INFINITY ? ceilf(top) : 0.f;
             const float keep = fresh ? 1.f : ex2(-by);  // nothing has been kept while nothing was seen
@@ -692,8 +633,8 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       if (!bar_wait(&sh->o_full[half], (n_s - 1) & 1, dead)) l = NAN;
       tc_fence_after();
     }
-    const int64_t token = s.q.first + a.by_group.of(x);
-    const int head = s.h * a.group + a.by_group.rest(x);
+    const int64_t token = s.q.first + i;
+    const int head = s.h * a.group + a.by_group.rest(row);
     T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
     if (fresh) m = -INFINITY;
     const bool done = seg == s.tiles;
@@ -760,19 +701,23 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
 }
 
 template <int D, class T>
-__global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __grid_constant__ AttendArgs a) {
-  extern __shared__ uint8_t s_raw[];
-  __shared__ __align__(16) Shared sh;
-  uint8_t* qbuf = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* kbuf = qbuf + 2 * Many<D>::kQBytes;
-  uint8_t* vbuf = kbuf + 2 * Many<D>::kTile;
+__global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(
+    const __grid_constant__ CUtensorMap qm, const __grid_constant__ AttendArgs a) {
+  // all but the last few of the 227 KB; the tiles first, for their alignment
+  extern __shared__ __align__(1024) uint8_t s_mem[];
+  uint8_t* const qbuf = s_mem;
+  uint8_t* const kbuf = qbuf + 2 * Many<D>::kQBytes;
+  uint8_t* const vbuf = kbuf + 2 * Many<D>::kTile;
+  uint8_t* const raw = vbuf + 2 * Many<D>::kTile;
+  Shared& sh = *(Shared*)(raw + 2 * Many<D>::kRaw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   asm volatile("griddepcontrol.launch_dependents;");
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
+      bar_init(&sh.raw_full[i], 1), bar_init(&sh.raw_empty[i], 4);
       bar_init(&sh.k_full[i], 128), bar_init(&sh.v_full[i], 128);
       bar_init(&sh.k_empty[i], 1), bar_init(&sh.v_empty[i], 1);
-      bar_init(&sh.q_full[i], 32 * kQueryWarps), bar_init(&sh.q_empty[i], 1), bar_init(&sh.s_full[i], 1);
+      bar_init(&sh.q_full[i], 1), bar_init(&sh.q_empty[i], 1), bar_init(&sh.s_full[i], 1);
       bar_init(&sh.ended[i][0], 128), bar_init(&sh.ended[i][1], 128);
       bar_init(&sh.p_full[i], 128), bar_init(&sh.o_full[i], 1);
     }
@@ -878,9 +823,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __gri
   __syncthreads();
   tc_fence_after();
   if (warp < kConvWarp) softmax<D, T>(a, s, count, &sh);
-  else if (warp < kMmaWarp) convert<D>(a, s, count, &sh, kbuf);
-  else if (warp == kMmaWarp) issue<D>(a, s, count, &sh, qbuf, kbuf, vbuf);
-  else queries<D, T>(a, s, count, &sh, qbuf);
+  else if (warp < kMmaWarp) convert<D, T>(a, s, count, &sh, raw, kbuf);
+  else if (warp == kMmaWarp) issue<D, T>(a, s, count, &sh, qbuf, kbuf, vbuf);
+  else if (warp == kFetchWarp) fetch<D>(a, s, count, &sh, raw);
+  else if (lane == 0) queries<D>(a, &qm, s, count, &sh, qbuf);
   __syncwarp();
   drain(&sh.dead);
   tc_fence_before();
@@ -890,18 +836,20 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(const __gri
 }
 
 template <int D, class T>
-cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t s) {
+cudaError_t launch(const CUtensorMap& qm, const AttendArgs& a, int blocks, cudaStream_t s) {
+  constexpr int kSmem = Many<D>::kTiles + (int)sizeof(Shared);
+  static_assert(kSmem <= 227 * 1024, "shared memory of a block");
   const auto kernel = hx_kv_attend_many<D, T>;
-  if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Many<D>::kSmem)) return e;
-  kernel<<<blocks, kManyThreads, Many<D>::kSmem, s>>>(a);
+  if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)) return e;
+  kernel<<<blocks, kManyThreads, kSmem, s>>>(qm, a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_attend_many(const AttendArgs& a, int head_dim, bool bf16, int blocks, cudaStream_t s) {
-  if (head_dim == 128) return bf16 ? launch<128, __nv_bfloat16>(a, blocks, s) : launch<128, __half>(a, blocks, s);
-  return bf16 ? launch<64, __nv_bfloat16>(a, blocks, s) : launch<64, __half>(a, blocks, s);
+cudaError_t launch_attend_many(const CUtensorMap& qm, const AttendArgs& a, int head_dim, bool bf16, int blocks, cudaStream_t s) {
+  if (head_dim == 128) return bf16 ? launch<128, __nv_bfloat16>(qm, a, blocks, s) : launch<128, __half>(qm, a, blocks, s);
+  return bf16 ? launch<64, __nv_bfloat16>(qm, a, blocks, s) : launch<64, __half>(qm, a, blocks, s);
 }
 
 }  // namespace hx
