@@ -139,7 +139,7 @@ typedef struct hx_kv_query {
   int32_t causal;             /* 1: a token sees what is before it and itself; 0: all that its row holds */
   int32_t window;             /* > 0: and of those only positions above its own - window */
   float sm_scale;             /* factor of q.k */
-  void* workspace;            /* 16-byte aligned, hx_kv_attend_workspace() bytes; used until the kernels end */
+  void* workspace;            /* 32-byte aligned, hx_kv_attend_workspace() bytes; used until the kernels end */
   int64_t workspace_bytes;
 } hx_kv_query;
 

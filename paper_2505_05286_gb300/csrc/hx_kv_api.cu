@@ -114,7 +114,7 @@ int hx_kv_attend(const hx_kv_cache* c, const hx_kv_query* a, void* stream) {
     return bad("queries: q's strides must be 0..2^38");
   const int64_t need = hx::kv_attend_workspace(*c, *a);
   if (a->workspace_bytes < need || (need && !a->workspace)) return bad("queries: workspace is too small");
-  if (need && !aligned(a->workspace)) return bad("queries: workspace must be 16-byte aligned");
+  if (need && !aligned(a->workspace, 32)) return bad("queries: workspace must be 32-byte aligned");
   return launched(hx::launch_kv_attend(*c, *a, (cudaStream_t)stream), "attend");
 }
 

@@ -802,7 +802,7 @@ struct Work {
 // Two partial results of a block at most, and what it joins.
 Work workspace(int head_dim, int blocks, int slot_rows) {
   Work w;
-  w.part = 0;
+  w.part = 0;  // rows on multiples of 32 bytes, as the workspace has to begin on one
   w.ml = w.part + 2 * (int64_t)blocks * slot_rows * head_dim * 4;
   w.joins = w.ml + 2 * (int64_t)blocks * slot_rows * 8;
   w.bytes = w.joins + (int64_t)blocks * 16;
@@ -879,6 +879,7 @@ AttendArgs args_of(const hx_kv_cache& c, const hx_kv_query& q) {
   a.half_tokens = kItemRows / 2 / a.group;
   a.max_q = q.max_q, a.causal = q.causal;
   a.window = q.window >= (1 << 30) ? 0 : q.window;  // no request holds so many tokens
+  a.out_by_32 = (((uintptr_t)q.out | 2 * (uintptr_t)q.out_token_stride | 2 * (uintptr_t)q.out_head_stride) & 31) == 0;
   a.sm_scale_log2 = q.sm_scale * kLog2e;
   return a;
 }

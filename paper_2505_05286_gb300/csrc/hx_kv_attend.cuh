@@ -47,6 +47,7 @@ struct AttendArgs {
   int64_t table_stride;
   int32_t table_width, n_blocks, n_tokens, n_rows, n_heads, n_kv_heads, group;
   int32_t block_shift, max_q, causal, window;
+  int32_t out_by_32;    // whether out's rows lie on multiples of 32 bytes
   int32_t few_rows;     // requests of so many rows at most are the few-rows kernel's
   Divisor by_group;     // rows to tokens
   int32_t half_tokens;  // of an item's half in the many-rows kernel: 128 / group

@@ -47,6 +47,7 @@ struct Segment {  // a stretch of one item's tiles
   int r, h, mt;           // request, kv head, which tokens
   int t, tiles;           // the next tile, and how many the item has
   int first_tile;
+  int items;              // of the request, for one kv head
   Request q;
   int i0;                 // its first token in the request
   int lo0, hi0, lo1, hi1; // tokens that any row of a half sees (no arrays: an index that is not
@@ -114,7 +115,7 @@ __device__ __forceinline__ void load_item(const AttendArgs& a, Segment& s) {
 // To the next item; false past the last.
 __device__ __forceinline__ bool next_item(const AttendArgs& a, Segment& s) {
   s.t = 0;
-  if (++s.mt < items_of(a, s.q)) {
+  if (++s.mt < s.items) {
     load_item(a, s);
     return true;
   }
@@ -128,6 +129,7 @@ __device__ __forceinline__ bool next_item(const AttendArgs& a, Segment& s) {
     if (++s.r >= a.n_rows) return false;
     s.q = request(a, s.r);
   } while (!many(a, s.q));
+  s.items = items_of(a, s.q);
   load_item(a, s);
   return true;
 }
@@ -503,6 +505,22 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
 
 // ---- the softmax warps
 
+// N 32-bit values in a row, 32 bytes at a time where their place allows it: a thread's own row, of which each store
+// then fills whole sectors.
+template <int N>
+__device__ __forceinline__ void store32(void* p, const uint32_t* w, bool wide) {
+  if (wide) {
+#pragma unroll
+    for (int y = 0; y < N; y += 8)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"((uint32_t*)p + y), "r"(w[y]), "r"(w[y + 1]),
+                   "r"(w[y + 2]), "r"(w[y + 3]), "r"(w[y + 4]), "r"(w[y + 5]), "r"(w[y + 6]), "r"(w[y + 7])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int y = 0; y < N; y += 4) *(uint4*)((uint32_t*)p + y) = uint4{w[y], w[y + 1], w[y + 2], w[y + 3]};
+  }
+}
+
 template <int D, class T>
 __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
   constexpr float kLag = 10.f;  // of f16's 2^16
@@ -642,52 +660,42 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     float* part = a.part + (slot * kItemRows + half * kHalf + row) * D;
     const bool none = l == 0;
     const float inv = done ? (none ? 0.f : 1.f / l) : 1.f;
+#pragma unroll 1
+    for (int ch = 0; ch < D; ch += 32) {
+      uint32_t u[32];
+      tm_load(to + ch, u);
+      const float by = has && !none ? inv : 0.f;
+#pragma unroll
+      for (int y = 0; y < 32; ++y) u[y] = by == 0.f ? 0 : __float_as_uint(__uint_as_float(u[y]) * by);
+      if (!real) continue;
+      if (done) {
+        uint32_t w[16];
+#pragma unroll
+        for (int y = 0; y < 16; ++y) w[y] = pack<T>(__uint_as_float(u[2 * y]), __uint_as_float(u[2 * y + 1]));
+        store32<16>(out + ch, w, a.out_by_32);
+      } else {
+        store32<32>(part + ch, u, true);
+      }
+    }
     // NaN among the values that this row sees
-    const int list = seg_no & 3;
-    int nans = 0;
-    if (has) nans = sh->nan_count[list];
-    uint32_t nan_cols[D / 32] = {};
+    const int nans = has ? sh->nan_count[seg_no & 3] : 0;
     if (nans && real) {
       const int p0 = max(lo, (s.first_tile + s.t) * kKv), p1 = min(hi, (s.first_tile + s.t + seg) * kKv);
       const bool listed = nans <= kNanList;
+#pragma unroll 1
       for (int e = listed ? 0 : p0; e < (listed ? nans : p1); ++e) {
-        const int p = listed ? sh->nan_pos[list][e] : e;
+        const int p = listed ? sh->nan_pos[seg_no & 3][e] : e;
         if (p < p0 || p >= p1) continue;
         const int id = a.block_table[s.r * a.table_stride + (p >> a.block_shift)];
         if ((unsigned)id >= (unsigned)a.n_blocks) continue;
         const int block = 1 << a.block_shift;
-        const uint32_t* v = (const uint32_t*)(a.v + id * a.block_stride + ((int64_t)s.h * block + (p & (block - 1))) * D);
-#pragma unroll
-        for (int y = 0; y < D / 4; ++y) {
-          const uint32_t f = (((v[y] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-          nan_cols[y >> 3] |= ((f & 1) | (f >> 7 & 2) | (f >> 14 & 4) | (f >> 21 & 8)) << (4 * (y & 7));
+        const uint8_t* v = a.v + id * a.block_stride + ((int64_t)s.h * block + (p & (block - 1))) * D;
+#pragma unroll 1
+        for (int y = 0; y < D; ++y) {
+          if ((v[y] & 0x7f) != 0x7f) continue;
+          if (done) out[y] = (T)NAN;
+          else part[y] = NAN;
         }
-      }
-    }
-#pragma unroll
-    for (int ch = 0; ch < D / 32; ++ch) {
-      uint32_t u[32];
-      if (has) tm_load(to + 32 * ch, u);
-#pragma unroll
-      for (int y = 0; y < 32; ++y) {
-        float o = has && !none ? __uint_as_float(u[y]) * inv : 0.f;
-        if (nan_cols[ch] >> y & 1) o = NAN;
-        u[y] = __float_as_uint(o);
-      }
-      if (!real) continue;
-      if (done) {
-#pragma unroll
-        for (int y = 0; y < 32; y += 8) {
-          uint4 w;
-          w.x = pack<T>(__uint_as_float(u[y]), __uint_as_float(u[y + 1]));
-          w.y = pack<T>(__uint_as_float(u[y + 2]), __uint_as_float(u[y + 3]));
-          w.z = pack<T>(__uint_as_float(u[y + 4]), __uint_as_float(u[y + 5]));
-          w.w = pack<T>(__uint_as_float(u[y + 6]), __uint_as_float(u[y + 7]));
-          *(uint4*)(out + 32 * ch + y) = w;
-        }
-      } else {
-#pragma unroll
-        for (int y = 0; y < 32; y += 4) *(uint4*)(part + 32 * ch + y) = uint4{u[y], u[y + 1], u[y + 2], u[y + 3]};
       }
     }
     if (real) {
@@ -801,6 +809,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(
   Segment s;
   s.r = sh.row;
   s.q = request(a, s.r);
+  s.items = items_of(a, s.q);
   s.h = sh.head;
   s.mt = sh.mt;
   const long long skip = sh.skip;
