@@ -196,6 +196,9 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t* r) {
       "r"(addr)
       : "memory");
 }
+__device__ __forceinline__ void tm_store8(uint32_t addr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr) : "memory");
+}
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Two 32-bit values at once.
@@ -576,33 +579,36 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
         constexpr bool masked = decltype(kind)::value;
 #pragma unroll 1
         for (int ch = 0; ch < 4; ++ch) {
-          uint32_t u[32], w[16];
-          tm_load(ts + 32 * ch, u);
+          uint32_t v[32];
+          tm_load(ts + 32 * ch, v);
           const uint32_t see = masked ? sees(ch) : 0;
-          float top = -INFINITY;
+          float4 z[2];
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const float4 z = info.g[2 * ch + g];
-            const float2 f = both(z.x * c), b = both(z.y - m);
+            z[g] = info.g[2 * ch + g];
+            const float2 f = both(z[g].x * c), b = both(z[g].y - m);
 #pragma unroll
             for (int y = 16 * g; y < 16 * g + 16; y += 2) {
-              float2 v = fma2(pair(u[y], u[y + 1]), f, b);
-              if (masked && !(see >> y & 1)) v.x = -INFINITY;
-              if (masked && !(see >> (y + 1) & 1)) v.y = -INFINITY;
-              top = fmaxf(top, fmaxf(v.x, v.y));
-              u[y] = __float_as_uint(v.x), u[y + 1] = __float_as_uint(v.y);
+              float2 s2 = fma2(pair(v[y], v[y + 1]), f, b);
+              if (masked && !(see >> y & 1)) s2.x = -INFINITY;
+              if (masked && !(see >> (y + 1) & 1)) s2.y = -INFINITY;
+              top[y / 2 % 4] = fmaxf(top[y / 2 % 4], fmaxf(s2.x, s2.y));
+              v[y] = __float_as_uint(s2.x), v[y + 1] = __float_as_uint(s2.y);
             }
           }
-          const bool late = real && (fresh ? top > -INFINITY : top > kLag);
+          const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+          const bool late = real && (fresh ? most > -INFINITY : most > kLag);
           if (__any_sync(~0u, late)) {
-            const float by = late && top < INFINITY ? ceilf(top) : 0.f;
+            const float by = late && most < INFINITY ? ceilf(most) : 0.f;
             const float keep = fresh ? 1.f : ex2(-by);  // nothing has been kept while nothing was seen
             fresh &= !late;
             m += by;
             l *= keep;
 #pragma unroll
-            for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) - by);
+            for (int y = 0; y < 32; ++y) v[y] = __float_as_uint(__uint_as_float(v[y]) - by);
             tm_stored();
+            uint32_t w[16];
 #pragma unroll 1
             for (int o = 0; o < 16 * ch; o += 16) {
               const __half2 k2 = __float2half2_rn(keep);
@@ -626,16 +632,18 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
           }
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            float2 part = {0, 0};
+            float2 part[2] = {{0, 0}, {0, 0}};
+            uint32_t w[8];
 #pragma unroll
-            for (int y = 16 * g; y < 16 * g + 16; y += 2) {
-              const float2 v = {ex2(__uint_as_float(u[y])), ex2(__uint_as_float(u[y + 1]))};
-              part = add2(part, v);
-              w[y / 2] = pack_half(v.x, v.y);
+            for (int y = 0; y < 16; y += 2) {
+              const float2 e = {ex2(__uint_as_float(v[16 * g + y])), ex2(__uint_as_float(v[16 * g + y + 1]))};
+              part[y / 2 % 2] = add2(part[y / 2 % 2], e);
+              w[y / 2] = pack_half(e.x, e.y);
             }
-            l = fmaf(part.x + part.y, info.g[2 * ch + g].z, l);
+            const float2 sum = add2(part[0], part[1]);
+            l = fmaf(sum.x + sum.y, z[g].z, l);
+            tm_store8(ts + 16 * ch + 8 * g, w);
           }
-          tm_store16(ts + 16 * ch, w);
         }
       };
       if (whole) weigh(std::false_type{});
