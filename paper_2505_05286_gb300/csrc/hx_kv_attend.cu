@@ -12,15 +12,15 @@ namespace {
 // out = softmax(c q k^T) v for up to 8 or 16 rows that share their keys: bound by
 // reading the cache once.  An item is one request and kv head; its tokens are cut
 // into tiles of kTokens, and all items' tiles, laid end to end, are dealt out to the blocks in
-// equal stretches, whatever the lengths.  One warp of a block fetches (tile copies
-// into a ring of kStages), the others compute, each on its own tiles with its own running
+// equal stretches, whatever the lengths.  Two warps of a block fetch, keys and values
+// (tile copies into a ring of kStages), the others compute, each on its own tiles with its own running
 // maximum, sum and rows x D sums, joined where an item ends.  An item that
 // several blocks share leaves partial results, joined by a second kernel in a fixed order, so
 // that a result never depends on the order in which blocks run.
 //
 // Tokens are the matrix instructions' 16 rows and the few rows their 8 columns:
 // S^T = K Q^T, O^T = V^T P^T.  So eight rows waste nothing (16 x 8 x 16 the other way round would
-// compute 16), and the sums take half the registers, which lets 14 computing warps reside on an SM.
+// compute 16), and the sums take half the registers, which lets 12 computing warps reside on an SM.
 constexpr int kRows = 16;  // most rows of an item
 constexpr int kStageBytes = 8192;
 constexpr int kTileBytes = kStageBytes / 2;
@@ -30,23 +30,23 @@ template <int D, int NR>
 struct Shape {
   static constexpr int kTokens = kTileBytes / D;  // of a tile: 32 or 64
   static constexpr int kGroups = kTokens / 16;    // 16 tokens lie in one block of the cache
-  static constexpr int kWarps = NR * D <= 128 ? 7 : 5;  // computing warps, by the registers of their sums
-  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr int kWarps = NR * D <= 128 ? 6 : 4;  // computing warps, by the registers of their sums
+  static constexpr int kThreads = 32 * (kWarps + 2);
   static constexpr int kMergeRow = D + 4;         // floats; padded against bank conflicts
   static constexpr int kMergeBytes = 4 * 8 * NR * kMergeRow * 4;
   static constexpr int kStages = (106 * 1024 - kMergeBytes) / kStageBytes;
   static constexpr int kSmem = kStages * kStageBytes + kMergeBytes + 1024;
 };
 
-// Where a tile lies, its scales, and which of its groups of 16 tokens are fetched.
+// Where a tile of keys or of values lies, its scales, and which of its groups of 16 tokens are fetched.
 struct __align__(16) Tile {
-  float ks[4], vs[4];
+  float scale[4];
   int id[4];  // blocks of the cache, -1: not fetched
   int y;      // row in the tile map
   uint32_t bytes, valid;
 };
-// Tiles are looked up 32 at a time, and a tile is read no later than kStages after it: 64 places.
-constexpr int kTiles = 64;
+// Tiles are looked up kAhead at a time, and a tile is read no later than kStages after it.
+constexpr int kAhead = 16, kTiles = 32;
 
 // The tiles of an item, 0: it is not this kernel's.  An item that sees nothing,
 // with any number of rows, counts as one, so that its zeros are written.
@@ -133,54 +133,61 @@ __device__ void write_empty(const AttendArgs& a, int D, const Request& q, int h,
   }
 }
 
-// The fetching warp: looks tiles up, a lane each, one batch ahead of the copies that
-// lane 0 issues.  A look-up is two loads that depend on one another (block number, its scales);
-// they are placed before and halfway through the copies of the batch before, which hide them.
-template <int D, int NR>
-__device__ void produce(const AttendArgs& a, const CUtensorMap* km, const CUtensorMap* vm, Place<D> at, int count,
-                        int skip, uint8_t* ring, Tile* tiles, uint64_t* full, uint64_t* empty, volatile int* dead) {
+// One thread of the warp, the same each time; what it does, the hardware takes from uniform registers.
+__device__ __forceinline__ bool elected() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p;
+}
+
+// A fetching warp, of keys (V = 0) or of values: looks tiles up, a lane each, one batch ahead of the
+// copies that it issues.  A look-up is two loads that depend on one another (block number, its
+// scale); they are placed before and halfway through the copies of the batch before, which hide them.
+template <int D, int NR, int V>
+__device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at, int count, int skip, uint8_t* ring, Tile* tiles,
+                        uint64_t* full, uint64_t* empty, volatile int* dead) {
   using S = Shape<D, NR>;
   const int lane = threadIdx.x & 31;
   const int block = 1 << a.block_shift;
   const int box = min(block, S::kTokens), pieces = S::kTokens / box;
   int stage = 0;
   uint32_t phase = 1;
-  bool more = at.step(a, skip + lane), tile = false, alive = true;
-  Tile x;
-  int h = 0;
+  bool more = at.step(a, skip + lane), tile = false;
+  int id[4] = {-1, -1, -1, -1}, y = 0, h = 0;
+  float scale[4];
+  uint32_t bytes = 0, valid = 0;
 
   const auto look_up = [&](int base) {
-    tile = more && base + lane < count && at.q.kv > 0;
+    tile = more && lane < kAhead && base + lane < count && at.q.kv > 0;
 #pragma unroll
-    for (int p = 0; p < 4; ++p) x.id[p] = -1;
+    for (int p = 0; p < 4; ++p) id[p] = -1;
     if (tile) {
       const int pos = (at.first_tile + at.t) * S::kTokens;
       const int32_t* row = a.block_table + at.r * a.table_stride + (pos >> a.block_shift);
       h = at.h;
-      x.y = h * block + (pos & (block - 1));
+      y = h * block + (pos & (block - 1));
 #pragma unroll
       for (int p = 0; p < 4; ++p)
-        if (p < pieces && pos + p * box < at.q.kv) x.id[p] = row[p];
+        if (p < pieces && pos + p * box < at.q.kv) id[p] = row[p];
     }
-    if (more) more = at.step(a, 32);
+    if (more) more = at.step(a, kAhead);
   };
   const auto scales = [&] {
-    x.bytes = x.valid = 0;
+    bytes = valid = 0;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      float ks = 0.f, vs = 0.f;
-      if ((unsigned)x.id[p] < (unsigned)a.n_blocks) {
-        ks = a.k_scale[x.id[p] * a.scale_stride + h];
-        vs = a.v_scale[x.id[p] * a.scale_stride + h];
-        x.bytes += 2 * box * D;
+      float x = 0.f;
+      if ((unsigned)id[p] < (unsigned)a.n_blocks) {
+        x = (V ? a.v_scale : a.k_scale)[id[p] * a.scale_stride + h];
+        bytes += box * D;
       } else {
-        x.id[p] = -1;
+        id[p] = -1;
       }
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g)
         if (g * 16 / box == p) {
-          x.ks[g] = ks, x.vs[g] = vs;
-          if (x.id[p] >= 0) x.valid |= 1u << g;
+          scale[g] = x;
+          if (id[p] >= 0) valid |= 1u << g;
         }
     }
   };
@@ -188,39 +195,50 @@ __device__ void produce(const AttendArgs& a, const CUtensorMap* km, const CUtens
   int number = 0;
   const auto store = [&]() -> int {
     const unsigned who = __ballot_sync(~0u, tile);
-    if (tile) tiles[(number + __popc(who & ((1u << lane) - 1))) & (kTiles - 1)] = x;
+    if (tile) {
+      Tile& x = tiles[(number + __popc(who & ((1u << lane) - 1))) & (kTiles - 1)];
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g) x.scale[g] = scale[g];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) x.id[p] = id[p];
+      x.y = y, x.bytes = bytes, x.valid = valid;
+    }
     __syncwarp();
     return __popc(who);
   };
-  const auto issue = [&](int from, int to) {
-    for (int k = from; k < to && alive; ++k) {
-      const Tile& y = tiles[k & (kTiles - 1)];
-      const int id = y.id[lane & 3], at_y = y.y;
-      const uint32_t bytes = y.bytes / 2;
-      uint8_t* dst = ring + stage * kStageBytes + lane * box * D;
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        alive &= __all_sync(~0u, bar_wait(&empty[2 * stage + v], phase, dead));
-        if (!alive) break;
-        if (lane == 0) bar_expect(&full[2 * stage + v], bytes);
-        __syncwarp();
-        if (lane < pieces && id >= 0) tile_load(dst + v * kTileBytes, v ? vm : km, &full[2 * stage + v], 0, at_y, id);
+  const auto issue = [&](int from, int to) -> bool {
+    for (int k = from; k < to; ++k) {
+      const Tile& x = tiles[k & (kTiles - 1)];
+      const int at_y = x.y;
+      const uint32_t expect = x.bytes;
+      const int4 ids = *(const int4*)x.id;
+      uint8_t* dst = ring + stage * kStageBytes + V * kTileBytes;
+      if (!__all_sync(~0u, bar_wait(&empty[2 * stage + V], phase, dead))) return false;
+      if (elected()) {
+        bar_expect(&full[2 * stage + V], expect);
+        if (ids.x >= 0) tile_load(dst, map, &full[2 * stage + V], 0, at_y, ids.x);
+        if (pieces > 1) {
+          if (ids.y >= 0) tile_load(dst + box * D, map, &full[2 * stage + V], 0, at_y, ids.y);
+          if (ids.z >= 0) tile_load(dst + 2 * box * D, map, &full[2 * stage + V], 0, at_y, ids.z);
+          if (ids.w >= 0) tile_load(dst + 3 * box * D, map, &full[2 * stage + V], 0, at_y, ids.w);
+        }
       }
+      __syncwarp();
       if (++stage == S::kStages) stage = 0, phase ^= 1;
     }
-    __syncwarp();
+    return true;
   };
 
   look_up(0);
   scales();
   for (int base = 0; base < count;) {
     const int have = store();
-    base += 32;
+    base += kAhead;
     const bool next = base < count;
     if (next) look_up(base);
-    issue(number, number + have / 2);
+    if (!issue(number, number + have / 2)) return;
     if (next) scales();
-    issue(number + have / 2, number + have);
+    if (!issue(number + have / 2, number + have)) return;
     number += have;
   }
 }
@@ -235,7 +253,7 @@ __device__ __forceinline__ int order(int n) {
 }
 
 template <int D, int NR, class T>
-__device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, const uint8_t* ring, const Tile* tiles,
+__device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, const uint8_t* ring, const Tile (*tiles)[kTiles],
                         uint64_t* full, uint64_t* empty, volatile int* dead, float* merge, float (*s_ml)[kRows][2]) {
   using S = Shape<D, NR>;
   constexpr int NT = S::kTokens, KJ = D / 64, ND = D / 16, W = S::kWarps;
@@ -325,12 +343,13 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
     float unit = 1.f, unit_top = 0.f;
 
     for (; left < seg; left += W) {
-      if (!landed(2 * stage)) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
+      bool ok = landed(2 * stage);
       const uint8_t* kt = ring + stage * kStageBytes;
       const uint8_t* vt = kt + kTileBytes;
-      const Tile& mt = tiles[(it + left) & (kTiles - 1)];
+      const Tile& key_tile = tiles[0][(it + left) & (kTiles - 1)];
+      const Tile& value_tile = tiles[1][(it + left) & (kTiles - 1)];
       const int pos = (at.first_tile + at.t + left) * NT;
-      const uint32_t valid = mt.valid;
+      const uint32_t valid = key_tile.valid;
       const bool whole = valid == (1u << S::kGroups) - 1 && pos >= all_lo && pos + NT <= all_hi;
 
       // scores: of group g, tokens tn and tn + 8 by rows 2 q4 and 2 q4 + 1
@@ -354,7 +373,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
             for (int r = 0; r < NR; ++r) mma16816(s[g][r], ak, bq[r][4 * j + w][0], bq[r][4 * j + w][1]);
           }
         }
-        const float ks = mt.ks[g];
+        const float ks = key_tile.scale[g];
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -369,6 +388,25 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
       }
       __syncwarp();
       if (lane == 0) bar_arrive(&empty[2 * stage]);
+      // values of tokens ta, tb, ta + 8, tb + 8 of each group, D / 8 columns each: on their way while the
+      // softmax is done, and their place free again
+      ok &= landed(2 * stage + 1);
+      if (!ok) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
+      uint32_t vw[S::kGroups][4][D / 32];
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const uint8_t* p = vt + (16 * g + 8 * (y >> 1) + (y & 1 ? tb : ta)) * D;
+          const int sw = y & 1 ? swb : swa;
+          if constexpr (D == 128) *(uint4*)vw[g][y] = *(const uint4*)(p + ((n ^ sw) << 4));
+          else *(uint2*)vw[g][y] = *(const uint2*)(p + (((n >> 1) ^ sw) << 4) + ((n & 1) << 3));
+        }
+      float value_scale[S::kGroups];
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g) value_scale[g] = value_tile.scale[g];
+      __syncwarp();
+      if (lane == 0) bar_arrive(&empty[2 * stage + 1]);
       bool late = false;
 #pragma unroll
       for (int r = 0; r < NR; ++r) late |= top[r][0] > m[r][0] + kLag || top[r][1] > m[r][1] + kLag;
@@ -402,11 +440,10 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
             }
         }
 
-      if (!landed(2 * stage + 1)) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g) {
         // the unit follows the values' scale, at most 2^60 below the largest so far
-        const float vs = valid >> g & 1 ? mt.vs[g] : unit;
+        const float vs = valid >> g & 1 ? value_scale[g] : unit;
         const bool other = vs != unit;
         float to = 1.f, pf = 1.f;
         if (other) {
@@ -431,15 +468,6 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
           bp[r][0] = transpose8(pack_half(s[g][r][0], s[g][r][1]));
           bp[r][1] = transpose8(pack_half(s[g][r][2], s[g][r][3]));
         }
-        // values of tokens ta, tb, ta + 8, tb + 8 of the group, D / 8 columns each
-        uint32_t vw[4][D / 32];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const uint8_t* p = vt + (16 * g + 8 * (y >> 1) + (y & 1 ? tb : ta)) * D;
-          const int sw = y & 1 ? swb : swa;
-          if constexpr (D == 128) *(uint4*)vw[y] = *(const uint4*)(p + ((n ^ sw) << 4));
-          else *(uint2*)vw[y] = *(const uint2*)(p + (((n >> 1) ^ sw) << 4) + ((n & 1) << 3));
-        }
         if (!whole) {
           // a masked position's values must not count, not even as 0 * NaN
           bool nan = false;
@@ -449,8 +477,8 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
             const bool in = p >= any_lo && p < any_hi && (valid >> g & 1);
 #pragma unroll
             for (int w = 0; w < D / 32; ++w) {
-              if (!in) vw[y][w] = 0;
-              nan |= (((vw[y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+              if (!in) vw[g][y][w] = 0;
+              nan |= (((vw[g][y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
             }
           }
           if (__any_sync(~0u, nan)) {
@@ -471,8 +499,8 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
               uint32_t f[4];
 #pragma unroll
               for (int y = 0; y < 4; ++y) {
-                f[y] = (((vw[y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-                vw[y][w] &= ~(f[y] * 0xffu);
+                f[y] = (((vw[g][y][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+                vw[g][y][w] &= ~(f[y] * 0xffu);
                 f[y] *= 0x38u;
               }
 #pragma unroll
@@ -495,15 +523,13 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
         for (int w = 0; w < D / 32; ++w)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const uint32_t x = __byte_perm(vw[0][w], vw[1][w], e ? 0x7362 : 0x5140);
-            const uint32_t y = __byte_perm(vw[2][w], vw[3][w], e ? 0x7362 : 0x5140);
+            const uint32_t x = __byte_perm(vw[g][0][w], vw[g][1][w], e ? 0x7362 : 0x5140);
+            const uint32_t y = __byte_perm(vw[g][2][w], vw[g][3][w], e ? 0x7362 : 0x5140);
             const uint32_t av[4] = {cvt2(x), cvt2_hi(x), cvt2(y), cvt2_hi(y)};
 #pragma unroll
             for (int r = 0; r < NR; ++r) mma16816(acc[r][2 * w + e], av, bp[r][0], bp[r][1]);
           }
       }
-      __syncwarp();
-      if (lane == 0) bar_arrive(&empty[2 * stage + 1]);
       stage += W;
       if (stage >= S::kStages) stage -= S::kStages, phase ^= 1;
     }
@@ -609,7 +635,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   constexpr int kThreads = S::kThreads, kWarps = S::kWarps;
   extern __shared__ uint8_t s_raw[];
   __shared__ uint64_t s_full[2 * S::kStages], s_empty[2 * S::kStages];  // of a place: keys, values
-  __shared__ Tile s_tiles[kTiles];
+  __shared__ Tile s_tiles[2][kTiles];
   __shared__ __align__(16) float s_ml[kWarps][kRows][2];
   __shared__ long long s_sum[kThreads / 32], s_skip;
   __shared__ int s_row, s_dead;
@@ -691,7 +717,9 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   }
   if (s_row < 0) return;
   if (warp == kWarps)
-    produce<D, NR>(a, &km, &vm, at, count, skip, ring, s_tiles, s_full, s_empty, &s_dead);
+    produce<D, NR, 0>(a, &km, at, count, skip, ring, s_tiles[0], s_full, s_empty, &s_dead);
+  else if (warp == kWarps + 1)
+    produce<D, NR, 1>(a, &vm, at, count, skip, ring, s_tiles[1], s_full, s_empty, &s_dead);
   else
     consume<D, NR, T>(a, at, count, skip, ring, s_tiles, s_full, s_empty, &s_dead, merge, s_ml);
   drain(&s_dead);
