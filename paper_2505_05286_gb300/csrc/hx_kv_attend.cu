@@ -151,7 +151,7 @@ __device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at
   const int block = 1 << a.block_shift;
   const int box = min(block, S::kTokens), pieces = S::kTokens / box;
   int stage = 0;
-  uint32_t phase = 1;
+  uint32_t turn = 0;
   bool more = at.step(a, skip + lane), tile = false;
   int id[4] = {-1, -1, -1, -1}, y = 0, h = 0;
   float scale[4];
@@ -213,18 +213,19 @@ __device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at
       const uint32_t expect = x.bytes;
       const int4 ids = *(const int4*)x.id;
       uint8_t* dst = ring + stage * kStageBytes + V * kTileBytes;
-      if (!__all_sync(~0u, bar_wait(&empty[2 * stage + V], phase, dead))) return false;
+      if (!__all_sync(~0u, bar_wait(&empty[2 * stage + V], (turn & 1) ^ 1, dead))) return false;
+      uint64_t* const landed = &full[2 * (2 * stage + V) + (turn & 1)];
       if (elected()) {
-        bar_expect(&full[2 * stage + V], expect);
-        if (ids.x >= 0) tile_load(dst, map, &full[2 * stage + V], 0, at_y, ids.x);
+        bar_expect(landed, expect);
+        if (ids.x >= 0) tile_load(dst, map, landed, 0, at_y, ids.x);
         if (pieces > 1) {
-          if (ids.y >= 0) tile_load(dst + box * D, map, &full[2 * stage + V], 0, at_y, ids.y);
-          if (ids.z >= 0) tile_load(dst + 2 * box * D, map, &full[2 * stage + V], 0, at_y, ids.z);
-          if (ids.w >= 0) tile_load(dst + 3 * box * D, map, &full[2 * stage + V], 0, at_y, ids.w);
+          if (ids.y >= 0) tile_load(dst + box * D, map, landed, 0, at_y, ids.y);
+          if (ids.z >= 0) tile_load(dst + 2 * box * D, map, landed, 0, at_y, ids.z);
+          if (ids.w >= 0) tile_load(dst + 3 * box * D, map, landed, 0, at_y, ids.w);
         }
       }
       __syncwarp();
-      if (++stage == S::kStages) stage = 0, phase ^= 1;
+      if (++stage == S::kStages) stage = 0, ++turn;
     }
     return true;
   };
@@ -268,10 +269,11 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
 
   int it = 0;  // tiles fetched so far, over all items
   int stage = warp, left = warp;  // this warp's next: its place in the ring, and its number less `it`
-  uint32_t phase = 0;
-  // Tiles land in any order, and the tile before this one in its place is another warp's: a
-  // barrier tells a phase from the one before it only, so that one's end is waited for first.
-  const auto landed = [&](int x) { return bar_wait(&empty[x], phase ^ 1, dead) && bar_wait(&full[x], phase, dead); };
+  uint32_t turn = 0;
+  // Tiles land in any order, and the tile before this one in its place is another warp's, which need not have
+  // landed: a barrier tells a phase from the one before it only.  So a place has two of them, for its tiles
+  // by turns; the tile two before has been used, or this one would not have been asked for.
+  const auto landed = [&](int x) { return bar_wait(&full[2 * x + (turn & 1)], turn >> 1 & 1, dead); };
   bool more = at.step(a, skip);
   while (more && count > 0) {
     const int seg = min(count, at.tiles - at.t);
@@ -358,21 +360,32 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
 #pragma unroll
       for (int r = 0; r < NR; ++r) top[r][0] = top[r][1] = -INFINITY;
 #pragma unroll
-      for (int g = 0; g < S::kGroups; ++g) {
+      for (int g = 0; g < S::kGroups; ++g)
 #pragma unroll
         for (int r = 0; r < NR; ++r) s[g][r][0] = s[g][r][1] = s[g][r][2] = s[g][r][3] = 0;
+      // two groups' products in turn: each waits for its own last one only
+#pragma unroll
+      for (int g0 = 0; g0 < S::kGroups; g0 += 2)
 #pragma unroll
         for (int j = 0; j < KJ; ++j) {
-          const uint8_t* p = kt + (16 * g + tn) * D + (((q4 + 4 * j) ^ swk) << 4);
-          const uint4 k0 = *(const uint4*)p, k1 = *(const uint4*)(p + 8 * D);
+          uint4 k[2][2];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t u0 = ((const uint32_t*)&k0)[w], u1 = ((const uint32_t*)&k1)[w];
-            const uint32_t ak[4] = {cvt2(u0), cvt2(u1), cvt2_hi(u0), cvt2_hi(u1)};
-#pragma unroll
-            for (int r = 0; r < NR; ++r) mma16816(s[g][r], ak, bq[r][4 * j + w][0], bq[r][4 * j + w][1]);
+          for (int g = 0; g < 2; ++g) {
+            const uint8_t* p = kt + (16 * (g0 + g) + tn) * D + (((q4 + 4 * j) ^ swk) << 4);
+            k[g][0] = *(const uint4*)p, k[g][1] = *(const uint4*)(p + 8 * D);
           }
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const uint32_t u0 = ((const uint32_t*)&k[g][0])[w], u1 = ((const uint32_t*)&k[g][1])[w];
+              const uint32_t ak[4] = {cvt2(u0), cvt2(u1), cvt2_hi(u0), cvt2_hi(u1)};
+#pragma unroll
+              for (int r = 0; r < NR; ++r) mma16816(s[g0 + g][r], ak, bq[r][4 * j + w][0], bq[r][4 * j + w][1]);
+            }
         }
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g) {
         const float ks = key_tile.scale[g];
 #pragma unroll
         for (int r = 0; r < NR; ++r)
@@ -531,7 +544,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
           }
       }
       stage += W;
-      if (stage >= S::kStages) stage -= S::kStages, phase ^= 1;
+      if (stage >= S::kStages) stage -= S::kStages, ++turn;
     }
     left -= seg;
 
@@ -634,7 +647,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   using S = Shape<D, NR>;
   constexpr int kThreads = S::kThreads, kWarps = S::kWarps;
   extern __shared__ uint8_t s_raw[];
-  __shared__ uint64_t s_full[2 * S::kStages], s_empty[2 * S::kStages];  // of a place: keys, values
+  __shared__ uint64_t s_full[4 * S::kStages], s_empty[2 * S::kStages];  // of a place: keys, values
   __shared__ Tile s_tiles[2][kTiles];
   __shared__ __align__(16) float s_ml[kWarps][kRows][2];
   __shared__ long long s_sum[kThreads / 32], s_skip;
@@ -645,7 +658,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   asm volatile("griddepcontrol.launch_dependents;");
 
   if (tid == 0) {
-    for (int i = 0; i < 2 * S::kStages; ++i) bar_init(&s_full[i], 1), bar_init(&s_empty[i], 1);
+    for (int i = 0; i < 2 * S::kStages; ++i) bar_init(&s_full[2 * i], 1), bar_init(&s_full[2 * i + 1], 1), bar_init(&s_empty[i], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s_dead = 0;
     s_row = -1;
