@@ -69,7 +69,7 @@ typedef struct hx_kv_map_args {
   int64_t* slots;             /* [n_tokens] out: block * block_tokens + place of each token, -1: none */
   int32_t* runs;              /* [n_runs][4] out, 16-byte aligned: for each block that the step writes, in token
                                  order: first token, tokens, block, first place; zeros behind them */
-  int32_t* counts;            /* [4] out: tokens, runs, refused rows, blocks taken */
+  int32_t* counts;            /* [4] out, 16-byte aligned: tokens, runs, refused rows, blocks taken */
   int64_t* ring_state_out;    /* [2] out, not ring_state itself */
 } hx_kv_map_args;
 

@@ -74,7 +74,7 @@ int hx_kv_map(const hx_kv_map_args* a, void* stream) {
       !a->counts || !a->ring_state_out || (a->n_tokens && (!a->slots || !a->runs)))
     return bad("map: NULL pointer");
   if (a->ring_state == a->ring_state_out) return bad("map: ring_state_out must not be ring_state");
-  if (!aligned(a->runs)) return bad("map: runs must be 16-byte aligned");
+  if (!aligned(a->runs) || !aligned(a->counts)) return bad("map: runs and counts must be 16-byte aligned");
   return launched(hx::launch_kv_map(*a, (cudaStream_t)stream), "map");
 }
 

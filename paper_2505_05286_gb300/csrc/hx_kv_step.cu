@@ -14,12 +14,15 @@ namespace {
 constexpr int kMapThreads = 512;
 constexpr int kMapChunk = 2048;  // tokens of one block
 
-// What the rows before a row take, and in the same form what one row takes.
+// What the rows before a row take, and in the same form what one row takes.  Sums stop at
+// kFull, above every limit that they are compared with: malformed lengths cannot overflow
+// them, and stopping sums may still be added in any order.
+constexpr uint32_t kFull = 0x7fffffffu;
 struct RowSum {
-  long long tok, need, runs, gone;
-  int live;  // rows with tokens
+  uint32_t tok, need, runs, gone, live;  // live: rows with tokens
   __device__ RowSum& operator+=(const RowSum& o) {
-    tok += o.tok, need += o.need, runs += o.runs, gone += o.gone, live += o.live;
+    tok = min(tok + o.tok, kFull), need = min(need + o.need, kFull), runs = min(runs + o.runs, kFull);
+    gone = min(gone + o.gone, kFull), live += o.live;
     return *this;
   }
 };
@@ -28,100 +31,110 @@ __device__ RowSum shfl_up(const RowSum& x, int d) {
   return {__shfl_up_sync(~0u, x.tok, d), __shfl_up_sync(~0u, x.need, d), __shfl_up_sync(~0u, x.runs, d),
           __shfl_up_sync(~0u, x.gone, d), __shfl_up_sync(~0u, x.live, d)};
 }
+// Of a warp's lanes up to and with each, and without it.
+__device__ RowSum scan(const RowSum& x, int lane, RowSum* before) {
+  RowSum s = x;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const RowSum o = shfl_up(s, d);
+    if (lane >= d) s += o;
+  }
+  *before = shfl_up(s, 1);
+  if (lane == 0) *before = RowSum{};
+  return s;
+}
 
 struct Row {
   int held, add, tok;
   bool bad;
 };
 
-__device__ Row read_row(const hx_kv_map_args& a, int r) {
+__device__ Row read_row(const hx_kv_map_args& a, int r, int shift) {
   Row w;
   w.held = a.held[r];
   w.add = a.add[r];
   w.tok = max(w.add, 0);
-  const long long B = a.block_tokens;
-  w.bad = w.held < 0 || w.add < -1 || ((long long)w.held + w.tok + B - 1) / B > a.table_width;
+  // table_width is at most 2^23: a row that fits it has 32-bit positions
+  w.bad = w.held < 0 || w.add < -1 || (((int64_t)w.held + w.tok + (1 << shift) - 1) >> shift) > a.table_width;
   return w;
 }
 
-__device__ RowSum sum_of(const Row& w, int B) {
-  RowSum s = {w.tok, 0, 0, 0, w.tok > 0};
+__device__ RowSum sum_of(const Row& w, int shift) {
+  RowSum s = {(uint32_t)w.tok, 0, 0, 0, w.tok > 0};
   if (w.bad) return s;
-  const int old = (w.held + B - 1) / B;
-  s.need = (w.held + w.tok + B - 1) / B - old;
-  if (w.tok > 0) s.runs = (w.held + w.tok - 1) / B - w.held / B + 1;
+  const int old = (w.held + (1 << shift) - 1) >> shift;
+  s.need = ((w.held + w.tok + (1 << shift) - 1) >> shift) - old;
+  if (w.tok > 0) s.runs = ((w.held + w.tok - 1) >> shift) - (w.held >> shift) + 1;
   if (w.add < 0) s.gone = old;
   return s;
 }
 
 // Every block scans all rows (8 bytes each, from L2) and then writes its own
-// kMapChunk tokens and kMapThreads rows: one launch, no block waits for another.  The
-// cost of a step's tables is this scan's latency up to some hundred
-// thousand tokens, and the slots' 8 bytes a token above.
-__global__ void __launch_bounds__(kMapThreads) hx_kv_map_kernel(const hx_kv_map_args a) {
-  __shared__ RowSum s_warp[kMapThreads / 32];
+// kMapChunk tokens and kMapThreads rows: one launch, no block waits for another.  A
+// step's tables cost this scan's latency, and from some hundred thousand tokens on the
+// slots' 8 bytes a token.
+__global__ void __launch_bounds__(kMapThreads) hx_kv_map_kernel(const hx_kv_map_args a, int shift) {
+  __shared__ RowSum s_warp[kMapThreads / 32], s_before[kMapThreads / 32];
   __shared__ RowSum s_total;
   // the rows that own tokens of this chunk, at their rank among rows with tokens modulo
   // kMapChunk: they are consecutive and each owns a token of it
   __shared__ int s_start[kMapChunk], s_held[kMapChunk], s_row[kMapChunk], s_take[kMapChunk], s_run[kMapChunk];
   __shared__ int s_gone[kMapThreads];  // of the block's own rows: where their blocks go, -1: nowhere
   __shared__ int s_first, s_last, s_refused;
-  __shared__ long long s_taken, s_zero;
+  __shared__ uint32_t s_taken, s_zero;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int B = a.block_tokens, n = a.n_rows;
+  const int B = 1 << shift, n = a.n_rows;
   const int per = (n + kMapThreads - 1) / kMapThreads;
   const int r0 = min(n, tid * per), r1 = min(n, r0 + per);
-  const long long c0 = (long long)blockIdx.x * kMapChunk;
+  const int64_t c0 = (int64_t)blockIdx.x * kMapChunk;
   const int own0 = blockIdx.x * kMapThreads;
 
-  const long long cap = a.n_blocks;
-  long long head = a.ring_state[0], free = a.ring_state[1];
-  if (head < 0 || head >= cap) head = 0;
-  free = min(max(free, 0LL), cap);
+  // the ring: places are head + x with x < cap, taken back by cap where they pass it
+  const uint32_t cap = a.n_blocks;
+  const int64_t head64 = a.ring_state[0], free64 = a.ring_state[1];
+  const uint32_t head = head64 < 0 || head64 >= cap ? 0 : (uint32_t)head64;
+  const uint32_t free = (uint32_t)min(max(free64, (int64_t)0), (int64_t)cap);
+  const auto place = [&](uint32_t x) {  // x < 2 cap
+    const uint32_t y = head + (x >= cap ? x - cap : x);
+    return y >= cap ? y - cap : y;
+  };
 
   RowSum mine = {};
-  for (int r = r0; r < r1; ++r) mine += sum_of(read_row(a, r), B);
-  RowSum upto = mine;
-  for (int d = 1; d < 32; d <<= 1) {
-    const RowSum o = shfl_up(upto, d);
-    if (lane >= d) upto += o;
-  }
+  for (int r = r0; r < r1; ++r) mine += sum_of(read_row(a, r, shift), shift);
+  RowSum at;
+  const RowSum upto = scan(mine, lane, &at);
   if (lane == 31) s_warp[warp] = upto;
   if (tid == 0) s_first = 0, s_last = -1, s_refused = 0, s_taken = 0;
   s_gone[tid] = -1;
   __syncthreads();
   if (warp == 0) {
-    RowSum w = lane < kMapThreads / 32 ? s_warp[lane] : RowSum{};
-    for (int d = 1; d < 32; d <<= 1) {
-      const RowSum o = shfl_up(w, d);
-      if (lane >= d) w += o;
-    }
-    if (lane < kMapThreads / 32) s_warp[lane] = w;
+    RowSum before;
+    const RowSum w = scan(lane < kMapThreads / 32 ? s_warp[lane] : RowSum{}, lane, &before);
+    if (lane < kMapThreads / 32) s_before[lane] = before;
     if (lane == 31) s_total = w, s_zero = w.runs;
   }
   __syncthreads();
   const RowSum total = s_total;
-  RowSum at = warp ? s_warp[warp - 1] : RowSum{};
-  at += upto;
-  at.tok -= mine.tok, at.need -= mine.need, at.runs -= mine.runs, at.gone -= mine.gone, at.live -= mine.live;
+  at += s_before[warp];
 
-  const long long c1 = min(c0 + kMapChunk, min(total.tok, (long long)a.n_tokens));
+  const uint32_t n_tok = a.n_tokens;
+  const int64_t c1 = min(c0 + kMapChunk, (int64_t)min(total.tok, n_tok));
   int refused = 0;
-  long long taken = 0;
+  uint32_t taken = 0;
   for (int r = r0; r < r1; ++r) {
-    const Row w = read_row(a, r);
-    const RowSum x = sum_of(w, B);
-    const long long end = at.tok + w.tok;
-    const bool no = w.bad || (w.tok > 0 && ((x.need > 0 && at.need + x.need > free) || end > a.n_tokens));
+    const Row w = read_row(a, r, shift);
+    const RowSum x = sum_of(w, shift);
+    const uint32_t end = min(at.tok + (uint32_t)w.tok, kFull);
+    const bool no = w.bad || (w.tok > 0 && ((x.need > 0 && at.need + x.need > free) || end > n_tok));
     const bool ok = !no && w.tok > 0;
     refused += no;
     if (ok) taken += x.need;
-    if (w.tok > 0 && end > a.n_tokens) atomicMin(&s_zero, at.runs);
+    if (w.tok > 0 && end > n_tok) atomicMin(&s_zero, at.runs);
     if (r >= own0 && r - own0 < kMapThreads) {
-      a.row_start[r] = (int)min(at.tok, (long long)a.n_tokens);
+      a.row_start[r] = (int)min(at.tok, n_tok);
       a.kv_len[r] = no || w.add < 0 ? 0 : w.held + w.tok;
-      if (x.gone) s_gone[r - own0] = (int)((head + free + at.gone) % cap);
+      if (x.gone) s_gone[r - own0] = (int)place(free + at.gone % cap);
     }
     if (w.tok > 0 && at.tok < c1 && end > c0) {
       const int i = at.live & (kMapChunk - 1);
@@ -129,26 +142,24 @@ __global__ void __launch_bounds__(kMapThreads) hx_kv_map_kernel(const hx_kv_map_
       s_held[i] = w.held;
       s_row[i] = ok ? r : -1;
       s_take[i] = ok ? (int)at.need : 0;
-      s_run[i] = w.bad ? -1 : (int)min(at.runs, (long long)a.n_runs);
+      s_run[i] = w.bad ? -1 : (int)min(at.runs, (uint32_t)a.n_runs);
       if (at.tok <= c0) s_first = at.live;
       if (end >= c1) s_last = at.live;
     }
     at += x;
   }
   if (blockIdx.x == 0) {
-    atomicAdd(&s_refused, refused);
-    atomicAdd((unsigned long long*)&s_taken, (unsigned long long)taken);
+    refused = __reduce_add_sync(~0u, refused);
+    taken = __reduce_add_sync(~0u, taken);
+    if (lane == 0) atomicAdd(&s_refused, refused), atomicAdd(&s_taken, taken);
   }
   __syncthreads();
 
   if (blockIdx.x == 0 && tid == 0) {
-    a.row_start[n] = (int)min(total.tok, (long long)a.n_tokens);
-    a.counts[0] = (int)min(total.tok, (long long)a.n_tokens);
-    a.counts[1] = (int)min(total.runs, 0x7fffffffLL);
-    a.counts[2] = s_refused;
-    a.counts[3] = (int)s_taken;
-    a.ring_state_out[0] = (head + s_taken) % cap;
-    a.ring_state_out[1] = min(free - s_taken + total.gone, cap);
+    a.row_start[n] = (int)min(total.tok, n_tok);
+    *(int4*)a.counts = int4{(int)min(total.tok, n_tok), (int)total.runs, s_refused, (int)s_taken};
+    a.ring_state_out[0] = place(s_taken);
+    a.ring_state_out[1] = min((int64_t)free - s_taken + total.gone, (int64_t)cap);
   }
 
   // ended rows give their blocks back
@@ -156,12 +167,16 @@ __global__ void __launch_bounds__(kMapThreads) hx_kv_map_kernel(const hx_kv_map_
     const int to = s_gone[i];
     if (to < 0) continue;
     const int32_t* row = a.block_table + (own0 + i) * a.table_stride;
-    const int blocks = (a.held[own0 + i] + B - 1) / B;
-    for (int j = lane; j < blocks; j += 32) a.ring[(to + (long long)j) % cap] = row[j];
+    const int blocks = (a.held[own0 + i] + B - 1) >> shift;
+    for (int j = lane; j < blocks; j += 32) {
+      const uint32_t y = to + (uint32_t)j % cap;
+      a.ring[y >= cap ? y - cap : y] = row[j];
+    }
   }
 
   // the chunk's tokens
-  for (long long t = c0 + tid; t < min(c0 + kMapChunk, (long long)a.n_tokens); t += kMapThreads) {
+  const int64_t stop = min(c0 + kMapChunk, (int64_t)n_tok);
+  for (int64_t t = c0 + tid; t < stop; t += kMapThreads) {
     if (t >= c1) {
       a.slots[t] = -1;
       continue;
@@ -174,36 +189,35 @@ __global__ void __launch_bounds__(kMapThreads) hx_kv_map_kernel(const hx_kv_map_
     }
     const int i = lo & (kMapChunk - 1);
     const int start = s_start[i], held = s_held[i], r = s_row[i];
+    const int64_t pos64 = (int64_t)held + (t - start);
     if (r < 0) {
       a.slots[t] = -1;
       if (s_run[i] >= 0) {  // a refused row's runs stay empty
-        const long long pos = (long long)held + (t - start);
-        const long long at_run = s_run[i] + pos / B - held / B;
-        if ((pos % B == 0 || t == start) && at_run < a.n_runs) ((int4*)a.runs)[at_run] = int4{0, 0, 0, 0};
+        const int64_t at_run = s_run[i] + (pos64 >> shift) - (held >> shift);
+        if (((pos64 & (B - 1)) == 0 || t == start) && at_run < a.n_runs) ((int4*)a.runs)[at_run] = int4{0, 0, 0, 0};
       }
       continue;
     }
-    const int pos = held + (int)(t - start), blk = pos / B, off = pos % B, old = (held + B - 1) / B;
+    const int pos = (int)pos64, blk = pos >> shift, off = pos & (B - 1), old = (held + B - 1) >> shift;
     const bool first = off == 0 || t == start;
     int id;
     if (blk >= old) {
-      id = a.ring[(head + s_take[i] + (blk - old)) % cap];
+      id = a.ring[place(s_take[i] + (blk - old))];
       if (first) a.block_table[r * a.table_stride + blk] = id;
     } else {
       id = a.block_table[r * a.table_stride + blk];
     }
-    a.slots[t] = (unsigned)id < (unsigned)a.n_blocks ? (int64_t)id * B + off : -1;
+    a.slots[t] = (unsigned)id < (unsigned)a.n_blocks ? ((int64_t)id << shift) + off : -1;
     if (first) {
-      const int next = i + 1;
-      const int end = lo < s_last ? s_start[next & (kMapChunk - 1)] : -1;
+      const int end = lo < s_last ? s_start[(i + 1) & (kMapChunk - 1)] : -1;
       // a row's end: where the next one starts, or for the chunk's last row from its own length
-      const int left = (end >= 0 ? end : (int)min((long long)start + a.add[r], (long long)a.n_tokens)) - (int)t;
-      const int at_run = s_run[i] + blk - held / B;
+      const int left = (end >= 0 ? end : (int)min((int64_t)start + a.add[r], (int64_t)n_tok)) - (int)t;
+      const int at_run = s_run[i] + blk - (held >> shift);
       if (at_run < a.n_runs) ((int4*)a.runs)[at_run] = int4{(int)t, min(B - off, left), id, off};
     }
   }
-  for (long long i = min(s_zero, (long long)a.n_runs) + (long long)blockIdx.x * kMapThreads + tid; i < a.n_runs;
-       i += (long long)gridDim.x * kMapThreads)
+  for (int64_t i = min(s_zero, (uint32_t)a.n_runs) + (int64_t)blockIdx.x * kMapThreads + tid; i < a.n_runs;
+       i += (int64_t)gridDim.x * kMapThreads)
     ((int4*)a.runs)[i] = int4{0, 0, 0, 0};
 }
 
@@ -266,60 +280,86 @@ __device__ void unpack4(uint32_t u, float* f) {
   f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
 }
 
-// One block of threads writes one run's tokens of one head, K or V: the largest
-// size first, then the values (read again, from L1), then, if the scale grew,
-// the block's older tokens.
-template <class T>
-__global__ void __launch_bounds__(128) hx_kv_append_kernel(const hx_kv_cache c, const hx_kv_new a) {
-  constexpr int kN = Unpack<T>::n;
-  __shared__ float s_max[4];
-  const int tid = threadIdx.x;
-  const int H = c.n_kv_heads, D = c.head_dim, B = c.block_tokens;
-  const unsigned which = blockIdx.x & 1, rest = blockIdx.x >> 1;
-  const int h = rest % H;
-  const int4 run = ((const int4*)a.runs)[rest / H];
-  const int t0 = run.x, n = run.y, blk = run.z, off = run.w;
-  if (n <= 0 || t0 < 0 || (long long)t0 + n > a.n_tokens || off < 0 || n > B || off > B - n ||
-      (unsigned)blk >= (unsigned)c.n_blocks)
-    return;
+// A team of TW warps writes one run's tokens of one head, K or V, in one pass over them: 32
+// values a lane (16 in a row, twice) stay in registers while their largest size is found, a whole
+// block of the cache being TW * 1024 values.  Bound by reading the tokens and writing them back in 8
+// bits where a step brings prompts, by latency where it brings single tokens.  If the scale grew, the
+// block's older tokens follow.
+constexpr int kAppendWarps = 4;
+
+template <class T, int TW>
+__global__ void __launch_bounds__(32 * (TW > kAppendWarps ? TW : kAppendWarps)) hx_kv_append_kernel(const hx_kv_cache c, const hx_kv_new a,
+                                                                                                   int d_shift) {
+  constexpr int kN = Unpack<T>::n;  // values of a 16-byte load
+  constexpr int kTeams = TW > kAppendWarps ? 1 : kAppendWarps / TW;
+  __shared__ float s_max[kTeams][TW];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team = warp / TW, part = warp % TW;
+  const int D = 1 << d_shift, B = c.block_tokens;
+  const unsigned item = blockIdx.x * kTeams + team;  // run, head, K or V
+  const unsigned which = item & 1, rest = item >> 1, run_no = rest / c.n_kv_heads;
+  const int h = rest % c.n_kv_heads;
+  int4 run = {0, 0, 0, 0};
+  if (run_no < (unsigned)a.n_runs) run = ((const int4*)a.runs)[run_no];
+  const int t0 = run.x, blk = run.z, off = run.w;
+  int n = run.y;
+  if (n <= 0 || t0 < 0 || (int64_t)t0 + n > a.n_tokens || off < 0 || n > B || off > B - n || (unsigned)blk >= (unsigned)c.n_blocks) n = 0;
   const int64_t ts = which ? a.v_token_stride : a.k_token_stride, hs = which ? a.v_head_stride : a.k_head_stride;
   const T* x = (const T*)(which ? a.v : a.k) + t0 * ts + h * hs;
-  uint8_t* to = (uint8_t*)(which ? c.v : c.k) + blk * c.block_stride + (int64_t)h * B * D;
-  float* scale = (which ? c.v_scale : c.k_scale) + blk * c.scale_stride + h;
 
-  const int units = D / kN;
+  // values part * 1024 + 512 u + 16 lane and on
+  uint4 raw[2][16 / kN];
   float amax = 0;
-  for (int i = tid; i < n * units; i += 128) {
-    float f[kN];
-    Unpack<T>::get(*(const uint4*)(x + (i / units) * ts + (i % units) * kN), f);
+  float* scale_at = (which ? c.v_scale : c.k_scale) + blk * c.scale_stride + h;
+  const float was = n && off ? *scale_at : 0.f;
 #pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      const float s = fabsf(f[j]);
-      if (s < INFINITY) amax = fmaxf(amax, s);
-    }
+  for (int u = 0; u < 2; ++u) {
+    const int i = part * 1024 + 512 * u + 16 * lane, tok = i >> d_shift;
+#pragma unroll
+    for (int y = 0; y < 16 / kN; ++y)
+      raw[u][y] = tok < n ? *(const uint4*)(x + tok * ts + (i & (D - 1)) + y * kN) : uint4{0, 0, 0, 0};
   }
-  for (int d = 16; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
-  if ((tid & 31) == 0) s_max[tid >> 5] = amax;
-  const float was = off ? *scale : 0.f;
-  __syncthreads();
-  amax = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-  const float need = exp2i(scale_exponent(amax)), now = fmaxf(was, need);
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int y = 0; y < 16 / kN; ++y) {
+      float f[kN];
+      Unpack<T>::get(raw[u][y], f);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const float s = fabsf(f[j]);
+        if (s < INFINITY) amax = fmaxf(amax, s);
+      }
+    }
+  amax = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(amax)));  // sizes order as integers
+  if constexpr (TW > 1) {
+    if (lane == 0) s_max[team][part] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < TW; ++w) amax = fmaxf(amax, s_max[team][w]);
+  }
+  if (n == 0) return;
+  const float now = fmaxf(was, exp2i(scale_exponent(amax)));
   const float inv = 1.f / now;  // exact for a power of two
-  for (int i = tid; i < n * units; i += 128) {
-    float f[kN];
-    Unpack<T>::get(*(const uint4*)(x + (i / units) * ts + (i % units) * kN), f);
-    uint32_t w[kN / 4];
+  uint8_t* to = (uint8_t*)(which ? c.v : c.k) + blk * c.block_stride + (((int64_t)h * B) << d_shift);
 #pragma unroll
-    for (int j = 0; j < kN; ++j) f[j] *= inv;
+  for (int u = 0; u < 2; ++u) {
+    const int i = part * 1024 + 512 * u + 16 * lane;
+    if ((i >> d_shift) >= n) break;
+    uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < kN / 4; ++j) w[j] = pack4(f + 4 * j);
-    uint8_t* p = to + (off + i / units) * D + (i % units) * kN;
-    if constexpr (kN == 8) *(uint2*)p = uint2{w[0], w[1]};
-    else *(uint32_t*)p = w[0];
+    for (int y = 0; y < 16 / kN; ++y) {
+      float f[kN];
+      Unpack<T>::get(raw[u][y], f);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) f[j] *= inv;
+#pragma unroll
+      for (int j = 0; j < kN / 4; ++j) w[y * (kN / 4) + j] = pack4(f + 4 * j);
+    }
+    *(uint4*)(to + (off << d_shift) + i) = uint4{w[0], w[1], w[2], w[3]};
   }
   if (now > was && off) {
     const float ratio = was * inv;
-    for (int i = tid; i < off * D / 4; i += 128) {
+    for (int i = 32 * part + lane; i < (off << d_shift) / 4; i += 32 * TW) {
       float f[4];
       unpack4(((uint32_t*)to)[i], f);
 #pragma unroll
@@ -327,7 +367,27 @@ __global__ void __launch_bounds__(128) hx_kv_append_kernel(const hx_kv_cache c, 
       ((uint32_t*)to)[i] = pack4(f);
     }
   }
-  if (tid == 0 && now != was) *scale = now;
+  if (part == 0 && lane == 0 && now != was) *scale_at = now;
+}
+
+template <class T, int TW>
+cudaError_t launch_team(const hx_kv_cache& c, const hx_kv_new& a, cudaStream_t s) {
+  constexpr int kTeams = TW > kAppendWarps ? 1 : kAppendWarps / TW;
+  const unsigned items = 2u * (unsigned)a.n_runs * (unsigned)c.n_kv_heads;
+  hx_kv_append_kernel<T, TW><<<(items + kTeams - 1) / kTeams, 32 * (TW > kAppendWarps ? TW : kAppendWarps), 0, s>>>(
+      c, a, c.head_dim == 128 ? 7 : 6);
+  return cudaGetLastError();
+}
+
+template <class T>
+cudaError_t launch_append(const hx_kv_cache& c, const hx_kv_new& a, cudaStream_t s) {
+  switch (c.block_tokens * c.head_dim / 1024) {
+    case 1: return launch_team<T, 1>(c, a, s);
+    case 2: return launch_team<T, 2>(c, a, s);
+    case 4: return launch_team<T, 4>(c, a, s);
+    case 8: return launch_team<T, 8>(c, a, s);
+    default: return launch_team<T, 16>(c, a, s);
+  }
 }
 
 }  // namespace
@@ -335,18 +395,16 @@ __global__ void __launch_bounds__(128) hx_kv_append_kernel(const hx_kv_cache c, 
 cudaError_t launch_kv_map(const hx_kv_map_args& a, cudaStream_t s) {
   const int by_token = (int)(((int64_t)a.n_tokens + kMapChunk - 1) / kMapChunk);
   const int by_row = (a.n_rows + kMapThreads - 1) / kMapThreads;
-  hx_kv_map_kernel<<<std::max(by_token, by_row), kMapThreads, 0, s>>>(a);
+  int shift = 4;
+  while ((1 << shift) < a.block_tokens) ++shift;
+  hx_kv_map_kernel<<<std::max(by_token, by_row), kMapThreads, 0, s>>>(a, shift);
   return cudaGetLastError();
 }
 
 cudaError_t launch_kv_append(const hx_kv_cache& c, const hx_kv_new& a, cudaStream_t s) {
-  const int64_t all = 2 * (int64_t)a.n_runs * c.n_kv_heads;
-  if (all > 0x7fffffff) return cudaErrorInvalidValue;
-  const unsigned grid = (unsigned)all;
-  if (a.dtype == HX_BF16) hx_kv_append_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(c, a);
-  else if (a.dtype == HX_F16) hx_kv_append_kernel<__half><<<grid, 128, 0, s>>>(c, a);
-  else hx_kv_append_kernel<float><<<grid, 128, 0, s>>>(c, a);
-  return cudaGetLastError();
+  if (a.dtype == HX_BF16) return launch_append<__nv_bfloat16>(c, a, s);
+  if (a.dtype == HX_F16) return launch_append<__half>(c, a, s);
+  return launch_append<float>(c, a, s);
 }
 
 }  // namespace hx

@@ -75,48 +75,59 @@ def _fail(msg: str):
     raise H.HxError(H.HX_ERR_INVALID, msg)
 
 
-def _want(x, name: str, dtypes, ndim: int, device=None):
-    """Check one tensor argument: type, dimensions, CUDA device."""
+def _want(x, name: str, dtypes, ndim: int, device: int):
+    """Check one tensor argument: type, dimensions, CUDA device (its index)."""
     if x.dtype not in dtypes:
         _fail(f"{name}: dtype {x.dtype} is not one of {[str(d) for d in dtypes]}")
     if x.dim() != ndim:
         _fail(f"{name} must have {ndim} dimensions")
-    if not x.is_cuda:
-        _fail(f"{name} must be a CUDA tensor")
-    if device is not None and x.device != device:
-        _fail(f"{name} is on {x.device}, not on {device}")
+    if x.get_device() != device or device < 0:
+        _fail(f"{name} must be a CUDA tensor" if x.get_device() < 0 else f"{name} is not on cuda:{device}")
 
 
-def _dense(x, name: str, dtypes, ndim: int, device=None):
+def _dense(x, name: str, dtypes, ndim: int, device: int):
     _want(x, name, dtypes, ndim, device)
     if not x.is_contiguous():
         _fail(f"{name} must be contiguous")
 
 
 class _On:
-    """The device and stream of a call: kernels go to `stream` (None: torch's current
-    one of the tensors' device), and what the binding allocates belongs to it."""
+    """The device and stream of a call that names a stream, or tensors of another device than the
+    current one: kernels go there, and so does what the binding allocates."""
 
-    def __init__(self, device, stream):
+    def __init__(self, device: int, stream):
         import torch
-        self.back = None
-        if device.index != torch.cuda.current_device():
-            self.back = torch.cuda.device(device)
-            self.back.__enter__()
-        self.ctx = None
+        self.ctx = [torch.cuda.device(device)]
         if stream is not None and not isinstance(stream, int):
-            self.ctx = torch.cuda.stream(stream)
-            self.ctx.__enter__()
-        self.handle = H._stream_handle(stream)
+            self.ctx.append(torch.cuda.stream(stream))
+        self.stream = stream
 
     def __enter__(self):
-        return self.handle
+        for c in self.ctx:
+            c.__enter__()
+        return H._stream_handle(self.stream)
 
     def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
-        if self.back is not None:
-            self.back.__exit__(*exc)
+        for c in reversed(self.ctx):
+            c.__exit__(*exc)
+
+
+class _Current:
+    """The usual case, torch's current device and stream."""
+
+    def __enter__(self):
+        return H._stream_handle(None)
+
+    def __exit__(self, *exc):
+        pass
+
+
+_CURRENT = _Current()
+
+
+def _on(device: int, stream):
+    import torch
+    return _CURRENT if stream is None and device == torch.cuda.current_device() else _On(device, stream)
 
 
 def max_runs(n_rows: int, n_tokens: int, block_tokens: int) -> int:
@@ -139,9 +150,12 @@ class Step:
     @staticmethod
     def empty(n_rows: int, n_tokens: int, block_tokens: int, device="cuda") -> "Step":
         import torch
-        e = lambda *shape, t=torch.int32: torch.empty(shape, dtype=t, device=device)
-        return Step(e(n_rows + 1), e(n_rows), e(n_tokens, t=torch.int64),
-                    e(max_runs(n_rows, n_tokens, block_tokens), 4), e(4), e(2, t=torch.int64))
+        runs = max_runs(n_rows, n_tokens, block_tokens)
+        # one allocation for each type; runs and counts first, for their alignment
+        c, r, s, k = torch.empty(4 + 4 * runs + 2 * n_rows + 1, dtype=torch.int32, device=device).split(
+            (4, 4 * runs, n_rows + 1, n_rows))
+        state, slots = torch.empty(2 + n_tokens, dtype=torch.int64, device=device).split((2, n_tokens))
+        return Step(s, k, slots, r.view(runs, 4), c, state)
 
 
 def map_step(held, add, block_table, ring, ring_state, n_tokens: int, block_tokens: int, out: Optional[Step] = None,
@@ -158,8 +172,8 @@ def map_step(held, add, block_table, ring, ring_state, n_tokens: int, block_toke
     """
     import torch
     i32, i64 = (torch.int32,), (torch.int64,)
-    dev = held.device
-    _dense(held, "held", i32, 1)
+    dev = held.get_device()
+    _dense(held, "held", i32, 1, dev)
     _dense(add, "add", i32, 1, dev)
     _want(block_table, "block_table", i32, 2, dev)
     _dense(ring, "ring", i32, 1, dev)
@@ -172,9 +186,9 @@ def map_step(held, add, block_table, ring, ring_state, n_tokens: int, block_toke
     if n < 1 or n_tokens < 0:
         _fail("map: n_rows must be at least 1 and n_tokens not negative")
     lib = load()
-    with _On(dev, stream) as handle:
+    with _on(dev, stream) as handle:
         if out is None:
-            out = Step.empty(n, n_tokens, block_tokens, dev)
+            out = Step.empty(n, n_tokens, block_tokens, held.device)
         else:
             for x, name, t, shape in ((out.row_start, "row_start", i32, (n + 1,)), (out.kv_len, "kv_len", i32, (n,)),
                                       (out.slots, "slots", i64, (n_tokens,)), (out.counts, "counts", i32, (4,)),
@@ -203,7 +217,7 @@ class Cache:
     def __init__(self, k, v, k_scale, v_scale):
         import torch
         f8, f32 = (torch.float8_e4m3fn,), (torch.float32,)
-        dev = k.device
+        dev = k.get_device()
         for x, name in ((k, "k"), (v, "v")):
             _want(x, name, f8, 4, dev)
         for x, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
@@ -252,7 +266,7 @@ class Cache:
             _fail("append: a head's values must be contiguous")
         a = hx_kv_new(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1), T,
                       kinds.index(k.dtype), runs.data_ptr(), runs.shape[0])
-        with _On(self.device, stream) as handle:
+        with _on(self.device, stream) as handle:
             H._check(self.lib, self.lib.hx_kv_append(self._ref, ctypes.byref(a), handle))
 
     def attend(self, q, block_table, row_start, kv_len, *, max_q: int = 0, sm_scale: Optional[float] = None,
@@ -283,14 +297,14 @@ class Cache:
             _fail("attend: row_start must have one entry more than kv_len, block_table as many")
         if block_table.shape[1] > 1 and block_table.stride(1) != 1:
             _fail("attend: block_table's rows must be contiguous")
-        with _On(dev, stream) as handle:
+        with _on(dev, stream) as handle:
             if out is None:
-                out = torch.empty((T, heads, dim), dtype=q.dtype, device=dev)
+                out = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device)
             else:
                 _want(out, "out", (q.dtype,), 3, dev)
                 if out.shape != q.shape or out.stride(2) != 1:
                     _fail("attend: out must have q's shape, a head's values contiguous")
-            lse = torch.empty((T, heads), dtype=torch.float32, device=dev) if return_lse else None
+            lse = torch.empty((T, heads), dtype=torch.float32, device=q.device) if return_lse else None
             a = hx_kv_query(q.data_ptr(), out.data_ptr(), lse.data_ptr() if return_lse else None, q.stride(0),
                             q.stride(1), out.stride(0), out.stride(1), T, heads, kinds.index(q.dtype), n,
                             row_start.data_ptr(), kv_len.data_ptr(), block_table.data_ptr(),
@@ -301,7 +315,7 @@ class Cache:
                 need = ctypes.c_int64()
                 H._check(self.lib, self.lib.hx_kv_attend_workspace(self._ref, ref, ctypes.byref(need)))
                 if need.value:
-                    workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+                    workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
             else:
                 _dense(workspace, "workspace", (torch.uint8,), 1, dev)
             if workspace is not None:
