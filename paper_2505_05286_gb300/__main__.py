@@ -1,12 +1,15 @@
 """Command line: simulate one of the seeded recipes on the GPU and print the
 best hyper-parameter point (Sec. 4.3's argmin of P95), or run the online
 alpha-tuning loop of Sec. 4.3 on a trace whose load shifts and print one line
-per window with the wall time of each triggered sweep (Table 3's overhead).
+per window with the wall time of each triggered sweep (Table 3's overhead), or
+replay one instance's calls of the best point's schedule as serving steps of the cache
+operators on this GPU.
 
     python -m paper_2505_05286_gb300 --recipe 1
     python -m paper_2505_05286_gb300 --recipe faulty --traces 2 --queries 500 --objective p95_slo95
     python -m paper_2505_05286_gb300 --tune 5,20,5 --seconds 60,40,60 --window-s 20
     python -m paper_2505_05286_gb300 --recipe 4 --tune 20,30,20 --seconds 1500 --window-s 300 --time-sweeps
+    python -m paper_2505_05286_gb300 --recipe 1 --traces 1 --queries 200 --replay 6
 """
 from __future__ import annotations
 
@@ -76,6 +79,24 @@ def tune(args) -> int:
     return 0
 
 
+def replay(args) -> int:
+    """The recipe's first trace at its best point, logged, and one instance's
+    calls of it as serving steps: one JSON line."""
+    from . import replay as R
+    recipe = int(args.recipe) if args.recipe.isdigit() else args.recipe
+    wl = W.make_workload(recipe, n_traces=1, n_queries=args.queries)
+    with H.Sim(wl.traces, wl.cluster, wl.grid) as sim:
+        sim.run()
+        point = max(0, sim.best(wl.objective)[0])
+    with H.Sim(wl.traces, wl.cluster, wl.grid, record_sims=[point], subset=[point]) as sim:
+        sim.run()
+        records = sim.records(0)
+    out = {"workload": wl.name, "point": point}
+    out.update(R.replay(wl.traces[0], records, wl.cluster, args.replay, chunk=args.chunk, max_steps=args.steps))
+    print(json.dumps(out))
+    return 0
+
+
 def main(argv=None) -> int:
     ap = argparse.ArgumentParser(prog="python -m paper_2505_05286_gb300")
     ap.add_argument("--recipe", default="0", help="index of workloads.RECIPES or a key of workloads.EXTRA")
@@ -90,9 +111,15 @@ def main(argv=None) -> int:
     ap.add_argument("--seed", type=int, default=1, help="--tune: trace seed")
     ap.add_argument("--time-sweeps", action="store_true",
                     help="--tune: also time an alpha sweep and a whole-grid sweep on every window")
+    ap.add_argument("--replay", type=int, default=None, metavar="INSTANCE",
+                    help="run this instance's calls of the best point's schedule as serving steps")
+    ap.add_argument("--steps", type=int, default=1000, help="--replay: steps at most")
+    ap.add_argument("--chunk", type=int, default=512, help="--replay: prompt tokens of a request in one step at most")
     args = ap.parse_args(argv)
     if args.tune is not None:
         return tune(args)
+    if args.replay is not None:
+        return replay(args)
     import torch
 
     recipe = int(args.recipe) if args.recipe.isdigit() else args.recipe

@@ -17,6 +17,8 @@ import ctypes
 from dataclasses import dataclass
 from typing import Optional
 
+import torch
+
 from . import hxsim as H
 
 HX_BF16, HX_F16, HX_F32 = range(3)
@@ -96,7 +98,6 @@ class _On:
     current one: kernels go there, and so does what the binding allocates."""
 
     def __init__(self, device: int, stream):
-        import torch
         self.ctx = [torch.cuda.device(device)]
         if stream is not None and not isinstance(stream, int):
             self.ctx.append(torch.cuda.stream(stream))
@@ -113,21 +114,29 @@ class _On:
 
 
 class _Current:
-    """The usual case, torch's current device and stream."""
+    """The usual case, torch's current device and stream.  (torch.cuda.current_stream() builds an object
+    around the same handle, which takes longer than a small step's kernels.)"""
+
+    def __init__(self, device: int):
+        self.device = device
 
     def __enter__(self):
-        return H._stream_handle(None)
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
     def __exit__(self, *exc):
         pass
 
 
-_CURRENT = _Current()
+_current: dict = {}
 
 
 def _on(device: int, stream):
-    import torch
-    return _CURRENT if stream is None and device == torch.cuda.current_device() else _On(device, stream)
+    if stream is not None or device != torch._C._cuda_getDevice():
+        return _On(device, stream)
+    on = _current.get(device)
+    if on is None:
+        on = _current[device] = _Current(device)
+    return on
 
 
 def max_runs(n_rows: int, n_tokens: int, block_tokens: int) -> int:
@@ -149,12 +158,11 @@ class Step:
 
     @staticmethod
     def empty(n_rows: int, n_tokens: int, block_tokens: int, device="cuda") -> "Step":
-        import torch
         runs = max_runs(n_rows, n_tokens, block_tokens)
         # one allocation for each type; runs and counts first, for their alignment
-        c, r, s, k = torch.empty(4 + 4 * runs + 2 * n_rows + 1, dtype=torch.int32, device=device).split(
+        c, r, s, k = torch.empty(4 + 4 * runs + 2 * n_rows + 1, dtype=torch.int32, device=device).split_with_sizes(
             (4, 4 * runs, n_rows + 1, n_rows))
-        state, slots = torch.empty(2 + n_tokens, dtype=torch.int64, device=device).split((2, n_tokens))
+        state, slots = torch.empty(2 + n_tokens, dtype=torch.int64, device=device).split_with_sizes((2, n_tokens))
         return Step(s, k, slots, r.view(runs, 4), c, state)
 
 
@@ -170,7 +178,6 @@ def map_step(held, add, block_table, ring, ring_state, n_tokens: int, block_toke
     n_tokens    the step's tokens, sum(max(add, 0)), known to the scheduler
     out         a Step to write to instead of a new one (not the one whose ring_state is passed in)
     """
-    import torch
     i32, i64 = (torch.int32,), (torch.int64,)
     dev = held.get_device()
     _dense(held, "held", i32, 1, dev)
@@ -215,7 +222,6 @@ class Cache:
     """
 
     def __init__(self, k, v, k_scale, v_scale):
-        import torch
         f8, f32 = (torch.float8_e4m3fn,), (torch.float32,)
         dev = k.get_device()
         for x, name in ((k, "k"), (v, "v")):
@@ -240,12 +246,12 @@ class Cache:
                                   k.stride(0) if N > 1 else whole, k_scale.stride(0) if N > 1 else heads, N, heads, block,
                                   dim)
         self._ref = ctypes.byref(self.struct)
+        self._work = {}  # workspaces by stream: calls on one stream follow one another
         self.lib = load()
 
     @staticmethod
     def empty(n_blocks: int, n_kv_heads: int, block_tokens: int, head_dim: int, device="cuda") -> "Cache":
         """A new cache; its contents are undefined until tokens are appended."""
-        import torch
         shape = (n_blocks, n_kv_heads, block_tokens, head_dim)
         k, v = (torch.empty(shape, dtype=torch.float8_e4m3fn, device=device) for _ in range(2))
         ks, vs = (torch.empty(shape[:2], dtype=torch.float32, device=device) for _ in range(2))
@@ -254,7 +260,6 @@ class Cache:
     def append(self, k, v, runs, stream=None) -> None:
         """Write a step's keys and values, [tokens, kv heads, head dim] in bf16, f16 or f32 (tokens and heads may be
         strided by multiples of 16 bytes), where `runs` (a Step's) says (hx_kv_append)."""
-        import torch
         kinds = (torch.bfloat16, torch.float16, torch.float32)
         _want(k, "k", kinds, 3, self.device)
         _want(v, "v", (k.dtype,), 3, self.device)
@@ -278,11 +283,10 @@ class Cache:
         max_q       the most tokens that a row has in this step, if the scheduler knows it (1: every row
                     decodes; fewer kernels run), 0 if not
         sm_scale    default head dim ** -0.5
-        workspace   uint8 tensor of `attend_workspace` bytes to use instead of a new one
+        workspace   uint8 tensor to use instead of the one that the cache keeps for each stream
 
         Returns out, or (out, lse) with lse float32 [tokens, heads].
         """
-        import torch
         kinds = (torch.bfloat16, torch.float16)
         dev = self.device
         _want(q, "q", kinds, 3, dev)
@@ -314,11 +318,14 @@ class Cache:
             if workspace is None:
                 need = ctypes.c_int64()
                 H._check(self.lib, self.lib.hx_kv_attend_workspace(self._ref, ref, ctypes.byref(need)))
-                if need.value:
+                graph = torch.cuda.is_current_stream_capturing()  # a graph has a workspace of its own
+                workspace = None if graph else self._work.get(handle)
+                if workspace is None or workspace.numel() < need.value:
                     workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+                    if not graph:
+                        self._work[handle] = workspace
             else:
                 _dense(workspace, "workspace", (torch.uint8,), 1, dev)
-            if workspace is not None:
-                a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
             H._check(self.lib, self.lib.hx_kv_attend(self._ref, ref, handle))
         return (out, lse) if return_lse else out
