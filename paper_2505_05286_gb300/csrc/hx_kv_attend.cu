@@ -48,39 +48,43 @@ struct __align__(16) Tile {
 // Tiles are looked up kAhead at a time, and a tile is read no later than kStages after it.
 constexpr int kAhead = 16, kTiles = 32;
 
-// The tiles of an item, 0: it is not this kernel's.  An item that sees nothing,
-// with any number of rows, counts as one, so that its zeros are written.
+// What an item costs a block beside its tiles (joining the warps' sums), in tiles.
+constexpr int kItemCost = 3;
+
+// The length of an item, 0: it is not this kernel's.  It begins with kItemCost places without a tile, so that
+// stretches with many items have fewer tiles.  An item that sees nothing, with any number of rows,
+// has no others, but is dealt out, so that its zeros are written.
 template <int D>
-__device__ __forceinline__ int tiles_of(const AttendArgs& a, const Request& q, int* first_tile) {
+__device__ __forceinline__ int length_of(const AttendArgs& a, const Request& q, int* first_tile) {
   constexpr int NT = kTileBytes / D;
   *first_tile = 0;
   if (q.n == 0) return 0;
-  if (q.kv == 0) return 1;
+  if (q.kv == 0) return kItemCost;
   if (q.n * a.group > a.few_rows) return 0;
   *first_tile = see_from(a, q, 0) / NT;
-  return (q.kv + NT - 1) / NT - *first_tile;
+  return kItemCost + (q.kv + NT - 1) / NT - *first_tile;
 }
 
-// A place in the sequence of all tiles.
+// A place in the sequence of all items.
 template <int D>
 struct Place {
-  int r, h, t, tiles, first_tile;
+  int r, h, o, length, first_tile;
   Request q;
   __device__ void load(const AttendArgs& a) {
     q = request(a, r);
-    tiles = tiles_of<D>(a, q, &first_tile);
+    length = length_of<D>(a, q, &first_tile);
   }
-  // Steps by d tiles; false past the last request.
+  // Steps by d places; false past the last request.
   __device__ bool step(const AttendArgs& a, int d) {
-    t += d;
-    while (t >= tiles) {
-      t -= tiles;
-      if (tiles && ++h < a.n_kv_heads) continue;
+    o += d;
+    while (o >= length) {
+      o -= length;
+      if (length && ++h < a.n_kv_heads) continue;
       h = 0;
       do {
         if (++r >= a.n_rows) return false;
         load(a);
-      } while (!tiles);
+      } while (!length);
     }
     return true;
   }
@@ -144,7 +148,7 @@ __device__ __forceinline__ bool elected() {
 // copies that it issues.  A look-up is two loads that depend on one another (block number, its
 // scale); they are placed before and halfway through the copies of the batch before, which hide them.
 template <int D, int NR, int V>
-__device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at, int count, int skip, uint8_t* ring, Tile* tiles,
+__device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at, int count, uint8_t* ring, Tile* tiles,
                         uint64_t* full, uint64_t* empty, volatile int* dead) {
   using S = Shape<D, NR>;
   const int lane = threadIdx.x & 31;
@@ -152,17 +156,17 @@ __device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at
   const int box = min(block, S::kTokens), pieces = S::kTokens / box;
   int stage = 0;
   uint32_t turn = 0;
-  bool more = at.step(a, skip + lane), tile = false;
+  bool more = at.step(a, lane), tile = false;
   int id[4] = {-1, -1, -1, -1}, y = 0, h = 0;
   float scale[4];
   uint32_t bytes = 0, valid = 0;
 
   const auto look_up = [&](int base) {
-    tile = more && lane < kAhead && base + lane < count && at.q.kv > 0;
+    tile = more && lane < kAhead && base + lane < count && at.o >= kItemCost;
 #pragma unroll
     for (int p = 0; p < 4; ++p) id[p] = -1;
     if (tile) {
-      const int pos = (at.first_tile + at.t) * S::kTokens;
+      const int pos = (at.first_tile + at.o - kItemCost) * S::kTokens;
       const int32_t* row = a.block_table + at.r * a.table_stride + (pos >> a.block_shift);
       h = at.h;
       y = h * block + (pos & (block - 1));
@@ -191,7 +195,7 @@ __device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at
         }
     }
   };
-  // Tiles are numbered without those of items that see nothing: `number` is the next batch's first.
+  // Tiles are numbered, places without one are not: `number` is the next batch's first.
   int number = 0;
   const auto store = [&]() -> int {
     const unsigned who = __ballot_sync(~0u, tile);
@@ -206,6 +210,8 @@ __device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at
     __syncwarp();
     return __popc(who);
   };
+  // The whole warp goes through the loop, and one elected thread issues: with the loop inside that thread's
+  // branch the operands leave the uniform registers (48 requests of 32000 tokens 705 us against 535).
   const auto issue = [&](int from, int to) -> bool {
     for (int k = from; k < to; ++k) {
       const Tile& x = tiles[k & (kTiles - 1)];
@@ -254,7 +260,7 @@ __device__ __forceinline__ int order(int n) {
 }
 
 template <int D, int NR, class T>
-__device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, const uint8_t* ring, const Tile (*tiles)[kTiles],
+__device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8_t* ring, const Tile (*tiles)[kTiles],
                         uint64_t* full, uint64_t* empty, volatile int* dead, float* merge, float (*s_ml)[kRows][2]) {
   using S = Shape<D, NR>;
   constexpr int NT = S::kTokens, KJ = D / 64, ND = D / 16, W = S::kWarps;
@@ -274,15 +280,17 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
   // landed: a barrier tells a phase from the one before it only.  So a place has two of them, for its tiles
   // by turns; the tile two before has been used, or this one would not have been asked for.
   const auto landed = [&](int x) { return bar_wait(&full[2 * x + (turn & 1)], turn >> 1 & 1, dead); };
-  bool more = at.step(a, skip);
+  bool more = true;
   while (more && count > 0) {
-    const int seg = min(count, at.tiles - at.t);
+    // this block's places of the item, and its tiles among them
+    const int places = min(count, at.length - at.o), tile0 = max(0, at.o - kItemCost);
+    const int seg = places - (at.o ? 0 : kItemCost);
     const Request q = at.q;
     const int rows = q.n * a.group;
     if (q.kv == 0) {
       write_empty<T>(a, D, q, at.h, threadIdx.x, 32 * W);
-      count -= seg;
-      more = at.step(a, seg);
+      count -= places;
+      more = at.step(a, places);
       continue;
     }
 
@@ -350,7 +358,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
       const uint8_t* vt = kt + kTileBytes;
       const Tile& key_tile = tiles[0][(it + left) & (kTiles - 1)];
       const Tile& value_tile = tiles[1][(it + left) & (kTiles - 1)];
-      const int pos = (at.first_tile + at.t + left) * NT;
+      const int pos = (at.first_tile + tile0 + left) * NT;
       const uint32_t valid = key_tile.valid;
       const bool whole = valid == (1u << S::kGroups) - 1 && pos >= all_lo && pos + NT <= all_hi;
 
@@ -605,8 +613,8 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
           }
     }
     sync_consumers<32 * W>();
-    const bool done = seg == at.tiles;
-    const int64_t slot = 2 * blockIdx.x + (at.t == 0);
+    const bool done = places == at.length;
+    const int64_t slot = 2 * blockIdx.x + (at.o == 0);
     for (int i = threadIdx.x; i < rows * (D / 4); i += 32 * W) {
       const int row = i / (D / 4), col = i % (D / 4) * 4;
       float mt = -INFINITY, lt = 0;
@@ -634,11 +642,31 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, int skip, c
       }
     }
     it += seg;
-    count -= seg;
-    more = at.step(a, seg);
+    count -= places;
+    more = at.step(a, places);
     if (more && count > 0) sync_consumers<32 * W>();  // s_ml and the sums have been read
   }
 }
+
+__device__ __forceinline__ long long divide(long long x, int d) {  // x >= 0
+  return (x >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : x / d;
+}
+
+// `total` places dealt out to `blocks` blocks, of which only as many as there are places get any: the first
+// `more` one more than the others.
+struct Stretches {
+  long long total, each;
+  int blocks, more;
+  __device__ Stretches(long long total, int grid) : total(total), blocks(total < grid ? max(1, (int)total) : grid) {
+    each = divide(total, blocks);
+    more = (int)(total - each * blocks);
+  }
+  __device__ long long begin(int b) const { return b >= blocks ? total : each * b + min(b, more); }
+  __device__ int owner(long long x) const {
+    const long long first = (each + 1) * more;
+    return x < first ? (int)divide(x, (int)(each + 1)) : more + (int)divide(x - first, (int)each);
+  }
+};
 
 template <int D, int NR, class T>
 __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
@@ -650,8 +678,8 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   __shared__ uint64_t s_full[4 * S::kStages], s_empty[2 * S::kStages];  // of a place: keys, values
   __shared__ Tile s_tiles[2][kTiles];
   __shared__ __align__(16) float s_ml[kWarps][kRows][2];
-  __shared__ long long s_sum[kThreads / 32], s_skip;
-  __shared__ int s_row, s_dead;
+  __shared__ long long s_sum[kThreads / 32];
+  __shared__ int s_row[2], s_head[2], s_place[2], s_moved[2], s_dead;
   uint8_t* ring = (uint8_t*)(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
   float* merge = (float*)(ring + S::kStages * kStageBytes);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -661,15 +689,16 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
     for (int i = 0; i < 2 * S::kStages; ++i) bar_init(&s_full[2 * i], 1), bar_init(&s_full[2 * i + 1], 1), bar_init(&s_empty[i], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s_dead = 0;
-    s_row = -1;
+    s_moved[0] = s_moved[1] = 0;
   }
 
-  // how many tiles there are before each thread's rows, and in all
+  // how long the items are before each thread's rows, and in all
+  const int owned = min(max(a.row_start[a.n_rows], 0), a.n_tokens);
   const int per = (a.n_rows + kThreads - 1) / kThreads;
   const int r0 = min(a.n_rows, tid * per), r1 = min(a.n_rows, r0 + per);
   long long mine = 0;
   int ft;
-  for (int r = r0; r < r1; ++r) mine += (long long)tiles_of<D>(a, request(a, r), &ft) * a.n_kv_heads;
+  for (int r = r0; r < r1; ++r) mine += (long long)length_of<D>(a, request(a, r), &ft) * a.n_kv_heads;
   long long upto = mine;
   for (int d = 1; d < 32; d <<= 1) {
     const long long o = __shfl_up_sync(~0u, upto, d);
@@ -684,65 +713,65 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
     total += s_sum[w];
   }
   before += upto - mine;
-  // this block's stretch of the tiles: none of the first G is empty
-  const long long G = max(1LL, min((long long)gridDim.x, total)), b = blockIdx.x;
-  const long long n0 = b < G ? total * b / G : 0, n1 = b < G ? total * (b + 1) / G : 0;
-  if (n0 < n1 && before <= n0 && n0 < before + mine) {
-    int r = r0;
-    for (;; ++r) {
-      const long long x = (long long)tiles_of<D>(a, request(a, r), &ft) * a.n_kv_heads;
-      if (n0 < before + x) break;
-      before += x;
+  // This block's stretch of them: [n0, n1).  A bound before an item's first tile is moved to the item's
+  // beginning, for both of its blocks: so an item's blocks follow one another, each with a tile at least.
+  const Stretches all(total, gridDim.x);
+  const int b = blockIdx.x;
+  const long long bound[2] = {all.begin(b), all.begin(b + 1)};
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    if (!(before <= bound[x] && bound[x] < before + mine)) continue;
+    long long at = before;
+    for (int r = r0;; ++r) {
+      const int length = length_of<D>(a, request(a, r), &ft);
+      if (bound[x] < at + (long long)length * a.n_kv_heads) {
+        const int h = (int)divide(bound[x] - at, length);
+        const int o = (int)(bound[x] - at - (long long)h * length);
+        s_row[x] = r, s_head[x] = h, s_place[x] = o <= kItemCost ? 0 : o;
+        s_moved[x] = o <= kItemCost ? o : 0;
+        break;
+      }
+      at += (long long)length * a.n_kv_heads;
     }
-    s_row = r;
-    s_skip = n0 - before;
   }
   __syncthreads();
 
   // tokens that no row owns
-  const int owned = min(max(a.row_start[a.n_rows], 0), a.n_tokens);
   for (int t = owned + blockIdx.x; t < a.n_tokens; t += gridDim.x) {
     const Request q = {t, 1, 0};
     for (int h = 0; h < a.n_kv_heads; ++h) write_empty<T>(a, D, q, h, tid, kThreads);
   }
 
+  const int count = (int)(bound[1] - bound[0] + s_moved[0] - s_moved[1]);
+  if (count <= 0) {
+    if (tid == 0) a.joins[b] = int4{0, 0, -1, 0};
+    return;
+  }
   Place<D> at;
-  const int count = (int)(n1 - n0);
-  int skip = 0;
-  if (s_row >= 0) {
-    at.r = s_row;
-    at.load(a);
-    at.h = (int)(s_skip / at.tiles);
-    at.t = 0;
-    skip = (int)(s_skip % at.tiles);
-  }
-  if (tid == 0) {
-    // an item that began in an earlier block and ends in this one is joined here
-    int4 join = {0, 0, -1, 0};
-    if (s_row >= 0 && skip > 0 && skip + (long long)count >= at.tiles) {
-      const long long f0 = n0 - skip;
-      long long c = f0 * G / total;
-      while (total * (c + 1) / G <= f0) ++c;
-      while (total * c / G > f0) --c;
-      join = int4{at.r, at.h, (int)c, 0};
-    }
-    a.joins[b] = join;
-  }
-  if (s_row < 0) return;
+  at.r = s_row[0];
+  at.load(a);
+  at.h = s_head[0];
+  at.o = s_place[0];
+  // an item that began in an earlier block and ends in this one is joined here
+  if (tid == 0)
+    a.joins[b] = at.o > 0 && at.o + (long long)count >= at.length
+                     ? int4{at.q.first, at.q.n, all.owner(bound[0] - at.o + kItemCost), at.h}
+                     : int4{0, 0, -1, 0};
   if (warp == kWarps)
-    produce<D, NR, 0>(a, &km, at, count, skip, ring, s_tiles[0], s_full, s_empty, &s_dead);
+    produce<D, NR, 0>(a, &km, at, count, ring, s_tiles[0], s_full, s_empty, &s_dead);
   else if (warp == kWarps + 1)
-    produce<D, NR, 1>(a, &vm, at, count, skip, ring, s_tiles[1], s_full, s_empty, &s_dead);
+    produce<D, NR, 1>(a, &vm, at, count, ring, s_tiles[1], s_full, s_empty, &s_dead);
   else
-    consume<D, NR, T>(a, at, count, skip, ring, s_tiles, s_full, s_empty, &s_dead, merge, s_ml);
+    consume<D, NR, T>(a, at, count, ring, s_tiles, s_full, s_empty, &s_dead, merge, s_ml);
   drain(&s_dead);
 }
 
 // Joins an item's partial results: block (e, y) rows 16 y and on of the item that ends in stretch e.
 // Each warp turns its rows' maxima and sums into a weight for every part; then D / 4 threads
 // take a row's sums (or an equal share of its parts, where there are fewer rows than
-// that), with eight loads in flight: what counts is the latency of few dependent loads.
-constexpr int kJoinThreads = 256;
+// that), with eight loads in flight, the first of them asked for before the weights: what counts is
+// the latency of few dependent loads.
+constexpr int kJoinThreads = 512;
 constexpr int kMaxBlocks = 512;  // and so of an item's parts
 
 template <int D, int kSlotRows, class T>
@@ -754,17 +783,28 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int4 join = a.joins[blockIdx.x];
   if (join.z < 0) return;
-  const Request q = request(a, join.x);
   // the token and head of this block's rows; a half's rows of the many-rows kernel begin at 0 and 128
   const int y0 = blockIdx.y * kRows;
   constexpr int kHalf = kSlotRows / 2;
   const bool halves = kSlotRows == kItemRows;
-  const int i0 = halves ? (join.w * 2 + y0 / kHalf) * a.half_tokens : 0, x0 = halves ? y0 % kHalf : y0;
-  const int rows = min(kRows, (halves ? min(a.half_tokens, q.n - i0) : q.n) * a.group - x0);
+  const int i0 = halves ? y0 / kHalf * a.half_tokens : 0, x0 = halves ? y0 % kHalf : y0;
+  const int rows = min(kRows, (halves ? min(a.half_tokens, join.y - i0) : join.y) * a.group - x0);
   const int parts = blockIdx.x - join.z + 1;
   if (rows <= 0) return;
   const auto slot = [&](int i) { return (2 * (int64_t)(join.z + i) + (i == 0)) * kSlotRows + y0; };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int team = threadIdx.x / kCols, col = threadIdx.x % kCols;
+  const int share = max(1, kTeams / rows), together = kTeams / share;  // teams of a row, rows at a time
+  const int sub = team % share;
+  const auto part_of = [&](int i, int row) { return *(const float4*)(a.part + (slot(i) + row) * D + 4 * col); };
+  constexpr int kMost = 8;
+  float4 p[kMost];
+  const auto ask = [&](int i0, int row) {
+#pragma unroll
+    for (int u = 0; u < kMost; ++u)
+      if (row < rows && team < share * together && i0 + u * share < parts) p[u] = part_of(i0 + u * share, row);
+  };
+  ask(sub, team / share);
   for (int row = warp; row < rows; row += kJoinThreads / 32) {
     float m = -INFINITY, l = 0;
     for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[(slot(i) + row) * 2]);
@@ -780,44 +820,36 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
     if (lane == 0) s_ml[row] = float2{m, l};
   }
   __syncthreads();
-  const int team = threadIdx.x / kCols, col = threadIdx.x % kCols;
-  const int share = max(1, kTeams / rows);  // teams of a row
-  for (int r0 = 0; r0 < rows; r0 += kTeams / share) {
-    const int row = r0 + team / share, sub = team % share;
+  for (int r0 = 0; r0 < rows; r0 += together) {
+    const int row = r0 + team / share;
     float4 o = {0, 0, 0, 0};
-    if (row < rows && team / share < kTeams / share) {
-      int i = sub;
-      for (; i + 7 * share < parts; i += 8 * share) {
-        float4 p[8];
+    if (r0) ask(sub, row);
+    if (row < rows && team < share * together)
+      for (int i = sub; i < parts;) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) p[u] = *(const float4*)(a.part + (slot(i + u * share) + row) * D + 4 * col);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const float w = s_w[row][i + u * share];
-          o.x += p[u].x * w, o.y += p[u].y * w, o.z += p[u].z * w, o.w += p[u].w * w;
-        }
+        for (int u = 0; u < kMost; ++u)
+          if (i + u * share < parts) {
+            const float w = s_w[row][i + u * share];
+            o.x += p[u].x * w, o.y += p[u].y * w, o.z += p[u].z * w, o.w += p[u].w * w;
+          }
+        i += kMost * share;
+        ask(i, row);
       }
-      for (; i < parts; i += share) {
-        const float4 p = *(const float4*)(a.part + (slot(i) + row) * D + 4 * col);
-        const float w = s_w[row][i];
-        o.x += p.x * w, o.y += p.y * w, o.z += p.z * w, o.w += p.w * w;
-      }
-    }
     if (share > 1) {
       s_o[team][col] = o;
       __syncthreads();
       if (sub == 0)
         for (int i = 1; i < share && team + i < kTeams; ++i) {
-          const float4 p = s_o[team + i][col];
-          o.x += p.x, o.y += p.y, o.z += p.z, o.w += p.w;
+          const float4 q = s_o[team + i][col];
+          o.x += q.x, o.y += q.y, o.z += q.z, o.w += q.w;
         }
       __syncthreads();
     }
-    if (sub == 0 && row < rows && team / share < kTeams / share) {
+    if (sub == 0 && row < rows && team < share * together) {
       const float2 ml = s_ml[row];
       const float inv = ml.y == 0 ? 0.f : 1.f / ml.y;
-      const int64_t token = q.first + i0 + a.by_group.of(x0 + row);
-      const int head = join.y * a.group + a.by_group.rest(x0 + row);
+      const int64_t token = join.x + i0 + a.by_group.of(x0 + row);
+      const int head = join.w * a.group + a.by_group.rest(x0 + row);
       T* to = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + 4 * col;
       *(uint2*)to = uint2{from_float2<T>(o.x * inv, o.y * inv), from_float2<T>(o.z * inv, o.w * inv)};
       if (col == 0 && a.lse)

@@ -54,7 +54,8 @@ struct AttendArgs {
   float sm_scale_log2;  // sm_scale * log2(e): scores are exponents of two
   float* part;          // partial results of items that several blocks share
   float* part_ml;
-  int4* joins;          // [blocks] {request, kv head, first block of the item, which rows} or -1 in third place
+  int4* joins;          // [blocks] of the item that ends in the block's stretch: its first token, its tokens, the block where
+                        // it begins (-1: nothing to join), its kv head
 };
 
 // Launches the many-rows kernel (hx_kv_attend_many.cu) on `blocks` blocks.

@@ -832,7 +832,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(
       long long c = f0 * G / total;
       while (total * (c + 1) / G <= f0) ++c;
       while (total * c / G > f0) --c;
-      join = int4{s.r, s.h, (int)c, s.mt};
+      join = int4{s.q.first + s.i0, min(s.q.n - s.i0, 2 * a.half_tokens), (int)c, s.h};
     }
     a.joins[b] = join;
   }
