@@ -804,10 +804,12 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
     for (int u = 0; u < kMost; ++u)
       if (row < rows && team < share * together && i0 + u * share < parts) p[u] = part_of(i0 + u * share, row);
   };
+  float first = -INFINITY;  // a warp's first row's maximum of part `lane`
+  if (warp < rows && lane < parts) first = a.part_ml[(slot(lane) + warp) * 2];
   ask(sub, team / share);
   for (int row = warp; row < rows; row += kJoinThreads / 32) {
-    float m = -INFINITY, l = 0;
-    for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[(slot(i) + row) * 2]);
+    float m = row == warp ? first : -INFINITY, l = 0;
+    for (int i = row == warp ? lane + 32 : lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[(slot(i) + row) * 2]);
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
     const float base = m == -INFINITY ? 0.f : m;
     for (int i = lane; i < parts; i += 32) {
