@@ -88,6 +88,7 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
   if (bar_try(b, parity)) return true;
   const long long t0 = clock64();
   do {
+#pragma unroll 1  // there are many waits: unrolled, they crowd the instruction cache
     for (int i = 0; i < 32; ++i)
       if (bar_try(b, parity)) return true;
   } while (!*dead && clock64() - t0 < kWaitCycles);
