@@ -407,6 +407,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
             top[r][y & 1] = fmaxf(top[r][y & 1], s[g][r][y]);
           }
       }
+      fence_async();
       __syncwarp();
       if (lane == 0) bar_arrive(&empty[2 * stage]);
       // values of tokens ta, tb, ta + 8, tb + 8 of each group, D / 8 columns each: on their way while the
@@ -426,6 +427,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       float value_scale[S::kGroups];
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g) value_scale[g] = value_tile.scale[g];
+      fence_async();
       __syncwarp();
       if (lane == 0) bar_arrive(&empty[2 * stage + 1]);
       bool late = false;

@@ -141,7 +141,6 @@ __device__ __forceinline__ bool active(const Segment& s, int half, int tile) {
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
@@ -343,6 +342,7 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, c
     const uint8_t* from = raw + v * Many<D>::kRaw + (32 * warp + sub) * D + unit * 8;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) u[j] = *(const uint2*)(from + j * kPer * D);
+    fence_async();
     __syncwarp();
     if (lane == 0) bar_arrive(&sh->raw_empty[v]);
   };

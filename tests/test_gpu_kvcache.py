@@ -475,6 +475,50 @@ def test_attend_offsets_past_32_bits():
         _near(got, lse, *P.attend_plain(q, k[sub], v[sub], ks[sub], vs[sub], small, start, kv, D ** -0.5, True, 0))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,heads,ctx,new", [(128, 8, [0] * 4, [4033, 4200, 4391, 4100]), (16, 2, [0] * 3, [3001, 2500, 2777]),
+                                             (128, 1, list(range(40, 3000, 7)), [1] * 423), (32, 4, list(range(9, 2400, 40)), [5] * 60)])
+def test_attend_takes_every_token_once(D, B, heads, ctx, new):
+    """With q = 0 all tokens that a row sees weigh the same, and values that name their token's group of 16
+    (and its 128) make the output count them: a tile that is read while the next one lands shows."""
+    H, group, n = heads, 4, len(ctx)
+    kv = torch.tensor(ctx) + torch.tensor(new)
+    blocks = -(-kv // B)
+    ids = torch.randperm(int(blocks.sum()), generator=torch.Generator().manual_seed(1))
+    table, pos = torch.full((n, int(blocks.max())), -1, dtype=torch.int32), torch.empty(len(ids), dtype=torch.long)
+    at = 0
+    for r in range(n):
+        m = int(blocks[r])
+        table[r, :m] = ids[at:at + m].int()
+        pos[ids[at:at + m]] = torch.arange(m) * B
+        at += m
+    half = D // 2
+    tok = pos.cuda()[:, None] + torch.arange(B, device="cuda")
+    v = torch.zeros((len(ids), B, D), device="cuda")
+    v.scatter_(2, (tok // 16 % half)[..., None], 1.0)
+    v.scatter_(2, (half + tok // 128 % half)[..., None], 1.0)
+    v = v[:, None].expand(len(ids), H, B, D).to(torch.float8_e4m3fn).contiguous()
+    scale = torch.ones((len(ids), H), device="cuda")
+    cache = KV.Cache(torch.zeros_like(v.view(torch.uint8)).view(v.dtype), v, scale, scale.clone())
+    start = torch.cumsum(torch.tensor([0] + new), 0).int().cuda()
+    T = sum(new)
+    q = torch.zeros((T, H * group, D), dtype=torch.bfloat16, device="cuda")
+    # what row i of a request sees: tokens 0 .. ctx + i
+    last = torch.cat([c + torch.arange(m) for c, m in zip(ctx, new)]).cuda()
+    seen = torch.arange(int(kv.max()), device="cuda")
+    code = torch.zeros((len(seen), D), dtype=torch.float64, device="cuda")
+    code[seen, seen // 16 % half] = 1
+    code[seen, half + seen // 128 % half] = 1
+    want = torch.cumsum(code, 0)[last] / (last[:, None] + 1)
+    for _ in range(12):
+        out, lse = cache.attend(q, table.cuda(), start, kv.int().cuda(), max_q=max(new), return_lse=True)
+        # a rounding to bf16 (2^-9), and those of the quotient in 32 bits
+        far = (out.double() - want[:, None]).abs() > 2.0 ** -8 * want[:, None]
+        assert not bool(far.any()), far.nonzero()[:4].tolist()
+        # a log of a whole number in 32 bits, and its factor
+        assert torch.allclose(lse.double(), torch.log((last + 1).double())[:, None].expand(T, H * group), rtol=0, atol=1e-5)
+
+
 def test_operators_on_another_stream_and_in_a_graph():
     g = gen(11)
     n, B, H, D = 5, 16, 2, 64
