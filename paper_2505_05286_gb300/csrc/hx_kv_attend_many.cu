@@ -436,7 +436,9 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
   int it = 0, seg_no = 0;
   volatile int* dead = &sh->dead;
   const auto scores = [&](int half, int st) {
-    // S's columns hold the half's last P, whose product was issued before: products are executed in order
+    // S's columns hold the half's last P; the order of products with different sums is not promised
+    if (n_s[half]) bar_wait(&sh->o_full[half], (n_s[half] - 1) & 1, dead);
+    tc_fence_after();
     if (elected()) {
       const uint64_t q = q0 + half * (Many<D>::kQBytes >> 4), k = k0 + st * (Many<D>::kTile >> 4);
 #pragma unroll
