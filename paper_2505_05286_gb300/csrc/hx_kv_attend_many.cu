@@ -34,6 +34,7 @@ constexpr int kGroups = kKv / 16;
 constexpr int kConvWarp = 8, kMmaWarp = 12, kFetchWarp = 13, kQueryWarp = 14;
 constexpr int kManyThreads = 32 * (kQueryWarp + 1);
 constexpr int kNanList = 16;
+constexpr int kNanLists = 8;  // the conversion may be four items ahead of a half that still writes one out
 
 template <int D>
 struct Many {
@@ -227,8 +228,8 @@ struct Shared {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], go[2], ended[2][2];  // go and ended: of even and odd items
   TileInfo info[8];
-  int nan_count[4];
-  int nan_pos[4][kNanList];
+  int nan_count[kNanLists];
+  int nan_pos[kNanLists][kNanList];
   long long sum[kManyThreads / 32];
   long long skip;  // tiles of the item before this block's stretch
   int row, head, mt, dead;
@@ -348,7 +349,7 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, c
   };
   HX_SEGMENTS(s, count) {
     if (s.empty) continue;
-    const int list = seg_no & 3;
+    const int list = seg_no & (kNanLists - 1);
     if (tid == 0) sh->nan_count[list] = 0;
     asm volatile("bar.sync 1, 128;" ::: "memory");
     for (int i = 0; i < seg && !__any_sync(~0u, *dead); ++i, ++it) {
@@ -688,13 +689,13 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       }
     }
     // NaN among the values that this row sees
-    const int nans = has ? sh->nan_count[seg_no & 3] : 0;
+    const int nans = has ? sh->nan_count[seg_no & (kNanLists - 1)] : 0;
     if (nans && real) {
       const int p0 = max(lo, (s.first_tile + s.t) * kKv), p1 = min(hi, (s.first_tile + s.t + seg) * kKv);
       const bool listed = nans <= kNanList;
 #pragma unroll 1
       for (int e = listed ? 0 : p0; e < (listed ? nans : p1); ++e) {
-        const int p = listed ? sh->nan_pos[seg_no & 3][e] : e;
+        const int p = listed ? sh->nan_pos[seg_no & (kNanLists - 1)][e] : e;
         if (p < p0 || p >= p1) continue;
         const int id = a.block_table[s.r * a.table_stride + (p >> a.block_shift)];
         if ((unsigned)id >= (unsigned)a.n_blocks) continue;
