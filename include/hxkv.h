@@ -106,7 +106,7 @@ typedef struct hx_kv_new {
   int32_t n_tokens;
   int32_t dtype;              /* HX_BF16, HX_F16 or HX_F32 */
   const int32_t* runs;        /* [n_runs][4], as hx_kv_map gives them; every block at most once */
-  int32_t n_runs;
+  int32_t n_runs;             /* 0.., n_runs * n_kv_heads below 2^30 */
 } hx_kv_new;
 
 /* Write the step's tokens into the cache.  A block's scale is the smallest power of two, 2^-100 at

@@ -21,6 +21,10 @@ namespace {
 // Tokens are the matrix instructions' 16 rows and the few rows their 8 columns:
 // S^T = K Q^T, O^T = V^T P^T.  So eight rows waste nothing (16 x 8 x 16 the other way round would
 // compute 16), and the sums take half the registers, which lets 12 computing warps reside on an SM.
+//
+// 48 requests of 32000 tokens, 32 heads on 8 of 128: 507 us, 6.35 TB/s, 95 % of a copy.  500 requests of 437 to
+// 18133 tokens, 28 heads on 4 of 64, blocks of 16: 248 us, 3.65 TB/s: instructions, of which a column of 64 takes as
+// many for its softmax as one of 128.  One request of 5065 tokens: 14.8 us, latency.
 constexpr int kRows = 16;  // most rows of an item
 constexpr int kStageBytes = 8192;
 constexpr int kTileBytes = kStageBytes / 2;
@@ -772,7 +776,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
 // Each warp turns its rows' maxima and sums into a weight for every part; then D / 4 threads
 // take a row's sums (or an equal share of its parts, where there are fewer rows than
 // that), with eight loads in flight, the first of them asked for before the weights: what counts is
-// the latency of few dependent loads.
+// the latency of few dependent loads (one request of 5065 tokens, 38 parts of each item: 5 us).
 constexpr int kJoinThreads = 512;
 constexpr int kMaxBlocks = 512;  // and so of an item's parts
 

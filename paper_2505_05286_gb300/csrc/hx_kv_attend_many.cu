@@ -23,6 +23,8 @@ namespace {
 //     softmax does,
 //   2 x 4 warps do a half's softmax, a row to a thread, and write P over S.
 // Tensor memory (512 columns): S, P of the halves at 0 and 128, O at 256 and 256 + D.
+// Four prompts of 5600 tokens, 32 heads on 8 of 128 in bf16: 1083 us, 982 TFLOP/s, 52 % of a plain product's rate; a
+// tile takes 3850 cycles where its products take 2048: a half's softmax, values and scores follow one another.
 //
 // Scales: a score is s * ks * c, and a value's scale vs goes into the weight, P = exp2(s ks c +
 // log2(vs) - m) with m within kLag of the largest of those exponents so far.  So P in f16 is accurate

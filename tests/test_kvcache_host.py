@@ -132,6 +132,17 @@ def test_attend_refusals(lib):
     assert lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(a), None) == H.HX_OK
 
 
+def test_limits_refused(lib):
+    a = KV.hx_kv_map_args(3, 10, 32, 8, 4, 6, 4, *[FAKE] * 10, FAKE + 64)
+    _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, counts=FAKE + 8)), None), "aligned")
+    c = _cache()
+    q = KV.hx_kv_query(FAKE, FAKE, None, 512, 64, 512, 64, 10, 8, KV.HX_F16, 3, FAKE, FAKE, FAKE, 4, 4, 1, 1, 0, 0.125,
+                       FAKE, 1 << 40)
+    for kw, msg in [(dict(n_tokens=2 ** 29 + 1), "2^30"), (dict(workspace=FAKE + 16), "32-byte"), (dict(q_token_stride=-512), "2^38"),
+                    (dict(q_head_stride=2 ** 38 + 8), "2^38"), (dict(table_width=2 ** 23 + 1, table_stride=2 ** 24), "table_width")]:
+        _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(_set(q, **kw)), None), msg)
+
+
 def test_binding_refuses_host_tensors():
     z = torch.zeros(3, dtype=torch.int32)
     with pytest.raises(H.HxError) as e:
