@@ -99,8 +99,13 @@ class _On:
 
     def __init__(self, device: int, stream):
         self.ctx = [torch.cuda.device(device)]
-        if stream is not None and not isinstance(stream, int):
-            self.ctx.append(torch.cuda.stream(stream))
+        if stream is not None:
+            # a handle too: what is allocated for the call may be freed before its kernels run
+            if isinstance(stream, int):
+                s = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+            else:
+                s = stream
+            self.ctx.append(torch.cuda.stream(s))
         self.stream = stream
 
     def __enter__(self):

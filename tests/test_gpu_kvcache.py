@@ -558,3 +558,20 @@ def test_operators_on_another_stream_and_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_named_stream_owns_what_a_call_allocates(handle):
+    """Outputs and workspaces come from the call's stream, named by an object or by its handle."""
+    side = torch.cuda.Stream()
+    name = side.cuda_stream if handle else side
+    with KV._on(torch.cuda.current_device(), name) as h:
+        assert h == torch.cuda.current_stream().cuda_stream == side.cuda_stream
+    with KV._on(torch.cuda.current_device(), 0) as h:
+        assert h == torch.cuda.current_stream().cuda_stream == 0
+    i = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    table, ring, state = i(-1, -1).view(1, 2), i(1, 0, 2), torch.tensor([0, 3], device="cuda")
+    torch.cuda.synchronize()
+    step = KV.map_step(i(0), i(20), table, ring, state, 20, 16, stream=name)
+    side.synchronize()
+    assert step.slots.tolist() == list(range(16, 32)) + list(range(4)) and table.tolist() == [[1, 0]]
