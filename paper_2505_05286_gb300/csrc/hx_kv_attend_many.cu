@@ -26,6 +26,11 @@ namespace {
 // Four prompts of 5600 tokens, 32 heads on 8 of 128 in bf16: 1083 us, 982 TFLOP/s, 52 % of a plain product's rate; a
 // tile takes 3850 cycles where its products take 2048: a half's softmax, values and scores follow one another.
 //
+// By turns (kTurns): where no request of the step has more tokens than a half (max_q says so), the second half
+// would have nothing to do.  Then both halves have the same rows, one takes the even tiles and the other the odd ones, and the
+// first half's threads join the two: 64 requests of 1 to 5 tokens at 810 to 11507, 32 heads on 8 of 128, 218 -> 184 us;
+// a chunk of 30 at 24001 46 -> 39 us.  As a branch in one kernel it cost prompts 4 %.
+//
 // Scales: a score is s * ks * c, and a value's scale vs goes into the weight, P = exp2(s ks c +
 // log2(vs) - m) with m within kLag of the largest of those exponents so far.  So P in f16 is accurate
 // relative to the row's largest weight times scale, however far apart scales lie, and the
@@ -35,7 +40,7 @@ constexpr int kKv = 128;       // tokens of a tile
 constexpr int kGroups = kKv / 16;
 constexpr int kConvWarp = 8, kMmaWarp = 12, kFetchWarp = 13, kQueryWarp = 14;
 constexpr int kManyThreads = 32 * (kQueryWarp + 1);
-constexpr int kNanList = 16;
+constexpr int kNanList = 8;
 constexpr int kNanLists = 8;  // the conversion may be four items ahead of a half that still writes one out
 
 template <int D>
@@ -101,6 +106,7 @@ __device__ long long tiles_per_head(const AttendArgs& a, const Request& q, bool 
   return sum;
 }
 
+template <bool kTurns>
 __device__ __forceinline__ void load_item(const AttendArgs& a, Segment& s) {
   int t0, t1;
   item_span(a, s.q, s.mt, &t0, &t1, &s.empty);
@@ -109,6 +115,10 @@ __device__ __forceinline__ void load_item(const AttendArgs& a, Segment& s) {
   s.i0 = s.mt * 2 * a.half_tokens;
   s.lo0 = see_from(a, s.q, s.i0);
   s.hi0 = see_to(a, s.q, min(s.i0 + a.half_tokens, s.q.n) - 1);
+  if (kTurns) {
+    s.lo1 = s.lo0, s.hi1 = s.hi0;
+    return;
+  }
   s.lo1 = s.hi1 = 0;
   if (s.i0 + a.half_tokens < s.q.n) {
     s.lo1 = see_from(a, s.q, s.i0 + a.half_tokens);
@@ -116,15 +126,16 @@ __device__ __forceinline__ void load_item(const AttendArgs& a, Segment& s) {
   }
 }
 // To the next item; false past the last.
+template <bool kTurns>
 __device__ __forceinline__ bool next_item(const AttendArgs& a, Segment& s) {
   s.t = 0;
   if (++s.mt < s.items) {
-    load_item(a, s);
+    load_item<kTurns>(a, s);
     return true;
   }
   s.mt = 0;
   if (++s.h < a.n_kv_heads) {
-    load_item(a, s);
+    load_item<kTurns>(a, s);
     return true;
   }
   s.h = 0;
@@ -133,10 +144,12 @@ __device__ __forceinline__ bool next_item(const AttendArgs& a, Segment& s) {
     s.q = request(a, s.r);
   } while (!many(a, s.q));
   s.items = items_of(a, s.q);
-  load_item(a, s);
+  load_item<kTurns>(a, s);
   return true;
 }
+template <bool kTurns>
 __device__ __forceinline__ bool active(const Segment& s, int half, int tile) {
+  if (kTurns && (tile & 1) != half) return false;
   return tile * kKv < (half ? s.hi1 : s.hi0) && (tile + 1) * kKv > (half ? s.lo1 : s.lo0);
 }
 
@@ -236,12 +249,13 @@ struct Shared {
   long long skip;  // tiles of the item before this block's stretch
   int row, head, mt, dead;
   uint32_t tmem;
+  float2 ml[kHalf];  // the second half's maxima and sums, where both have the same rows
 };
 
 // The end of a stretch: `count` tiles from s.t on that lie in s's item.
 #define HX_SEGMENTS(s, count)                                                                       \
   for (int seg = min((count), (s).tiles - (s).t); (count) > 0;                                      \
-       (count) -= seg, (s).t += seg, seg = (count) > 0 && next_item(a, (s)) ? min((count), (s).tiles - (s).t) : (count))
+       (count) -= seg, (s).t += seg, seg = (count) > 0 && next_item<kTurns>(a, (s)) ? min((count), (s).tiles - (s).t) : (count))
 
 template <class T>
 __device__ __forceinline__ float2 two(uint32_t u) {
@@ -259,7 +273,7 @@ __device__ __forceinline__ uint32_t pack(float x, float y) {
 
 // Lane g looks up the block of a tile's 16 tokens g, a tile ahead; the lanes whose block begins
 // there (or is the tile's first) have it copied.
-template <int D>
+template <int D, bool kTurns>
 __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uint8_t* raw) {
   const int lane = threadIdx.x & 31, block = 1 << a.block_shift;
   const int tokens = min(block, kKv);  // of a copy
@@ -273,7 +287,7 @@ __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uin
   };
   const auto skip_empty = [&] {  // items that see nothing have one tile, and nothing in it
     while (count > 0 && s.empty)
-      if (--count > 0) next_item(a, s);
+      if (--count > 0) next_item<kTurns>(a, s);
   };
   skip_empty();
   if (count > 0) look_up();
@@ -285,7 +299,7 @@ __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uin
     if (ok) ks = a.k_scale[id * a.scale_stride + h], vs = a.v_scale[id * a.scale_stride + h];
     --count;
     if (count > 0 && ++s.t == s.tiles) {
-      next_item(a, s);
+      next_item<kTurns>(a, s);
       skip_empty();
     }
     if (count > 0) look_up();
@@ -311,7 +325,7 @@ __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uin
 
 // What has not been copied (no such block) is converted as it lies there: its scores are masked, and its
 // values are numbers times weights of zero.
-template <int D, class T>
+template <int D, class T, bool kTurns>
 __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, const uint8_t* raw, uint8_t* kbuf) {
   // 8 bytes a lane: a lane's 8 f16 are one 16-byte unit, and eight lanes' units lie on different banks
   constexpr int kLanes = D / 8;            // lanes of a token
@@ -398,19 +412,19 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, c
 
 // A half's q: rows of token and head of the group, as they lie in q; what lies past the request
 // or past q is not used.
-template <int D>
+template <int D, bool kTurns>
 __device__ void queries(const AttendArgs& a, const CUtensorMap* qm, Segment s, int count, Shared* sh, uint8_t* qbuf) {
   const uint32_t bytes = (uint32_t)(a.half_tokens * a.group) * D * 2;
   int seg_no = 0;
   HX_SEGMENTS(s, count) {
     if (s.empty) continue;
     for (int half = 0; half < 2; ++half) {
-      const int token = s.q.first + s.i0 + half * a.half_tokens;
+      const int token = s.q.first + s.i0 + (kTurns ? 0 : half * a.half_tokens);
 #pragma unroll
       for (int x = 0; x < D; x += 64) tile_prefetch(qm, x, s.h * a.group, token);
     }
     for (int half = 0; half < 2; ++half) {
-      const int token = s.q.first + s.i0 + half * a.half_tokens;
+      const int token = s.q.first + s.i0 + (kTurns ? 0 : half * a.half_tokens);
       if (!bar_wait(&sh->q_empty[half], (seg_no & 1) ^ 1, &sh->dead)) return;
       bar_expect(&sh->q_full[half], bytes);
 #pragma unroll
@@ -430,7 +444,7 @@ __device__ __forceinline__ bool elected() {
   return p;
 }
 
-template <int D, class T>
+template <int D, class T, bool kTurns>
 __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, const uint8_t* qbuf, const uint8_t* kbuf,
                       const uint8_t* vbuf) {
   const uint32_t tm = sh->tmem;
@@ -438,9 +452,10 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
   uint32_t n_s[2] = {0, 0};  // products P V issued per half
   int it = 0, seg_no = 0;
   volatile int* dead = &sh->dead;
+  const auto issued = [&](int half) { return half ? n_s[1] : n_s[0]; };
   const auto scores = [&](int half, int st) {
     // S's columns hold the half's last P; the order of products with different sums is not promised
-    if (n_s[half]) bar_wait(&sh->o_full[half], (n_s[half] - 1) & 1, dead);
+    if (issued(half)) bar_wait(&sh->o_full[half], (issued(half) - 1) & 1, dead);
     tc_fence_after();
     if (elected()) {
       const uint64_t q = q0 + half * (Many<D>::kQBytes >> 4), k = k0 + st * (Many<D>::kTile >> 4);
@@ -454,7 +469,7 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
     __syncwarp();
   };
   const auto values = [&](int half, int st, bool add) {
-    bar_wait(&sh->p_full[half], n_s[half] & 1, dead);
+    bar_wait(&sh->p_full[half], issued(half) & 1, dead);
     tc_fence_after();
     if (elected()) {
       const uint64_t v = v0 + st * (Many<D>::kTile >> 4);
@@ -464,7 +479,7 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
       tc_commit(&sh->o_full[half]);
     }
     __syncwarp();
-    ++n_s[half];
+    n_s[0] += half == 0, n_s[1] += half == 1;
   };
   const auto commit = [&](uint64_t* bar) {
     if (elected()) tc_commit(bar);
@@ -479,12 +494,37 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
       bar_wait(&sh->ended[1][seg_no & 1], ((seg_no - 2) >> 1) & 1, dead);
     }
     if ((threadIdx.x & 31) == 0) bar_arrive(&sh->go[seg_no & 1]);
+    if (kTurns) {
+      // a half's next tile is the one after next
+      bar_wait(&sh->q_full[0], seg_no & 1, dead), bar_wait(&sh->q_full[1], seg_no & 1, dead);
+      uint32_t had = 0;  // the halves whose O holds something
+#pragma unroll 1
+      for (int i = -2; i < seg && !__any_sync(~0u, *dead); ++i) {
+        const int tile = tile0 + i, half = tile & 1, st = (it + i) & 1;
+        if (i >= 0) {
+          bar_wait(&sh->v_full[st], ((it + i) >> 1) & 1, dead);
+          if (active<kTurns>(s, half, tile)) {
+            values(half, st, had >> half & 1);
+            had |= 1u << half;
+          }
+          commit(&sh->v_empty[st]);
+        }
+        if (i + 2 >= seg) continue;
+        bar_wait(&sh->k_full[st], ((it + i + 2) >> 1) & 1, dead);
+        if (active<kTurns>(s, half, tile + 2)) scores(half, st);
+        commit(&sh->k_empty[st]);
+        if (i + 3 == seg) commit(&sh->q_empty[0]), commit(&sh->q_empty[1]);
+      }
+      it += seg;
+      ++seg_no;
+      continue;
+    }
     bool has[2] = {false, false};  // a half's O holds something
     bar_wait(&sh->k_full[it & 1], (it >> 1) & 1, dead);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       bar_wait(&sh->q_full[half], seg_no & 1, dead);
-      if (active(s, half, tile0)) scores(half, it & 1);
+      if (active<kTurns>(s, half, tile0)) scores(half, it & 1);
       if (seg == 1) commit(&sh->q_empty[half]);
     }
     commit(&sh->k_empty[it & 1]);
@@ -494,14 +534,14 @@ __device__ void issue(const AttendArgs& a, Segment s, int count, Shared* sh, con
       bar_wait(&sh->v_full[st], (it >> 1) & 1, dead);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        if (active(s, half, tile)) {
+        if (active<kTurns>(s, half, tile)) {
           values(half, st, has[half]);
           has[half] = true;
         }
         if (half == 1) commit(&sh->v_empty[st]);
         if (more) {
           if (half == 0) bar_wait(&sh->k_full[st ^ 1], ((it + 1) >> 1) & 1, dead);
-          if (active(s, half, tile + 1)) scores(half, st ^ 1);
+          if (active<kTurns>(s, half, tile + 1)) scores(half, st ^ 1);
           if (i + 2 == seg) commit(&sh->q_empty[half]);
         }
       }
@@ -529,7 +569,7 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w, bool wide) {
   }
 }
 
-template <int D, class T>
+template <int D, class T, bool kTurns>
 __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
   constexpr float kLag = 10.f;  // of f16's 2^16
   const int half = threadIdx.x >> 7, row = threadIdx.x & 127;
@@ -539,10 +579,11 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
   uint32_t n_s = 0;
   volatile int* dead = &sh->dead;
   HX_SEGMENTS(s, count) {
-    const int i = s.i0 + half * a.half_tokens + a.by_group.of(row);  // the row's token in its request
+    const int first = s.i0 + (kTurns ? 0 : half * a.half_tokens);
+    const int i = first + a.by_group.of(row);  // the row's token in its request
     const bool real = row < a.half_tokens * a.group && i < s.q.n;
     if (s.empty) {
-      if (real) {
+      if (real && !(kTurns && half)) {
         const int64_t token = s.q.first + i;
         const int head = s.h * a.group + a.by_group.rest(row);
         T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
@@ -555,14 +596,14 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     __all_sync(~0u, bar_wait(&sh->go[seg_no & 1], (seg_no >> 1) & 1, dead));
     const int lo = real ? see_from(a, s.q, i) : 0, hi = real ? see_to(a, s.q, i) : 0;
     // what all rows of the half see: [all_lo, all_hi); rows without a token do not matter
-    const int first = s.i0 + half * a.half_tokens, last = min(first + a.half_tokens, s.q.n) - 1;
+    const int last = min(first + a.half_tokens, s.q.n) - 1;
     const int all_lo = last < first ? 0 : see_from(a, s.q, last), all_hi = last < first ? 0 : see_to(a, s.q, first);
     const float c = a.sm_scale_log2;
     float m = 0, l = 0;
     bool has = false, fresh = true;  // fresh: the row has seen nothing yet
     for (int j = 0; j < seg && !__any_sync(~0u, *dead); ++j, ++it) {
       const int tile = s.first_tile + s.t + j;
-      if (!active(s, half, tile)) continue;
+      if (!active<kTurns>(s, half, tile)) continue;
       const int pos = tile * kKv;
       const TileInfo& info = sh->info[it & 7];
       if (!bar_wait(&sh->s_full[half], n_s & 1, dead)) l = NAN;
@@ -664,10 +705,30 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       if (!bar_wait(&sh->o_full[half], (n_s - 1) & 1, dead)) l = NAN;
       tc_fence_after();
     }
+    if (fresh) m = -INFINITY;
+    float scale = has ? 1.f : 0.f, scale1 = 0;  // of the halves' sums in the row's
+    if (kTurns) {
+      // the first half's threads join the two; a thread reaches the other half's row in tensor memory, its lane
+      if (half) sh->ml[row] = float2{m, l};
+      tc_fence_before();
+      __syncwarp();
+      asm volatile("bar.sync 2, 256;" ::: "memory");
+      tc_fence_after();
+      if (half) {
+        asm volatile("bar.sync 2, 256;" ::: "memory");
+        bar_arrive(&sh->ended[half][seg_no & 1]);
+        ++seg_no;
+        continue;
+      }
+      const float2 other = sh->ml[row];
+      const float most = fmaxf(m, other.x);
+      if (most > -INFINITY) scale = ex2(m - most), scale1 = ex2(other.x - most);
+      l = l * scale + other.y * scale1;
+      m = most;
+    }
     const int64_t token = s.q.first + i;
     const int head = s.h * a.group + a.by_group.rest(row);
     T* out = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride;
-    if (fresh) m = -INFINITY;
     const bool done = seg == s.tiles;
     const int64_t slot = 2 * blockIdx.x + (s.t == 0);
     float* part = a.part + (slot * kItemRows + half * kHalf + row) * D;
@@ -677,9 +738,16 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     for (int ch = 0; ch < D; ch += 32) {
       uint32_t u[32];
       tm_load(to + ch, u);
-      const float by = has && !none ? inv : 0.f;
+      const float by = none ? 0.f : scale * inv;
 #pragma unroll
       for (int y = 0; y < 32; ++y) u[y] = by == 0.f ? 0 : __float_as_uint(__uint_as_float(u[y]) * by);
+      if (kTurns) {
+        uint32_t w[32];
+        tm_load(to + D + ch, w);
+        const float by1 = none ? 0.f : scale1 * inv;
+#pragma unroll
+        for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) + (by1 == 0.f ? 0.f : __uint_as_float(w[y]) * by1));
+      }
       if (!real) continue;
       if (done) {
         uint32_t w[16];
@@ -690,8 +758,13 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
         store32<32>(part + ch, u, true);
       }
     }
+    if (kTurns) {
+      tc_fence_before();
+      __syncwarp();
+      asm volatile("bar.sync 2, 256;" ::: "memory");
+    }
     // NaN among the values that this row sees
-    const int nans = has ? sh->nan_count[seg_no & (kNanLists - 1)] : 0;
+    const int nans = has || kTurns ? sh->nan_count[seg_no & (kNanLists - 1)] : 0;
     if (nans && real) {
       const int p0 = max(lo, (s.first_tile + s.t) * kKv), p1 = min(hi, (s.first_tile + s.t + seg) * kKv);
       const bool listed = nans <= kNanList;
@@ -721,7 +794,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
   }
 }
 
-template <int D, class T>
+template <int D, class T, bool kTurns>
 __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(
     const __grid_constant__ CUtensorMap qm, const __grid_constant__ AttendArgs a) {
   // all but the last few of the 227 KB; the tiles first, for their alignment
@@ -826,7 +899,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(
   s.h = sh.head;
   s.mt = sh.mt;
   const long long skip = sh.skip;
-  load_item(a, s);
+  load_item<kTurns>(a, s);
   s.t = (int)skip;
   int count = (int)(n1 - n0);
   if (tid == 0) {
@@ -844,11 +917,11 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp < kConvWarp) softmax<D, T>(a, s, count, &sh);
-  else if (warp < kMmaWarp) convert<D, T>(a, s, count, &sh, raw, kbuf);
-  else if (warp == kMmaWarp) issue<D, T>(a, s, count, &sh, qbuf, kbuf, vbuf);
-  else if (warp == kFetchWarp) fetch<D>(a, s, count, &sh, raw);
-  else if (lane == 0) queries<D>(a, &qm, s, count, &sh, qbuf);
+  if (warp < kConvWarp) softmax<D, T, kTurns>(a, s, count, &sh);
+  else if (warp < kMmaWarp) convert<D, T, kTurns>(a, s, count, &sh, raw, kbuf);
+  else if (warp == kMmaWarp) issue<D, T, kTurns>(a, s, count, &sh, qbuf, kbuf, vbuf);
+  else if (warp == kFetchWarp) fetch<D, kTurns>(a, s, count, &sh, raw);
+  else if (lane == 0) queries<D, kTurns>(a, &qm, s, count, &sh, qbuf);
   __syncwarp();
   drain(&sh.dead);
   tc_fence_before();
@@ -857,11 +930,11 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem) : "memory");
 }
 
-template <int D, class T>
+template <int D, class T, bool kTurns>
 cudaError_t launch(const CUtensorMap& qm, const AttendArgs& a, int blocks, cudaStream_t s) {
   constexpr int kSmem = Many<D>::kTiles + (int)sizeof(Shared);
   static_assert(kSmem <= 227 * 1024, "shared memory of a block");
-  const auto kernel = hx_kv_attend_many<D, T>;
+  const auto kernel = hx_kv_attend_many<D, T, kTurns>;
   if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)) return e;
   kernel<<<blocks, kManyThreads, kSmem, s>>>(qm, a);
   return cudaGetLastError();
@@ -870,8 +943,15 @@ cudaError_t launch(const CUtensorMap& qm, const AttendArgs& a, int blocks, cudaS
 }  // namespace
 
 cudaError_t launch_attend_many(const CUtensorMap& qm, const AttendArgs& a, int head_dim, bool bf16, int blocks, cudaStream_t s) {
-  if (head_dim == 128) return bf16 ? launch<128, __nv_bfloat16>(qm, a, blocks, s) : launch<128, __half>(qm, a, blocks, s);
-  return bf16 ? launch<64, __nv_bfloat16>(qm, a, blocks, s) : launch<64, __half>(qm, a, blocks, s);
+  const bool turns = a.max_q > 0 && a.max_q <= a.half_tokens;
+  const auto typed = [&](auto d, auto type) {
+    using T = decltype(type);
+    return turns ? launch<decltype(d)::value, T, true>(qm, a, blocks, s) : launch<decltype(d)::value, T, false>(qm, a, blocks, s);
+  };
+  const std::integral_constant<int, 64> d64{};
+  const std::integral_constant<int, 128> d128{};
+  if (head_dim == 128) return bf16 ? typed(d128, __nv_bfloat16{}) : typed(d128, __half{});
+  return bf16 ? typed(d64, __nv_bfloat16{}) : typed(d64, __half{});
 }
 
 }  // namespace hx

@@ -575,3 +575,20 @@ def test_a_named_stream_owns_what_a_call_allocates(handle):
     step = KV.map_step(i(0), i(20), table, ring, state, 20, 16, stream=name)
     side.synchronize()
     assert step.slots.tolist() == list(range(16, 32)) + list(range(4)) and table.tolist() == [[1, 0]]
+
+
+@pytest.mark.parametrize("B,D,group,most,dtype", [(16, 64, 4, 32, torch.float16), (64, 128, 8, 16, torch.bfloat16),
+                                                  (128, 128, 16, 8, torch.float16), (32, 64, 3, 42, torch.bfloat16)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 70), (True, 130), (True, 1000)])
+def test_attend_chunks_of_half_an_item(B, D, group, most, dtype, causal, window):
+    """No more tokens a request than a half of an item has: with a bound that says so and without one, over lengths of
+    one tile, of few, and of more than a block's stretch."""
+    q_len = [most, 0, 6, most - 1, 7, most, 6, 1, most, 5, most]
+    kv_len = [most, 100, 6, 127, 129, 256, 0, 4, 3, 385, 9003]
+    for max_q in (most, 0):
+        _attend(q_len, kv_len, 2, group, D, B, dtype, causal=causal, window=window, seed=group + window, max_q=max_q)
+
+
+@pytest.mark.parametrize("group,chunk", [(4, 5), (4, 32), (16, 8), (3, 42)])
+def test_attend_nan_in_chunks_of_half_an_item(group, chunk):
+    test_attend_nan_stays_where_it_is_seen(group, chunk)
