@@ -23,7 +23,7 @@ namespace {
 // compute 16), and the sums take half the registers, which lets 12 computing warps reside on an SM.
 //
 // 48 requests of 32000 tokens, 32 heads on 8 of 128: 507 us, 6.35 TB/s, 95 % of a copy.  500 requests of 437 to
-// 18133 tokens, 28 heads on 4 of 64, blocks of 16: 248 us, 3.65 TB/s: instructions, of which a column of 64 takes as
+// 18133 tokens, 28 heads on 4 of 64, blocks of 16: 223 us, 4.05 TB/s: instructions, of which a column of 64 takes as
 // many for its softmax as one of 128.  One request of 5065 tokens: 14.8 us, latency.
 constexpr int kRows = 16;  // most rows of an item
 constexpr int kStageBytes = 8192;
@@ -353,9 +353,6 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       for (int i = 0; i < ND; ++i) acc[r][i][0] = acc[r][i][1] = acc[r][i][2] = acc[r][i][3] = 0;
       m[r][0] = m[r][1] = -INFINITY, l[r][0] = l[r][1] = 0;
     }
-    // sums are kept in units of the values' scale, so that scales far apart lose nothing in 16 bits
-    float unit = 1.f, unit_top = 0.f;
-
     for (; left < seg; left += W) {
       bool ok = landed(2 * stage);
       const uint8_t* kt = ring + stage * kStageBytes;
@@ -467,33 +464,41 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
             }
         }
 
+      if (moved) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+            acc[r][d][0] *= keep[r][0], acc[r][d][1] *= keep[r][1], acc[r][d][2] *= keep[r][0], acc[r][d][3] *= keep[r][1];
+      }
+      // A scale that is infinite or no number reaches the rows that see something of its group, and no others.
+      bool odd = false;
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g) odd |= !(fabsf(value_scale[g]) < INFINITY);
+      if (odd) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            bool none = false;
+#pragma unroll
+            for (int g = 0; g < S::kGroups; ++g)
+              none |= !(fabsf(value_scale[g]) < INFINITY) && pos + 16 * g + 16 > lo[r][x] && pos + 16 * g < hi[r][x];
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+              if (none) acc[r][d][x] = acc[r][d][2 + x] = NAN;
+          }
+#pragma unroll
+        for (int g = 0; g < S::kGroups; ++g)
+          if (!(fabsf(value_scale[g]) < INFINITY)) value_scale[g] = 0.f;
+      }
+      uint32_t bp[S::kGroups][NR][2];
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g) {
-        // the unit follows the values' scale, at most 2^60 below the largest so far
-        const float vs = valid >> g & 1 ? value_scale[g] : unit;
-        const bool other = vs != unit;
-        float to = 1.f, pf = 1.f;
-        if (other) {
-          unit_top = fmaxf(unit_top, vs);
-          const float next = fmaxf(fmaxf(vs, unit_top * 0x1p-60f), 0x1p-110f);
-          to = unit / next, pf = vs / next;
-          unit = next;
-        }
-        if (other || (g == 0 && moved)) {
-#pragma unroll
-          for (int r = 0; r < NR; ++r) {
-            const float f0 = g == 0 && moved ? to * keep[r][0] : to, f1 = g == 0 && moved ? to * keep[r][1] : to;
-#pragma unroll
-            for (int d = 0; d < ND; ++d) acc[r][d][0] *= f0, acc[r][d][1] *= f1, acc[r][d][2] *= f0, acc[r][d][3] *= f1;
-#pragma unroll
-            for (int y = 0; y < 4; ++y) s[g][r][y] *= pf;
-          }
-        }
-        uint32_t bp[NR][2];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-          bp[r][0] = transpose8(pack_half(s[g][r][0], s[g][r][1]));
-          bp[r][1] = transpose8(pack_half(s[g][r][2], s[g][r][3]));
+          bp[g][r][0] = transpose8(pack_half(s[g][r][0], s[g][r][1]));
+          bp[g][r][1] = transpose8(pack_half(s[g][r][2], s[g][r][3]));
         }
         if (!whole) {
           // a masked position's values must not count, not even as 0 * NaN
@@ -546,17 +551,28 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
             }
           }
         }
+      }
+      // O^T += scale * (V^T P^T), 16 columns at a time: the scale's product and the sum over groups are in 32 bits, so that
+      // scales far apart cost each other nothing, and one that a row does not see is multiplied by zero.  (Sums in units
+      // of the last scale, rescaled where it changed, let a masked block's scale into the row; 500 ragged requests took 248 us, now 223.)
 #pragma unroll
-        for (int w = 0; w < D / 32; ++w)
+      for (int w = 0; w < D / 32; ++w)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+          for (int g = 0; g < S::kGroups; ++g) {
             const uint32_t x = __byte_perm(vw[g][0][w], vw[g][1][w], e ? 0x7362 : 0x5140);
             const uint32_t y = __byte_perm(vw[g][2][w], vw[g][3][w], e ? 0x7362 : 0x5140);
             const uint32_t av[4] = {cvt2(x), cvt2_hi(x), cvt2(y), cvt2_hi(y)};
 #pragma unroll
-            for (int r = 0; r < NR; ++r) mma16816(acc[r][2 * w + e], av, bp[r][0], bp[r][1]);
+            for (int r = 0; r < NR; ++r) {
+              float o[4] = {0, 0, 0, 0};
+              mma16816(o, av, bp[g][r][0], bp[g][r][1]);
+#pragma unroll
+              for (int z = 0; z < 4; ++z) acc[r][2 * w + e][z] = fmaf(value_scale[g], o[z], acc[r][2 * w + e][z]);
+            }
           }
-      }
+        }
       stage += W;
       if (stage >= S::kStages) stage -= S::kStages, ++turn;
     }
@@ -582,7 +598,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
         float z = -INFINITY;
 #pragma unroll
         for (int w = 0; w < W; ++w) z = fmaxf(z, s_ml[w][2 * q4 + x + 8 * r][0]);
-        part[r][x] = (z == -INFINITY ? 0.f : ex2(m[r][x] - z)) * unit;
+        part[r][x] = z == -INFINITY ? 0.f : ex2(m[r][x] - z);
       }
     // this thread's columns are D / 8 in a row from n * D / 8, for rows 2 q4 and 2 q4 + 1
     const auto place = [&](int buf, int r, int x) {

@@ -1,0 +1,95 @@
+"""Attention over the paged cache where scales, weights and lengths leave the ordinary range, on
+both of its kernels, against the plain 64-bit implementation."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_05286_gb300 import build as B_
+from paper_2505_05286_gb300 import kvcache as KV
+from tests import kv_cases as P
+from tests.test_gpu_kvcache import gen
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    B_.build()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def near(got, lse, want, wlse, tol, ltol):
+    """Within the bounds where the 64-bit result is a number, not a finite number where it is not."""
+    num = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), num), "which results are numbers"
+    e = torch.where(num, (got.double() - want).abs(), 0)
+    tol = torch.where(num, tol, 0)
+    assert bool((e <= tol).all()), f"out: {float((e / tol.clamp(min=1e-300)).max())} of the bound"
+    empty = wlse == -math.inf
+    assert torch.equal(lse == -math.inf, empty)
+    e = torch.where(empty, 0, (lse.double() - wlse).abs())
+    assert bool((e <= torch.where(empty, 0, ltol)).all()), f"lse: {float((e / ltol.clamp(min=1e-300)).max())} of the bound"
+
+
+def check(q, cache, table, q_len, kv_len, sm, causal=True, window=0, max_q=(0,)):
+    start = np.concatenate([[0], np.cumsum(q_len)]).astype(np.int32)
+    want = P.attend_plain(q, cache.k, cache.v, cache.k_scale, cache.v_scale, table, start, kv_len, sm, causal, window)
+    for mq in max_q:
+        out = torch.full_like(q, math.nan)
+        got, lse = cache.attend(q, table, i32(start), i32(kv_len), sm_scale=sm, causal=causal, window=window, max_q=mq,
+                                out=out, return_lse=True)
+        near(got, lse, *want)
+
+
+# ---- blocks that no token sees, or not all tokens
+
+FORMS = [([1, 1, 1], 2, (1, 0)), ([1, 1, 1], 12, (1,)), ([4, 3, 1], 2, (4, 0)), ([4, 2, 4], 4, (4, 0)), ([40, 1, 21], 3, (40, 0, 100))]
+
+
+@pytest.mark.parametrize("scale", [math.nan, math.inf, 2.0 ** 100])
+@pytest.mark.parametrize("D,B", [(64, 16), (64, 32), (128, 16), (64, 64), (128, 64)])
+@pytest.mark.parametrize("q_len,group,max_q", FORMS)
+def test_scales_before_the_window_take_no_part(scale, D, B, q_len, group, max_q):
+    """Table entries wholly before what any token of the request sees name blocks of any contents."""
+    g = gen(B + D)
+    window, kv_len = 70, [300, 171, 209]
+    table, N = P.paged(g, kv_len, B)
+    k, v, ks, vs = P.random_cache(g, N, 2, B, D)
+    for r, (n, kv) in enumerate(zip(q_len, kv_len)):
+        gone = table[r, :max(0, kv - n - window + 1) // B].long()
+        assert len(gone) > 0
+        ks[gone], vs[gone] = scale, scale
+        k.view(torch.uint8)[gone, :, ::3], v.view(torch.uint8)[gone, :, ::5] = 0x7f, 0x7f
+    q = torch.randn((sum(q_len), 2 * group, D), generator=g, device="cuda").bfloat16()
+    check(q, KV.Cache(k, v, ks, vs), table, q_len, kv_len, D ** -0.5, window=window, max_q=max_q)
+
+
+def _one_block(scale, D, n, group, max_q, edge):
+    """One block is seen by the first token of a chunk only (through the window), or by the last only: a scale that is
+    no number there makes that token's result none, one far above the others' costs the other tokens nothing."""
+    g, B, window = gen(D + n), 16, 20
+    if edge == "first":
+        kv = 16 * 3 + window + n - 2  # token 0 sees from the last position of block 2 on
+        block = 2
+    else:
+        kv, block = 16 * 4 + 1, 4
+    table, N = P.paged(g, [kv], B)
+    k, v, ks, vs = P.random_cache(g, N, 2, B, D)
+    b = v.view(torch.uint8)
+    b[(b & 0x7f) == 0] = 0x38  # an infinite scale times zero is no number either, but times one it is infinite
+    vs[table[0, block].long()] = scale
+    q = torch.randn((n, 2 * group, D), generator=g, device="cuda").bfloat16()
+    check(q, KV.Cache(k, v, ks, vs), table, [n], [kv], D ** -0.5, window=window, max_q=max_q)
+
+
+@pytest.mark.parametrize("scale", [math.nan, math.inf, 2.0 ** 100])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,group,max_q", [(4, 2, (4, 0)), (4, 4, (4,))])
+@pytest.mark.parametrize("edge", ["first", "last"])
+def test_a_value_scale_reaches_the_few_rows_that_see_its_block(scale, D, n, group, max_q, edge):
+    _one_block(scale, D, n, group, max_q, edge)
