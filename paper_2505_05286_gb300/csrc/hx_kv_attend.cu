@@ -715,7 +715,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   }
 
   // how long the items are before each thread's rows, and in all
-  const int owned = min(max(a.row_start[a.n_rows], 0), a.n_tokens);
+  const int ahead = min(max(a.row_start[0], 0), a.n_tokens), owned = min(max(a.row_start[a.n_rows], ahead), a.n_tokens);
   const int per = (a.n_rows + kThreads - 1) / kThreads;
   const int r0 = min(a.n_rows, tid * per), r1 = min(a.n_rows, r0 + per);
   long long mine = 0;
@@ -758,9 +758,9 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
   }
   __syncthreads();
 
-  // tokens that no row owns
-  for (int t = owned + blockIdx.x; t < a.n_tokens; t += gridDim.x) {
-    const Request q = {t, 1, 0};
+  // tokens that no row owns, before the first row's and behind the last one's
+  for (int i = blockIdx.x; i < ahead + a.n_tokens - owned; i += gridDim.x) {
+    const Request q = {i < ahead ? i : owned + i - ahead, 1, 0};
     for (int h = 0; h < a.n_kv_heads; ++h) write_empty<T>(a, D, q, h, tid, kThreads);
   }
 
