@@ -657,12 +657,12 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
             uint32_t w[16];
 #pragma unroll 1
             for (int o = 0; o < 16 * ch; o += 16) {
-              const __half2 k2 = __float2half2_rn(keep);
               tm_load16(ts + o, w);
 #pragma unroll
               for (int y = 0; y < 16; ++y) {
-                const __half2 h = __hmul2(*(const __half2*)&w[y], k2);
-                w[y] = *(const uint32_t*)&h;
+                // in 32 bits: the factor alone may be too small for f16 where its product with a weight is not
+                const float2 e = __half22float2(*(const __half2*)&w[y]);
+                w[y] = pack_half(e.x * keep, e.y * keep);
               }
               tm_store16(ts + o, w);
             }

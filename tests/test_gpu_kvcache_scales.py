@@ -93,3 +93,39 @@ def _one_block(scale, D, n, group, max_q, edge):
 @pytest.mark.parametrize("edge", ["first", "last"])
 def test_a_value_scale_reaches_the_few_rows_that_see_its_block(scale, D, n, group, max_q, edge):
     _one_block(scale, D, n, group, max_q, edge)
+
+
+# ---- weights that are rescaled
+
+def one_column_cache(scores, values, D, B, k_scale=1.0, v_scale=None):
+    """A cache of one request and head in which token p's score is scores[p] powers of two for a q of ones in
+    its first two columns (sums of two e4m3 numbers) and whose value is values[p] in every column."""
+    n = len(scores)
+    blocks = -(-n // B)
+    k = torch.zeros((blocks * B, D))
+    hi = torch.tensor(scores, dtype=torch.float32).to(torch.float8_e4m3fn).float()
+    k[:n, 0], k[:n, 1] = hi, torch.tensor(scores, dtype=torch.float32) - hi
+    v = torch.zeros((blocks * B, D))
+    v[:n] = torch.tensor(values, dtype=torch.float32)[:, None]
+    f8 = lambda x: x.view(blocks, 1, B, D).to(torch.float8_e4m3fn).cuda()
+    assert torch.equal(f8(k).float().cpu().view(-1, D), k)
+    vs = torch.ones((blocks, 1)) if v_scale is None else torch.tensor(v_scale, dtype=torch.float32).view(blocks, 1)
+    return KV.Cache(f8(k), f8(v), torch.full((blocks, 1), k_scale, device="cuda"), vs.cuda()), i32([list(range(blocks))])
+
+
+def two_columns(n, heads, D, dtype):
+    q = torch.zeros((n, heads, D), dtype=dtype, device="cuda")
+    q[:, :, :2] = 1
+    return q
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20, 200)), (130, (0, 130))])
+@pytest.mark.parametrize("jump", [11.875, 20.875, 24.875, 26.875, 29.875])
+def test_weights_keep_their_bits_when_the_maximum_moves(D, n, max_q, jump):
+    """64 tokens at 2^9.875 above the first 32 of their tile, then one far above those: each of the 64 counts little,
+    but their values are all that there is."""
+    scores = [0.0] * 32 + [9.875] * 64 + [jump] + [0.0] * 31
+    values = [0.0] * 32 + [1.0] * 64 + [0.0] * 32
+    cache, table = one_column_cache(scores, values, D, 16)
+    check(two_columns(n, 1, D, torch.float16), cache, table, [n], [128], math.log(2), causal=False, max_q=max_q)
