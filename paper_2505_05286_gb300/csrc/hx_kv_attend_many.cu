@@ -33,13 +33,17 @@ namespace {
 //
 // Scales: a score is s * ks * c, and a value's scale vs goes into the weight, P = exp2(s ks c +
 // log2(vs) - m) with m within kLag of the largest of those exponents so far.  So P in f16 is accurate
-// relative to the row's largest weight times scale, however far apart scales lie, and the
-// softmax's sum is that of P / vs.
+// relative to the row's largest weight times scale, however far apart scales lie.  The softmax's sum l is that of
+// P 2^ref / vs, in units of 2^(m - ref) where ref is the power of two of a scale of the item, as long as all its scales lie
+// within 2^kNear of that.  Past this P may be zero where its share of l is not: from the first such tile on l is
+// summed from the scores alone, in units of 2^ml with a maximum of its own (64 blocks of zeros, as hx_kv_append leaves them
+// under 2^-100, beside one under 2^20: the result was too large by what they weigh).
 constexpr int kHalf = 128;
 constexpr int kKv = 128;       // tokens of a tile
 constexpr int kGroups = kKv / 16;
 constexpr int kConvWarp = 8, kMmaWarp = 12, kFetchWarp = 13, kQueryWarp = 14;
 constexpr int kManyThreads = 32 * (kQueryWarp + 1);
+constexpr float kNear = 40.f;  // so that what P / vs loses below 2^-126 is less than 2^-46 of l
 constexpr int kNanList = 8;
 constexpr int kNanLists = 8;  // the conversion may be four items ahead of a half that still writes one out
 
@@ -231,7 +235,9 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(x)), "l"(bits(y)));
   return floats(r);
 }
-// What a tile's groups of 16 tokens are scaled by: {ks, log2 vs, 1 / vs, -}, and which of them exist.
+// What a tile's groups of 16 tokens are scaled by: {ks, log2 vs, 2^ref / vs, -}, and which of them exist; kFar: the
+// item's scales lie far apart.
+constexpr uint32_t kFar = 1u << 31;
 struct TileInfo {
   float4 g[kGroups];
   uint32_t valid;
@@ -244,12 +250,14 @@ struct Shared {
   uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], go[2], ended[2][2];  // go and ended: of even and odd items
   TileInfo info[8];
   int nan_count[kNanLists];
+  float ref[kNanLists];  // by items, as the lists are
   int nan_pos[kNanLists][kNanList];
   long long sum[kManyThreads / 32];
   long long skip;  // tiles of the item before this block's stretch
   int row, head, mt, dead;
   uint32_t tmem;
-  float2 ml[kHalf];  // the second half's maxima and sums, where both have the same rows
+  float2 ml[kHalf];  // the second half's ml and l, where both have the same rows
+  signed char up[kHalf];  // and its m - ml, -128: it holds nothing
 };
 
 // The end of a stretch: `count` tiles from s.t on that lie in s's item.
@@ -280,6 +288,9 @@ __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uin
   const bool copies = lane < kGroups && (16 * lane & (tokens - 1)) == 0;
   volatile int* dead = &sh->dead;
   int id = -1, pos = 0, h = 0;
+  float ref = 0;
+  bool has_ref = false, far = false;  // of the item
+  int item = 0;
   const auto look_up = [&] {
     pos = (s.first_tile + s.t) * kKv + 16 * lane;
     h = s.h;
@@ -297,8 +308,11 @@ __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uin
     const int64_t at = id * a.block_stride + ((int64_t)h * block + (pos & (block - 1))) * D;
     float ks = 0, vs = 0;
     if (ok) ks = a.k_scale[id * a.scale_stride + h], vs = a.v_scale[id * a.scale_stride + h];
+    const bool seen = ok && pos + 16 > s.lo0;  // by any row of the item
+    bool last = false;                         // of its tiles here
     --count;
     if (count > 0 && ++s.t == s.tiles) {
+      last = true;
       next_item<kTurns>(a, s);
       skip_empty();
     }
@@ -309,9 +323,14 @@ __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uin
       if (!__all_sync(~0u, bar_wait(&sh->raw_empty[v], (it & 1) ^ 1, dead))) return;
       if (v == 0) {
         TileInfo& info = sh->info[it & 7];
-        const float r = fmaxf(vs, 0x1p-100f);
-        if (lane < kGroups) info.g[lane] = float4{ks, log2f(r), 1.f / r, 0.f};
-        if (lane == 0) info.valid = valid;
+        const float r = fmaxf(vs, 0x1p-100f), lv = log2f(r);
+        const uint32_t who = __ballot_sync(~0u, seen);
+        if (who && !has_ref) ref = rintf(__shfl_sync(~0u, lv, __ffs(who) - 1)), has_ref = true;
+        const bool near = fabsf(lv - ref) <= kNear;
+        far |= __any_sync(~0u, seen && !near);
+        if (lane < kGroups) info.g[lane] = float4{ks, lv, near ? exp2f(ref) / r : 1.f, 0.f};
+        if (lane == 0) info.valid = valid | (far ? kFar : 0), sh->ref[item & (kNanLists - 1)] = ref;
+        if (last) has_ref = far = false, ++item;
         __syncwarp();
       }
       if (lane == 0) bar_expect(&sh->raw_full[v], bytes);
@@ -599,8 +618,10 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     const int last = min(first + a.half_tokens, s.q.n) - 1;
     const int all_lo = last < first ? 0 : see_from(a, s.q, last), all_hi = last < first ? 0 : see_to(a, s.q, first);
     const float c = a.sm_scale_log2;
-    float m = 0, l = 0;
+    const float* ref = &sh->ref[seg_no & (kNanLists - 1)];
+    float m = 0, l = 0, ml = -INFINITY;
     bool has = false, fresh = true;  // fresh: the row has seen nothing yet
+    bool apart = false;              // l has a maximum of its own, ml
     for (int j = 0; j < seg && !__any_sync(~0u, *dead); ++j, ++it) {
       const int tile = s.first_tile + s.t + j;
       if (!active<kTurns>(s, half, tile)) continue;
@@ -609,6 +630,10 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       if (!bar_wait(&sh->s_full[half], n_s & 1, dead)) l = NAN;
       tc_fence_after();
       const uint32_t valid = info.valid;
+      if ((valid & kFar) && !apart) {
+        apart = true;
+        if (l != 0) ml = m - *ref;
+      }
       const bool whole = valid == (1u << kGroups) - 1 && pos >= all_lo && pos + kKv <= all_hi;
       // what this row sees of 32 tokens
       const auto sees = [&](int ch) -> uint32_t {
@@ -622,12 +647,27 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       // (by a whole number) only when a weight would pass 2^kLag, and then what it has written of this tile
       // and O follow.
       const auto weigh = [&](auto kind) {
-        constexpr bool masked = decltype(kind)::value;
+        constexpr bool masked = decltype(kind)::value > 0, far = decltype(kind)::value > 1;
 #pragma unroll 1
         for (int ch = 0; ch < 4; ++ch) {
           uint32_t v[32];
           tm_load(ts + 32 * ch, v);
           const uint32_t see = masked ? sees(ch) : 0;
+          if constexpr (far) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (see >> y & 1) top = fmaxf(top, __uint_as_float(v[y]) * (info.g[2 * ch + (y >> 4)].x * c));
+            if (top > ml && top < INFINITY) {
+              const float up = ceilf(top);
+              l *= ex2(ml - up);
+              ml = up;
+            }
+            const float base = ml == -INFINITY ? 0.f : ml;
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (see >> y & 1) l += ex2(fmaf(__uint_as_float(v[y]), info.g[2 * ch + (y >> 4)].x * c, -base));
+          }
           float4 z[2];
           float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -650,7 +690,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
             const float keep = fresh ? 1.f : ex2(-by);  // nothing has been kept while nothing was seen
             fresh &= !late;
             m += by;
-            l *= keep;
+            if (!far) l *= keep;
 #pragma unroll
             for (int y = 0; y < 32; ++y) v[y] = __float_as_uint(__uint_as_float(v[y]) - by);
             tm_stored();
@@ -687,13 +727,14 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
               w[y / 2] = pack_half(e.x, e.y);
             }
             const float2 sum = add2(part[0], part[1]);
-            l = fmaf(sum.x + sum.y, z[g].z, l);
+            if (!far) l = fmaf(sum.x + sum.y, z[g].z, l);
             tm_store8(ts + 16 * ch + 8 * g, w);
           }
         }
       };
-      if (whole) weigh(std::false_type{});
-      else weigh(std::true_type{});
+      if (whole) weigh(std::integral_constant<int, 0>{});
+      else if (!apart) weigh(std::integral_constant<int, 1>{});
+      else weigh(std::integral_constant<int, 2>{});
       tm_stored();
       tc_fence_before();
       bar_arrive(&sh->p_full[half]);
@@ -705,11 +746,15 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       if (!bar_wait(&sh->o_full[half], (n_s - 1) & 1, dead)) l = NAN;
       tc_fence_after();
     }
+    // O is in units of 2^m, l in units of 2^ml: so is what is stored of both
+    // (what has seen nothing has not waited for ref either)
     if (fresh) m = -INFINITY;
-    float scale = has ? 1.f : 0.f, scale1 = 0;  // of the halves' sums in the row's
+    if (!apart && !fresh) ml = m - *ref;
+    float up = m - ml, up1 = 0;  // what brings the halves' O there, powers of two
+    bool holds = has && !fresh, holds1 = false;
     if (kTurns) {
       // the first half's threads join the two; a thread reaches the other half's row in tensor memory, its lane
-      if (half) sh->ml[row] = float2{m, l};
+      if (half) sh->ml[row] = float2{ml, l}, sh->up[row] = (signed char)(holds ? fminf(fmaxf(m - ml, -127.f), 127.f) : -128.f);
       tc_fence_before();
       __syncwarp();
       asm volatile("bar.sync 2, 256;" ::: "memory");
@@ -721,10 +766,10 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
         continue;
       }
       const float2 other = sh->ml[row];
-      const float most = fmaxf(m, other.x);
-      if (most > -INFINITY) scale = ex2(m - most), scale1 = ex2(other.x - most);
-      l = l * scale + other.y * scale1;
-      m = most;
+      const float most = fmaxf(ml, other.x), base = most > -INFINITY ? most : 0.f;
+      up = m - base, up1 = sh->up[row] + other.x - base, holds1 = sh->up[row] != -128;
+      l = l * ex2(ml - base) + other.y * ex2(other.x - base);
+      ml = most;
     }
     const int64_t token = s.q.first + i;
     const int head = s.h * a.group + a.by_group.rest(row);
@@ -734,19 +779,24 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     float* part = a.part + (slot * kItemRows + half * kHalf + row) * D;
     const bool none = l == 0;
     const float inv = done ? (none ? 0.f : 1.f / l) : 1.f;
+    const auto factor = [&](float up) {  // 2^up * inv, in two steps: 2^up alone may leave the range
+      up = fminf(fmaxf(up, -252.f), 252.f);
+      const float part = rintf(0.5f * up);
+      return ex2(part) * (ex2(up - part) * inv);
+    };
+    const float by = factor(up), by1 = factor(up1);
 #pragma unroll 1
     for (int ch = 0; ch < D; ch += 32) {
       uint32_t u[32];
       tm_load(to + ch, u);
-      const float by = none ? 0.f : scale * inv;
 #pragma unroll
-      for (int y = 0; y < 32; ++y) u[y] = by == 0.f ? 0 : __float_as_uint(__uint_as_float(u[y]) * by);
+      for (int y = 0; y < 32; ++y) u[y] = holds ? __float_as_uint(__uint_as_float(u[y]) * by) : 0;
       if (kTurns) {
         uint32_t w[32];
         tm_load(to + D + ch, w);
-        const float by1 = none ? 0.f : scale1 * inv;
 #pragma unroll
-        for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) + (by1 == 0.f ? 0.f : __uint_as_float(w[y]) * by1));
+        for (int y = 0; y < 32; ++y)
+          u[y] = __float_as_uint(__uint_as_float(u[y]) + (holds1 ? __uint_as_float(w[y]) * by1 : 0.f));
       }
       if (!real) continue;
       if (done) {
@@ -785,8 +835,8 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       }
     }
     if (real) {
-      if (!done) *(float2*)(a.part_ml + (slot * kItemRows + half * kHalf + row) * 2) = float2{m, l};
-      else if (a.lse) a.lse[token * a.n_heads + head] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      if (!done) *(float2*)(a.part_ml + (slot * kItemRows + half * kHalf + row) * 2) = float2{ml, l};
+      else if (a.lse) a.lse[token * a.n_heads + head] = none ? -INFINITY : (ml + log2f(l)) * 0.6931471805599453f;
     }
     tc_fence_before();
     bar_arrive(&sh->ended[half][seg_no & 1]);

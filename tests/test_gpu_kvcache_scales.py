@@ -129,3 +129,56 @@ def test_weights_keep_their_bits_when_the_maximum_moves(D, n, max_q, jump):
     values = [0.0] * 32 + [1.0] * 64 + [0.0] * 32
     cache, table = one_column_cache(scores, values, D, 16)
     check(two_columns(n, 1, D, torch.float16), cache, table, [n], [128], math.log(2), causal=False, max_q=max_q)
+
+
+# ---- sums of weights under scales far apart
+
+def _far(first, other, shift, D, blocks=64, B=16):
+    """`blocks` blocks of values zero, as hx_kv_append leaves them (scale 2^-100), and one token of values one
+    under the scale `other` whose score is `shift` powers of two above theirs; it comes first or last."""
+    n = blocks * B
+    scores, values, vs = [0.0] * n, [0.0] * n, [2.0 ** -100] * blocks
+    own = [shift] + [-100.0] * (B - 1)
+    val = [1.0] * B
+    if first:
+        return one_column_cache(own + scores, val + values, D, B, v_scale=[other] + vs)
+    return one_column_cache(scores + own, values + val, D, B, v_scale=vs + [other])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20, 200)), (150, (0, 150))])
+@pytest.mark.parametrize("first", [False, True])
+@pytest.mark.parametrize("other,shift", [(1.0, 7.0), (2.0 ** 20, 7.0), (2.0 ** 20, -3.0), (2.0 ** 60, 9.0), (2.0 ** 110, 0.0), (2.0 ** 110, 26.0)])
+def test_tokens_of_zeros_count_under_any_scale(D, n, max_q, first, other, shift):
+    cache, table = _far(first, other, shift, D)
+    q = two_columns(n, 1, D, torch.bfloat16)
+    check(q, cache, table, [n], [65 * 16], math.log(2), causal=False, max_q=max_q)
+
+
+@pytest.mark.parametrize("n,max_q", [(1, (1,)), (20, (0, 20)), (150, (0,))])
+def test_long_requests_with_scales_far_apart_are_joined(n, max_q):
+    """The same over many blocks of the grid, whose partial results are joined: 20000 tokens of zeros, then values
+    under 2^20 and under 2^-60, and in the middle."""
+    B, D, blocks = 16, 64, 1250
+    rng = np.random.default_rng(n)
+    scores, values = [0.0] * (blocks * B), [0.0] * (blocks * B)
+    vs = [2.0 ** -100] * blocks
+    for b, s, x in ((3, 2.0 ** -60, 9.0), (600, 2.0 ** 20, 7.0), (601, 2.0 ** -100, 11.0), (1249, 2.0 ** 30, -4.0)):
+        vs[b] = s
+        scores[b * B], values[b * B:(b + 1) * B] = x, rng.choice([-1.5, 1.0, 2.0], B).tolist()
+    cache, table = one_column_cache(scores, values, D, B, v_scale=vs)
+    check(two_columns(n, 2, D, torch.bfloat16), cache, table, [n], [blocks * B], math.log(2), causal=False, max_q=max_q)
+
+
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20, 200)), (150, (0, 150))])
+def test_scales_of_every_size_side_by_side(n, max_q):
+    """Every block and head under a power of two from 2^-100 to 2^100, rows that see different ones of them."""
+    g, B, H, D = gen(n), 16, 2, 64
+    kv = [700, 333]
+    table, N = P.paged(g, kv, B)
+    k, v, ks, vs = P.random_cache(g, N, H, B, D)
+    vs.copy_(torch.exp2(torch.randint(-100, 101, vs.shape, generator=g, device="cuda").float()))
+    ks.fill_(2.0 ** -9)
+    q = torch.randn((2 * n, 2 * H, D), generator=g, device="cuda").bfloat16()
+    for window in (0, 40):
+        check(q, KV.Cache(k, v, ks, vs), table, [n, n], kv, D ** -0.5, window=window, max_q=max_q)
