@@ -82,7 +82,9 @@ int hx_kv_map(const hx_kv_map_args* a, void* stream);
 
 /* A cache: k and v [n_blocks][n_kv_heads][block_tokens][head_dim] e4m3, with
  * block_stride bytes from one block to the next; k_scale and v_scale
- * [n_blocks][n_kv_heads], with scale_stride floats from one block to the next. */
+ * [n_blocks][n_kv_heads], with scale_stride floats from one block to the next.  A scale under which
+ * a token sees something is zero or 2^-110 to 2^100; one that is infinite or no number makes what such tokens get
+ * infinite or no number, and that of no other token. */
 typedef struct hx_kv_cache {
   void* k;                    /* 16-byte aligned */
   void* v;                    /* 16-byte aligned */

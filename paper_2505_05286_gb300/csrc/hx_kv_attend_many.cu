@@ -323,12 +323,12 @@ __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uin
       if (!__all_sync(~0u, bar_wait(&sh->raw_empty[v], (it & 1) ^ 1, dead))) return;
       if (v == 0) {
         TileInfo& info = sh->info[it & 7];
-        const float r = fmaxf(vs, 0x1p-100f), lv = log2f(r);
-        const uint32_t who = __ballot_sync(~0u, seen);
+        const float lv = log2f(vs);  // -inf: the values are zeros
+        const uint32_t who = __ballot_sync(~0u, seen && fabsf(lv) < INFINITY);
         if (who && !has_ref) ref = rintf(__shfl_sync(~0u, lv, __ffs(who) - 1)), has_ref = true;
         const bool near = fabsf(lv - ref) <= kNear;
         far |= __any_sync(~0u, seen && !near);
-        if (lane < kGroups) info.g[lane] = float4{ks, lv, near ? exp2f(ref) / r : 1.f, 0.f};
+        if (lane < kGroups) info.g[lane] = float4{ks, lv, near ? exp2f(ref) / vs : 1.f, 0.f};
         if (lane == 0) info.valid = valid | (far ? kFar : 0), sh->ref[item & (kNanLists - 1)] = ref;
         if (last) has_ref = far = false, ++item;
         __syncwarp();
@@ -751,7 +751,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     if (fresh) m = -INFINITY;
     if (!apart && !fresh) ml = m - *ref;
     float up = m - ml, up1 = 0;  // what brings the halves' O there, powers of two
-    bool holds = has && !fresh, holds1 = false;
+    bool holds = has && l != 0, holds1 = false;
     if (kTurns) {
       // the first half's threads join the two; a thread reaches the other half's row in tensor memory, its lane
       if (half) sh->ml[row] = float2{ml, l}, sh->up[row] = (signed char)(holds ? fminf(fmaxf(m - ml, -127.f), 127.f) : -128.f);

@@ -182,3 +182,41 @@ def test_scales_of_every_size_side_by_side(n, max_q):
     q = torch.randn((2 * n, 2 * H, D), generator=g, device="cuda").bfloat16()
     for window in (0, 40):
         check(q, KV.Cache(k, v, ks, vs), table, [n, n], kv, D ** -0.5, window=window, max_q=max_q)
+
+
+# ---- scales that are small, zero or no numbers
+
+@pytest.mark.parametrize("scale", [math.nan, math.inf, 2.0 ** 100])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,group,max_q", [(4, 4, (0,)), (20, 3, (20, 0, 100))])
+@pytest.mark.parametrize("edge", ["first", "last"])
+def test_a_value_scale_reaches_the_many_rows_that_see_its_block(scale, D, n, group, max_q, edge):
+    _one_block(scale, D, n, group, max_q, edge)
+
+
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20, 200)), (150, (0, 150))])
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -110, 3 * 2.0 ** -108, 2.0 ** -101])
+def test_small_value_scales_are_followed(n, max_q, scale):
+    """The whole cache under one small scale, and one block under it beside ordinary ones."""
+    g, B, D = gen(n), 16, 64
+    kv = [260]
+    table, N = P.paged(g, kv, B)
+    k, v, ks, vs = P.random_cache(g, N, 1, B, D)
+    q = torch.randn((n, 3, D), generator=g, device="cuda").bfloat16()
+    one = vs.clone()
+    one[table[0, 4].long()] = scale
+    for s in (torch.full_like(vs, scale), one):
+        check(q, KV.Cache(k, v, ks, s), table, [n], kv, D ** -0.5, max_q=max_q)
+
+
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20, 200)), (150, (0, 150))])
+@pytest.mark.parametrize("scale", [math.nan, math.inf])
+def test_a_request_whose_scales_are_all_no_numbers(n, max_q, scale):
+    g, B, D = gen(n), 16, 64
+    kv = [100]
+    table, N = P.paged(g, kv, B)
+    k, v, ks, vs = P.random_cache(g, N, 1, B, D)
+    b = v.view(torch.uint8)
+    b[(b & 0x7f) == 0] = 0x38
+    q = torch.randn((n, 3, D), generator=g, device="cuda").bfloat16()
+    check(q, KV.Cache(k, v, ks, torch.full_like(vs, scale)), table, [n], kv, D ** -0.5, max_q=max_q)
