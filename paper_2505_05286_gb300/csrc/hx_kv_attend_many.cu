@@ -750,6 +750,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     // (what has seen nothing has not waited for ref either)
     if (fresh) m = -INFINITY;
     if (!apart && !fresh) ml = m - *ref;
+    if (l == INFINITY) l = NAN;  // of an infinite score: exp(inf - inf), and not 1 / inf
     float up = m - ml, up1 = 0;  // what brings the halves' O there, powers of two
     bool holds = has && l != 0, holds1 = false;
     if (kTurns) {

@@ -220,3 +220,22 @@ def test_a_request_whose_scales_are_all_no_numbers(n, max_q, scale):
     b[(b & 0x7f) == 0] = 0x38
     q = torch.randn((n, 3, D), generator=g, device="cuda").bfloat16()
     check(q, KV.Cache(k, v, ks, torch.full_like(vs, scale)), table, [n], kv, D ** -0.5, max_q=max_q)
+
+
+# ---- infinite scores
+
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20, 200)), (90, (0, 90))])
+@pytest.mark.parametrize("kv", [100, 300, 5000])
+def test_infinite_scores_give_no_number(n, max_q, kv):
+    """exp(inf - inf) is no number: not zeros, which is what a token that sees nothing gets."""
+    D, B = 64, 16
+    cache, table = one_column_cache([1.0] * kv, [1.0] * kv, D, B)
+    q = torch.zeros((n, 4, D), dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 1
+    q[n // 2, 1, 0] = math.inf
+    for mq in max_q:
+        got, lse = cache.attend(q, table, i32([0, n]), i32([kv]), max_q=mq, return_lse=True)
+        want = torch.zeros_like(got, dtype=torch.bool)
+        want[n // 2, 1] = True
+        assert torch.equal(torch.isnan(got), want)
+        assert not bool(torch.isfinite(lse[n // 2, 1])) and int((~torch.isfinite(lse)).sum()) == 1
