@@ -143,6 +143,8 @@ typedef struct hx_kv_query {
   float sm_scale;             /* factor of q.k */
   void* workspace;            /* 32-byte aligned, hx_kv_attend_workspace() bytes; used until the kernels end */
   int64_t workspace_bytes;
+  int32_t* status;            /* one int in memory that the device can write (host memory mapped for it, or its own), or
+                                 NULL: set to 1 if a wait inside a kernel ran out, and never to 0 */
 } hx_kv_query;
 
 /* Bytes of workspace that hx_kv_attend needs for these queries. */
@@ -151,7 +153,8 @@ int hx_kv_attend_workspace(const hx_kv_cache* c, const hx_kv_query* a, int64_t* 
 /* out = softmax(sm_scale * q k^T) v over the positions that each token sees.  A token that sees
  * nothing gets zeros and lse = -inf; so do tokens that no row owns.  Positions past kv_len, in blocks
  * whose number is out of range, or masked take no part, whatever the cache holds there.  A row with more than
- * max_q > 0 tokens gets zeros. */
+ * max_q > 0 tokens gets zeros.  The kernels' waits on their own copies and products are bounded, by about two
+ * seconds: a block whose wait runs out leaves NaN in what it had left to compute, and *status says so. */
 int hx_kv_attend(const hx_kv_cache* c, const hx_kv_query* a, void* stream);
 
 #ifdef __cplusplus

@@ -48,6 +48,7 @@ int check_query(const hx_kv_cache* c, const hx_kv_query* a) {
   if (a->causal != 0 && a->causal != 1) return bad("queries: causal must be 0 or 1");
   if (a->window < 0) return bad("queries: window is negative");
   if (!std::isfinite(a->sm_scale)) return bad("queries: sm_scale is not finite");
+  if (!aligned(a->status, 4)) return bad("queries: status must be 4-byte aligned");
   return HX_OK;
 }
 

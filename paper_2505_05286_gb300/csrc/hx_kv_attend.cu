@@ -354,7 +354,8 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       m[r][0] = m[r][1] = -INFINITY, l[r][0] = l[r][1] = 0;
     }
     for (; left < seg; left += W) {
-      bool ok = landed(2 * stage);
+      // (a place whose tile has not been waited for to its end must not be filled again)
+      const bool keys = landed(2 * stage);
       const uint8_t* kt = ring + stage * kStageBytes;
       const uint8_t* vt = kt + kTileBytes;
       const Tile& key_tile = tiles[0][(it + left) & (kTiles - 1)];
@@ -410,11 +411,10 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       }
       fence_async();
       __syncwarp();
-      if (lane == 0) bar_arrive(&empty[2 * stage]);
+      if (lane == 0 && keys) bar_arrive(&empty[2 * stage]);
       // values of tokens ta, tb, ta + 8, tb + 8 of each group, D / 8 columns each: on their way while the
       // softmax is done, and their place free again
-      ok &= landed(2 * stage + 1);
-      if (!ok) l[0][0] = l[0][1] = l[NR - 1][0] = l[NR - 1][1] = NAN;
+      const bool values = landed(2 * stage + 1);
       uint32_t vw[S::kGroups][4][D / 32];
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g)
@@ -430,7 +430,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       for (int g = 0; g < S::kGroups; ++g) value_scale[g] = value_tile.scale[g];
       fence_async();
       __syncwarp();
-      if (lane == 0) bar_arrive(&empty[2 * stage + 1]);
+      if (lane == 0 && values) bar_arrive(&empty[2 * stage + 1]);
       bool late = false;
 #pragma unroll
       for (int r = 0; r < NR; ++r) late |= top[r][0] > m[r][0] + kLag || top[r][1] > m[r][1] + kLag;
@@ -577,6 +577,10 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       if (stage >= S::kStages) stage -= S::kStages, ++turn;
     }
     left -= seg;
+    if (__any_sync(~0u, *dead)) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) l[r][0] = l[r][1] = NAN;
+    }
 
     // the warps' results as one
     float part[NR][2];
@@ -785,7 +789,7 @@ __global__ void __launch_bounds__(Shape<D, NR>::kThreads, 2)
     produce<D, NR, 1>(a, &vm, at, count, ring, s_tiles[1], s_full, s_empty, &s_dead);
   else
     consume<D, NR, T>(a, at, count, ring, s_tiles, s_full, s_empty, &s_dead, merge, s_ml);
-  drain(&s_dead);
+  drain(&s_dead, a.status);
 }
 
 // Joins an item's partial results: block (e, y) rows 16 y and on of the item that ends in stretch e.
@@ -978,6 +982,7 @@ AttendArgs args_of(const hx_kv_cache& c, const hx_kv_query& q) {
   a.window = q.window >= (1 << 30) ? 0 : q.window;  // no request holds so many tokens
   a.out_by_32 = (((uintptr_t)q.out | 2 * (uintptr_t)q.out_token_stride | 2 * (uintptr_t)q.out_head_stride) & 31) == 0;
   a.sm_scale_log2 = q.sm_scale * kLog2e;
+  a.status = q.status;
   return a;
 }
 

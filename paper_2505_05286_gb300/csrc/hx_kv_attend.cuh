@@ -56,6 +56,7 @@ struct AttendArgs {
   float* part_ml;
   int4* joins;          // [blocks] of the item that ends in the block's stretch: its first token, its tokens, the block where
                         // it begins (-1: nothing to join), its kv head
+  int32_t* status;      // set to 1 if a wait gives up, or NULL
 };
 
 // Launches the many-rows kernel (hx_kv_attend_many.cu) on `blocks` blocks.
@@ -85,10 +86,25 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
       : "memory");
   return ok;
 }
-// Waits for a phase, but not for ever: after kWaitCycles (about two seconds) it gives up, says
-// so in *dead, and from then on no wait of the block waits.
-constexpr long long kWaitCycles = 4000000000LL;
+// Waits for a phase, but not for ever: after kWaitCycles (about two seconds; 0: a phase that is not over yet is not
+// waited for) it gives up, says so in *dead, and from then on no wait of the block waits.  What a warp has computed stands only if
+// *dead is still 0 behind its last wait: whoever gives up says so before it arrives anywhere.  And a barrier that bytes may
+// still be due at is not armed again: nobody arrives where that would be asked for.
+#ifndef HX_KV_WAIT_CYCLES
+#define HX_KV_WAIT_CYCLES 4000000000LL
+#endif
+constexpr long long kWaitCycles = HX_KV_WAIT_CYCLES;
 __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead) {
+  if constexpr (kWaitCycles == 0) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(smem_addr(b)), "r"(parity)
+        : "memory");
+    if (!ok) *dead = 1;
+    return ok;
+  }
   if (bar_try(b, parity)) return true;
   const long long t0 = clock64();
   do {
@@ -99,9 +115,10 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
   *dead = 1;
   return false;
 }
-// Before a block that gave up ends: time for its own copies in flight to land.
-__device__ __forceinline__ void drain(volatile int* dead) {
+// Before a block that gave up ends: says so to the caller, and leaves its own copies in flight the time to land.
+__device__ __forceinline__ void drain(volatile int* dead, int32_t* status) {
   if (!*dead) return;
+  if (status) *status = 1;
   const long long t0 = clock64();
   while (clock64() - t0 < 20000000LL) __nanosleep(1000);
 }

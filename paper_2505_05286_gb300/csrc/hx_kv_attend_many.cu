@@ -374,13 +374,13 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, c
     return h;
   };
   const auto take = [&](int v, uint2* u) {
-    bar_wait(&sh->raw_full[v], it & 1, dead);
+    const bool landed = bar_wait(&sh->raw_full[v], it & 1, dead);
     const uint8_t* from = raw + v * Many<D>::kRaw + (32 * warp + sub) * D + unit * 8;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) u[j] = *(const uint2*)(from + j * kPer * D);
     fence_async();
     __syncwarp();
-    if (lane == 0) bar_arrive(&sh->raw_empty[v]);
+    if (lane == 0 && landed) bar_arrive(&sh->raw_empty[v]);  // else its copy may be on its way still
   };
   HX_SEGMENTS(s, count) {
     if (s.empty) continue;
@@ -434,6 +434,7 @@ __device__ void convert(const AttendArgs& a, Segment s, int count, Shared* sh, c
 template <int D, bool kTurns>
 __device__ void queries(const AttendArgs& a, const CUtensorMap* qm, Segment s, int count, Shared* sh, uint8_t* qbuf) {
   const uint32_t bytes = (uint32_t)(a.half_tokens * a.group) * D * 2;
+  volatile int* dead = &sh->dead;
   int seg_no = 0;
   HX_SEGMENTS(s, count) {
     if (s.empty) continue;
@@ -444,7 +445,7 @@ __device__ void queries(const AttendArgs& a, const CUtensorMap* qm, Segment s, i
     }
     for (int half = 0; half < 2; ++half) {
       const int token = s.q.first + s.i0 + (kTurns ? 0 : half * a.half_tokens);
-      if (!bar_wait(&sh->q_empty[half], (seg_no & 1) ^ 1, &sh->dead)) return;
+      if (!bar_wait(&sh->q_empty[half], (seg_no & 1) ^ 1, dead) || *dead) return;
       bar_expect(&sh->q_full[half], bytes);
 #pragma unroll
       for (int x = 0; x < D; x += 64)
@@ -627,7 +628,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       if (!active<kTurns>(s, half, tile)) continue;
       const int pos = tile * kKv;
       const TileInfo& info = sh->info[it & 7];
-      if (!bar_wait(&sh->s_full[half], n_s & 1, dead)) l = NAN;
+      bar_wait(&sh->s_full[half], n_s & 1, dead);
       tc_fence_after();
       const uint32_t valid = info.valid;
       if ((valid & kFar) && !apart) {
@@ -743,13 +744,14 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     }
 
     if (has) {
-      if (!bar_wait(&sh->o_full[half], (n_s - 1) & 1, dead)) l = NAN;
+      bar_wait(&sh->o_full[half], (n_s - 1) & 1, dead);
       tc_fence_after();
     }
     // O is in units of 2^m, l in units of 2^ml: so is what is stored of both
     // (what has seen nothing has not waited for ref either)
     if (fresh) m = -INFINITY;
     if (!apart && !fresh) ml = m - *ref;
+    if (*dead) l = NAN;          // a wait gave up: what has been computed does not stand
     if (l == INFINITY) l = NAN;  // of an infinite score: exp(inf - inf), and not 1 / inf
     float up = m - ml, up1 = 0;  // what brings the halves' O there, powers of two
     bool holds = has && l != 0, holds1 = false;
@@ -779,6 +781,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     const int64_t slot = 2 * blockIdx.x + (s.t == 0);
     float* part = a.part + (slot * kItemRows + half * kHalf + row) * D;
     const bool none = l == 0;
+    const float nothing = l == l ? 0.f : NAN;
     const float inv = done ? (none ? 0.f : 1.f / l) : 1.f;
     const auto factor = [&](float up) {  // 2^up * inv, in two steps: 2^up alone may leave the range
       up = fminf(fmaxf(up, -252.f), 252.f);
@@ -791,7 +794,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       uint32_t u[32];
       tm_load(to + ch, u);
 #pragma unroll
-      for (int y = 0; y < 32; ++y) u[y] = holds ? __float_as_uint(__uint_as_float(u[y]) * by) : 0;
+      for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(holds ? __uint_as_float(u[y]) * by : nothing);
       if (kTurns) {
         uint32_t w[32];
         tm_load(to + D + ch, w);
@@ -974,7 +977,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) hx_kv_attend_many(
   else if (warp == kFetchWarp) fetch<D, kTurns>(a, s, count, &sh, raw);
   else if (lane == 0) queries<D, kTurns>(a, &qm, s, count, &sh, qbuf);
   __syncwarp();
-  drain(&sh.dead);
+  drain(&sh.dead, a.status);
   tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp)

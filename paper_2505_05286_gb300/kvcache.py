@@ -51,7 +51,7 @@ class hx_kv_query(ctypes.Structure):
                [(n, _i32) for n in ("n_tokens", "n_heads", "dtype", "n_rows")] + \
                [(n, _vp) for n in ("row_start", "kv_len", "block_table")] + \
                [("table_stride", _i64)] + [(n, _i32) for n in ("table_width", "max_q", "causal", "window")] + \
-               [("sm_scale", ctypes.c_float), ("workspace", _vp), ("workspace_bytes", _i64)]
+               [("sm_scale", ctypes.c_float), ("workspace", _vp), ("workspace_bytes", _i64), ("status", _vp)]
 
 
 _lib = None
@@ -252,6 +252,8 @@ class Cache:
                                   dim)
         self._ref = ctypes.byref(self.struct)
         self._work = {}  # workspaces by stream: calls on one stream follow one another
+        # in host memory that the kernels write to: it holds its zero without any stream's doing
+        self._status = torch.zeros(1, dtype=torch.int32, pin_memory=True)
         self.lib = load()
 
     @staticmethod
@@ -261,6 +263,12 @@ class Cache:
         k, v = (torch.empty(shape, dtype=torch.float8_e4m3fn, device=device) for _ in range(2))
         ks, vs = (torch.empty(shape[:2], dtype=torch.float32, device=device) for _ in range(2))
         return Cache(k, v, ks, vs)
+
+    def check(self) -> None:
+        """Raise if a wait inside a kernel of an `attend` ran out, whose tokens then hold NaN.  Of calls whose work is
+        done: synchronize with their stream first."""
+        if self._status.item():
+            raise H.HxError(H.HX_ERR_CUDA, "attend: a wait inside a kernel ran out; results hold NaN")
 
     def append(self, k, v, runs, stream=None) -> None:
         """Write a step's keys and values, [tokens, kv heads, head dim] in bf16, f16 or f32 (tokens and heads may be
@@ -318,7 +326,7 @@ class Cache:
                             q.stride(1), out.stride(0), out.stride(1), T, heads, kinds.index(q.dtype), n,
                             row_start.data_ptr(), kv_len.data_ptr(), block_table.data_ptr(),
                             block_table.stride(0) if n > 1 else block_table.shape[1], block_table.shape[1], max_q,
-                            1 if causal else 0, window, dim ** -0.5 if sm_scale is None else sm_scale, None, 0)
+                            1 if causal else 0, window, dim ** -0.5 if sm_scale is None else sm_scale, None, 0, self._status.data_ptr())
             ref = ctypes.byref(a)
             if workspace is None:
                 need = ctypes.c_int64()

@@ -167,3 +167,10 @@ def test_plain_e4m3_agrees_with_the_type():
     x = np.concatenate([x, mid, -mid, P._POS]).astype(np.float32)
     t = torch.from_numpy(x).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
     assert np.array_equal(P.to_e4m3(x), t)
+
+
+def test_attend_status_refused_where_it_cannot_be_written(lib):
+    c = _cache()
+    q = KV.hx_kv_query(FAKE, FAKE, None, 512, 64, 512, 64, 10, 8, KV.HX_F16, 3, FAKE, FAKE, FAKE, 4, 4, 1, 1, 0, 0.125,
+                       FAKE, 1 << 40)
+    _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(_set(q, status=FAKE + 2)), None), "status")
