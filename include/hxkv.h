@@ -141,7 +141,8 @@ typedef struct hx_kv_query {
   int32_t causal;             /* 1: a token sees what is before it and itself; 0: all that its row holds */
   int32_t window;             /* > 0: and of those only positions above its own - window */
   float sm_scale;             /* factor of q.k */
-  void* workspace;            /* 32-byte aligned, hx_kv_attend_workspace() bytes; used until the kernels end */
+  void* workspace;            /* 32-byte aligned, hx_kv_attend_workspace() bytes; used until the kernels end: a call hands partial
+                                 results on through it, so another call may use it only behind all of this one's launches, on the same stream */
   int64_t workspace_bytes;
   int32_t* status;            /* one int in memory that the device can write (host memory mapped for it, or its own), or
                                  NULL: set to 1 if a wait inside a kernel ran out, and never to 0 */

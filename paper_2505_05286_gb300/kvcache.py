@@ -14,6 +14,7 @@ the kernels are done, as for any asynchronous call.
 from __future__ import annotations
 
 import ctypes
+import threading
 from dataclasses import dataclass
 from typing import Optional
 
@@ -251,7 +252,8 @@ class Cache:
                                   k.stride(0) if N > 1 else whole, k_scale.stride(0) if N > 1 else heads, N, heads, block,
                                   dim)
         self._ref = ctypes.byref(self.struct)
-        self._work = {}  # workspaces by stream: calls on one stream follow one another
+        self._work = {}  # workspaces by stream: calls on one stream follow one another,
+        self._turn = threading.Lock()  # and all launches of one call those of another, whatever threads they are from
         # in host memory that the kernels write to: it holds its zero without any stream's doing
         self._status = torch.zeros(1, dtype=torch.int32, pin_memory=True)
         self.lib = load()
@@ -296,7 +298,8 @@ class Cache:
         max_q       the most tokens that a row has in this step, if the scheduler knows it (1: every row
                     decodes; fewer kernels run), 0 if not
         sm_scale    default head dim ** -0.5
-        workspace   uint8 tensor to use instead of the one that the cache keeps for each stream
+        workspace   uint8 tensor to use instead of the one that the cache keeps for each stream (not by calls
+                    on another cache at the same time)
 
         Returns out, or (out, lse) with lse float32 [tokens, heads].
         """
@@ -328,17 +331,18 @@ class Cache:
                             block_table.stride(0) if n > 1 else block_table.shape[1], block_table.shape[1], max_q,
                             1 if causal else 0, window, dim ** -0.5 if sm_scale is None else sm_scale, None, 0, self._status.data_ptr())
             ref = ctypes.byref(a)
-            if workspace is None:
-                need = ctypes.c_int64()
-                H._check(self.lib, self.lib.hx_kv_attend_workspace(self._ref, ref, ctypes.byref(need)))
-                graph = torch.cuda.is_current_stream_capturing()  # a graph has a workspace of its own
-                workspace = None if graph else self._work.get(handle)
-                if workspace is None or workspace.numel() < need.value:
-                    workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-                    if not graph:
-                        self._work[handle] = workspace
-            else:
+            if workspace is not None:
                 _dense(workspace, "workspace", (torch.uint8,), 1, dev)
-            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-            H._check(self.lib, self.lib.hx_kv_attend(self._ref, ref, handle))
+            with self._turn:
+                if workspace is None:
+                    need = ctypes.c_int64()
+                    H._check(self.lib, self.lib.hx_kv_attend_workspace(self._ref, ref, ctypes.byref(need)))
+                    graph = torch.cuda.is_current_stream_capturing()  # a graph has a workspace of its own
+                    workspace = None if graph else self._work.get(handle)
+                    if workspace is None or workspace.numel() < need.value:
+                        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+                        if not graph:
+                            self._work[handle] = workspace
+                a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+                H._check(self.lib, self.lib.hx_kv_attend(self._ref, ref, handle))
         return (out, lse) if return_lse else out

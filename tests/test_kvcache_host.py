@@ -4,6 +4,7 @@ import ctypes
 import os
 import re
 import subprocess
+import threading
 
 import numpy as np
 import pytest
@@ -174,3 +175,57 @@ def test_attend_status_refused_where_it_cannot_be_written(lib):
     q = KV.hx_kv_query(FAKE, FAKE, None, 512, 64, 512, 64, 10, 8, KV.HX_F16, 3, FAKE, FAKE, FAKE, 4, 4, 1, 1, 0, 0.125,
                        FAKE, 1 << 40)
     _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(_set(q, status=FAKE + 2)), None), "status")
+
+
+class _Interleaved:
+    """Stands in for the library: notes which workspaces are in use by calls that have not returned."""
+
+    def __init__(self):
+        self.gate, self.busy, self.clash = threading.Barrier(2), [], False
+
+    def hx_kv_attend_workspace(self, cache, query, need):
+        need._obj.value = 64
+        return H.HX_OK
+
+    def hx_kv_attend(self, cache, query, stream):
+        work = query._obj.workspace
+        self.clash |= work in self.busy
+        self.busy.append(work)
+        try:  # the launches of one call take a while; the other thread comes in here if nothing holds it
+            self.gate.wait(0.5)
+        except threading.BrokenBarrierError:
+            pass
+        self.busy.remove(work)
+        return H.HX_OK
+
+
+def test_calls_of_two_threads_do_not_share_a_workspace_at_a_time(monkeypatch):
+    """A call's kernels hand partial results on through its workspace: launches of two calls on one stream must not
+    alternate."""
+    class On:
+        def __enter__(self):
+            return 0
+
+        def __exit__(self, *exc):
+            pass
+
+    monkeypatch.setattr(KV, "_want", lambda *a: None)
+    monkeypatch.setattr(KV, "_dense", lambda *a: None)
+    monkeypatch.setattr(KV, "_on", lambda *a: On())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    fake = _Interleaved()
+    monkeypatch.setattr(KV, "load", lambda: fake)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: empty(*a, **{k: v for k, v in kw.items() if k != "device"}))
+    zeros = torch.zeros
+    monkeypatch.setattr(torch, "zeros", lambda *a, **kw: zeros(*a, **{k: v for k, v in kw.items() if k != "pin_memory"}))
+    f = empty((2, 1, 16, 64), dtype=torch.uint8).view(torch.float8_e4m3fn)
+    cache = KV.Cache(f, f.clone(), torch.ones(2, 1), torch.ones(2, 1))
+    q, i32 = empty((1, 2, 64), dtype=torch.float16), torch.int32
+    args = (q, zeros((1, 2), dtype=i32), zeros(2, dtype=i32), zeros(1, dtype=i32))
+    threads = [threading.Thread(target=cache.attend, args=args) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not fake.clash
