@@ -72,7 +72,7 @@ int hx_kv_map(const hx_kv_map_args* a, void* stream) {
   if (a->table_stride < a->table_width) return bad("map: table_stride is less than table_width");
   if (a->n_runs < hx_kv_max_runs(a->n_rows, a->n_tokens, a->block_tokens)) return bad("map: n_runs is too small");
   if (!a->held || !a->add || !a->block_table || !a->ring || !a->ring_state || !a->row_start || !a->kv_len ||
-      !a->counts || !a->ring_state_out || (a->n_tokens && (!a->slots || !a->runs)))
+      !a->counts || !a->ring_state_out || (a->n_tokens && !a->slots) || (a->n_runs && !a->runs))
     return bad("map: NULL pointer");
   if (a->ring_state == a->ring_state_out) return bad("map: ring_state_out must not be ring_state");
   if (!aligned(a->runs) || !aligned(a->counts)) return bad("map: runs and counts must be 16-byte aligned");

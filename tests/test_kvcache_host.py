@@ -229,3 +229,15 @@ def test_calls_of_two_threads_do_not_share_a_workspace_at_a_time(monkeypatch):
     for t in threads:
         t.join()
     assert not fake.clash
+
+
+def _map_args(**kw):
+    """Arguments of a map call with every array at an address of its own."""
+    a = KV.hx_kv_map_args(3, 10, 32, 8, 4, 6, 4, *[FAKE + 4096 * i for i in range(11)])
+    return _set(a, **kw)
+
+
+def test_map_refuses_runs_without_an_array(lib):
+    """Runs are cleared up to their length even where the step has no tokens."""
+    for kw in (dict(n_tokens=0, runs=None), dict(n_tokens=0, n_runs=1, runs=None, slots=None), dict(runs=None)):
+        _refused(lib, lib.hx_kv_map(ctypes.byref(_map_args(**kw)), None), "NULL")
