@@ -76,6 +76,10 @@ int hx_kv_map(const hx_kv_map_args* a, void* stream) {
     return bad("map: NULL pointer");
   if (a->ring_state == a->ring_state_out) return bad("map: ring_state_out must not be ring_state");
   if (!aligned(a->runs) || !aligned(a->counts)) return bad("map: runs and counts must be 16-byte aligned");
+  if (!aligned(a->held, 4) || !aligned(a->add, 4) || !aligned(a->block_table, 4) || !aligned(a->ring, 4) ||
+      !aligned(a->row_start, 4) || !aligned(a->kv_len, 4) || !aligned(a->ring_state, 8) || !aligned(a->ring_state_out, 8) ||
+      !aligned(a->slots, 8))
+    return bad("map: an array is not aligned to its type");
   return launched(hx::launch_kv_map(*a, (cudaStream_t)stream), "map");
 }
 
@@ -109,6 +113,8 @@ int hx_kv_attend(const hx_kv_cache* c, const hx_kv_query* a, void* stream) {
   if (a->table_width < 1 || a->table_width > (1 << 23)) return bad("queries: table_width must be 1..2^23");
   if (a->table_stride < a->table_width) return bad("queries: table_stride is less than table_width");
   if (!aligned(a->q) || !aligned(a->out)) return bad("queries: q and out must be 16-byte aligned");
+  if (!aligned(a->lse, 4) || !aligned(a->row_start, 4) || !aligned(a->kv_len, 4) || !aligned(a->block_table, 4))
+    return bad("queries: lse, row_start, kv_len and block_table must be 4-byte aligned");
   if (a->q_token_stride % 8 || a->q_head_stride % 8 || a->out_token_stride % 8 || a->out_head_stride % 8)
     return bad("queries: strides must be multiples of 8 elements");
   if (a->q_token_stride < 0 || a->q_head_stride < 0 || a->q_token_stride >= (int64_t)1 << 38 || a->q_head_stride >= (int64_t)1 << 38)

@@ -241,3 +241,23 @@ def test_map_refuses_runs_without_an_array(lib):
     """Runs are cleared up to their length even where the step has no tokens."""
     for kw in (dict(n_tokens=0, runs=None), dict(n_tokens=0, n_runs=1, runs=None, slots=None), dict(runs=None)):
         _refused(lib, lib.hx_kv_map(ctypes.byref(_map_args(**kw)), None), "NULL")
+
+
+@pytest.mark.parametrize("name", ["held", "add", "block_table", "ring", "row_start", "kv_len"])
+def test_map_refuses_misaligned_ints(lib, name):
+    a = _map_args()
+    _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, **{name: getattr(a, name) + 2})), None), "aligned")
+
+
+@pytest.mark.parametrize("name", ["ring_state", "ring_state_out", "slots"])
+def test_map_refuses_misaligned_long_ints(lib, name):
+    a = _map_args()
+    _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, **{name: getattr(a, name) + 4})), None), "aligned")
+
+
+@pytest.mark.parametrize("name", ["lse", "row_start", "kv_len", "block_table"])
+def test_attend_refuses_misaligned_arrays(lib, name):
+    q = KV.hx_kv_query(FAKE, FAKE, None, 512, 64, 512, 64, 10, 8, KV.HX_F16, 3, FAKE, FAKE, FAKE, 4, 4, 1, 1, 0, 0.125,
+                       FAKE, 1 << 40)
+    c = _cache()
+    _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(_set(q, **{name: FAKE + 2})), None), "aligned")
