@@ -76,7 +76,7 @@ typedef struct hx_kv_map_args {
 /* The runs that n_tokens of n_rows requests can give at most. */
 int64_t hx_kv_max_runs(int32_t n_rows, int32_t n_tokens, int32_t block_tokens);
 
-/* Build the tables of one step.  The same inputs give the same tables, also when the
+/* Build the tables of one step.  Outputs may not overlap what is read (held may not be this step's kv_len).  The same inputs give the same tables, also when the
  * call is repeated on the table and ring that it has changed. */
 int hx_kv_map(const hx_kv_map_args* a, void* stream);
 

@@ -17,6 +17,14 @@ int launched(cudaError_t e, const char* what) {
 }
 
 bool aligned(const void* p, uintptr_t n = 16) { return ((uintptr_t)p & (n - 1)) == 0; }
+struct Range {
+  const void* p;
+  int64_t bytes;
+};
+bool overlap(const Range& x, const Range& y) {
+  const uintptr_t a = (uintptr_t)x.p, b = (uintptr_t)y.p;
+  return x.bytes > 0 && y.bytes > 0 && (a < b ? b - a < (uint64_t)x.bytes : a - b < (uint64_t)y.bytes);
+}
 bool block_size(int b) { return b == 16 || b == 32 || b == 64 || b == 128; }
 
 int check_cache(const hx_kv_cache* c) {
@@ -80,6 +88,14 @@ int hx_kv_map(const hx_kv_map_args* a, void* stream) {
       !aligned(a->row_start, 4) || !aligned(a->kv_len, 4) || !aligned(a->ring_state, 8) || !aligned(a->ring_state_out, 8) ||
       !aligned(a->slots, 8))
     return bad("map: an array is not aligned to its type");
+  const int64_t n = a->n_rows;
+  const Range in[] = {{a->held, 4 * n}, {a->add, 4 * n}, {a->ring_state, 16}, {a->ring, 4 * (int64_t)a->n_blocks},
+                      {a->block_table, 4 * ((n - 1) * a->table_stride + a->table_width)}};
+  const Range out[] = {{a->row_start, 4 * (n + 1)}, {a->kv_len, 4 * n}, {a->slots, 8 * (int64_t)a->n_tokens},
+                       {a->runs, 16 * (int64_t)a->n_runs}, {a->counts, 16}, {a->ring_state_out, 16}};
+  for (const Range& x : in)
+    for (const Range& y : out)
+      if (overlap(x, y)) return bad("map: an output overlaps the lengths, the table or the ring");
   return launched(hx::launch_kv_map(*a, (cudaStream_t)stream), "map");
 }
 

@@ -182,7 +182,7 @@ def map_step(held, add, block_table, ring, ring_state, n_tokens: int, block_toke
     ring, ring_state  int32 [blocks], int64 [2]: the free blocks and (first, count); ended rows' blocks are
                 entered in the ring, the new state is in the result
     n_tokens    the step's tokens, sum(max(add, 0)), known to the scheduler
-    out         a Step to write to instead of a new one (not the one whose ring_state is passed in)
+    out         a Step to write to instead of a new one (not the one whose ring_state or kv_len is passed in)
     """
     i32, i64 = (torch.int32,), (torch.int64,)
     dev = held.get_device()

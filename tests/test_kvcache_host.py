@@ -261,3 +261,15 @@ def test_attend_refuses_misaligned_arrays(lib, name):
                        FAKE, 1 << 40)
     c = _cache()
     _refused(lib, lib.hx_kv_attend(ctypes.byref(c), ctypes.byref(_set(q, **{name: FAKE + 2})), None), "aligned")
+
+
+@pytest.mark.parametrize("out,into", [("kv_len", "held"), ("kv_len", "add"), ("row_start", "held"), ("slots", "add"),
+                                      ("runs", "ring"), ("counts", "ring_state"), ("ring_state_out", "held"),
+                                      ("kv_len", "block_table")])
+def test_map_refuses_to_write_over_what_it_reads(lib, out, into):
+    """Blocks of threads read all lengths while others already write theirs."""
+    a = _map_args()
+    _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, **{out: getattr(a, into)})), None), "overlap")
+    if (out, into) == ("kv_len", "held"):  # its last entry only
+        _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, kv_len=a.held + 8)), None), "overlap")
+        _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, kv_len=a.held - 8)), None), "overlap")
