@@ -89,13 +89,18 @@ int hx_kv_map(const hx_kv_map_args* a, void* stream) {
       !aligned(a->slots, 8))
     return bad("map: an array is not aligned to its type");
   const int64_t n = a->n_rows;
-  const Range in[] = {{a->held, 4 * n}, {a->add, 4 * n}, {a->ring_state, 16}, {a->ring, 4 * (int64_t)a->n_blocks},
-                      {a->block_table, 4 * ((n - 1) * a->table_stride + a->table_width)}};
+  const Range lengths[] = {{a->held, 4 * n}, {a->add, 4 * n}, {a->ring_state, 16}, {a->ring, 4 * (int64_t)a->n_blocks}};
   const Range out[] = {{a->row_start, 4 * (n + 1)}, {a->kv_len, 4 * n}, {a->slots, 8 * (int64_t)a->n_tokens},
                        {a->runs, 16 * (int64_t)a->n_runs}, {a->counts, 16}, {a->ring_state_out, 16}};
-  for (const Range& x : in)
-    for (const Range& y : out)
-      if (overlap(x, y)) return bad("map: an output overlaps the lengths, the table or the ring");
+  const Range table = {a->block_table, 4 * ((n - 1) * a->table_stride + a->table_width)};
+  for (const Range& y : out) {
+    for (const Range& x : lengths)
+      if (overlap(x, y)) return bad("map: an output overlaps held, add, ring or ring_state");
+    if (!overlap(table, y)) continue;
+    for (int64_t r = 0; r < n; ++r)  // its rows; what lies between them may be anything
+      if (overlap({a->block_table + r * a->table_stride, 4 * (int64_t)a->table_width}, y))
+        return bad("map: an output overlaps block_table");
+  }
   return launched(hx::launch_kv_map(*a, (cudaStream_t)stream), "map");
 }
 

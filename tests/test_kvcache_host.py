@@ -273,3 +273,12 @@ def test_map_refuses_to_write_over_what_it_reads(lib, out, into):
     if (out, into) == ("kv_len", "held"):  # its last entry only
         _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, kv_len=a.held + 8)), None), "overlap")
         _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, kv_len=a.held - 8)), None), "overlap")
+
+
+def test_map_lets_outputs_lie_between_the_rows_of_a_table(lib):
+    """A strided table's rows are what may not be written over, not what lies between them."""
+    a = _map_args(table_stride=64)
+    gap = a.block_table + 4 * 16
+    row = a.block_table + 4 * 64
+    _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, counts=gap, kv_len=row + 12)), None), "overlap")
+    _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, row_start=row + 16, kv_len=a.held)), None), "held")
