@@ -94,6 +94,12 @@ def _dense(x, name: str, dtypes, ndim: int, device: int):
         _fail(f"{name} must be contiguous")
 
 
+def _count(x: int, name: str, least: int = 0):
+    """Check a whole number that goes into an int32: ctypes would cut off what does not fit."""
+    if not least <= x < 1 << 31:
+        _fail(f"{name} must be {least}..2^31-1")
+
+
 class _On:
     """The device and stream of a call that names a stream, or tensors of another device than the
     current one: kernels go there, and so does what the binding allocates."""
@@ -184,6 +190,8 @@ def map_step(held, add, block_table, ring, ring_state, n_tokens: int, block_toke
     n_tokens    the step's tokens, sum(max(add, 0)), known to the scheduler
     out         a Step to write to instead of a new one (not the one whose ring_state or kv_len is passed in)
     """
+    _count(n_tokens, "map: n_tokens")
+    _count(block_tokens, "map: block_tokens", 1)
     i32, i64 = (torch.int32,), (torch.int64,)
     dev = held.get_device()
     _dense(held, "held", i32, 1, dev)
@@ -196,8 +204,8 @@ def map_step(held, add, block_table, ring, ring_state, n_tokens: int, block_toke
         _fail("map: held, add and block_table must have one entry per row, ring_state two")
     if block_table.shape[1] > 1 and block_table.stride(1) != 1:
         _fail("map: block_table's rows must be contiguous")
-    if n < 1 or n_tokens < 0:
-        _fail("map: n_rows must be at least 1 and n_tokens not negative")
+    if n < 1:
+        _fail("map: n_rows must be at least 1")
     lib = load()
     with _on(dev, stream) as handle:
         if out is None:
@@ -303,6 +311,8 @@ class Cache:
 
         Returns out, or (out, lse) with lse float32 [tokens, heads].
         """
+        _count(window, "attend: window")
+        _count(max_q, "attend: max_q")
         kinds = (torch.bfloat16, torch.float16)
         dev = self.device
         _want(q, "q", kinds, 3, dev)

@@ -282,3 +282,18 @@ def test_map_lets_outputs_lie_between_the_rows_of_a_table(lib):
     row = a.block_table + 4 * 64
     _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, counts=gap, kv_len=row + 12)), None), "overlap")
     _refused(lib, lib.hx_kv_map(ctypes.byref(_set(a, row_start=row + 16, kv_len=a.held)), None), "held")
+
+
+@pytest.mark.parametrize("value", [2 ** 32, 2 ** 32 + 5, -2 ** 32 + 3, 2 ** 31])
+def test_binding_refuses_whole_numbers_past_32_bits(value):
+    """ctypes would cut them off: a window of 2^32 + 5 would be one of 5."""
+    cache = object.__new__(KV.Cache)
+    for kw in (dict(window=value), dict(max_q=value)):
+        with pytest.raises(H.HxError) as e:
+            cache.attend(None, None, None, None, **kw)
+        assert e.value.code == H.HX_ERR_INVALID and list(kw)[0] in str(e.value)
+    z = torch.zeros(3, dtype=torch.int32)
+    for args, name in (((value, 16), "n_tokens"), ((1, value), "block_tokens"), ((1, 0), "block_tokens")):
+        with pytest.raises(H.HxError) as e:
+            KV.map_step(z, z, z[None], z, z.long(), *args)
+        assert e.value.code == H.HX_ERR_INVALID and name in str(e.value)
