@@ -79,6 +79,13 @@ def tune(args) -> int:
     return 0
 
 
+def objective(args, wl) -> int:
+    """The objective asked for, else the recipe's own."""
+    if args.objective is None:
+        return wl.objective
+    return W.OBJ_P95 if args.objective == "p95" else W.OBJ_P95_SLO95
+
+
 def replay(args) -> int:
     """The recipe's first trace at its best point, logged, and one instance's
     calls of it as serving steps: one JSON line."""
@@ -87,7 +94,7 @@ def replay(args) -> int:
     wl = W.make_workload(recipe, n_traces=1, n_queries=args.queries)
     with H.Sim(wl.traces, wl.cluster, wl.grid) as sim:
         sim.run()
-        point = max(0, sim.best(wl.objective)[0])
+        point = max(0, sim.best(objective(args, wl))[0])
     with H.Sim(wl.traces, wl.cluster, wl.grid, record_sims=[point], subset=[point]) as sim:
         sim.run()
         records = sim.records(0)
@@ -124,7 +131,7 @@ def main(argv=None) -> int:
 
     recipe = int(args.recipe) if args.recipe.isdigit() else args.recipe
     wl = W.make_workload(recipe, n_traces=args.traces, n_queries=args.queries)
-    obj = wl.objective if args.objective is None else (W.OBJ_P95 if args.objective == "p95" else W.OBJ_P95_SLO95)
+    obj = objective(args, wl)
     sim = H.Sim(wl.traces, wl.cluster, wl.grid, timing=True)
     t0 = time.perf_counter()
     sim.run(torch.cuda.current_stream())

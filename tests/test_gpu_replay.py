@@ -75,3 +75,36 @@ def test_replay_of_a_simulated_schedule(capsys):
     assert out["instance"] == 6 and out["slots"] == 16 and out["steps"] > 50 and out["decode_steps"] >= 2
     assert out["tokens"] > 0 and out["us_per_step"] + out["us_per_1000_tokens"] * out["mean_context"] / 1000 > 0
     assert out["prompt_us_per_token"] > 0
+
+
+@pytest.mark.parametrize("objective,slo", [(None, 0), ("p95", 0), ("p95_slo95", 1)])
+def test_replay_takes_the_objective_that_it_is_given(monkeypatch, capsys, objective, slo):
+    """The schedule replayed is the best point's by --objective, as without --replay."""
+    asked = []
+
+    class Sim:
+        def __init__(self, *a, **kw):
+            pass
+
+        def __enter__(self):
+            return self
+
+        def __exit__(self, *exc):
+            pass
+
+        def run(self):
+            pass
+
+        def best(self, objective):
+            asked.append(objective)
+            return 0, 0, 0, np.zeros(1, np.int32)
+
+        def records(self, i):
+            return {}
+
+    monkeypatch.setattr(H, "Sim", Sim)
+    monkeypatch.setattr(R, "replay", lambda *a, **kw: {})
+    wl = W.make_workload(0, n_traces=1, n_queries=20)
+    want = wl.objective if objective is None else (W.OBJ_P95_SLO95 if slo else W.OBJ_P95)
+    M.main(["--recipe", "0", "--queries", "20", "--replay", "0"] + (["--objective", objective] if objective else []))
+    assert asked == [want]
