@@ -156,7 +156,7 @@ def replay(trace, records: dict, cluster, instance: int, shape: Optional[Shape] 
         events = batch.run(add)
         steps.append(_Step(int(np.maximum(add, 0).sum()), context, bool((add <= 1).all()) and bool((add == 1).any()), events))
     torch.cuda.synchronize()
-    steps = steps[warmup:] if len(steps) > 2 * warmup else steps
+    steps = steps[warmup if len(steps) > 2 * warmup else 0:][-max_steps:]
     us = np.array([1000 * s.events[0].elapsed_time(s.events[1]) for s in steps])
     out = {"instance": instance, "slots": slots, "calls": n_calls, "steps": len(steps), "tokens": sum(s.tokens for s in steps),
            "prefill_tok_s": int(cluster.prefill_tok_s[kind]), "decode_us_tok": int(cluster.decode_us_tok[kind])}

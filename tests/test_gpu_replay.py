@@ -108,3 +108,26 @@ def test_replay_takes_the_objective_that_it_is_given(monkeypatch, capsys, object
     want = wl.objective if objective is None else (W.OBJ_P95_SLO95 if slo else W.OBJ_P95)
     M.main(["--recipe", "0", "--queries", "20", "--replay", "0"] + (["--objective", objective] if objective else []))
     assert asked == [want]
+
+
+def test_replay_keeps_no_more_steps_than_asked_for(monkeypatch):
+    """Steps to warm up with are on top of max_steps and are not counted, however few those are."""
+    class Event:
+        def elapsed_time(self, other):
+            return 0.001
+
+    class Batch:
+        def __init__(self, slots, longest, shape):
+            self.held = np.zeros(slots, np.int32)
+
+        def run(self, add):
+            self.held = np.where(add < 0, 0, self.held + np.maximum(add, 0)).astype(np.int32)
+            return Event(), Event()
+
+    monkeypatch.setattr(R, "Batch", Batch)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda: None)
+    cl = W.make_workload(0, n_queries=20).cluster
+    for steps in (1, 2, 3, 4, 50):
+        out = R.replay(_Trace([5], [100]), _records([0], [0]), cl, 0, max_steps=steps)
+        assert out["steps"] == steps
+    assert R.replay(_Trace([5], [1]), _records([0], [0]), cl, 0, max_steps=50)["steps"] == 3
