@@ -309,7 +309,8 @@ class Cache:
         workspace   uint8 tensor to use instead of the one that the cache keeps for each stream (not by calls
                     on another cache at the same time)
 
-        Returns out, or (out, lse) with lse float32 [tokens, heads].
+        Returns out, or (out, lse) with lse float32 [tokens, heads].  There is no backward pass: no gradient flows
+        from them to q.
         """
         _count(window, "attend: window")
         _count(max_q, "attend: max_q")
