@@ -349,11 +349,13 @@ class Cache:
                     need = ctypes.c_int64()
                     H._check(self.lib, self.lib.hx_kv_attend_workspace(self._ref, ref, ctypes.byref(need)))
                     graph = torch.cuda.is_current_stream_capturing()  # a graph has a workspace of its own
-                    workspace = None if graph else self._work.get(handle)
+                    workspace = None if graph else self._work.pop(handle, None)
                     if workspace is None or workspace.numel() < need.value:
                         workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-                        if not graph:
-                            self._work[handle] = workspace
+                    if not graph:  # the streams used last are the dict's last (what goes, goes back to its own stream's memory)
+                        self._work[handle] = workspace
+                        if len(self._work) > 16:
+                            del self._work[next(iter(self._work))]
                 a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
                 H._check(self.lib, self.lib.hx_kv_attend(self._ref, ref, handle))
         return (out, lse) if return_lse else out

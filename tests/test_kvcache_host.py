@@ -297,3 +297,44 @@ def test_binding_refuses_whole_numbers_past_32_bits(value):
         with pytest.raises(H.HxError) as e:
             KV.map_step(z, z, z[None], z, z.long(), *args)
         assert e.value.code == H.HX_ERR_INVALID and name in str(e.value)
+
+
+def test_workspaces_of_streams_gone_by_are_given_back(monkeypatch):
+    """The cache keeps one for each of the streams used last, not for every stream that there ever was."""
+    class On:
+        def __init__(self, device, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            return self.stream
+
+        def __exit__(self, *exc):
+            pass
+
+    class Lib:
+        used = []
+
+        def hx_kv_attend_workspace(self, cache, query, need):
+            need._obj.value = 64
+            return H.HX_OK
+
+        def hx_kv_attend(self, cache, query, stream):
+            self.used.append(query._obj.workspace)
+            return H.HX_OK
+
+    lib = Lib()
+    monkeypatch.setattr(KV, "_want", lambda *a: None)
+    monkeypatch.setattr(KV, "_dense", lambda *a: None)
+    monkeypatch.setattr(KV, "_on", On)
+    monkeypatch.setattr(KV, "load", lambda: lib)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    zeros = torch.zeros
+    monkeypatch.setattr(torch, "zeros", lambda *a, **kw: zeros(*a, **{k: v for k, v in kw.items() if k != "pin_memory"}))
+    f = torch.empty((2, 1, 16, 64), dtype=torch.uint8).view(torch.float8_e4m3fn)
+    cache = KV.Cache(f, f.clone(), torch.ones(2, 1), torch.ones(2, 1))
+    q, i32 = torch.empty((1, 2, 64), dtype=torch.float16), torch.int32
+    args = (q, zeros((1, 2), dtype=i32), zeros(2, dtype=i32), zeros(1, dtype=i32))
+    for handle in range(100):
+        cache.attend(*args, stream=7)
+        cache.attend(*args, stream=1000 + handle)
+    assert len(cache._work) <= 16 and len(set(lib.used[::2])) == 1
