@@ -631,6 +631,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
       bar_wait(&sh->s_full[half], n_s & 1, dead);
       tc_fence_after();
       const uint32_t valid = info.valid;
+      if (!has) m = *ref;  // near the first exponents, so that they are rounded as the scores themselves are
       if ((valid & kFar) && !apart) {
         apart = true;
         if (l != 0) ml = m - *ref;

@@ -239,3 +239,16 @@ def test_infinite_scores_give_no_number(n, max_q, kv):
         want[n // 2, 1] = True
         assert torch.equal(torch.isnan(got), want)
         assert not bool(torch.isfinite(lse[n // 2, 1])) and int((~torch.isfinite(lse)).sum()) == 1
+
+
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20, 200)), (150, (0, 150))])
+@pytest.mark.parametrize("scale", [2.0 ** 100, 2.0 ** -100, 3 * 2.0 ** 60])
+@pytest.mark.parametrize("window", [0, 1, 2])
+def test_sums_are_no_worse_under_large_or_small_scales(n, max_q, scale, window):
+    """The values' scale is no part of the softmax, and must not cost its sum any bits either."""
+    g, B, D = gen(n), 16, 64
+    kv = [300]
+    table, N = P.paged(g, kv, B)
+    k, v, ks, vs = P.random_cache(g, N, 2, B, D)
+    q = torch.randn((n, 48, D), generator=g, device="cuda").bfloat16()
+    check(q, KV.Cache(k, v, ks, torch.full_like(vs, scale)), table, [n], kv, 1e-5, window=window, max_q=max_q)
