@@ -155,7 +155,10 @@ int hx_kv_attend_workspace(const hx_kv_cache* c, const hx_kv_query* a, int64_t* 
  * nothing gets zeros and lse = -inf; so do tokens that no row owns.  Positions past kv_len, in blocks
  * whose number is out of range, or masked take no part, whatever the cache holds there.  A row with more than
  * max_q > 0 tokens gets zeros.  The kernels' waits on their own copies and products are bounded, by about two
- * seconds: a block whose wait runs out leaves NaN in what it had left to compute, and *status says so. */
+ * seconds: a block whose wait runs out leaves NaN in what it had left to compute, and *status says so.  Scores, sums and
+ * outputs are in 32 bits until they are rounded to q's type; weights are rounded to 16 bits before they multiply
+ * the values (2^-11 of a weight; a weight times its block's value scale that is below 2^-25 of the token's largest may count as
+ * zero there, and counts in full in the softmax's sum). */
 int hx_kv_attend(const hx_kv_cache* c, const hx_kv_query* a, void* stream);
 
 #ifdef __cplusplus

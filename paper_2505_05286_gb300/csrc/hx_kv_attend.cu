@@ -22,9 +22,9 @@ namespace {
 // S^T = K Q^T, O^T = V^T P^T.  So eight rows waste nothing (16 x 8 x 16 the other way round would
 // compute 16), and the sums take half the registers, which lets 12 computing warps reside on an SM.
 //
-// 48 requests of 32000 tokens, 32 heads on 8 of 128: 507 us, 6.35 TB/s, 95 % of a copy.  500 requests of 437 to
-// 18133 tokens, 28 heads on 4 of 64, blocks of 16: 223 us, 4.05 TB/s: instructions, of which a column of 64 takes as
-// many for its softmax as one of 128.  One request of 5065 tokens: 14.8 us, latency.
+// 48 requests of 32000 tokens, 32 heads on 8 of 128: 505 us, 6.4 TB/s, 95 % of a copy.  500 requests of 437 to
+// 18133 tokens, 28 heads on 4 of 64, blocks of 16: 221 us, 4.1 TB/s: instructions, of which a column of 64 takes as
+// many for its softmax as one of 128.  One request of 5065 tokens: 14.6 us, latency.
 constexpr int kRows = 16;  // most rows of an item
 constexpr int kStageBytes = 8192;
 constexpr int kTileBytes = kStageBytes / 2;
@@ -298,7 +298,8 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       continue;
     }
 
-    // q of row n (of each eight) in f16, scaled by a power of two so that no value leaves f16's range
+    // q of row n (of each eight) in f16, scaled by a power of two so that no value leaves f16's range: exact down to
+    // 2^-14 of the row's largest, what lies below is off by 2^-25 of that at most
     uint32_t bq[NR][KJ * 4][2];
     float c[NR][2];  // factors of the scores of rows 2 q4 and 2 q4 + 1, and what those rows see
     int lo[NR][2], hi[NR][2];
@@ -492,7 +493,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
         for (int g = 0; g < S::kGroups; ++g)
           if (!(fabsf(value_scale[g]) < INFINITY)) value_scale[g] = 0.f;
       }
-      uint32_t bp[S::kGroups][NR][2];
+      uint32_t bp[S::kGroups][NR][2];  // the weights, rounded to 2^-11 of themselves or 2^-25
 #pragma unroll
       for (int g = 0; g < S::kGroups; ++g) {
 #pragma unroll
@@ -554,7 +555,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       }
       // O^T += scale * (V^T P^T), 16 columns at a time: the scale's product and the sum over groups are in 32 bits, so that
       // scales far apart cost each other nothing, and one that a row does not see is multiplied by zero.  (Sums in units
-      // of the last scale, rescaled where it changed, let a masked block's scale into the row; 500 ragged requests took 248 us, now 223.)
+      // of the last scale, rescaled where it changed, let a masked block's scale into the row; 500 ragged requests took 248 us, now 221.)
 #pragma unroll
       for (int w = 0; w < D / 32; ++w)
 #pragma unroll

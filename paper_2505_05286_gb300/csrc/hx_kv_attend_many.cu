@@ -23,17 +23,17 @@ namespace {
 //     softmax does,
 //   2 x 4 warps do a half's softmax, a row to a thread, and write P over S.
 // Tensor memory (512 columns): S, P of the halves at 0 and 128, O at 256 and 256 + D.
-// Four prompts of 5600 tokens, 32 heads on 8 of 128 in bf16: 1083 us, 982 TFLOP/s, 52 % of a plain product's rate; a
-// tile takes 3850 cycles where its products take 2048: a half's softmax, values and scores follow one another.
+// Four prompts of 5600 tokens, 32 heads on 8 of 128 in bf16: 1130 us, 941 TFLOP/s, 49 % of a plain product's rate; a
+// tile takes some 4000 cycles where its products take 2048: a half's softmax, values and scores follow one another.
 //
 // By turns (kTurns): where no request of the step has more tokens than a half (max_q says so), the second half
 // would have nothing to do.  Then both halves have the same rows, one takes the even tiles and the other the odd ones, and the
-// first half's threads join the two: 64 requests of 1 to 5 tokens at 810 to 11507, 32 heads on 8 of 128, 218 -> 184 us;
-// a chunk of 30 at 24001 46 -> 39 us.  As a branch in one kernel it cost prompts 4 %.
+// first half's threads join the two: 64 requests of 1 to 5 tokens at 810 to 11507, 32 heads on 8 of 128, 221 -> 193 us;
+// a chunk of 30 at 24001 47 -> 40 us.  As a branch in one kernel it cost prompts 4 %.
 //
 // Scales: a score is s * ks * c, and a value's scale vs goes into the weight, P = exp2(s ks c +
 // log2(vs) - m) with m within kLag of the largest of those exponents so far.  So P in f16 is accurate
-// relative to the row's largest weight times scale, however far apart scales lie.  The softmax's sum l is that of
+// relative to the row's largest weight times scale (a token below 2^-25 of that adds nothing to O), however far apart scales lie.  The softmax's sum l is that of
 // P 2^ref / vs, in units of 2^(m - ref) where ref is the power of two of a scale of the item, as long as all its scales lie
 // within 2^kNear of that.  Past this P may be zero where its share of l is not: from the first such tile on l is
 // summed from the scores alone, in units of 2^ml with a maximum of its own (64 blocks of zeros, as hx_kv_append leaves them
