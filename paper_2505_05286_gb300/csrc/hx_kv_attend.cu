@@ -23,7 +23,7 @@ namespace {
 // compute 16), and the sums take half the registers, which lets 12 computing warps reside on an SM.
 //
 // 48 requests of 32000 tokens, 32 heads on 8 of 128: 505 us, 6.4 TB/s, 95 % of a copy.  500 requests of 437 to
-// 18133 tokens, 28 heads on 4 of 64, blocks of 16: 221 us, 4.1 TB/s: instructions, of which a column of 64 takes as
+// 18133 tokens, 28 heads on 4 of 64, blocks of 16: 224 us, 4.0 TB/s: instructions, of which a column of 64 takes as
 // many for its softmax as one of 128.  One request of 5065 tokens: 14.6 us, latency.
 constexpr int kRows = 16;  // most rows of an item
 constexpr int kStageBytes = 8192;
@@ -44,7 +44,7 @@ struct Shape {
 
 // Where a tile of keys or of values lies, its scales, and which of its groups of 16 tokens are fetched.
 struct __align__(16) Tile {
-  float scale[4];
+  float scale[4];  // (values': times kSumDown)
   int id[4];  // blocks of the cache, -1: not fetched
   int y;      // row in the tile map
   uint32_t bytes, valid;
@@ -206,7 +206,7 @@ __device__ void produce(const AttendArgs& a, const CUtensorMap* map, Place<D> at
     if (tile) {
       Tile& x = tiles[(number + __popc(who & ((1u << lane) - 1))) & (kTiles - 1)];
 #pragma unroll
-      for (int g = 0; g < S::kGroups; ++g) x.scale[g] = scale[g];
+      for (int g = 0; g < S::kGroups; ++g) x.scale[g] = V ? scale[g] * kSumDown : scale[g];
 #pragma unroll
       for (int p = 0; p < 4; ++p) x.id[p] = id[p];
       x.y = y, x.bytes = bytes, x.valid = valid;
@@ -555,7 +555,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
       }
       // O^T += scale * (V^T P^T), 16 columns at a time: the scale's product and the sum over groups are in 32 bits, so that
       // scales far apart cost each other nothing, and one that a row does not see is multiplied by zero.  (Sums in units
-      // of the last scale, rescaled where it changed, let a masked block's scale into the row; 500 ragged requests took 248 us, now 221.)
+      // of the last scale, rescaled where it changed, let a masked block's scale into the row; 500 ragged requests took 248 us, now 224.)
 #pragma unroll
       for (int w = 0; w < D / 32; ++w)
 #pragma unroll
@@ -657,7 +657,7 @@ __device__ void consume(const AttendArgs& a, Place<D> at, int count, const uint8
         o.x += p.x, o.y += p.y, o.z += p.z, o.w += p.w;
       }
       if (done) {
-        const float inv = lt == 0 ? 0.f : 1.f / lt;
+        const float inv = lt == 0 ? 0.f : kSumUp / lt;
         const int token = q.first + row / a.group, head = at.h * a.group + row % a.group;
         *(uint2*)((T*)a.out + token * a.out_token_stride + head * a.out_head_stride + col) =
             uint2{from_float2<T>(o.x * inv, o.y * inv), from_float2<T>(o.z * inv, o.w * inv)};
@@ -876,7 +876,7 @@ __global__ void __launch_bounds__(kJoinThreads) hx_kv_attend_join(const __grid_c
     }
     if (sub == 0 && row < rows && team < share * together) {
       const float2 ml = s_ml[row];
-      const float inv = ml.y == 0 ? 0.f : 1.f / ml.y;
+      const float inv = ml.y == 0 ? 0.f : kSumUp / ml.y;
       const int64_t token = join.x + i0 + a.by_group.of(x0 + row);
       const int head = join.w * a.group + a.by_group.rest(x0 + row);
       T* to = (T*)a.out + token * a.out_token_stride + head * a.out_head_stride + 4 * col;

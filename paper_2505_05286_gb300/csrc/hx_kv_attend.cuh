@@ -12,6 +12,10 @@
 namespace hx {
 
 constexpr float kLog2e = 1.4426950408889634f;
+// Sums of weighted values are kept, and left to the join, in units of 2^kSumUnit: before they are divided by the softmax's sum
+// they are larger than a result by up to 2^30 tokens and the 2^8 or 2^10 by which a maximum may lag.
+constexpr int kSumUnit = 20;
+constexpr float kSumUp = 1 << kSumUnit, kSumDown = 1 / kSumUp;
 constexpr int kItemRows = 256;  // places for rows of an item of the many-rows kernel: two halves of 128
 
 // Division by a divisor known on the host (Granlund and Montgomery's invariant

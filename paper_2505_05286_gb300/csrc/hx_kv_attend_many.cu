@@ -783,7 +783,7 @@ __device__ void softmax(const AttendArgs& a, Segment s, int count, Shared* sh) {
     float* part = a.part + (slot * kItemRows + half * kHalf + row) * D;
     const bool none = l == 0;
     const float nothing = l == l ? 0.f : NAN;
-    const float inv = done ? (none ? 0.f : 1.f / l) : 1.f;
+    const float inv = done ? (none ? 0.f : 1.f / l) : kSumDown;
     const auto factor = [&](float up) {  // 2^up * inv, in two steps: 2^up alone may leave the range
       up = fminf(fmaxf(up, -252.f), 252.f);
       const float part = rintf(0.5f * up);

@@ -252,3 +252,14 @@ def test_sums_are_no_worse_under_large_or_small_scales(n, max_q, scale, window):
     k, v, ks, vs = P.random_cache(g, N, 2, B, D)
     q = torch.randn((n, 48, D), generator=g, device="cuda").bfloat16()
     check(q, KV.Cache(k, v, ks, torch.full_like(vs, scale)), table, [n], kv, 1e-5, window=window, max_q=max_q)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20)), (150, (0,))])
+@pytest.mark.parametrize("tokens", [100, 1000000])
+def test_sums_of_large_values_stay_in_range(D, n, max_q, tokens):
+    """Before they are divided, sums are larger than results by as many tokens as there are and by what the maximum lags."""
+    B = 16
+    blocks = -(-tokens // B)
+    cache, table = one_column_cache([0.0] * 16 + [7.875] * (tokens - 16), [448.0] * tokens, D, B, v_scale=[2.0 ** 100] * blocks)
+    check(two_columns(n, 1, D, torch.bfloat16), cache, table, [n], [tokens], math.log(2), causal=False, max_q=max_q)
