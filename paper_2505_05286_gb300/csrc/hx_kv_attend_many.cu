@@ -43,7 +43,7 @@ constexpr int kKv = 128;       // tokens of a tile
 constexpr int kGroups = kKv / 16;
 constexpr int kConvWarp = 8, kMmaWarp = 12, kFetchWarp = 13, kQueryWarp = 14;
 constexpr int kManyThreads = 32 * (kQueryWarp + 1);
-constexpr float kNear = 40.f;  // so that what P / vs loses below 2^-126 is less than 2^-46 of l
+constexpr float kNear = 16.f;  // what l loses of P below 2^-126 is then less than 2^-90 of it, by its exponents' rounding 2^-20
 constexpr int kNanList = 8;
 constexpr int kNanLists = 8;  // the conversion may be four items ahead of a half that still writes one out
 
@@ -323,12 +323,12 @@ __device__ void fetch(const AttendArgs& a, Segment s, int count, Shared* sh, uin
       if (!__all_sync(~0u, bar_wait(&sh->raw_empty[v], (it & 1) ^ 1, dead))) return;
       if (v == 0) {
         TileInfo& info = sh->info[it & 7];
-        const float lv = log2f(vs);  // -inf: the values are zeros
+        const float lv = log2f(vs);  // rounded, which the sum takes out again; -inf: the values are zeros
         const uint32_t who = __ballot_sync(~0u, seen && fabsf(lv) < INFINITY);
         if (who && !has_ref) ref = rintf(__shfl_sync(~0u, lv, __ffs(who) - 1)), has_ref = true;
         const bool near = fabsf(lv - ref) <= kNear;
         far |= __any_sync(~0u, seen && !near);
-        if (lane < kGroups) info.g[lane] = float4{ks, lv, near ? exp2f(ref) / vs : 1.f, 0.f};
+        if (lane < kGroups) info.g[lane] = float4{ks, lv, near ? exp2f(ref - lv) : 1.f, 0.f};
         if (lane == 0) info.valid = valid | (far ? kFar : 0), sh->ref[item & (kNanLists - 1)] = ref;
         if (last) has_ref = far = false, ++item;
         __syncwarp();

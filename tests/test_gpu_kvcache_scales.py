@@ -263,3 +263,18 @@ def test_sums_of_large_values_stay_in_range(D, n, max_q, tokens):
     blocks = -(-tokens // B)
     cache, table = one_column_cache([0.0] * 16 + [7.875] * (tokens - 16), [448.0] * tokens, D, B, v_scale=[2.0 ** 100] * blocks)
     check(two_columns(n, 1, D, torch.bfloat16), cache, table, [n], [tokens], math.log(2), causal=False, max_q=max_q)
+
+
+@pytest.mark.parametrize("n,max_q", [(1, (1, 0)), (20, (0, 20, 200)), (150, (0, 150))])
+@pytest.mark.parametrize("one,other", [(3 * 2.0 ** 97, 3 * 2.0 ** 97), (1.0, 3 * 2.0 ** 37), (5 * 2.0 ** -105, 3 * 2.0 ** -69)])
+@pytest.mark.parametrize("window", [0, 1, 2])
+def test_sums_are_no_worse_under_scales_that_differ(n, max_q, one, other, window):
+    """Nor under scales that are no powers of two, or that differ from block to block."""
+    g, B, D = gen(n), 16, 64
+    kv = [300]
+    table, N = P.paged(g, kv, B)
+    k, v, ks, vs = P.random_cache(g, N, 2, B, D)
+    vs.fill_(one)
+    vs[table[0, 1:18:2].long()] = other
+    q = torch.randn((n, 48, D), generator=g, device="cuda").bfloat16()
+    check(q, KV.Cache(k, v, ks, vs), table, [n], kv, 1e-5, window=window, max_q=max_q)
