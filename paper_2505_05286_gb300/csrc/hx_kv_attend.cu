@@ -24,7 +24,7 @@ namespace {
 //
 // 48 requests of 32000 tokens, 32 heads on 8 of 128: 505 us, 6.4 TB/s, 95 % of a copy.  500 requests of 437 to
 // 18133 tokens, 28 heads on 4 of 64, blocks of 16: 224 us, 4.0 TB/s: instructions, of which a column of 64 takes as
-// many for its softmax as one of 128.  One request of 5065 tokens: 14.6 us, latency.
+// many for its softmax as one of 128.  One request of 5065 tokens: 14.8 us, latency.
 constexpr int kRows = 16;  // most rows of an item
 constexpr int kStageBytes = 8192;
 constexpr int kTileBytes = kStageBytes / 2;

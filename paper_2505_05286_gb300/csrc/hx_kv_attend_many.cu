@@ -23,12 +23,12 @@ namespace {
 //     softmax does,
 //   2 x 4 warps do a half's softmax, a row to a thread, and write P over S.
 // Tensor memory (512 columns): S, P of the halves at 0 and 128, O at 256 and 256 + D.
-// Four prompts of 5600 tokens, 32 heads on 8 of 128 in bf16: 1130 us, 941 TFLOP/s, 49 % of a plain product's rate; a
+// Four prompts of 5600 tokens, 32 heads on 8 of 128 in bf16: 1125 us, 945 TFLOP/s, 50 % of a plain product's rate; a
 // tile takes some 4000 cycles where its products take 2048: a half's softmax, values and scores follow one another.
 //
 // By turns (kTurns): where no request of the step has more tokens than a half (max_q says so), the second half
 // would have nothing to do.  Then both halves have the same rows, one takes the even tiles and the other the odd ones, and the
-// first half's threads join the two: 64 requests of 1 to 5 tokens at 810 to 11507, 32 heads on 8 of 128, 221 -> 193 us;
+// first half's threads join the two: 64 requests of 1 to 5 tokens at 810 to 11507, 32 heads on 8 of 128, 221 -> 191 us;
 // a chunk of 30 at 24001 47 -> 40 us.  As a branch in one kernel it cost prompts 4 %.
 //
 // Scales: a score is s * ks * c, and a value's scale vs goes into the weight, P = exp2(s ks c +

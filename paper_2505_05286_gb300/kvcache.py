@@ -264,6 +264,7 @@ class Cache:
         self._turn = threading.Lock()  # and all launches of one call those of another, whatever threads they are from
         # in host memory that the kernels write to: it holds its zero without any stream's doing
         self._status = torch.zeros(1, dtype=torch.int32, pin_memory=True)
+        self._status_at = self._status.data_ptr()
         self.lib = load()
 
     @staticmethod
@@ -340,7 +341,7 @@ class Cache:
                             q.stride(1), out.stride(0), out.stride(1), T, heads, kinds.index(q.dtype), n,
                             row_start.data_ptr(), kv_len.data_ptr(), block_table.data_ptr(),
                             block_table.stride(0) if n > 1 else block_table.shape[1], block_table.shape[1], max_q,
-                            1 if causal else 0, window, dim ** -0.5 if sm_scale is None else sm_scale, None, 0, self._status.data_ptr())
+                            1 if causal else 0, window, dim ** -0.5 if sm_scale is None else sm_scale, None, 0, self._status_at)
             ref = ctypes.byref(a)
             if workspace is not None:
                 _dense(workspace, "workspace", (torch.uint8,), 1, dev)
