@@ -1,0 +1,107 @@
+/*
+ * hxstep.h -- C ABI of the operators on either side of a serving step's cache
+ * (hxkv.h) on GB300.
+ *
+ * Before the cache: queries and keys are turned by their positions (rotary
+ * positions, Su et al. 2021).  Behind it: the step's logits are adjusted by what each
+ * request has said, may say and is asked to say.
+ *
+ * Pointers, streams and errors are as in hxkv.h: device memory of the current device, structs in
+ * host memory, every call enqueues its kernel on `stream` and returns, nothing is allocated,
+ * and calls can be captured into a graph.  Values in device memory are checked by the
+ * kernels, which treat what is out of range as each call says and never read or write outside
+ * the arrays described.
+ */
+#ifndef HXSTEP_H
+#define HXSTEP_H
+
+#include "hxkv.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Queries and keys of a step, [n_tokens][heads][head_dim], to be turned.  A head's first rotary_dim
+ * values are rotary_dim / 2 pairs: values i and i + rotary_dim / 2, or 2i and 2i + 1 if
+ * interleaved.  Pair i of a token at position p is turned by p * turns[i] * 2^-64 full turns and multiplied by
+ * `scale`; the values behind rotary_dim are copied.  p is positions[token], or follows from the step's
+ * rows: row r's tokens are row_start[r] to row_start[r + 1], the last of the kv_len[r] that it holds.
+ * Tokens that no row owns are left as they are: nothing is written for them.  (A row that was refused, whose kv_len
+ * is 0, has positions below zero.)  An output is its input (the same address and strides) or shares no value
+ * with either input, and the outputs none with one another. */
+typedef struct hx_rotate_args {
+  const void* q;
+  const void* k;              /* NULL: queries alone, n_kv_heads is 0 */
+  void* q_out;                /* aligned to the type, as q and k */
+  void* k_out;
+  int64_t q_token_stride, q_head_stride;          /* elements, 0..2^38 */
+  int64_t k_token_stride, k_head_stride;
+  int64_t q_out_token_stride, q_out_head_stride;  /* elements, 0..2^38; no two values at one place */
+  int64_t k_out_token_stride, k_out_head_stride;
+  int32_t n_tokens;           /* 0..HX_KV_MAX_TOKENS */
+  int32_t n_heads;            /* 1..2048 */
+  int32_t n_kv_heads;         /* 0..2048 */
+  int32_t head_dim;           /* 2..1024 */
+  int32_t rotary_dim;         /* even, 2..head_dim */
+  int32_t dtype;              /* HX_BF16, HX_F16 or HX_F32 */
+  int32_t interleaved;        /* 0 or 1 */
+  int32_t inverse;            /* 1: turned back (with scale 1 also the gradient's way) */
+  float scale;                /* finite */
+  int32_t n_rows;             /* 1..HX_KV_MAX_ROWS; 0 with positions */
+  const uint64_t* turns;      /* [rotary_dim / 2] turns a position, in units of 2^-64 */
+  const int32_t* positions;   /* [n_tokens], or NULL */
+  const int32_t* row_start;   /* [n_rows + 1]; NULL with positions */
+  const int32_t* kv_len;      /* [n_rows] */
+} hx_rotate_args;
+
+/* The angles are exact to 2^-32 of a turn at every position, their sines and cosines and the
+ * products are in 32 bits, rounded once to dtype. */
+int hx_rotate(const hx_rotate_args* a, void* stream);
+
+#define HX_MAX_VOCAB 393216
+#define HX_MAX_HISTORY 524287  /* entries of a row */
+#define HX_MAX_BIAS 4095       /* entries of a row that count */
+
+/* What holds for the rows of a step's logits.  Every array may be NULL where it says so. */
+typedef struct hx_rules {
+  int32_t n_rows;             /* 1..HX_KV_MAX_ROWS */
+  int32_t history_width;      /* entries of a row of history, 0..HX_MAX_HISTORY */
+  const int32_t* history;     /* [n_rows][history_stride] a request's tokens, or NULL; what is no token of the vocabulary is passed over */
+  int64_t history_stride;     /* >= history_width */
+  const int32_t* length;      /* [n_rows] tokens in history (at most history_width count; below 0: 0) */
+  const int32_t* prompt_len;  /* [n_rows] of them the first so many are the prompt, the others were written; NULL: all were written */
+  const float* repetition;    /* [n_rows] factor for tokens in history, > 0; NULL: 1 */
+  const float* presence;      /* [n_rows] taken off once for tokens that were written; NULL: 0 */
+  const float* frequency;     /* [n_rows] taken off as often as they were written; NULL: 0 */
+  const int32_t* bias_start;  /* [n_rows + 1] row r's entries are bias_start[r] to bias_start[r + 1] (within 0..n_bias), or NULL */
+  const int32_t* bias_token;  /* [n_bias] */
+  const float* bias_value;    /* [n_bias] */
+  const uint32_t* mask;       /* [n_masks][mask_stride] one bit a token, 1: allowed; or NULL */
+  const int32_t* mask_row;    /* [n_rows] which mask holds (out of range: none); NULL: row r's is mask r */
+  int64_t mask_stride;        /* words, >= mask_width */
+  int32_t n_bias;             /* 0.. */
+  int32_t n_masks;            /* >= 1 with a mask; >= n_rows if mask_row is NULL */
+  int32_t mask_width;         /* words of a mask: at least ceil(n_vocab / 32) of every call */
+} hx_rules;
+
+/* Logits of a step, a row for each request. */
+typedef struct hx_logits {
+  const void* x;              /* [n_rows][stride], aligned to the type */
+  int64_t stride;             /* elements, n_vocab..2^38 */
+  int32_t n_rows;             /* 0..HX_KV_MAX_ROWS */
+  int32_t n_vocab;            /* 1..HX_MAX_VOCAB */
+  int32_t dtype;              /* HX_BF16, HX_F16 or HX_F32 */
+} hx_logits;
+
+/* out = adjusted logits, in 32 bits until they are rounded to out's type:
+ *   a token in history:  x > 0 ? x / repetition : x * repetition
+ *   less  frequency * times written + presence * (written at all)
+ *   plus  its bias (the last of the row's entries for it)
+ *   a token that the row's mask does not allow: -infinity, whatever x is.
+ * out is x itself (the same address, stride and type) or does not overlap it. */
+int hx_adjust(const hx_logits* x, const hx_rules* r, void* out, int64_t out_stride, int32_t out_dtype, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

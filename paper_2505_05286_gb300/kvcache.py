@@ -1,8 +1,10 @@
-"""Python binding of the serving step's cache operators (include/hxkv.h).
+"""Python binding of the serving step's cache operators (include/hxkv.h), and of the rotary positions
+before them (include/hxstep.h).
 
 One step of an instance's running batch over a paged 8-bit cache:
 
     step = map_step(held, add, block_table, ring, ring_state, n_tokens, block)   # where its tokens go
+    q, k = rope.rotate(q, k, step.row_start, step.kv_len)                        # turned by their positions
     cache.append(k, v, step.runs)                                                # their keys and values, in e4m3
     out = cache.attend(q, block_table, step.row_start, step.kv_len)              # what each token reads
 
@@ -14,8 +16,10 @@ the kernels are done, as for any asynchronous call.
 from __future__ import annotations
 
 import ctypes
+import math
 import threading
 from dataclasses import dataclass
+from fractions import Fraction
 from typing import Optional
 
 import torch
@@ -55,18 +59,29 @@ class hx_kv_query(ctypes.Structure):
                [("sm_scale", ctypes.c_float), ("workspace", _vp), ("workspace_bytes", _i64), ("status", _vp)]
 
 
+class hx_rotate_args(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("q", "k", "q_out", "k_out")] + \
+               [(n, _i64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "q_out_token_stride",
+                                    "q_out_head_stride", "k_out_token_stride", "k_out_head_stride")] + \
+               [(n, _i32) for n in ("n_tokens", "n_heads", "n_kv_heads", "head_dim", "rotary_dim", "dtype", "interleaved",
+                                    "inverse")] + \
+               [("scale", ctypes.c_float), ("n_rows", _i32)] + \
+               [(n, _vp) for n in ("turns", "positions", "row_start", "kv_len")]
+
+
 _lib = None
 
 
 def load():
-    """The library with the prototypes of hxkv.h; raises if it has not been built."""
+    """The library with the prototypes of hxkv.h and hx_rotate; raises if it has not been built."""
     global _lib
     if _lib is None:
         lib = H.load()
         lib.hx_kv_max_runs.restype = _i64
         lib.hx_kv_max_runs.argtypes = [_i32, _i32, _i32]
         for name, args in [("hx_kv_map", [_vp, _vp]), ("hx_kv_append", [_vp, _vp, _vp]),
-                           ("hx_kv_attend_workspace", [_vp, _vp, _vp]), ("hx_kv_attend", [_vp, _vp, _vp])]:
+                           ("hx_kv_attend_workspace", [_vp, _vp, _vp]), ("hx_kv_attend", [_vp, _vp, _vp]),
+                           ("hx_rotate", [_vp, _vp])]:
             fn = getattr(lib, name)
             fn.restype = ctypes.c_int
             fn.argtypes = args
@@ -225,6 +240,122 @@ def map_step(held, add, block_table, ring, ring_state, n_tokens: int, block_toke
                            out.ring_state.data_ptr())
         H._check(lib, lib.hx_kv_map(ctypes.byref(a), handle))
     return out
+
+
+_PI = Fraction(31415926535897932384626433832795028841971693993751, 10 ** 49)
+
+
+class Rope:
+    """Rotary positions (hx_rotate): the table of a model's frequencies, on one device.
+
+    frequencies   radians a position for each pair of values, in 64 bits; they set how much of a head is turned
+                  (2 values for each; see Rope.frequencies)
+    interleaved   pairs are values 2i and 2i + 1 of a head, not i and i + len(frequencies)
+    scale         factor of what is turned
+    """
+
+    def __init__(self, frequencies, *, interleaved: bool = False, scale: float = 1.0, device="cuda"):
+        f = torch.as_tensor(frequencies, dtype=torch.float64).cpu()
+        if f.dim() != 1 or not 1 <= f.shape[0] <= 512 or not bool(torch.isfinite(f).all()):
+            _fail("rope: frequencies must be 1 to 512 finite numbers")
+        if not math.isfinite(scale):
+            _fail("rope: scale is not finite")
+        turns = [round(Fraction(x) / (2 * _PI) * (1 << 64)) % (1 << 64) for x in f.tolist()]
+        self.turns = torch.tensor([t - (t >> 63 << 64) for t in turns], dtype=torch.int64).to(device)
+        self.device = self.turns.get_device()
+        self.rotary_dim, self.interleaved, self.scale = 2 * len(turns), bool(interleaved), float(scale)
+        self.lib = load()
+
+    @staticmethod
+    def frequencies(rotary_dim: int, theta: float = 10000.0, *, scaling: str = "linear", factor: float = 1.0,
+                    original: int = 0, low: float = 1.0, high: float = 32.0):
+        """theta ** (-2i / rotary_dim) for the rotary_dim / 2 pairs, scaled for contexts `factor` times as long as trained:
+
+        "linear"  every frequency / factor (Chen et al. 2023)
+        "base"    theta * factor ** (rotary_dim / (rotary_dim - 2)): the slowest / factor, the fastest as they are
+        "bands"   those that turn fewer than `low` times in the `original` tokens / factor, those that
+                  turn more than `high` times as they are, the others between (Peng et al. 2023)
+        """
+        if rotary_dim < 2 or rotary_dim % 2 or not theta > 0 or not factor > 0:
+            _fail("rope: rotary_dim must be even and at least 2, theta and factor above 0")
+        if scaling == "base" and factor != 1:
+            if rotary_dim == 2:
+                _fail("rope: one pair alone has no base to scale")
+            theta *= factor ** (rotary_dim / (rotary_dim - 2))
+        f = theta ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64) / rotary_dim)
+        if scaling == "linear":
+            return f / factor
+        if scaling == "base":
+            return f
+        if scaling != "bands" or original < 1 or not high > low:
+            _fail("rope: scaling must be linear, base, or bands with original >= 1 and high above low")
+        keep = ((original * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        return keep * f + (1 - keep) * f / factor
+
+    def rotate(self, q, k=None, row_start=None, kv_len=None, *, positions=None, out=None, inverse: bool = False, stream=None):
+        """Turn a step's queries and keys by their positions (hx_rotate).
+
+        q, k       bf16, f16 or f32 [tokens, heads, head dim] and [tokens, kv heads, head dim] (tokens and heads may
+                   be strided: the projections' output with q, k and v side by side)
+        row_start, kv_len   int32, as map_step leaves them; tokens behind the last row are left as they are, in
+                   new outputs too, where they are then undefined
+        positions  int32 [tokens] in their place
+        out        (q's, k's) tensors to write to; (q, k) itself: in place
+        inverse    turn back
+
+        Returns q's and k's, or q's alone where there is no k.  The gradient of what is turned is the gradient of the result,
+        turned back: no other backward pass is recorded.
+        """
+        dev = self.device
+        kinds = (torch.bfloat16, torch.float16, torch.float32)
+        _want(q, "q", kinds, 3, dev)
+        T, heads, dim = q.shape
+        if q.stride(2) != 1 and dim > 1:
+            _fail("rotate: a head's values must be contiguous")
+        n = 0
+        if positions is not None:
+            if row_start is not None or kv_len is not None:
+                _fail("rotate: either positions or row_start and kv_len")
+            _dense(positions, "positions", (torch.int32,), 1, dev)
+            if positions.shape[0] != T:
+                _fail("rotate: positions must have one entry per token")
+        else:
+            if row_start is None or kv_len is None:
+                _fail("rotate: either positions or row_start and kv_len")
+            _dense(row_start, "row_start", (torch.int32,), 1, dev)
+            _dense(kv_len, "kv_len", (torch.int32,), 1, dev)
+            n = kv_len.shape[0]
+            if row_start.shape[0] != n + 1:
+                _fail("rotate: row_start must have one entry more than kv_len")
+        kv_heads = 0
+        if k is not None:
+            _want(k, "k", (q.dtype,), 3, dev)
+            kv_heads = k.shape[1]
+            if k.shape[0] != T or k.shape[2] != dim or (k.stride(2) != 1 and dim > 1):
+                _fail("rotate: k must be [tokens, kv heads, head dim] with q's tokens and head dim, a head's values contiguous")
+            if kv_heads < 1:
+                _fail("rotate: k has no heads")
+        with _on(dev, stream) as handle:
+            if out is None:
+                q_out = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device)
+                k_out = None if k is None else torch.empty((T, kv_heads, dim), dtype=q.dtype, device=q.device)
+            else:
+                q_out, k_out = (out, None) if k is None else out
+                for x, like, name in ((q_out, q, "q"), (k_out, k, "k")):
+                    if like is not None:
+                        _want(x, f"out: {name}'s", (q.dtype,), 3, dev)
+                        if x.shape != like.shape or (x.stride(2) != 1 and dim > 1):
+                            _fail(f"rotate: out must have {name}'s shape, a head's values contiguous")
+            none = k is None
+            a = hx_rotate_args(
+                q.data_ptr(), None if none else k.data_ptr(), q_out.data_ptr(), None if none else k_out.data_ptr(),
+                q.stride(0), q.stride(1), 0 if none else k.stride(0), 0 if none else k.stride(1), q_out.stride(0), q_out.stride(1),
+                0 if none else k_out.stride(0), 0 if none else k_out.stride(1), T, heads, kv_heads, dim, self.rotary_dim,
+                kinds.index(q.dtype), self.interleaved, 1 if inverse else 0, self.scale, n, self.turns.data_ptr(),
+                None if positions is None else positions.data_ptr(), None if n == 0 else row_start.data_ptr(),
+                None if n == 0 else kv_len.data_ptr())
+            H._check(self.lib, self.lib.hx_rotate(ctypes.byref(a), handle))
+        return q_out if none else (q_out, k_out)
 
 
 class Cache:
