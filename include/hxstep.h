@@ -4,7 +4,8 @@
  *
  * Before the cache: queries and keys are turned by their positions (rotary
  * positions, Su et al. 2021).  Behind it: the step's logits are adjusted by what each
- * request has said, may say and is asked to say.
+ * request has said, may say and is asked to say, and the next token is drawn
+ * from them.
  *
  * Pointers, streams and errors are as in hxkv.h: device memory of the current device, structs in
  * host memory, every call enqueues its kernel on `stream` and returns, nothing is allocated,
@@ -100,6 +101,35 @@ typedef struct hx_logits {
  *   a token that the row's mask does not allow: -infinity, whatever x is.
  * out is x itself (the same address, stride and type) or does not overlap it. */
 int hx_adjust(const hx_logits* x, const hx_rules* r, void* out, int64_t out_stride, int32_t out_dtype, void* stream);
+
+/* How a row's token is picked from its adjusted logits x.  For each parameter an array by row, or NULL
+ * and one value for all rows. */
+typedef struct hx_pick {
+  const float* noise;         /* [n_rows][noise_stride] random numbers > 0 of the exponential distribution; NULL: the likeliest token */
+  int64_t noise_stride;       /* >= n_vocab */
+  const float* temperature;   /* T; not above 0: the likeliest token is picked */
+  const int32_t* top_k;       /* above 0: only the k likeliest */
+  const float* top_p;         /* below 1: only the likeliest, as few as have that share of the top_k's weight */
+  const float* min_p;         /* above 0: only those with at least that share of the likeliest's weight */
+  float all_temperature, all_top_p, all_min_p;
+  int32_t all_top_k;
+  int32_t* token;             /* [n_rows] out */
+  float* logprob;             /* [n_rows] out, or NULL */
+  void* workspace;            /* 16-byte aligned, hx_sample_workspace() bytes; used until the kernels end, by one call at a time */
+  int64_t workspace_bytes;
+} hx_pick;
+
+/* Bytes of workspace that hx_sample needs for these logits. */
+int64_t hx_sample_workspace(const hx_logits* x, const hx_rules* r, const hx_pick* p);
+
+/* Tokens are ordered by x, the larger first, equal ones by their number; weights are exp((x - largest x) / T).
+ * What the filters leave is a beginning of that order, of one token at least.  Of it the token with the largest
+ * x / T - log(noise) is picked (the lowest of equals), which is one by their weights; logprob is the logarithm of its
+ * share of all tokens' weights, before the filters (of exp(x) where T is not above 0).  Tokens with x = -infinity or NaN take no
+ * part; a NaN makes the row's logprob NaN.  Where none is left, token is -1 and logprob -infinity.  A noise that is
+ * not a number above 0, or infinite, never wins; if no token's does, the first of the order is picked.  Weights are in 32 bits
+ * and are summed in 64-bit whole numbers, scores near the largest are compared in 64 bits: the same inputs give the same token. */
+int hx_sample(const hx_logits* x, const hx_rules* r, const hx_pick* p, void* stream);
 
 #ifdef __cplusplus
 }

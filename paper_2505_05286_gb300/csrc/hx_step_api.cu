@@ -194,4 +194,43 @@ int hx_adjust(const hx_logits* x, const hx_rules* r, void* out, int64_t out_stri
   return launched(hx::launch_adjust(*x, *r, out, out_stride, out_dtype, (cudaStream_t)stream), "adjust");
 }
 
+int64_t hx_sample_workspace(const hx_logits* x, const hx_rules* r, const hx_pick* p) {
+  if (check_logits(x) || !p || (r && check_rules(x, r))) return 0;
+  return hx::sample_workspace(*x, r ? *r : hx_rules{}, *p);
+}
+
+int hx_sample(const hx_logits* x, const hx_rules* r, const hx_pick* p, void* stream) {
+  if (int rc = check_logits(x)) return rc;
+  if (!p) return bad("sample: NULL argument");
+  if (r)
+    if (int rc = check_rules(x, r)) return rc;
+  if (p->noise && (p->noise_stride < x->n_vocab || p->noise_stride >= (int64_t)1 << 38))
+    return bad("sample: noise_stride must be n_vocab..2^38");
+  if (x->n_rows == 0) return HX_OK;
+  if (!p->token) return bad("sample: NULL pointer");
+  const void* words[] = {p->noise, p->temperature, p->top_k, p->top_p, p->min_p, p->token, p->logprob};
+  for (const void* w : words)
+    if (!aligned(w, 4)) return bad("sample: arrays must be 4-byte aligned");
+  const int64_t n = x->n_rows;
+  const hx_rules rules = r ? *r : hx_rules{};
+  const Range out[] = {of_rows(p->token, 1, 0, n, 4), of_rows(p->logprob, 1, 0, n, 4)};
+  const Range in[] = {of_rows(x->x, n, x->stride, x->n_vocab, size_of(x->dtype)), of_rows(p->noise, n, p->noise_stride, x->n_vocab, 4),
+                      of_rows(p->temperature, 1, 0, n, 4), of_rows(p->top_k, 1, 0, n, 4), of_rows(p->top_p, 1, 0, n, 4),
+                      of_rows(p->min_p, 1, 0, n, 4)};
+  for (const Range& o : out) {
+    for (const Range& i : in)
+      if (overlap(i, o)) return bad("sample: an output overlaps what is read");
+    if (over_rules(rules, o)) return bad("sample: an output overlaps the rules");
+  }
+  if (overlap(out[0], out[1])) return bad("sample: token and logprob overlap");
+  const int64_t need = hx::sample_workspace(*x, rules, *p);
+  if (p->workspace_bytes < need || !p->workspace) return bad("sample: workspace is too small");
+  if (!aligned(p->workspace, 16)) return bad("sample: workspace must be 16-byte aligned");
+  const Range work = {p->workspace, need};
+  for (const Range& i : in)
+    if (overlap(i, work)) return bad("sample: workspace overlaps what is read");
+  if (overlap(out[0], work) || overlap(out[1], work) || over_rules(rules, work)) return bad("sample: workspace overlaps an array");
+  return launched(hx::launch_sample(*x, rules, *p, (cudaStream_t)stream), "sample");
+}
+
 }  // extern "C"

@@ -1,7 +1,8 @@
 """Python binding of what follows a serving step's last product (include/hxstep.h): from logits to tokens.
 
     rules = Rules(history=h, length=n, prompt_len=m, repetition=r, mask=bits, mask_row=state)   # what holds for the requests
-    logits = adjust(logits, rules)
+    token, logprob = sample(logits, noise, temperature=t, top_p=0.9, rules=rules)               # the next token of each
+    logits = adjust(logits, rules)                                                              # or the adjusted logits
 
 Arguments are torch tensors on one CUDA device; everything runs in the library's kernels on torch's
 current stream (or `stream`), and there is no CPU fallback.  The tensors must not be freed or reused on another
@@ -16,9 +17,9 @@ import torch
 
 from . import hxsim as H
 from . import kvcache as KV
-from .kvcache import _dense, _fail, _on, _want
+from .kvcache import _count, _dense, _fail, _on, _want
 
-_vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+_vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
 MAX_VOCAB = 393216
 MAX_HISTORY = 524287
@@ -38,6 +39,12 @@ class hx_logits(ctypes.Structure):
     _fields_ = [("x", _vp), ("stride", _i64)] + [(n, _i32) for n in ("n_rows", "n_vocab", "dtype")]
 
 
+class hx_pick(ctypes.Structure):
+    _fields_ = [("noise", _vp), ("noise_stride", _i64)] + [(n, _vp) for n in ("temperature", "top_k", "top_p", "min_p")] + \
+               [(n, _f32) for n in ("all_temperature", "all_top_p", "all_min_p")] + [("all_top_k", _i32)] + \
+               [(n, _vp) for n in ("token", "logprob", "workspace")] + [("workspace_bytes", _i64)]
+
+
 _lib = None
 
 
@@ -46,10 +53,12 @@ def load():
     global _lib
     if _lib is None:
         lib = KV.load()
-        for name, args in [("hx_adjust", [_vp, _vp, _vp, _i64, _i32, _vp])]:
+        for name, args in [("hx_adjust", [_vp, _vp, _vp, _i64, _i32, _vp]), ("hx_sample", [_vp, _vp, _vp, _vp])]:
             fn = getattr(lib, name)
             fn.restype = ctypes.c_int
             fn.argtypes = args
+        lib.hx_sample_workspace.restype = _i64
+        lib.hx_sample_workspace.argtypes = [_vp, _vp, _vp]
         _lib = lib
     return _lib
 
@@ -176,3 +185,59 @@ def adjust(logits, rules: Rules, *, out=None, dtype=None, stream=None):
         H._check(lib, lib.hx_adjust(ctypes.byref(a), ref, out.data_ptr(), out.stride(0) if n > 1 else vocab,
                                     _KINDS.index(out.dtype), handle))
     return out
+
+
+def sample(logits, noise=None, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, rules: Optional[Rules] = None, out=None,
+           stream=None):
+    """The next token of each row of logits [rows, vocabulary] in bf16, f16 or f32 (hx_sample; rows may be strided).
+
+    noise        float32 [rows, vocabulary], random numbers of the exponential distribution (Tensor.exponential_), rows may be
+                 strided; None: the likeliest token of every row
+    temperature, top_p, min_p   float32 [rows] or a number
+    top_k        int32 [rows] or a number
+                 (temperature 0: the likeliest token; top_k 0, top_p 1, min_p 0: no tokens left out)
+    rules        how the logits are adjusted before
+    out          (token int32 [rows], logprob float32 [rows]) to write to
+
+    Returns (token, logprob): -1 and -infinity where the rules leave no token; logprob is the token's share of
+    all that the rules leave, at the row's temperature, before tokens are left out for being unlikely.
+    """
+    a = _logits(logits)
+    dev = logits.get_device()
+    n, vocab = logits.shape
+    ref = None if rules is None else rules._for(logits)
+    p = hx_pick()
+    if noise is not None:
+        _want(noise, "noise", (torch.float32,), 2, dev)
+        if noise.shape != logits.shape or (vocab > 1 and noise.stride(1) != 1):
+            _fail("sample: noise must have the logits' shape, a row contiguous")
+        p.noise, p.noise_stride = noise.data_ptr(), noise.stride(0) if n > 1 else vocab
+    for x, name, kind in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                          (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+        if isinstance(x, torch.Tensor):
+            _dense(x, name, (kind,), 1, dev)
+            if x.shape[0] != n:
+                _fail(f"sample: {name} must have one entry per row")
+            setattr(p, name, x.data_ptr())
+        else:
+            if kind == torch.int32:
+                _count(x, "sample: " + name)
+            setattr(p, "all_" + name, x)
+    lib = load()
+    with _on(dev, stream) as handle:
+        if out is None:
+            token = torch.empty(n, dtype=torch.int32, device=logits.device)
+            logprob = torch.empty(n, dtype=torch.float32, device=logits.device)
+        else:
+            token, logprob = out
+            _dense(token, "out: token", (torch.int32,), 1, dev)
+            _dense(logprob, "out: logprob", (torch.float32,), 1, dev)
+            if token.shape[0] != n or logprob.shape[0] != n:
+                _fail("sample: out must have one entry per row")
+        p.token, p.logprob = token.data_ptr(), logprob.data_ptr()
+        x, p_ref = ctypes.byref(a), ctypes.byref(p)
+        p.workspace_bytes = lib.hx_sample_workspace(x, ref, p_ref)
+        work = torch.empty(p.workspace_bytes, dtype=torch.uint8, device=logits.device)  # its stream's, or its graph's
+        p.workspace = work.data_ptr()
+        H._check(lib, lib.hx_sample(x, ref, p_ref, handle))
+    return token, logprob

@@ -113,11 +113,10 @@ def sample_plain(x, noise, temperature, top_k, top_p, min_p):
         if (score > -np.inf).any():
             token = int(kept[score == score.max()].min())
     lp = z[token] - math.log(total)
-    # weights: five roundings of the exponent (difference, 1 / T, product, 1 / log 2, product) and exp2f's two last places; each thread's
-    # share of a row is summed in 32 bits, at most V / 512 (4096 in a block at least) terms; whole numbers of 2^-44
+    # weights: five roundings of the exponent (difference, 1 / T, product, 1 / log 2, product) and exp2f's two last places (4
+    # roundings' worth); at most 16 + 5 + 5 additions in a row; the result's own rounding
     y = float((np.where(w > 0, -z, 0) * w).sum() / total)
-    terms = max(8, -(-V // 4096))
-    tol = U * (5 * y + 4 + terms + abs(lp)) + V * 2.0 ** -45
+    tol = U * (5 * y + 4 + 26 + abs(lp))
     return token, (math.nan if nan else lp), tol
 
 

@@ -225,9 +225,38 @@ def test_adjust_refusals(lib):
     assert adjust(_logits(n_rows=0, x=None), _rules(n_rows=0)) == H.HX_OK
 
 
+def _pick(**kw):
+    at = [FAKE + MB * i for i in range(50, 58)]
+    return _set(L.hx_pick(at[0], 100, at[1], at[2], at[3], at[4], 1.0, 1.0, 0.0, 0, at[5], at[6], FAKE + 100 * MB, 1 << 30), **kw)
+
+
+def test_sample_refusals(lib):
+    sample = lambda x, r, p: lib.hx_sample(*(None if v is None else ctypes.byref(v) for v in (x, r, p)), None)
+    _refused(lib, sample(None, _rules(), _pick()), "NULL")
+    _refused(lib, sample(_logits(), _rules(), None), "NULL")
+    for kw, msg in LOGITS_BAD:
+        _refused(lib, sample(_logits(**kw), _rules(), _pick()), msg)
+    for kw, msg in RULES_BAD:
+        _refused(lib, sample(_logits(), _rules(**kw), _pick()), msg)
+    for kw, msg in [(dict(noise_stride=99), "noise_stride"), (dict(noise_stride=2 ** 38), "noise_stride"), (dict(token=None), "NULL"),
+                    (dict(workspace=None), "too small"), (dict(workspace_bytes=0), "too small"), (dict(workspace=FAKE + 100 * MB + 8), "16-byte"),
+                    (dict(workspace=_pick().noise), "workspace overlaps"), (dict(workspace=_pick().token - 16), "workspace overlaps"),
+                    (dict(workspace=_rules().mask), "workspace overlaps"), (dict(logprob=_pick().token + 4), "token and logprob"),
+                    (dict(token=FAKE + 4), "overlaps what is read"), (dict(logprob=_pick().temperature), "overlaps what is read"),
+                    (dict(token=_rules().history + 40), "overlaps the rules")] + \
+            [({name: FAKE + 50 * MB + 2}, "aligned") for name in ("noise", "temperature", "top_k", "top_p", "min_p", "token", "logprob")]:
+        _refused(lib, sample(_logits(), _rules(), _pick(**kw)), msg)
+    assert sample(_logits(n_rows=0, x=None), None, _pick(workspace=None)) == H.HX_OK
+    size = lambda x, r, p: lib.hx_sample_workspace(*(None if v is None else ctypes.byref(v) for v in (x, r, p)))
+    need = size(_logits(), _rules(), _pick())
+    _refused(lib, sample(_logits(), _rules(), _pick(workspace_bytes=need - 1)), "too small")
+    assert need > size(_logits(), None, _pick()) > size(_logits(), None, _pick(noise=None)) > 0
+    assert size(None, None, _pick()) == 0 and size(_logits(), None, None) == 0
+
+
 def test_binding_refuses_host_tensors():
     x = torch.zeros((2, 5))
-    for call in (lambda: L.adjust(x, L.Rules()), lambda: L.Rules(history=torch.zeros((2, 3), dtype=torch.int32),
+    for call in (lambda: L.adjust(x, L.Rules()), lambda: L.sample(x), lambda: L.Rules(history=torch.zeros((2, 3), dtype=torch.int32),
                                                                   length=torch.zeros(2, dtype=torch.int32))):
         with pytest.raises(H.HxError) as e:
             call()
