@@ -23,56 +23,104 @@ constexpr uint32_t kTimes = (1u << 19) - 1, kRead = 1u << 19;
 constexpr int kBiasShift = 20;
 static_assert(HX_MAX_HISTORY <= kTimes && HX_MAX_BIAS < 1 << (32 - kBiasShift), "fields of a token's word");
 
+// What holds for one row, as its first loads give it: all of them are on their way at once.
 struct RowRules {
   float repetition, presence, frequency;
-  const uint32_t* mask;   // or null
-  const float* bias;      // entry 1 is bias[0]
-};
+  const uint32_t* mask;     // or null
+  const float* bias;        // entry 1 is bias[0]
+  const int32_t* history;
+  const int32_t* bias_token;
+  int n_bias, length, read;
 
-// Words of places [p0, p0 + kStretch) of row r; all threads of the block call.
-__device__ inline RowRules begin_row(const hx_rules& r, int row, int p0, int shift, int n_vocab, uint32_t* word) {
-  RowRules o = {1.f, 0.f, 0.f, nullptr, nullptr};
-  const int e0 = p0 - shift;
-  auto place = [&](int token) { return (unsigned)token < (unsigned)n_vocab ? (unsigned)(token - e0) : ~0u; };
-  if (r.mask) {
-    const int m = r.mask_row ? r.mask_row[row] : row;
-    if ((unsigned)m < (unsigned)r.n_masks) o.mask = r.mask + m * r.mask_stride;
+  __device__ RowRules(const hx_rules& r, int row) {
+    const int b0 = r.bias_start ? r.bias_start[row] : 0, b1 = r.bias_start ? r.bias_start[row + 1] : 0;
+    const int len = r.history ? r.length[row] : 0;
+    read = r.history && r.prompt_len ? r.prompt_len[row] : 0;
+    repetition = r.history && r.repetition ? r.repetition[row] : 1.f;
+    presence = r.history && r.presence ? r.presence[row] : 0.f;
+    frequency = r.history && r.frequency ? r.frequency[row] : 0.f;
+    const int m = r.mask && r.mask_row ? r.mask_row[row] : row;
+    mask = r.mask && (unsigned)m < (unsigned)r.n_masks ? r.mask + m * r.mask_stride : nullptr;
+    const int first = max(0, min(b0, r.n_bias));
+    n_bias = min(min(max(first, b1), r.n_bias) - first, HX_MAX_BIAS);
+    bias = r.bias_value + first;
+    bias_token = r.bias_token + first;
+    length = min(len, r.history_width);
+    history = r.history + row * r.history_stride;
   }
-  if (!r.bias_start && !r.history) return o;
+
+  // Words of places [p0, p0 + kPlaces) up to the load with the last token; all threads of the block call.
+  template <int kPlaces>
+  __device__ void count(int p0, int shift, int n_vocab, uint32_t* word) const {
+    // the stretch's tokens are [e0, e0 + span), the first at word[at0]
+    const int e0 = max(p0 - shift, 0), at0 = e0 - (p0 - shift);
+    const unsigned span = (unsigned)max(min(kPlaces - at0, n_vocab - e0), 0);
+    word += at0;
 #pragma unroll
-  for (int i = 0; i < kEach / 4; ++i) ((uint4*)word)[threadIdx.x + i * kRowThreads] = uint4{0, 0, 0, 0};
-  __syncthreads();
-  if (r.bias_start) {
-    const int b0 = max(0, min(r.bias_start[row], r.n_bias));
-    const int b1 = min(min(max(b0, r.bias_start[row + 1]), r.n_bias), b0 + HX_MAX_BIAS);
-    o.bias = r.bias_value + b0;
-    for (int j = b0 + threadIdx.x; j < b1; j += kRowThreads) {
-      const unsigned at = place(r.bias_token[j]);
-      if (at < kStretch) atomicMax(&word[at], (uint32_t)(j - b0 + 1) << kBiasShift);
-    }
+    for (int i = 0; i < kPlaces / kRowThreads / 4; ++i)
+      if (4 * i * kRowThreads < (int)span + at0) ((uint4*)(word - at0))[threadIdx.x + i * kRowThreads] = uint4{0, 0, 0, 0};
+    // 16 bytes a load from the boundary at or before the row's first entry, every block of the row reads all of it: one pair of
+    // loads is on its way while the last is counted
+    const int before = (int)((uintptr_t)history % 16 / 4);
+    auto load = [&](int i) {
+      int4 t = {-1, -1, -1, -1};
+      if (i >= 0 && i + 4 <= length) {
+        t = *(const int4*)(history + i);
+      } else if (i + 4 > 0 && i < length) {
+        if (i >= 0) t.x = history[i];
+        if (i + 1 >= 0 && i + 1 < length) t.y = history[i + 1];
+        if (i + 2 >= 0 && i + 2 < length) t.z = history[i + 2];
+        if (i + 3 < length) t.w = history[i + 3];
+      }
+      return t;
+    };
+    constexpr int kStep = 4 * kRowThreads;
+    int i0 = 4 * (int)threadIdx.x - before;
+    int4 a = load(i0), b = load(i0 + kStep);  // while the words are cleared and the biases entered
     __syncthreads();
-  }
-  if (r.history) {
-    if (r.repetition) o.repetition = r.repetition[row];
-    if (r.presence) o.presence = r.presence[row];
-    if (r.frequency) o.frequency = r.frequency[row];
-    const int len = min(r.length[row], r.history_width);
-    const int read = r.prompt_len ? r.prompt_len[row] : 0;
-    const int32_t* h = r.history + row * r.history_stride;
-    for (int i = threadIdx.x; i < len; i += kRowThreads) {
-      const unsigned at = place(h[i]);
-      if (at < kStretch) {
-        if (i < read)
-          atomicOr(&word[at], kRead);
-        else
-          atomicAdd(&word[at], 1u);
+    if (n_bias > 0) {
+      for (int j = threadIdx.x; j < n_bias; j += kRowThreads) {
+        const unsigned at = (unsigned)(bias_token[j] - e0);
+        if (at < span) atomicMax(&word[at], (uint32_t)(j + 1) << kBiasShift);
       }
     }
+    __syncthreads();  // a maximum with what is counted already would not be one of entries
+    // without a branch: of a warp's tokens hardly ever none is in the stretch
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(word);
+    auto add = [&](int token) {
+      const uint32_t at = (uint32_t)(token - e0);
+      asm volatile("{.reg .pred p;\n\tsetp.lt.u32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;}" ::"r"(at), "r"(span), "r"(base + 4 * at) : "memory");
+    };
+    auto see = [&](int token) {
+      const uint32_t at = (uint32_t)(token - e0);
+      asm volatile("{.reg .pred p;\n\tsetp.lt.u32 p, %0, %1;\n\t@p red.shared.or.b32 [%2], %3;}" ::"r"(at), "r"(span), "r"(base + 4 * at), "r"(kRead) : "memory");
+    };
+    auto count4 = [&](int i, const int4& t) {
+      if (i >= read) {
+        add(t.x), add(t.y), add(t.z), add(t.w);
+      } else if (i + 4 <= read) {
+        see(t.x), see(t.y), see(t.z), see(t.w);
+      } else {
+        see(t.x);
+        i + 1 < read ? see(t.y) : add(t.y);
+        i + 2 < read ? see(t.z) : add(t.z);
+        add(t.w);
+      }
+    };
+    while (i0 < length) {
+      const int4 a2 = load(i0 + 2 * kStep), b2 = load(i0 + 3 * kStep);
+      count4(i0, a);
+      if (i0 + kStep < length) count4(i0 + kStep, b);
+      a = a2, b = b2;
+      i0 += 2 * kStep;
+    }
     __syncthreads();
   }
-  return o;
-}
+};
 
+// Few tokens have a word: 3 of 100 after 4000 tokens of 131072, but hardly a warp has none among its 256.  So every thread takes
+// its own words one after the other, and the warp as many turns as the lane that has the most, where adjusting
+// all places of a load with a word in it took 900 instructions a thread (256 rows, all rules: 75 us; so KKK).
 // Each operation is rounded by itself: the same logits give the same adjusted ones wherever they are adjusted.
 __device__ inline float adjusted(const RowRules& o, float x, uint32_t word) {
   if (word & (kTimes | kRead)) {
@@ -96,49 +144,46 @@ struct RowOf {
   __device__ int token(int vec) const { return vec * kVec - shift; }  // of a load's first place
   __device__ bool whole(int e) const { return e >= 0 && e + kVec <= n_vocab; }
   // Load `vec` of the row; places that are no token are -infinity.
-  __device__ void load(int vec, float* x) const {
+  __device__ Pack<T, kVec> load(int vec) const {
     const int e = token(vec);
-    if (whole(e)) {
-      const Pack<T, kVec> v = *(const Pack<T, kVec>*)(first + e);
+    if (whole(e)) return *(const Pack<T, kVec>*)(first + e);
+    Pack<T, kVec> v;
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) x[j] = to_float(v.v[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) x[j] = (unsigned)(e + j) < (unsigned)n_vocab ? to_float(first[e + j]) : -INFINITY;
-    }
+    for (int j = 0; j < kVec; ++j) v.v[j] = (unsigned)(e + j) < (unsigned)n_vocab ? first[e + j] : from_float<T>(-INFINITY);
+    return v;
   }
-  // A load's values adjusted; `word` are its places', or null.
-  __device__ void adjust(const RowRules& o, int vec, const uint32_t* word, float* x) const {
+  __device__ void load(int vec, float* x) const {
+    const Pack<T, kVec> v = load(vec);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) x[j] = to_float(v.v[j]);
+  }
+  // Which of a load's places the row's mask allows, one bit each.
+  __device__ uint32_t allowed(const uint32_t* mask, int vec) const {
     const int e = token(vec);
-    if (word) {
-      alignas(16) uint32_t w[kVec];
-      uint32_t any = 0;
+    if (whole(e)) return __funnelshift_r(mask[e >> 5], mask[(e + kVec - 1) >> 5], e & 31);
+    uint32_t bits = 0;
 #pragma unroll
-      for (int j = 0; j < kVec; j += 4) *(uint4*)(w + j) = *(const uint4*)(word + j);
+    for (int j = 0; j < kVec; ++j)
+      if ((unsigned)(e + j) < (unsigned)n_vocab) bits |= (mask[(e + j) >> 5] >> ((e + j) & 31) & 1) << j;
+    return bits;
+  }
+  // Which of a load's words there is anything in, one bit each.
+  __device__ static uint32_t worded(const uint32_t* word) {
+    uint32_t bits = 0;
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) any |= w[j];
-      if (any) {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) x[j] = adjusted(o, x[j], w[j]);
-      }
+    for (int j = 0; j < kVec; j += 4) {
+      const uint4 w = *(const uint4*)(word + j);
+      bits |= (w.x ? 1u : 0u) << j | (w.y ? 2u : 0u) << j | (w.z ? 4u : 0u) << j | (w.w ? 8u : 0u) << j;
     }
-    if (o.mask) {
-      uint32_t bits = 0;
-      if (whole(e)) {
-        bits = __funnelshift_r(o.mask[e >> 5], o.mask[(e + kVec - 1) >> 5], e & 31);
-      } else {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j)
-          if ((unsigned)(e + j) < (unsigned)n_vocab) bits |= (o.mask[(e + j) >> 5] >> ((e + j) & 31) & 1) << j;
-      }
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        if (!(bits >> j & 1)) x[j] = -INFINITY;
-    }
+    return bits;
   }
 };
 
-// Stretches of a row, wherever it begins.
-inline int stretches(int n_vocab, int vec) { return (n_vocab + vec - 1 + kStretch - 1) / kStretch; }
+// Stretches of any of the rows.
+inline int stretches(const hx_logits& x, int places = kStretch) {
+  const int size = x.dtype == HX_F32 ? 4 : 2;
+  const bool even = (uintptr_t)x.x % 16 == 0 && (x.n_rows == 1 || x.stride * size % 16 == 0);  // all begin at a boundary
+  return (x.n_vocab + (even ? 0 : 16 / size - 1) + places - 1) / places;
+}
 
 }  // namespace hx

@@ -179,18 +179,30 @@ __global__ void __launch_bounds__(kRowThreads) hx_sample_scan(const hx_logits in
   float x[kEach];
 #pragma unroll
   for (int u = 0; u < kEach / kVec; ++u) from.load(p0 / kVec + u * kRowThreads + t, x + u * kVec);
-  const RowRules o = begin_row(r, row, p0, from.shift, in.n_vocab, word);
+  const RowRules o(r, row);
+  if (kWords) o.count<kStretch>(p0, from.shift, in.n_vocab, word);
   auto token = [&](int i) { return from.token(p0 / kVec + i / kVec * kRowThreads + t) + i % kVec; };  // of x[i]
   float best = -INFINITY;
   int best_e = 0, count = 0;
   bool nan = false;
 #pragma unroll
   for (int u = 0; u < kEach / kVec; ++u) {
-    const int i = u * kRowThreads + t;
-    from.adjust(o, p0 / kVec + i, kWords ? word + i * kVec : nullptr, x + u * kVec);
+    const int i = u * kRowThreads + t, vec = p0 / kVec + i;
+    if (kWords && from.token(vec) < in.n_vocab) {
+      const uint32_t worded = R::worded(word + i * kVec);
+      for (uint32_t rest = worded; rest; rest &= rest - 1) {
+        const int j = i * kVec + __ffs(rest) - 1, e = p0 + j - from.shift;
+        word[j] = __float_as_uint(adjusted(o, to_float(from.first[e]), word[j]));
+      }
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (worded >> j & 1) x[u * kVec + j] = __uint_as_float(word[i * kVec + j]);
+    }
+    const uint32_t bits = o.mask ? from.allowed(o.mask, vec) : ~0u;
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
       float& v = x[u * kVec + j];
+      if (!(bits >> j & 1)) v = -INFINITY;
       if (v != v) nan = true, v = -INFINITY;
       v = clean(v);
       if (v > best) best = v, best_e = token(u * kVec + j);
@@ -663,7 +675,7 @@ bool may_cut(const hx_pick& p) { return p.noise && (p.top_k || p.top_p || p.min_
 // The parts of a call's workspace.
 Work work_of(const hx_logits& x, const hx_rules& r, const hx_pick& p, void* at) {
   const int vec = x.dtype == HX_F32 ? 4 : 8;
-  const int64_t blocks = (int64_t)x.n_rows * stretches(x.n_vocab, vec);
+  const int64_t blocks = (int64_t)x.n_rows * stretches(x);
   Work w = {};
   char* base = (char*)at;
   auto part = [&](int64_t bytes) {
@@ -684,7 +696,7 @@ Work work_of(const hx_logits& x, const hx_rules& r, const hx_pick& p, void* at) 
 template <class T>
 cudaError_t sample_typed(const hx_logits& x, const hx_rules& r, const hx_pick& p, cudaStream_t s) {
   const Work w = work_of(x, r, p, p.workspace);
-  const int blocks = stretches(x.n_vocab, RowOf<T>::kVec);
+  const int blocks = stretches(x);
   const unsigned grid = (unsigned)x.n_rows * blocks;
   if (r.history || r.bias_start)
     hx_sample_scan<T, true><<<grid, kRowThreads, 0, s>>>(x, r, p, w, blocks);
