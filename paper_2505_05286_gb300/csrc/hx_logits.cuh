@@ -57,8 +57,8 @@ struct RowRules {
     const unsigned span = (unsigned)max(min(kPlaces - at0, n_vocab - e0), 0);
     word += at0;
 #pragma unroll
-    for (int i = 0; i < kPlaces / kRowThreads / 4; ++i)
-      if (4 * i * kRowThreads < (int)span + at0) ((uint4*)(word - at0))[threadIdx.x + i * kRowThreads] = uint4{0, 0, 0, 0};
+    for (int i = 4 * (int)threadIdx.x; i < kPlaces; i += 4 * kRowThreads)
+      if (i - 4 * (int)threadIdx.x < (int)span + at0) *(uint4*)(word - at0 + i) = uint4{0, 0, 0, 0};
     // 16 bytes a load from the boundary at or before the row's first entry, every block of the row reads all of it: one pair of
     // loads is on its way while the last is counted
     const int before = (int)((uintptr_t)history % 16 / 4);

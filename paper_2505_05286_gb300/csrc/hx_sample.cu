@@ -4,15 +4,20 @@
 // token is the winner of a race within it: the largest x / T - log(e), e exponential, wins in
 // proportion to exp(x / T).  Two launches:
 //
-//   scan   blocks of 512 threads have 8192 logits each, 16 in a thread's registers, read once.  Each finds its stretch's first
-//          token, the sum of its weights and, where nothing is filtered, the race's winner; where something is, it counts its tokens
-//          and sums their weights in bins of 1/16 of x / T;
-//   pick   a block for each row adds up the stretches.  From the bins it sees how far down the order the filters can
-//          reach: the tokens of those bins are read again, sorted, cut exactly where the filters say, and raced.  Where they
-//          are too many for one list, the last bin is cut by its keys until what is left fits, and the race reads the row.
+//   scan   blocks of 512 threads have 8192 logits each, 16 in a thread's registers, read once.  Every warp's 512 tokens, a segment, leave their
+//          first token, the sum of their weights and their race's winner, whether the filters leave it or not; where filters go by
+//          the order, a block counts its tokens or sums their weights in bins of 1/16 of x / T;
+//   pick   a block for each row adds up the segments.  From the bins it sees which tokens the filters leave for sure: those of
+//          the bins before the one in which a filter ends.  The best of the segments' winners that are left for sure is nearly the row's: only
+//          the few segments whose winner scores more, or as much but for rounding, can hold a better one, and are read again.
+//
+// Where the race turns on a token of the bin in which a filter ends, or no winner is left for sure, that bin is resolved: all tokens
+// down to it are sorted and cut exactly where the filters say, and raced; where they are too many for one list,
+// the bin is cut by its keys until what is left fits, and the race reads the row.
 //
 // Sums that decide where an order is cut are of whole numbers, so that no order of additions is of matter;
-// those of the log-probability are 32-bit sums of 16 weights, added up in a fixed order.
+// those of the log-probability are 32-bit sums in a fixed order, without the first token, whose
+// weight is 1: the logarithm of a share near 1 keeps its bits.
 #include <algorithm>
 
 #include "hx_logits.cuh"
@@ -24,33 +29,37 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int kWarps = kRowThreads / 32;
-constexpr int kBins = kRowThreads;     // a thread each
+constexpr int kSegment = kStretch / kWarps;  // places of a warp
+constexpr int kBins = kRowThreads;           // a thread each
 constexpr float kBinsPerUnit = 16.f;
-constexpr int kWeightBits = 18;        // a weight within its bin: 8192 of them stay below 2^32
-constexpr int kList = 2048;            // tokens of a row that are sorted at once
+constexpr int kWeightBits = 18;              // a weight within its bin: 8192 of them stay below 2^32
+constexpr int kList = 2048;                  // tokens of a row that are sorted at once
 constexpr int kMaxStretches = 64;
+constexpr int kMostAgain = 64;               // segments that are read again before the filters are resolved
 static_assert((HX_MAX_VOCAB + 8 + kStretch - 1) / kStretch <= kMaxStretches, "stretches of a row");
 static_assert(kList % kRowThreads == 0, "tokens of a list by threads");
 
-// What a stretch's block leaves for the row's.
-struct alignas(16) Record {
-  u64 top;       // key of its first token, 0: no token takes part
-  float sum;     // weights, of its first token's
-  int nan;
-  int token;     // the race's winner, -1: none
-  float token_x;
-  int count;     // tokens that take part
-  int k;         // the row's parameters, as this block read them
+struct Pick {
+  int k;
   float T, p, m;
+  __device__ bool by_order() const { return T > 0.f && (k > 0 || p < 1.f); }
+};
+
+// What a warp leaves of its segment.
+struct alignas(16) Segment {
+  u64 top;         // key of its first token, 0: no token takes part
+  float sum;       // the other tokens' weights, of the first one's; NaN if a logit is
+  float score;     // the race's best, in units of log 2, of the first token's weight
+  int token;       // that has it
+  float token_x;
+  unsigned count;  // tokens in the warp's 32nd part of its block's bins
   int pad;
 };
 
 struct Work {
-  Record* record;     // [rows][stretches]
-  unsigned* bin_n;    // [rows][stretches][kBins]: tokens, and sums of their weights
-  unsigned* bin_w;
-  float* x;           // [rows][places] adjusted logits, or null: the row's own
-  int places;
+  Segment* segment;   // [rows][stretches][kWarps]
+  Pick* pick;         // [rows] the parameters as the scan read them
+  unsigned* bins;     // [rows][stretches][2][kBins]: tokens, and sums of their weights
   int64_t bytes;
 };
 
@@ -69,9 +78,17 @@ __device__ u64 key_of(double x) {
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
+// 32-bit numbers in the order of whole ones; of NaN the result is of no matter.
+__device__ uint32_t order(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ float unorder(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+
 __device__ u64 warp_max(u64 x) {
-  for (int d = 16; d; d /= 2) x = max(x, __shfl_xor_sync(~0u, x, d));
-  return x;
+  const uint32_t hi = __reduce_max_sync(~0u, (uint32_t)(x >> 32));
+  const uint32_t lo = __reduce_max_sync(~0u, (uint32_t)(x >> 32) == hi ? (uint32_t)x : 0u);
+  return (u64)hi << 32 | lo;
 }
 __device__ float warp_sum(float x) {
   for (int d = 16; d; d /= 2) x = __fadd_rn(x, __shfl_xor_sync(~0u, x, d));
@@ -86,6 +103,13 @@ __device__ u64 block_max(u64 x, u64* room) {
   __syncthreads();
   return warp_max(room[threadIdx.x % kWarps]);
 }
+__device__ float block_max(float x, uint32_t* room) {
+  const uint32_t u = __reduce_max_sync(~0u, order(x));
+  __syncthreads();
+  if (threadIdx.x % 32 == 0) room[threadIdx.x / 32] = u;
+  __syncthreads();
+  return unorder(__reduce_max_sync(~0u, room[threadIdx.x % kWarps]));
+}
 __device__ float block_sum(float x, float* room) {
   x = warp_sum(x);
   __syncthreads();
@@ -93,6 +117,13 @@ __device__ float block_sum(float x, float* room) {
   __syncthreads();
   const float y = threadIdx.x % 32 < kWarps ? room[threadIdx.x % kWarps] : 0.f;
   return warp_sum(y);
+}
+__device__ unsigned block_sum_int(unsigned x, uint32_t* room) {
+  x = __reduce_add_sync(~0u, x);
+  __syncthreads();
+  if (threadIdx.x % 32 == 0) room[threadIdx.x / 32] = x;
+  __syncthreads();
+  return __reduce_add_sync(~0u, threadIdx.x % 32 < kWarps ? room[threadIdx.x % kWarps] : 0u);
 }
 // The sum over the threads before this one.
 template <class N>
@@ -115,174 +146,233 @@ __device__ N block_before(N x, N* room) {
   return (warp > 0 ? before : N(0)) + in - x;
 }
 
-// x / T below that of the row's (or stretch's) first token.
-struct Scale {
-  float top, T, inv, inv_bin;
-  float zero = 0.f;   // where the grid of bins begins
-  __device__ Scale(float top, float t) : top(top), T(t > 0.f ? t : 1.f) {
-    inv = 1.f / T;
-    inv_bin = kBinsPerUnit / T;
-  }
-  // Whether the grid has steps of 1 / 2 at least where the first token is.
-  __device__ bool fine() const { return fabsf(top * inv_bin) < 4e6f; }
-  __device__ float below(float x) const { return x == top ? 0.f : fmaxf(__fmul_rn(__fsub_rn(x, top), inv), -1e30f); }
-  __device__ float weight(float x) const { return exp2f(__fmul_rn(below(x), 1.44269504f)); }
-  // Bins lie on a grid of x / T that is the same for all stretches of a row: what lies between two numbers' bins is the
-  // same from either.  The last bin holds all that is further down.
-  __device__ float grid(float x) const { return floorf(__fmul_rn(__fsub_rn(x, zero), inv_bin)); }
-  __device__ int bin(float x) const { return x == top ? 0 : (int)fminf(__fsub_rn(grid(top), grid(x)), (float)(kBins - 1)); }
-  // The weight within its bin, of that of the bin's upper edge; the last bin's tokens, all below e^-31 of the first's, have none.
-  __device__ unsigned share(float x, int bin) const {
-    const float z = __fsub_rn(x, zero), y = __fmul_rn(z, inv_bin), rest = __fmaf_rn(z, inv_bin, -y);
-    const float down = fminf(fmaxf(__fsub_rn(__fsub_rn(__fadd_rn(floorf(y), 1.f), y), rest), 0.f), 1.f);
-    return bin < kBins - 1 ? __float2uint_rn(exp2f(__fmul_rn(down, -1.44269504f / kBinsPerUnit)) * (float)(1 << kWeightBits)) : 0u;
-  }
-  __device__ u64 exact(float x, float e) const {
-    const double z = x == top ? 0. : ((double)x - (double)top) / (double)T;
-    return key_of(z - log((double)e));
-  }
-  // The same in 32 bits; a number that is not fit never wins, nor what weighs nothing beside an infinite logit.
-  __device__ float score(float x, float e) const {
-    return e > 0.f && e < INFINITY && (x == top || top < INFINITY) ? __fsub_rn(below(x), logf(e)) : -INFINITY;
-  }
-  // Scores in 32 bits are off by less than this difference; those so near the largest are formed in 64.
-  __device__ static float near(float best) { return best - (2e-4f + fabsf(best) * 0x1p-19f); }
-};
-
-struct Pick {
-  int k;
-  float T, p, m;
-  __device__ bool cut() const { return T > 0.f && (k > 0 || p < 1.f || m > 0.f); }
-};
-
 __device__ float clean(float x) { return __fadd_rn(x, 0.f); }  // -0 is 0
 
+// 2^x and log2(x) of the special function unit: 2^-22 relative, and 2^-22 relative or absolute near 1.
+__device__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ float log2_fast(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Scores in 32 bits, in units of log 2.  Those near the largest are off by less than a third of this difference: four roundings of
+// a difference of logits over T, which is at most the score and the logarithm of a 32-bit number (150), and the logarithm's.
+__device__ float near_score(float best) { return best - (3e-4f + fabsf(best) * 0x1p-19f); }
+
+// x / T below that of the row's (or segment's) first token.
+struct Scale {
+  float top, T, unit, inv_bin;
+  float zero = 0.f;   // where the grid of bins begins
+  float first;        // the first token's place on it
+  int first_bin;
+  static constexpr float kMagic = 12582912.f;  // 1.5 * 2^23: added, the bits below the point are gone, to the nearest
+
+  __device__ Scale(float top, float t) : top(top), T(t > 0.f ? t : 1.f) {
+    // within what keeps products with 0 and infinity what they should be
+    unit = fminf(fmaxf(1.44269504f / T, 0x1p-149f), 1e30f);
+    inv_bin = kBinsPerUnit / T;
+    begin(0.f);
+  }
+  __device__ void begin(float at) {
+    zero = at;
+    first = __fmul_rn(__fsub_rn(top, zero), inv_bin);
+    first_bin = __float_as_int(__fadd_rn(first, kMagic));
+  }
+  // Whether the grid has steps of 1 / 2 at least where the first token is.
+  __device__ bool fine() const { return fabsf(first) < 4e6f; }
+  // log2 of the weight
+  __device__ float below(float x) const { return x == top ? 0.f : __fmul_rn(__fsub_rn(x, top), unit); }
+  // Bins lie on a grid of x / T that is the same for all stretches of a row, of its whole numbers of 1 / kBinsPerUnit and what
+  // rounds to them: what lies between two numbers' bins is the same from either.  The last bin holds all that is further down.
+  // `share`: the weight within its bin, of that of the bin's middle, in 1 / 2^kWeightBits; the last bin's tokens, all below e^-31 of the
+  // first's, have none.
+  __device__ int bin(float x, unsigned* share = nullptr) const {
+    const float z = __fsub_rn(x, zero), y = __fmul_rn(z, inv_bin), rest = __fmaf_rn(z, inv_bin, -y);
+    const float m = __fadd_rn(fmaxf(y, first - 600.f), kMagic);
+    // whatever a number that is none makes of the difference, it is a bin
+    const int b = x == top ? 0 : top < INFINITY ? (int)min((unsigned)first_bin - (unsigned)__float_as_int(m), (unsigned)(kBins - 1)) : kBins - 1;
+    if (share) {
+      // exp(d), |d| <= 1 / 32: the series to its third power, 2^-24 of it; of no number (the first token's at an infinite T): 1
+      const float off = __fadd_rn(__fsub_rn(y, __fsub_rn(m, kMagic)), rest) * (1.f / kBinsPerUnit);
+      const float d = fminf(fmaxf(off, -0.04f), 0.04f);
+      const float f = __fmaf_rn(d, __fmaf_rn(d, __fmaf_rn(d, 1.f / 6, 0.5f), 1.f), 1.f);
+      *share = b < kBins - 1 ? __float_as_uint(__fmaf_rn(f, (float)(1 << kWeightBits), 8388608.f)) & 0x7fffffu : 0u;
+    }
+    return b;
+  }
+  __device__ unsigned share(float x) const {
+    unsigned s;
+    bin(x, &s);
+    return s;
+  }
+  // A score in 32 bits, in units of log 2; a number that is not fit never wins, nor what weighs nothing beside an infinite logit.
+  __device__ float score(float x, float e) const {
+    const float s = __fsub_rn(below(x), log2_fast(e));
+    return e > 0.f && e < INFINITY && (x == top || top < INFINITY) ? s : -INFINITY;
+  }
+};
+
+// The score that decides, in 64 bits.  (Not inline: few calls, many registers.)
+__device__ __noinline__ u64 exact_score(float top, float T, float x, float e) {
+  const double z = x == top ? 0. : ((double)x - (double)top) / (double)T;
+  return key_of(z - log((double)e));
+}
+
 template <class T, bool kWords>
-__global__ void __launch_bounds__(kRowThreads) hx_sample_scan(const hx_logits in, const hx_rules r, const hx_pick p, const Work w, int blocks) {
+__global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits in, const hx_rules r, const hx_pick p, const Work w, int blocks) {
   __shared__ alignas(16) uint32_t word[kWords ? kStretch : 4];
-  __shared__ alignas(16) u64 room[kWarps];
-  __shared__ alignas(16) float room_f[kWarps];
-  __shared__ int room_n[kWarps];
   __shared__ unsigned bin_n[kBins], bin_w[kBins];
+  __shared__ uint32_t warp_top[kWarps];
   __shared__ Pick s_pick;
   using R = RowOf<T>;
   constexpr int kVec = R::kVec;
-  const int row = blockIdx.x / blocks, stretch = blockIdx.x - row * blocks, p0 = stretch * kStretch, t = threadIdx.x;
+  const int row = blockIdx.x / blocks, stretch = blockIdx.x - row * blocks, p0 = stretch * kStretch;
+  const int t = threadIdx.x, lane = t % 32, warp = t / 32;
   if (t == 0) {
-    s_pick.k = p.top_k ? p.top_k[row] : p.all_top_k;
-    s_pick.T = !p.noise ? 0.f : p.temperature ? p.temperature[row] : p.all_temperature;
-    s_pick.p = p.top_p ? p.top_p[row] : p.all_top_p;
-    s_pick.m = p.min_p ? p.min_p[row] : p.all_min_p;
+    Pick a;
+    a.k = p.top_k ? p.top_k[row] : p.all_top_k;
+    a.T = !p.noise ? 0.f : p.temperature ? p.temperature[row] : p.all_temperature;
+    a.p = p.top_p ? p.top_p[row] : p.all_top_p;
+    a.m = p.min_p ? p.min_p[row] : p.all_min_p;
+    s_pick = a;
+    if (stretch == 0) w.pick[row] = a;
   }
   bin_n[t] = bin_w[t] = 0;
   const R from(in, row);
-  float x[kEach];
+  // a warp's places are one after the other; load u of a lane is at place(u) of the stretch
+  auto place = [&](int u) { return warp * kSegment + (u * 32 + lane) * kVec; };
+  Pack<T, kVec> raw[kEach / kVec];
 #pragma unroll
-  for (int u = 0; u < kEach / kVec; ++u) from.load(p0 / kVec + u * kRowThreads + t, x + u * kVec);
+  for (int u = 0; u < kEach / kVec; ++u) raw[u] = from.load((p0 + place(u)) / kVec);
   const RowRules o(r, row);
-  if (kWords) o.count<kStretch>(p0, from.shift, in.n_vocab, word);
-  auto token = [&](int i) { return from.token(p0 / kVec + i / kVec * kRowThreads + t) + i % kVec; };  // of x[i]
-  float best = -INFINITY;
-  int best_e = 0, count = 0;
-  bool nan = false;
+  if (kWords)
+    o.count<kStretch>(p0, from.shift, in.n_vocab, word);
+  else
+    __syncthreads();
+  const Pick pick = s_pick;
+  float x[kEach], top = -INFINITY;
 #pragma unroll
   for (int u = 0; u < kEach / kVec; ++u) {
-    const int i = u * kRowThreads + t, vec = p0 / kVec + i;
+    const int at = place(u), vec = (p0 + at) / kVec;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) x[u * kVec + j] = to_float(raw[u].v[j]);
     if (kWords && from.token(vec) < in.n_vocab) {
-      const uint32_t worded = R::worded(word + i * kVec);
+      const uint32_t worded = R::worded(word + at);
       for (uint32_t rest = worded; rest; rest &= rest - 1) {
-        const int j = i * kVec + __ffs(rest) - 1, e = p0 + j - from.shift;
+        const int j = at + __ffs(rest) - 1, e = p0 + j - from.shift;
         word[j] = __float_as_uint(adjusted(o, to_float(from.first[e]), word[j]));
       }
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        if (worded >> j & 1) x[u * kVec + j] = __uint_as_float(word[i * kVec + j]);
+        if (worded >> j & 1) x[u * kVec + j] = __uint_as_float(word[at + j]);
     }
-    const uint32_t bits = o.mask ? from.allowed(o.mask, vec) : ~0u;
+    if (o.mask) {
+      const uint32_t bits = from.allowed(o.mask, vec);
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      float& v = x[u * kVec + j];
-      if (!(bits >> j & 1)) v = -INFINITY;
-      if (v != v) nan = true, v = -INFINITY;
-      v = clean(v);
-      if (v > best) best = v, best_e = token(u * kVec + j);
-      count += v > -INFINITY;
+      for (int j = 0; j < kVec; ++j)
+        if (!(bits >> j & 1)) x[u * kVec + j] = -INFINITY;
     }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) top = fmaxf(top, x[u * kVec + j]);
   }
-  const u64 top = block_max(best > -INFINITY ? key_of(best, best_e) : 0, room);
-  nan = __syncthreads_or(nan);
-  const Pick pick = s_pick;
-  Record* rec = w.record + (int64_t)row * blocks + stretch;
-  const Scale s(x_of(top), pick.T);
-  float sum = 0.f;
-  int token_out = -1;
-  float token_x = 0.f;
-  if (top) {
-    float part = 0.f;
+  top = clean(unorder(__reduce_max_sync(~0u, order(top))));
+  Segment s = {};
+  if (top > -INFINITY) {
+    Scale scale(top, pick.T);
+    float base = top;
+    if (top == INFINITY) {  // beside it the others weigh nothing
+      base = 0.f;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (x[i] > -INFINITY) part += s.weight(x[i]);
-    sum = block_sum(part, room_f);
-    if (pick.cut()) {
+      for (int i = 0; i < kEach; ++i)
+        if (x[i] == x[i]) x[i] = x[i] == INFINITY ? 0.f : -INFINITY;
+    }
+    float part = 0.f;
+    uint32_t ties = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const float weight = exp2_fast(__fmul_rn(__fsub_rn(x[i], base), scale.unit));
+      const bool tie = x[i] == base;
+      part = __fadd_rn(part, tie ? 0.f : weight);
+      ties |= tie ? 1u << i : 0u;
+    }
+    auto token = [&](int i) { return p0 - from.shift + place(i / kVec) + i % kVec; };  // of x[i]
+    const uint32_t first = __reduce_min_sync(~0u, ties ? (uint32_t)token(__ffs(ties) - 1) : ~0u);
+    s.top = key_of(top, (int)first);
+    s.sum = warp_sum(part) + (float)((int)__reduce_add_sync(~0u, (unsigned)__popc(ties)) - 1);
+    s.score = -INFINITY, s.token = -1;
+    if (pick.T > 0.f) {
+      const float* noise = p.noise + row * p.noise_stride - from.shift + p0;  // by place
+      const bool even = ((uintptr_t)noise & 15) == 0;
+      float best = -INFINITY, best_x = 0.f;
+      int best_i = 0;
+#pragma unroll
+      for (int u = 0; u < kEach / 4; ++u) {
+        const int at = place(4 * u / kVec) + 4 * u % kVec;
+        float4 e = {0.f, 0.f, 0.f, 0.f};
+        const int first_token = p0 + at - from.shift;
+        if (even && first_token >= 0 && first_token + 4 <= in.n_vocab) {
+          e = *(const float4*)(noise + at);
+        } else {
+          if ((unsigned)first_token < (unsigned)in.n_vocab) e.x = noise[at];
+          if ((unsigned)(first_token + 1) < (unsigned)in.n_vocab) e.y = noise[at + 1];
+          if ((unsigned)(first_token + 2) < (unsigned)in.n_vocab) e.z = noise[at + 2];
+          if ((unsigned)(first_token + 3) < (unsigned)in.n_vocab) e.w = noise[at + 3];
+        }
+        const float es[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = 4 * u + j;
+          const float f = __fsub_rn(__fmul_rn(__fsub_rn(x[i], base), scale.unit), log2_fast(es[j]));
+          if (es[j] > 0.f && f > best) best = f, best_x = x[i], best_i = i;  // an infinite one's logarithm is infinite too
+        }
+      }
+      const uint32_t most = __reduce_max_sync(~0u, order(best));
+      if (unorder(most) > -INFINITY) {
+        const uint32_t mine = order(best) == most ? (uint32_t)token(best_i) : ~0u, e = __reduce_min_sync(~0u, mine);
+        const int src = __ffs(__ballot_sync(~0u, mine == e)) - 1;
+        s.score = unorder(most), s.token = (int)e, s.token_x = __shfl_sync(~0u, best_x, src);
+        if (top == INFINITY) s.token_x = top;
+      }
+    }
+  } else {
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) nan |= x[i] != x[i];
+    s.sum = __any_sync(~0u, nan) ? NAN : 0.f;
+    s.token = -1;
+  }
+  if (pick.by_order()) {
+    if (lane == 0) warp_top[warp] = order(top);
+    __syncthreads();
+    const Scale scale(unorder(__reduce_max_sync(~0u, warp_top[lane % kWarps])), pick.T);
+    const bool fine = scale.fine(), by_k = pick.k > 0, by_p = pick.p < 1.f;
+    if (top < INFINITY) {  // bins of a row with an infinite logit are not read
 #pragma unroll
       for (int i = 0; i < kEach; ++i)
         if (x[i] > -INFINITY) {
-          const int b = s.bin(x[i]);
-          atomicAdd(&bin_n[b], 1u);
-          const unsigned share = s.share(x[i], b);
-          if (share) atomicAdd(&bin_w[b], share);
+          unsigned share = 0;
+          const int b = fine ? scale.bin(x[i], &share) : kBins - 1;
+          if (by_k) atomicAdd(&bin_n[b], 1u);
+          if (by_p && share) atomicAdd(&bin_w[b], share);
         }
-      for (int d = 16; d; d /= 2) count += __shfl_xor_sync(~0u, count, d);
-      if (t % 32 == 0) room_n[t / 32] = count;
-      __syncthreads();
-      const int64_t at = ((int64_t)row * blocks + stretch) * kBins + t;
-      w.bin_n[at] = bin_n[t], w.bin_w[at] = bin_w[t];
-      count = 0;
-      for (int i = 0; i < kWarps; ++i) count += room_n[i];
-    } else if (pick.T > 0.f) {
-      const float* noise = p.noise + row * p.noise_stride;
-      float e[kEach], fast = -INFINITY;
+    } else if (by_k) {
+      int n = 0;
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) e[i] = x[i] > -INFINITY ? noise[token(i)] : 0.f;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) fast = fmaxf(fast, s.score(x[i], e[i]));
-      const u64 all = block_max(fast > -INFINITY ? key_of(fast, 0) : 0, room);
-      if (all) {
-        const float near = Scale::near(x_of(all));
-        u64 mine = 0;
-        int mine_e = 0;
-        float mine_x = 0.f;
-        if (fast >= near) {
-#pragma unroll 1
-          for (int i = 0; i < kEach; ++i) {
-            // by its place again: an index that is not known when compiled would put x and e in memory
-            float v = x[0], f = e[0];
-#pragma unroll
-            for (int j = 1; j < kEach; ++j)
-              if (i == j) v = x[j], f = e[j];
-            if (s.score(v, f) < near) continue;
-            const u64 key = s.exact(v, f);
-            if (key > mine) mine = key, mine_e = token(i), mine_x = v;
-          }
-        }
-        const u64 high = block_max(mine, room);
-        const u64 low = block_max(mine && mine == high ? (u64)(uint32_t)~mine_e << 32 | __float_as_uint(mine_x) : 0, room);
-        token_out = (int)~(uint32_t)(low >> 32), token_x = __uint_as_float((uint32_t)low);
-      }
+      for (int i = 0; i < kEach; ++i) n += x[i] > -INFINITY;
+      atomicAdd(&bin_n[kBins - 1], (unsigned)n);
     }
+    __syncthreads();
+    unsigned* bins = w.bins + ((int64_t)row * blocks + stretch) * 2 * kBins;
+    if (by_k) bins[t] = bin_n[t];
+    if (by_p) bins[kBins + t] = bin_w[t];
+    s.count = __reduce_add_sync(~0u, bin_n[t]);
   }
-  if (w.x && pick.cut()) {
-    float* to = w.x + (int64_t)row * w.places;
-#pragma unroll
-    for (int u = 0; u < kEach / 4; ++u) {
-      const int at = p0 + (u * 4 / kVec * kRowThreads + t) * kVec + u * 4 % kVec;
-      if (at < w.places) *(float4*)(to + at) = float4{x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]};
-    }
-  }
-  if (t == 0) {
-    Record c = {top, sum, nan, token_out, token_x, count, pick.k, pick.T, pick.p, pick.m, 0};
-    *rec = c;
-  }
+  if (lane == 0) w.segment[((int64_t)row * blocks + stretch) * kWarps + warp] = s;
 }
 
 // ---------------------------------------------------------------- the row's pick
@@ -293,42 +383,66 @@ struct Shared {
   u64 mass_total;
   u64 border_mass, base_mass;
   float room_f[kWarps];
-  unsigned room_n[kWarps];
+  uint32_t room_n[kWarps];
   unsigned bin_n[kBins], bin_lo[kBins], bin_hi[kBins];
+  uint32_t stretch_top[kMaxStretches];
   int away[kMaxStretches];  // bins from the row's first token to the stretch's, kBins: no token
-  int found, at, last, n_list;
+  int at, last, n_list, unsure;
   unsigned base_count, bin_count;
+  int again[kMostAgain];
 };
 
-// A row's logits, adjusted, as loads of several; f(x, token) for each that takes part.
-template <class T>
+// A row's logits once more, adjusted; f(x, token) for each that takes part.  All threads of the block call.
+template <class T, bool kWords>
 struct RowAgain {
   RowOf<T> row;
-  const float* x;   // adjusted and stored by place, or null
-  int places;
+  RowRules rules;
+  uint32_t* word;
+  int blocks;
+
   template <class F>
-  __device__ void each(int p0, int p1, F f) const {
+  __device__ void stretch(int c, F f) const {
     constexpr int kVec = RowOf<T>::kVec;
-    const int end = min(p1, places);
-    for (int q = p0 + threadIdx.x * kVec; q < end; q += kRowThreads * kVec) {
-      float v[kVec];
-      if (x) {
+    const int p0 = c * kStretch;
+    if (kWords) rules.template count<kStretch>(p0, row.shift, row.n_vocab, word);
+    Pack<T, kVec> raw[kEach / kVec];
 #pragma unroll
-        for (int j = 0; j < kVec; j += 4) {
-          const float4 a = *(const float4*)(x + q + j);
-          v[j] = a.x, v[j + 1] = a.y, v[j + 2] = a.z, v[j + 3] = a.w;
-        }
-      } else {
-        row.load(q / kVec, v);
+    for (int u = 0; u < kEach / kVec; ++u) raw[u] = row.load(p0 / kVec + u * kRowThreads + threadIdx.x);
+#pragma unroll
+    for (int u = 0; u < kEach / kVec; ++u) {
+      const int i = u * kRowThreads + threadIdx.x, vec = p0 / kVec + i;
+      if (row.token(vec) >= row.n_vocab) continue;
+      const uint32_t worded = kWords ? RowOf<T>::worded(word + i * kVec) : 0u, bits = rules.mask ? row.allowed(rules.mask, vec) : ~0u;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        float x = to_float(raw[u].v[j]);
+        if (worded >> j & 1) x = adjusted(rules, x, word[i * kVec + j]);
+        if (bits >> j & 1 && x > -INFINITY) f(clean(x), row.token(vec) + j);
       }
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        if (v[j] > -INFINITY) f(clean(v[j]), q - row.shift + j);
     }
+    if (kWords) __syncthreads();  // the words are the next stretch's
+  }
+  template <class F>
+  __device__ void each(F f) const {
+    for (int c = 0; c < blocks; ++c) stretch(c, f);
+  }
+  // One segment, a place for each thread.
+  template <class F>
+  __device__ void segment(int s, F f) const {
+    const int p0 = s * kSegment;
+    if (kWords) rules.template count<kSegment>(p0, row.shift, row.n_vocab, word);
+    for (int i = threadIdx.x; i < kSegment; i += kRowThreads) {
+      const int e = p0 + i - row.shift;
+      if ((unsigned)e >= (unsigned)row.n_vocab) continue;
+      float x = to_float(row.first[e]);
+      if (kWords && word[i]) x = adjusted(rules, x, word[i]);
+      if ((!rules.mask || rules.mask[e >> 5] >> (e & 31) & 1) && x > -INFINITY) f(clean(x), e);
+    }
+    if (kWords) __syncthreads();
   }
 };
 
-// Smallest number whose share of 2^64 parts p is of `all`: the whole number at or above p * all.
+// The whole number at or above p * all, at least 1.
 __device__ u64 part_of(float p, u64 all) {
   if (!(p > 0.f)) return 1;
   const u64 f = __float2ull_rn(p * 0x1p63f);  // p < 1 has 24 bits: exact above 2^-40
@@ -337,15 +451,19 @@ __device__ u64 part_of(float p, u64 all) {
   return max(up, (u64)1);
 }
 
-template <class T>
+template <class Again>
 struct Picker {
   Shared& s;
   Scale& scale;
-  const RowAgain<T>& row;
+  const Again& row;
   float one;               // 2^shift: weights of 1 / 2^kWeightBits of the first token's bin in whole numbers
 
   __device__ u64 mass_of_bin(int b) const { return __float2ull_rn(exp2f((float)b * (-1.44269504f / kBinsPerUnit)) * one); }
-  __device__ u64 mass(float x, int b) const { return scale.share(x, b) * mass_of_bin(b); }
+  __device__ u64 mass(float x) const {
+    unsigned share;
+    const int b = scale.bin(x, &share);
+    return share * mass_of_bin(b);
+  }
 
   // Adds a token of this weight to a bin of the row's.
   __device__ void count(int bin, unsigned w) {
@@ -363,7 +481,7 @@ struct Picker {
     for (int run = 2; run <= size; run *= 2)
       for (int d = run / 2; d; d /= 2) {
         for (int i = threadIdx.x; i < size / 2; i += kRowThreads) {
-          const int a = i / d * 2 * d + i % d, b = a + d;
+          const int a = (i & ~(d - 1)) * 2 + (i & (d - 1)), b = a + d;
           const u64 x = s.list[a], y = s.list[b];
           if ((x < y) == ((a & run) == 0)) s.list[a] = y, s.list[b] = x;
         }
@@ -371,27 +489,35 @@ struct Picker {
       }
   }
 
-  // Collects the tokens that f holds for.  Returns their number (at most kList are kept).
-  template <class F>
-  __device__ void collect(int p0, int p1, F f) {
-    row.each(p0, p1, [&](float x, int e) {
-      if (f(x, e)) {
-        const int at = atomicAdd(&s.n_list, 1);
-        if (at < kList) s.list[at] = key_of(x, e);
-      }
-    });
+  // Enters a token in the list; at most kList are kept.
+  __device__ void enter(float x, int e) {
+    const int at = atomicAdd(&s.n_list, 1);
+    if (at < kList) s.list[at] = key_of(x, e);
+  }
+  __device__ void clear() {
+    __syncthreads();
+    if (threadIdx.x == 0) s.n_list = 0;
+    __syncthreads();
   }
 
   // The key at which the sum over the order (of tokens, or of their mass) first reaches target, the tokens of bin `bin` being
   // those in question, `base` what is before them.  Leaves the mass up to there in s.border_mass.
-  __device__ u64 border(bool by_mass, u64 target, int bin, unsigned n, u64 base, u64 base_mass) {
+  __device__ u64 border(bool by_mass, u64 target, int bin, u64 base, u64 base_mass) {
     const int t = threadIdx.x;
     u64 lo = 0, hi = ~0ull;
-    for (int turn = 0; n > kList && turn < 16; ++turn) {
+    auto in = [&](float x, u64 key) { return key >= lo && key <= hi && scale.bin(x) == bin; };
+    for (int turn = 0; turn < 16; ++turn) {
+      clear();
+      row.each([&](float x, int e) {
+        if (in(x, key_of(x, e))) enter(x, e);
+      });
+      __syncthreads();
+      if (s.n_list <= kList) break;
+      // narrow the keys to those of the tokens, and cut them in parts
       u64 a = 0, b = 0;  // the largest of ~key and of key
-      row.each(0, row.places, [&](float x, int e) {
+      row.each([&](float x, int e) {
         const u64 key = key_of(x, e);
-        if (key >= lo && key <= hi && scale.bin(x) == bin) a = max(a, ~key), b = max(b, key);
+        if (in(x, key)) a = max(a, ~key), b = max(b, key);
       });
       lo = ~block_max(a, s.room), hi = block_max(b, s.room);
       int shift = 0;
@@ -399,10 +525,9 @@ struct Picker {
       __syncthreads();
       s.bin_n[t] = s.bin_lo[t] = s.bin_hi[t] = 0;
       __syncthreads();
-      row.each(0, row.places, [&](float x, int e) {
+      row.each([&](float x, int e) {
         const u64 key = key_of(x, e);
-        if (key < lo || key > hi || scale.bin(x) != bin) return;
-        count((int)((hi - key) >> shift), scale.share(x, bin));
+        if (in(x, key)) count((int)((hi - key) >> shift), scale.share(x));
       });
       __syncthreads();
       const unsigned mine_n = s.bin_n[t];
@@ -411,25 +536,14 @@ struct Picker {
       if (t == 0) s.at = -1;
       __syncthreads();
       const u64 before = base + (by_mass ? before_w : before_n), mine = by_mass ? mine_w : mine_n;
-      if (before < target && before + mine >= target) {
-        s.at = t, s.bin_count = mine_n, s.base_mass = base_mass + before_w, s.base_count = (unsigned)before_n;
-      }
+      if (before < target && before + mine >= target) s.at = t, s.base_mass = base_mass + before_w, s.base_count = (unsigned)before_n;
       __syncthreads();
       if (s.at < 0) break;  // no token reaches it: cannot be, as the sums are of the same whole numbers
       base = by_mass ? s.base_mass : base + s.base_count, base_mass = s.base_mass;
-      n = s.bin_count;
       hi -= (u64)s.at << shift;
       const u64 least = hi - ((1ull << shift) - 1);
       if (least > lo && least <= hi) lo = least;
-      __syncthreads();
     }
-    if (t == 0) s.n_list = 0;
-    __syncthreads();
-    collect(0, row.places, [&](float x, int e) {
-      const u64 key = key_of(x, e);
-      return key >= lo && key <= hi && scale.bin(x) == bin;
-    });
-    __syncthreads();
     const int m = min(s.n_list, kList);
     sort(m);
     return along(m, by_mass, target, base, base_mass);
@@ -443,8 +557,7 @@ struct Picker {
 #pragma unroll
     for (int j = 0; j < kMine; ++j) {
       const int i = t * kMine + j;
-      const float x = i < m ? x_of(s.list[i]) : 0.f;
-      part[j] = i < m ? mass(x, scale.bin(x)) : 0;
+      part[j] = i < m ? mass(x_of(s.list[i])) : 0;
       sum += part[j];
     }
     u64 w = base_mass + block_before<u64>(sum, s.room);
@@ -463,218 +576,282 @@ struct Picker {
   }
 };
 
-template <class T>
-__global__ void __launch_bounds__(kRowThreads) hx_sample_pick(const hx_logits in, const hx_pick p, const Work w, int blocks) {
+template <class T, bool kWords>
+__global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits in, const hx_rules r, const hx_pick p, const Work w, int blocks) {
+  extern __shared__ __align__(16) uint32_t word[];
   __shared__ Shared s;
-  const int row = blockIdx.x, t = threadIdx.x, lane = t % 32;
-  const Record* rec = w.record + (int64_t)row * blocks;
-  // every warp adds up the stretches by itself
+  const int row = blockIdx.x, t = threadIdx.x;
+  const Segment* seg = w.segment + (int64_t)row * blocks * kWarps;
+  const int n_seg = blocks * kWarps;
+  constexpr int kMine = (kMaxStretches * kWarps + kRowThreads - 1) / kRowThreads;  // segments of a thread
+  const Pick pick = w.pick[row];
+  if (t < kMaxStretches) s.stretch_top[t] = 0;
+  __syncthreads();
+  // add up the segments
   u64 top = 0;
-  bool nan = false;
-  for (int c = lane; c < blocks; c += 32) top = max(top, rec[c].top), nan |= rec[c].nan != 0;
-  top = warp_max(top);
-  nan = __any_sync(~0u, nan);
-  const Pick pick = {rec[0].k, rec[0].T, rec[0].p, rec[0].m};
-  Scale scale(x_of(top), pick.T);
-  const bool cut = top && pick.cut();
-  double sum = 0.;
-  if (t < 32) {
-    for (int c = lane; c < blocks; c += 32)
-      if (rec[c].top) {
-        const float x = x_of(rec[c].top);
-        if (scale.top < INFINITY || x == scale.top) sum += x == scale.top ? (double)rec[c].sum : (double)rec[c].sum * exp(((double)x - (double)scale.top) / (double)scale.T);
-      }
-    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+  int all = 0;
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) {
+    const int i = t + j * kRowThreads;
+    if (i < n_seg) {
+      const u64 k = seg[i].top;
+      top = max(top, k);
+      if (k) atomicMax(&s.stretch_top[i / kWarps], (uint32_t)(k >> 32));
+      if (pick.by_order()) all += (int)seg[i].count;
+    }
   }
-  u64 best = 0;       // the race's best score, in 64 bits
+  top = block_max(top, s.room);
+  Scale scale(x_of(top), pick.T);
+  float part = 0.f, best_mine = -INFINITY;  // of the others' weights
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) {
+    const int i = t + j * kRowThreads;
+    if (i >= n_seg) continue;
+    const Segment g = seg[i];
+    const float x = x_of(g.top);
+    if (!g.top || g.top == top)
+      part += g.sum;
+    else if (scale.top < INFINITY || x == scale.top)
+      part += (g.sum + 1.f) * exp2_fast(scale.below(x));
+    else if (g.sum != g.sum)
+      part += g.sum;
+  }
+  const float others = block_sum(part, s.room_f);
   int token = token_of(top);
   float token_x = scale.top;
   const float* noise = p.noise + row * p.noise_stride;
-  if (cut) {
-    RowAgain<T> again = {RowOf<T>(in, row), w.x ? w.x + (int64_t)row * w.places : nullptr, w.places};
-    Picker<T> a{s, scale, again, 1.f};
-    // bins of the whole row: of its stretches'; where the grid is too coarse for them (T is small), of its tokens', from
-    // the first token down
-    const bool fine = scale.fine();
-    if (t < blocks) {
-      const u64 first = rec[t].top;
-      s.away[t] = !first ? kBins : fine ? scale.bin(x_of(first)) : 0;
-    }
-    s.bin_n[t] = s.bin_lo[t] = s.bin_hi[t] = 0;
-    __syncthreads();
-    unsigned n = 0;
-    u64 sum_w = 0;
-    int all = 0;
-    for (int c = 0; c < blocks; ++c) {
-      const int b = t - s.away[c];
-      if (s.away[c] < kBins) all += rec[c].count;
-      if (fine && b >= 0 && t < kBins - 1) {
-        const int64_t at = ((int64_t)row * blocks + c) * kBins + b;
-        n += w.bin_n[at], sum_w += w.bin_w[at];
-      }
-    }
-    if (!fine) {
-      scale.zero = scale.top;
-      again.each(0, w.places, [&](float x, int e) {
-        const int b = scale.bin(x);
-        a.count(b, scale.share(x, b));
-      });
+  if (top && pick.T > 0.f) {
+    RowAgain<T, kWords> again = {RowOf<T>(in, row), RowRules(r, row), word, blocks};
+    Picker<RowAgain<T, kWords>> a{s, scale, again, 1.f};
+    const float log_least = !(pick.m > 0.f) ? -INFINITY : pick.m < 1.f ? log2f(pick.m) : pick.m > 1.f ? INFINITY : 0.f;
+    const bool by_order = pick.by_order();
+    bool by_k = false, by_p = false;
+    int sure = kBins, out = kBins;  // tokens of bins before `sure` are left, of those behind `out` they are not
+    int bin_k = kBins - 1, bin_p = kBins - 1;
+    unsigned n_before = 0, n = 0;
+    u64 mass = 0, mass_before = 0, total = 0;
+    if (by_order) {
+      all = (int)block_sum_int((unsigned)all, s.room_n);
+      // bins of the whole row: of its stretches'; where the grid is too coarse for them (T is small), of its tokens', from
+      // the first token down
+      const bool fine = scale.fine();
+      if (t < blocks) s.away[t] = !s.stretch_top[t] ? kBins : fine ? scale.bin(clean(unorder(s.stretch_top[t]))) : 0;
+      s.bin_n[t] = s.bin_lo[t] = s.bin_hi[t] = 0;
       __syncthreads();
-      if (t < kBins - 1) n = s.bin_n[t], sum_w = (u64)s.bin_hi[t] << 32 | s.bin_lo[t];
-    }
-    unsigned n_before = block_before<unsigned>(n, s.room_n);
-    if (t == kBins - 1) n = (unsigned)all - n_before;  // all that is further down
-    // as many bits for the sums as fit
-    const float about = block_sum(exp2f((float)t * (-1.44269504f / kBinsPerUnit)) * (float)sum_w, s.room_f);
-    const int bits = min(44, 60 - (int)(__float_as_uint(fmaxf(about, 1.f)) >> 23) + 127);
-    a.one = __uint_as_float((uint32_t)(127 + max(bits, 0)) << 23);
-    const u64 mass = sum_w * a.mass_of_bin(t);
-    const u64 mass_before = block_before<u64>(mass, s.room);
-    if (t == kBins - 1) s.mass_total = mass_before + mass;
-    if (t == 0) s.at = kBins - 1, s.last = kBins - 1;
-    __syncthreads();
-    const u64 total = s.mass_total;
-    const bool by_k = pick.k > 0 && pick.k < all, by_p = pick.p < 1.f;
-    const u64 want = by_p ? min(part_of(pick.p, total), total) : 0;
-    // the bins that k and p end in (p of all mass)
-    if (by_k && n_before < (unsigned)pick.k && n_before + n >= (unsigned)pick.k) s.at = t;
-    if (by_p && mass_before < want && mass_before + mass >= want) s.last = t;
-    __syncthreads();
-    const int bin_k = s.at, bin_p = s.last;
-    int reach = by_k ? bin_k : by_p ? bin_p : kBins - 1;
-    if (pick.m > 0.f && !(by_k && by_p)) {
-      // what has at least m of the first token's weight is no further down than this
-      const float far = -logf(pick.m) * kBinsPerUnit + 3.f;
-      reach = min(reach, far < (float)kBins ? max((int)far, 0) : kBins - 1);
-    }
-    const float log_least = pick.m > 0.f ? logf(pick.m) : -INFINITY;
-    __syncthreads();
-    if (t == reach) s.bin_count = n_before + n;
-    if (t == 0) s.n_list = 0;
-    __syncthreads();
-    float fast = -INFINITY;
-    if (s.bin_count <= kList) {
-      // all that the filters can leave fits the list
-      for (int c = 0; c < blocks; ++c)
-        if (s.away[c] <= reach)
-          a.collect(c * kStretch, (c + 1) * kStretch, [&](float x, int e) { return scale.bin(x) <= reach; });
+      u64 sum_w = 0;
+      if (fine) {
+        const unsigned* bins = w.bins + (int64_t)row * blocks * 2 * kBins;
+        for (int c = 0; c < blocks; ++c) {
+          const int b = t - s.away[c];
+          if (b < 0 || t == kBins - 1) continue;
+          if (pick.k > 0) n += bins[c * 2 * kBins + b];
+          if (pick.p < 1.f) sum_w += bins[(c * 2 + 1) * kBins + b];
+        }
+      } else {
+        scale.begin(scale.top);
+        again.each([&](float x, int) {
+          unsigned share;
+          const int b = scale.bin(x, &share);
+          a.count(b, share);
+        });
+        __syncthreads();
+        if (t < kBins - 1) n = s.bin_n[t], sum_w = (u64)s.bin_hi[t] << 32 | s.bin_lo[t];
+      }
+      n_before = block_before<unsigned>(n, s.room_n);
+      if (t == kBins - 1) n = (unsigned)all - n_before;  // all that is further down
+      // as many bits for the sums as fit
+      const float about = block_sum(exp2f((float)t * (-1.44269504f / kBinsPerUnit)) * (float)sum_w, s.room_f);
+      const int bits = min(44, 60 - (int)(__float_as_uint(fmaxf(about, 1.f)) >> 23) + 127);
+      a.one = __uint_as_float((uint32_t)(127 + max(bits, 0)) << 23);
+      mass = sum_w * a.mass_of_bin(t);
+      mass_before = block_before<u64>(mass, s.room);
+      if (t == kBins - 1) s.mass_total = mass_before + mass;
+      if (t == 0) s.at = kBins - 1;
       __syncthreads();
-      const int m = min(s.n_list, kList);
-      a.sort(m);
-      int left = m;
-      u64 of = total;
-      if (by_k && reach == bin_k) {
-        a.along(m, false, (u64)pick.k, 0, 0);
-        left = s.last, of = s.border_mass;
+      total = s.mass_total;
+      by_k = pick.k > 0 && pick.k < all, by_p = pick.p < 1.f;
+      u64 least = total, most = total;  // mass that p is of
+      auto bin_at = [&](u64 target) {  // where the sum reaches it
         __syncthreads();
-      }
-      if (by_p) {
-        a.along(left, true, min(part_of(pick.p, of), of), 0, 0);
-        left = min(left, s.last);
-        __syncthreads();
-      }
-      constexpr int kMine = kList / kRowThreads;
-      float e[kMine];
-#pragma unroll
-      for (int j = 0; j < kMine; ++j) {
-        const int i = t + j * kRowThreads;
-        e[j] = 0.f;
-        if (i < left) {
-          const float x = x_of(s.list[i]);
-          if (i == 0 || !(scale.below(x) < log_least)) e[j] = noise[token_of(s.list[i])];
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kMine; ++j)
-        if (e[j] != 0.f) fast = fmaxf(fast, scale.score(x_of(s.list[t + j * kRowThreads]), e[j]));
-      const u64 most = block_max(fast > -INFINITY ? key_of(fast, 0) : 0, s.room);
-      if (most) {
-        const float near = Scale::near(x_of(most));
-        u64 mine = 0, at = 0;
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-          if (e[j] == 0.f) continue;
-          const u64 key = s.list[t + j * kRowThreads];
-          if (scale.score(x_of(key), e[j]) < near) continue;
-          const u64 f = scale.exact(x_of(key), e[j]);
-          if (f > mine || (f == mine && (uint32_t)key > (uint32_t)(at >> 32))) mine = f, at = key << 32 | __float_as_uint(x_of(key));
-        }
-        best = block_max(mine, s.room);
-        const u64 low = block_max(mine && mine == best ? at : 0, s.room);
-        token = (int)~(uint32_t)(low >> 32), token_x = __uint_as_float((uint32_t)low);
-      }
-    } else {
-      u64 border = 0, of = total;
-      auto start = [&](int bin) {  // what lies before a bin
-        __syncthreads();
-        if (t == bin) s.bin_count = n, s.base_count = n_before, s.base_mass = mass_before;
-        __syncthreads();
-      };
-      if (by_k) {
-        start(bin_k);
-        const unsigned c = s.bin_count, c0 = s.base_count;
-        const u64 m0 = s.base_mass;
-        border = a.border(false, (u64)pick.k, bin_k, c, c0, m0);
-        of = s.border_mass;
-        __syncthreads();
-      }
-      if (by_p) {
-        const u64 target = min(part_of(pick.p, of), of);
-        if (t == 0) s.at = bin_k;
+        if (t == 0) s.at = kBins - 1;
         __syncthreads();
         if (mass_before < target && mass_before + mass >= target) s.at = t;
         __syncthreads();
-        const int bin = s.at;
-        start(bin);
-        const unsigned c = s.bin_count;
-        const u64 m0 = s.base_mass;
-        border = max(border, a.border(true, target, bin, c, m0, m0));
+        return s.at;
+      };
+      if (by_k) {
+        if (n_before < (unsigned)pick.k && n_before + n >= (unsigned)pick.k) s.at = t, s.base_mass = mass_before, s.border_mass = mass_before + mass;
         __syncthreads();
+        bin_k = s.at, least = s.base_mass, most = s.border_mass;
+        sure = out = bin_k;
       }
-      auto kept = [&](float x, u64 key) { return key >= border && (key == top || !(scale.below(x) < log_least)); };
-      again.each(0, w.places, [&](float x, int e) {
-        if (kept(x, key_of(x, e))) fast = fmaxf(fast, scale.score(x, noise[e]));
-      });
-      const u64 most = block_max(fast > -INFINITY ? key_of(fast, 0) : 0, s.room);
-      if (most) {
-        const float near = Scale::near(x_of(most));
-        u64 mine = 0, at = 0;
-        if (fast >= near)
-          again.each(0, w.places, [&](float x, int e) {
-            if (!kept(x, key_of(x, e)) || scale.score(x, noise[e]) < near) return;
-            const u64 f = scale.exact(x, noise[e]);
-            if (f > mine) mine = f, at = (u64)(uint32_t)~e << 32 | __float_as_uint(x);
-          });
-        best = block_max(mine, s.room);
-        const u64 low = block_max(mine && mine == best ? at : 0, s.room);
-        token = (int)~(uint32_t)(low >> 32), token_x = __uint_as_float((uint32_t)low);
+      if (by_p) {
+        bin_p = bin_at(min(part_of(pick.p, most), most));
+        const int from = by_k ? bin_at(min(part_of(pick.p, least), max(least, (u64)1))) : bin_p;
+        sure = min(sure, from), out = min(out, bin_p);
       }
     }
-  } else if (top && pick.T > 0.f && t < 32) {
-    u64 mine = 0, at = 0;
-    for (int c = lane; c < blocks; c += 32)
-      if (rec[c].token >= 0) {
-        const u64 f = scale.score(rec[c].token_x, noise[rec[c].token]) > -INFINITY ? scale.exact(rec[c].token_x, noise[rec[c].token]) : 0;
-        if (f > mine) mine = f, at = (u64)(uint32_t)~rec[c].token << 32 | __float_as_uint(rec[c].token_x);
+    // 1: the filters leave it, 0: they do not, -1: it is in a bin where they end
+    auto left = [&](float x, u64 key) {
+      if (key == top) return 1;
+      if (scale.below(x) < log_least) return 0;
+      if (!by_order) return 1;
+      const int b = scale.bin(x);
+      return b < sure ? 1 : b > out ? 0 : -1;
+    };
+    float unsure = -INFINITY, score[kMine];
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      const int i = t + j * kRowThreads;
+      score[j] = -INFINITY;
+      if (i >= n_seg) continue;
+      const Segment g = seg[i];
+      if (g.token < 0 || (scale.top == INFINITY && g.token_x < INFINITY)) continue;
+      score[j] = g.score + scale.below(x_of(g.top));
+      const int l = left(g.token_x, key_of(g.token_x, g.token));
+      if (l > 0) best_mine = fmaxf(best_mine, score[j]);
+      if (l < 0) unsure = fmaxf(unsure, score[j]);
+    }
+    const float best = block_max(best_mine, s.room_n);
+    unsure = block_max(unsure, s.room_n);
+    const float near = near_score(best);
+    bool found = best > -INFINITY && unsure < near;
+    u64 mine = 0, mine_at = 0;
+    auto take = [&](float x, int e) {
+      const u64 f = exact_score(scale.top, scale.T, x, noise[e]);
+      if (f > mine || (f == mine && (u64)(uint32_t)~e << 32 > (mine_at | 0xffffffffu))) mine = f, mine_at = (u64)(uint32_t)~e << 32 | __float_as_uint(x);
+    };
+    if (found) {
+      __syncthreads();
+      if (t == 0) s.n_list = 0, s.unsure = 0;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kMine; ++j)
+        if (score[j] >= near) {
+          const int at = atomicAdd(&s.n_list, 1);
+          if (at < kMostAgain) s.again[at] = t + j * kRowThreads;
+        }
+      __syncthreads();
+      const int n_again = s.n_list;
+      found = n_again <= kMostAgain;
+      if (found) {
+        for (int i = 0; i < n_again; ++i)
+          again.segment(s.again[i], [&](float x, int e) {
+            if (scale.score(x, noise[e]) < near) return;
+            const int l = left(x, key_of(x, e));
+            if (l > 0) take(x, e);
+            if (l < 0) s.unsure = 1;
+          });
+        __syncthreads();
+        found = !s.unsure;
       }
-    best = warp_max(mine);
-    const u64 low = warp_max(mine && mine == best ? at : 0);
-    if (best) token = (int)~(uint32_t)(low >> 32), token_x = __uint_as_float((uint32_t)low);
+    }
+    if (!found) {
+      // resolve the filters
+      mine = 0, mine_at = 0;
+      int reach = by_k ? bin_k : by_p ? bin_p : kBins - 1;
+      if (by_order && pick.m > 0.f && !(by_k && by_p)) {
+        // what has at least m of the first token's weight is no further down than this
+        const float far = -log_least * (kBinsPerUnit / 1.44269504f) + 3.f;
+        reach = min(reach, far < (float)kBins ? max((int)far, 0) : kBins - 1);
+      }
+      a.clear();
+      if (t == reach) s.bin_count = by_k ? n_before + n : 0u;
+      __syncthreads();
+      bool listed = by_order && s.bin_count <= kList;
+      if (listed) {
+        // all that the filters can leave, if it fits the list
+        for (int c = 0; c < blocks; ++c)
+          if (s.away[c] <= reach)
+            again.stretch(c, [&](float x, int e) {
+              if (scale.bin(x) <= reach) a.enter(x, e);
+            });
+        __syncthreads();
+        listed = s.n_list <= kList;
+      }
+      float fast = -INFINITY;
+      if (listed) {
+        const int m = s.n_list;
+        a.sort(m);
+        int n_left = m;
+        u64 of = total;
+        if (by_k && reach == bin_k) {
+          a.along(m, false, (u64)pick.k, 0, 0);
+          n_left = s.last, of = s.border_mass;
+          __syncthreads();
+        }
+        if (by_p) {
+          a.along(n_left, true, min(part_of(pick.p, of), of), 0, 0);
+          n_left = min(n_left, s.last);
+          __syncthreads();
+        }
+        constexpr int kOf = kList / kRowThreads;
+        float f[kOf];
+#pragma unroll
+        for (int j = 0; j < kOf; ++j) {
+          const int i = t + j * kRowThreads;
+          f[j] = -INFINITY;
+          if (i < n_left) {
+            const float x = x_of(s.list[i]);
+            if (i == 0 || !(scale.below(x) < log_least)) f[j] = scale.score(x, noise[token_of(s.list[i])]);
+          }
+          fast = fmaxf(fast, f[j]);
+        }
+        const float least = near_score(block_max(fast, s.room_n));
+#pragma unroll
+        for (int j = 0; j < kOf; ++j)
+          if (f[j] > -INFINITY && f[j] >= least) take(x_of(s.list[t + j * kRowThreads]), token_of(s.list[t + j * kRowThreads]));
+      } else {
+        u64 border = 0, of = total;
+        auto start = [&](int bin) {  // what lies before a bin
+          __syncthreads();
+          if (t == bin) s.base_count = n_before, s.base_mass = mass_before;
+          __syncthreads();
+        };
+        if (by_k) {
+          start(bin_k);
+          const u64 c0 = s.base_count, m0 = s.base_mass;
+          border = a.border(false, (u64)pick.k, bin_k, c0, m0);
+          of = s.border_mass;
+          __syncthreads();
+        }
+        if (by_p) {
+          const u64 target = min(part_of(pick.p, of), of);
+          if (t == 0) s.at = bin_k;
+          __syncthreads();
+          if (mass_before < target && mass_before + mass >= target) s.at = t;
+          __syncthreads();
+          const int bin = s.at;
+          start(bin);
+          const u64 m0 = s.base_mass;
+          border = max(border, a.border(true, target, bin, m0, m0));
+          __syncthreads();
+        }
+        auto kept = [&](float x, u64 key) { return key >= border && (key == top || !(scale.below(x) < log_least)); };
+        again.each([&](float x, int e) {
+          if (kept(x, key_of(x, e))) fast = fmaxf(fast, scale.score(x, noise[e]));
+        });
+        const float least = near_score(block_max(fast, s.room_n));
+        again.each([&](float x, int e) {
+          if (fast > -INFINITY && fast >= least && kept(x, key_of(x, e)) && scale.score(x, noise[e]) >= least) take(x, e);
+        });
+      }
+    }
+    const u64 high = block_max(mine, s.room);
+    const u64 low = block_max(mine && mine == high ? mine_at : 0, s.room);
+    if (high) token = (int)~(uint32_t)(low >> 32), token_x = __uint_as_float((uint32_t)low);
   }
   if (t == 0) {
     p.token[row] = top ? token : -1;
     if (p.logprob) {
       const double y = token_x == scale.top ? 0. : ((double)token_x - (double)scale.top) / (double)scale.T;
-      p.logprob[row] = nan ? NAN : top ? (float)(y - log(sum)) : -INFINITY;
+      p.logprob[row] = others != others ? NAN : top ? (float)(y - log1p((double)others)) : -INFINITY;
     }
   }
 }
 
-bool may_cut(const hx_pick& p) { return p.noise && (p.top_k || p.top_p || p.min_p || p.all_top_k > 0 || p.all_top_p < 1.f || p.all_min_p > 0.f); }
-
 // The parts of a call's workspace.
-Work work_of(const hx_logits& x, const hx_rules& r, const hx_pick& p, void* at) {
-  const int vec = x.dtype == HX_F32 ? 4 : 8;
+Work work_of(const hx_logits& x, const hx_pick& p, void* at) {
   const int64_t blocks = (int64_t)x.n_rows * stretches(x);
   Work w = {};
   char* base = (char*)at;
@@ -683,33 +860,34 @@ Work work_of(const hx_logits& x, const hx_rules& r, const hx_pick& p, void* at) 
     w.bytes += (bytes + 255) / 256 * 256;
     return here;
   };
-  w.places = (x.n_vocab + 2 * vec - 2) / vec * vec;
-  w.record = (Record*)part(blocks * (int64_t)sizeof(Record));
-  if (may_cut(p)) {
-    w.bin_n = (unsigned*)part(blocks * kBins * 4);
-    w.bin_w = (unsigned*)part(blocks * kBins * 4);
-    if (r.history || r.bias_start || r.mask) w.x = (float*)part((int64_t)x.n_rows * w.places * 4);
-  }
+  w.segment = (Segment*)part(blocks * kWarps * (int64_t)sizeof(Segment));
+  w.pick = (Pick*)part(x.n_rows * (int64_t)sizeof(Pick));
+  if (p.noise && (p.top_k || p.top_p || p.all_top_k > 0 || p.all_top_p < 1.f)) w.bins = (unsigned*)part(blocks * 2 * kBins * 4);
   return w;
+}
+
+template <class T, bool kWords>
+cudaError_t launch(const hx_logits& x, const hx_rules& r, const hx_pick& p, cudaStream_t s) {
+  const Work w = work_of(x, p, p.workspace);
+  const int blocks = stretches(x);
+  hx_sample_scan<T, kWords><<<(unsigned)x.n_rows * blocks, kRowThreads, 0, s>>>(x, r, p, w, blocks);
+  if (cudaError_t e = cudaGetLastError()) return e;
+  constexpr int kSmem = kWords ? 4 * kStretch : 0;
+  const auto kernel = hx_sample_pick<T, kWords>;
+  if (kWords)
+    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)) return e;
+  kernel<<<x.n_rows, kRowThreads, kSmem, s>>>(x, r, p, w, blocks);
+  return cudaGetLastError();
 }
 
 template <class T>
 cudaError_t sample_typed(const hx_logits& x, const hx_rules& r, const hx_pick& p, cudaStream_t s) {
-  const Work w = work_of(x, r, p, p.workspace);
-  const int blocks = stretches(x);
-  const unsigned grid = (unsigned)x.n_rows * blocks;
-  if (r.history || r.bias_start)
-    hx_sample_scan<T, true><<<grid, kRowThreads, 0, s>>>(x, r, p, w, blocks);
-  else
-    hx_sample_scan<T, false><<<grid, kRowThreads, 0, s>>>(x, r, p, w, blocks);
-  if (cudaError_t e = cudaGetLastError()) return e;
-  hx_sample_pick<T><<<x.n_rows, kRowThreads, 0, s>>>(x, p, w, blocks);
-  return cudaGetLastError();
+  return r.history || r.bias_start ? launch<T, true>(x, r, p, s) : launch<T, false>(x, r, p, s);
 }
 
 }  // namespace
 
-int64_t sample_workspace(const hx_logits& x, const hx_rules& r, const hx_pick& p) { return work_of(x, r, p, nullptr).bytes; }
+int64_t sample_workspace(const hx_logits& x, const hx_pick& p) { return work_of(x, p, nullptr).bytes; }
 
 cudaError_t launch_sample(const hx_logits& x, const hx_rules& r, const hx_pick& p, cudaStream_t s) {
   if (x.dtype == HX_BF16) return sample_typed<__nv_bfloat16>(x, r, p, s);

@@ -17,7 +17,7 @@ int report(int code, const char* msg) noexcept;
 cudaError_t launch_rotate(const hx_rotate_args& a, cudaStream_t s);
 cudaError_t launch_adjust(const hx_logits& x, const hx_rules& r, void* out, int64_t out_stride, int32_t out_dtype, cudaStream_t s);
 cudaError_t launch_sample(const hx_logits& x, const hx_rules& r, const hx_pick& p, cudaStream_t s);
-int64_t sample_workspace(const hx_logits& x, const hx_rules& r, const hx_pick& p);
+int64_t sample_workspace(const hx_logits& x, const hx_pick& p);
 
 // N values of T that are loaded and stored together.
 template <class T, int N>

@@ -196,7 +196,7 @@ int hx_adjust(const hx_logits* x, const hx_rules* r, void* out, int64_t out_stri
 
 int64_t hx_sample_workspace(const hx_logits* x, const hx_rules* r, const hx_pick* p) {
   if (check_logits(x) || !p || (r && check_rules(x, r))) return 0;
-  return hx::sample_workspace(*x, r ? *r : hx_rules{}, *p);
+  return hx::sample_workspace(*x, *p);
 }
 
 int hx_sample(const hx_logits* x, const hx_rules* r, const hx_pick* p, void* stream) {
@@ -223,7 +223,7 @@ int hx_sample(const hx_logits* x, const hx_rules* r, const hx_pick* p, void* str
     if (over_rules(rules, o)) return bad("sample: an output overlaps the rules");
   }
   if (overlap(out[0], out[1])) return bad("sample: token and logprob overlap");
-  const int64_t need = hx::sample_workspace(*x, rules, *p);
+  const int64_t need = hx::sample_workspace(*x, *p);
   if (p->workspace_bytes < need || !p->workspace) return bad("sample: workspace is too small");
   if (!aligned(p->workspace, 16)) return bad("sample: workspace must be 16-byte aligned");
   const Range work = {p->workspace, need};
