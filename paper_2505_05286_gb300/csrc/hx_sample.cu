@@ -167,43 +167,44 @@ __device__ float near_score(float best) { return best - (3e-4f + fabsf(best) * 0
 // x / T below that of the row's (or segment's) first token.
 struct Scale {
   float top, T, unit, inv_bin;
-  float zero = 0.f;   // where the grid of bins begins
-  float first;        // the first token's place on it
+  float zero = 0.f;     // where the grid of bins begins
+  bool coarse = false;  // at the first token itself
+  float first;          // the first token's place on it
   int first_bin;
-  static constexpr float kMagic = 12582912.f;  // 1.5 * 2^23: added, the bits below the point are gone, to the nearest
+  static constexpr float kMagic = 12582912.f;  // 1.5 * 2^23
 
   __device__ Scale(float top, float t) : top(top), T(t > 0.f ? t : 1.f) {
     // within what keeps products with 0 and infinity what they should be
     unit = fminf(fmaxf(1.44269504f / T, 0x1p-149f), 1e30f);
     inv_bin = kBinsPerUnit / T;
-    begin(0.f);
+    first = __fmul_rn(top, inv_bin);
+    first_bin = __float_as_int(__fmaf_rn(top, inv_bin, kMagic));
   }
-  __device__ void begin(float at) {
-    zero = at;
-    first = __fmul_rn(__fsub_rn(top, zero), inv_bin);
-    first_bin = __float_as_int(__fadd_rn(first, kMagic));
-  }
-  // Whether the grid has steps of 1 / 2 at least where the first token is.
+  // Whether the grid has steps of 1 / 2 at least where the first token is, and numbers at all.
   __device__ bool fine() const { return fabsf(first) < 4e6f; }
+  __device__ void begin_at_top() { zero = top, coarse = true, first = 0.f, first_bin = __float_as_int(kMagic); }
   // log2 of the weight
   __device__ float below(float x) const { return x == top ? 0.f : __fmul_rn(__fsub_rn(x, top), unit); }
-  // Bins lie on a grid of x / T that is the same for all stretches of a row, of its whole numbers of 1 / kBinsPerUnit and what
-  // rounds to them: what lies between two numbers' bins is the same from either.  The last bin holds all that is further down.
-  // `share`: the weight within its bin, of that of the bin's middle, in 1 / 2^kWeightBits; the last bin's tokens, all below e^-31 of the
-  // first's, have none.
+  // Bins lie on a grid of x / T that is the same for all stretches of a row, of the whole numbers of 1 / kBinsPerUnit and what
+  // rounds to them: what lies between two numbers' bins is the same from either.  Added to 1.5 * 2^23, x / T is rounded to a whole number that
+  // stands in the sum's last bits; what is far down differs by more than there are bins, whatever stands there.  The last bin
+  // holds all that is further down.
+  // `share`: the weight within its bin, of that of the bin's middle, in 1 / 2^kWeightBits: exp(d / 16), |d| <= 1 / 2, by the series to
+  // its third power, off by 2^-24 of it.  The last bin's tokens, all below e^-31 of the first's, have none.
   __device__ int bin(float x, unsigned* share = nullptr) const {
-    const float z = __fsub_rn(x, zero), y = __fmul_rn(z, inv_bin), rest = __fmaf_rn(z, inv_bin, -y);
-    const float m = __fadd_rn(fmaxf(y, first - 600.f), kMagic);
-    // whatever a number that is none makes of the difference, it is a bin
-    const int b = x == top ? 0 : top < INFINITY ? (int)min((unsigned)first_bin - (unsigned)__float_as_int(m), (unsigned)(kBins - 1)) : kBins - 1;
-    if (share) {
-      // exp(d), |d| <= 1 / 32: the series to its third power, 2^-24 of it; of no number (the first token's at an infinite T): 1
-      const float off = __fadd_rn(__fsub_rn(y, __fsub_rn(m, kMagic)), rest) * (1.f / kBinsPerUnit);
-      const float d = fminf(fmaxf(off, -0.04f), 0.04f);
-      const float f = __fmaf_rn(d, __fmaf_rn(d, __fmaf_rn(d, 1.f / 6, 0.5f), 1.f), 1.f);
-      *share = b < kBins - 1 ? __float_as_uint(__fmaf_rn(f, (float)(1 << kWeightBits), 8388608.f)) & 0x7fffffu : 0u;
+    if (coarse && (x == top || top == INFINITY)) {
+      if (share) *share = x == top ? 1u << kWeightBits : 0u;
+      return x == top ? 0 : kBins - 1;
     }
-    return b;
+    const float z = __fsub_rn(x, zero), m = __fmaf_rn(z, inv_bin, kMagic);
+    const unsigned b = min((unsigned)first_bin - (unsigned)__float_as_int(m), (unsigned)(kBins - 1));
+    if (share) {
+      constexpr float k1 = (float)(1 << kWeightBits), k = 1.f / kBinsPerUnit;
+      const float d = __fmaf_rn(z, inv_bin, -__fsub_rn(m, kMagic));
+      const float f = __fmaf_rn(__fmaf_rn(__fmaf_rn(d, k1 * k * k * k / 6, k1 * k * k / 2), d, k1 * k), d, k1 + 8388608.f);
+      *share = b < kBins - 1 ? __float_as_uint(f) & 0x7fffffu : 0u;
+    }
+    return (int)b;
   }
   __device__ unsigned share(float x) const {
     unsigned s;
@@ -216,6 +217,10 @@ struct Scale {
     return e > 0.f && e < INFINITY && (x == top || top < INFINITY) ? s : -INFINITY;
   }
 };
+
+__device__ void add_shared(uint32_t at, unsigned x, bool on) {
+  asm volatile("{.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.shared.add.u32 [%0], %1;}" ::"r"(at), "r"(x), "r"((unsigned)on) : "memory");
+}
 
 // The score that decides, in 64 bits.  (Not inline: few calls, many registers.)
 __device__ __noinline__ u64 exact_score(float top, float T, float x, float e) {
@@ -244,6 +249,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
   }
   bin_n[t] = bin_w[t] = 0;
   const R from(in, row);
+  if (p.noise && (p.temperature ? p.temperature[row] : p.all_temperature) > 0.f) {
+    // the noise is asked for now and read when the logits are done: a line for each of some threads
+    const int e = p0 - from.shift + 32 * t;
+    if (t < kStretch / 32 && (unsigned)e < (unsigned)in.n_vocab)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(p.noise + row * p.noise_stride + e));
+  }
   // a warp's places are one after the other; load u of a lane is at place(u) of the stretch
   auto place = [&](int u) { return warp * kSegment + (u * 32 + lane) * kVec; };
   Pack<T, kVec> raw[kEach / kVec];
@@ -351,20 +362,21 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
     __syncthreads();
     const Scale scale(unorder(__reduce_max_sync(~0u, warp_top[lane % kWarps])), pick.T);
     const bool fine = scale.fine(), by_k = pick.k > 0, by_p = pick.p < 1.f;
-    if (top < INFINITY) {  // bins of a row with an infinite logit are not read
+    if (fine) {
+      // without branches: of a warp's tokens hardly ever none is entered
+      const uint32_t n0 = (uint32_t)__cvta_generic_to_shared(bin_n), w0 = (uint32_t)__cvta_generic_to_shared(bin_w);
 #pragma unroll
-      for (int i = 0; i < kEach; ++i)
-        if (x[i] > -INFINITY) {
-          unsigned share = 0;
-          const int b = fine ? scale.bin(x[i], &share) : kBins - 1;
-          if (by_k) atomicAdd(&bin_n[b], 1u);
-          if (by_p && share) atomicAdd(&bin_w[b], share);
-        }
-    } else if (by_k) {
-      int n = 0;
+      for (int i = 0; i < kEach; ++i) {
+        unsigned share;
+        const unsigned b = scale.bin(x[i], &share);
+        if (by_k) add_shared(n0 + 4 * b, 1u, x[i] > -INFINITY);
+        if (by_p) add_shared(w0 + 4 * b, share, share != 0);
+      }
+    } else if (by_k) {  // the row's grid begins elsewhere, or all is far below it
+      unsigned n = 0;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) n += x[i] > -INFINITY;
-      atomicAdd(&bin_n[kBins - 1], (unsigned)n);
+      if (n) atomicAdd(&bin_n[kBins - 1], n);
     }
     __syncthreads();
     unsigned* bins = w.bins + ((int64_t)row * blocks + stretch) * 2 * kBins;
@@ -648,7 +660,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
           if (pick.p < 1.f) sum_w += bins[(c * 2 + 1) * kBins + b];
         }
       } else {
-        scale.begin(scale.top);
+        scale.begin_at_top();
         again.each([&](float x, int) {
           unsigned share;
           const int b = scale.bin(x, &share);
