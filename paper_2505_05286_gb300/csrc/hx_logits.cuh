@@ -55,10 +55,15 @@ struct RowRules {
     // the stretch's tokens are [e0, e0 + span), the first at word[at0]
     const int e0 = max(p0 - shift, 0), at0 = e0 - (p0 - shift);
     const unsigned span = (unsigned)max(min(kPlaces - at0, n_vocab - e0), 0);
-    word += at0;
 #pragma unroll
     for (int i = 4 * (int)threadIdx.x; i < kPlaces; i += 4 * kRowThreads)
-      if (i - 4 * (int)threadIdx.x < (int)span + at0) *(uint4*)(word - at0 + i) = uint4{0, 0, 0, 0};
+      if (i - 4 * (int)threadIdx.x < (int)span + at0) *(uint4*)(word + i) = uint4{0, 0, 0, 0};
+    enter(word + at0, span, [&](int token) { return (uint32_t)(token - e0); });
+  }
+
+  // Enters what the row's lists hold in words that the threads have cleared: token t's is word[where(t)], if that is below n.
+  template <class Where>
+  __device__ void enter(uint32_t* word, unsigned n, Where where) const {
     // 16 bytes a load from the boundary at or before the row's first entry, every block of the row reads all of it: one pair of
     // loads is on its way while the last is counted
     const int before = (int)((uintptr_t)history % 16 / 4);
@@ -80,20 +85,20 @@ struct RowRules {
     __syncthreads();
     if (n_bias > 0) {
       for (int j = threadIdx.x; j < n_bias; j += kRowThreads) {
-        const unsigned at = (unsigned)(bias_token[j] - e0);
-        if (at < span) atomicMax(&word[at], (uint32_t)(j + 1) << kBiasShift);
+        const uint32_t at = where(bias_token[j]);
+        if (at < n) atomicMax(&word[at], (uint32_t)(j + 1) << kBiasShift);
       }
     }
     __syncthreads();  // a maximum with what is counted already would not be one of entries
     // without a branch: of a warp's tokens hardly ever none is in the stretch
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(word);
     auto add = [&](int token) {
-      const uint32_t at = (uint32_t)(token - e0);
-      asm volatile("{.reg .pred p;\n\tsetp.lt.u32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;}" ::"r"(at), "r"(span), "r"(base + 4 * at) : "memory");
+      const uint32_t at = where(token);
+      asm volatile("{.reg .pred p;\n\tsetp.lt.u32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;}" ::"r"(at), "r"(n), "r"(base + 4 * at) : "memory");
     };
     auto see = [&](int token) {
-      const uint32_t at = (uint32_t)(token - e0);
-      asm volatile("{.reg .pred p;\n\tsetp.lt.u32 p, %0, %1;\n\t@p red.shared.or.b32 [%2], %3;}" ::"r"(at), "r"(span), "r"(base + 4 * at), "r"(kRead) : "memory");
+      const uint32_t at = where(token);
+      asm volatile("{.reg .pred p;\n\tsetp.lt.u32 p, %0, %1;\n\t@p red.shared.or.b32 [%2], %3;}" ::"r"(at), "r"(n), "r"(base + 4 * at), "r"(kRead) : "memory");
     };
     auto count4 = [&](int i, const int4& t) {
       if (i >= read) {

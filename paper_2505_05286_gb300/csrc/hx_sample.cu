@@ -35,7 +35,8 @@ constexpr float kBinsPerUnit = 16.f;
 constexpr int kWeightBits = 18;              // a weight within its bin: 8192 of them stay below 2^32
 constexpr int kList = 2048;                  // tokens of a row that are sorted at once
 constexpr int kMaxStretches = 64;
-constexpr int kMostAgain = 64;               // segments that are read again before the filters are resolved
+constexpr int kMostAgain = 64;               // segments that are read again, where not the whole row is
+constexpr int kMostNear = 64;                // tokens in them whose scores are next to the best
 static_assert((HX_MAX_VOCAB + 8 + kStretch - 1) / kStretch <= kMaxStretches, "stretches of a row");
 static_assert(kList % kRowThreads == 0, "tokens of a list by threads");
 
@@ -401,7 +402,11 @@ struct Shared {
   int away[kMaxStretches];  // bins from the row's first token to the stretch's, kBins: no token
   int at, last, n_list, unsure;
   unsigned base_count, bin_count;
-  int again[kMostAgain];
+  int again[kMostAgain];    // segments
+  uint8_t slot[kMaxStretches * kWarps];
+  int n_near;
+  float near_score[kMostNear], near_x[kMostNear];
+  int near_token[kMostNear];
 };
 
 // A row's logits once more, adjusted; f(x, token) for each that takes part.  All threads of the block call.
@@ -438,19 +443,48 @@ struct RowAgain {
   __device__ void each(F f) const {
     for (int c = 0; c < blocks; ++c) stretch(c, f);
   }
-  // One segment, a place for each thread.
+  // Segments list[0, n), a place of each for every thread and four segments at a time; f(x, token, noise), the noise read only if
+  // there is one.  slot: room for a byte for each of the row's segments.
   template <class F>
-  __device__ void segment(int s, F f) const {
-    const int p0 = s * kSegment;
-    if (kWords) rules.template count<kSegment>(p0, row.shift, row.n_vocab, word);
-    for (int i = threadIdx.x; i < kSegment; i += kRowThreads) {
-      const int e = p0 + i - row.shift;
-      if ((unsigned)e >= (unsigned)row.n_vocab) continue;
-      float x = to_float(row.first[e]);
-      if (kWords && word[i]) x = adjusted(rules, x, word[i]);
-      if ((!rules.mask || rules.mask[e >> 5] >> (e & 31) & 1) && x > -INFINITY) f(clean(x), e);
+  __device__ void segments(const int* list, int n, uint8_t* slot, const float* noise, F f) const {
+    static_assert(kSegment % kRowThreads == 0, "places of a segment by threads");
+    constexpr int kAtOnce = kStretch / kSegment;  // whose words there is room for
+    for (int i0 = 0; i0 < n; i0 += kAtOnce) {
+      const int m = min(kAtOnce, n - i0);
+      if (kWords) {
+        for (int i = threadIdx.x; i < blocks * kWarps; i += kRowThreads) slot[i] = 255;
+        __syncthreads();
+        if (threadIdx.x < m) slot[list[i0 + threadIdx.x]] = (uint8_t)threadIdx.x;
+        for (int i = 4 * (int)threadIdx.x; i < m * kSegment; i += 4 * kRowThreads) *(uint4*)(word + i) = uint4{0, 0, 0, 0};
+        __syncthreads();
+        rules.enter(word, m * kSegment, [&](int token) {
+          const int place = token + row.shift;
+          return (unsigned)token < (unsigned)row.n_vocab ? (uint32_t)slot[place / kSegment] * kSegment + place % kSegment : ~0u;
+        });
+      }
+      for (int at = threadIdx.x; at < kSegment; at += kRowThreads)
+#pragma unroll 1
+        for (int j = 0; j < m; j += 4) {
+          float x[4], z[4];
+          int e[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            e[q] = j + q < m ? list[i0 + j + q] * kSegment + at - row.shift : -1;
+            const bool is = (unsigned)e[q] < (unsigned)row.n_vocab && (!rules.mask || rules.mask[e[q] >> 5] >> (e[q] & 31) & 1);
+            x[q] = is ? to_float(row.first[e[q]]) : -INFINITY;
+            z[q] = is && noise ? noise[e[q]] : 0.f;
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if (kWords && x[q] != -INFINITY) {
+              const uint32_t w = word[(j + q) * kSegment + at];
+              if (w) x[q] = adjusted(rules, x[q], w);
+            }
+            if (x[q] > -INFINITY) f(clean(x[q]), e[q], z[q]);
+          }
+        }
+      if (kWords) __syncthreads();
     }
-    if (kWords) __syncthreads();
   }
 };
 
@@ -733,29 +767,42 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
       const u64 f = exact_score(scale.top, scale.T, x, noise[e]);
       if (f > mine || (f == mine && (u64)(uint32_t)~e << 32 > (mine_at | 0xffffffffu))) mine = f, mine_at = (u64)(uint32_t)~e << 32 | __float_as_uint(x);
     };
-    if (found) {
+    // lists the segments that f holds for; whether there is room for them
+    auto list_segments = [&](auto f) {
       __syncthreads();
-      if (t == 0) s.n_list = 0, s.unsure = 0;
+      if (t == 0) s.n_list = 0, s.unsure = 0, s.n_near = 0;
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < kMine; ++j)
-        if (score[j] >= near) {
+      for (int j = 0; j < kMine; ++j) {
+        const int i = t + j * kRowThreads;
+        if (i < n_seg && f(j, i)) {
           const int at = atomicAdd(&s.n_list, 1);
-          if (at < kMostAgain) s.again[at] = t + j * kRowThreads;
+          if (at < kMostAgain) s.again[at] = i;
         }
+      }
       __syncthreads();
-      const int n_again = s.n_list;
-      found = n_again <= kMostAgain;
+      return s.n_list <= kMostAgain;
+    };
+    if (found) found = list_segments([&](int j, int) { return score[j] >= near; });
+    if (found) {
+      again.segments(s.again, s.n_list, s.slot, noise, [&](float x, int e, float z) {
+        const float f = scale.score(x, z);
+        if (f < near) return;
+        const int l = left(x, key_of(x, e));
+        if (l < 0) s.unsure = 1;
+        if (l <= 0) return;
+        const int at = atomicAdd(&s.n_near, 1);
+        if (at < kMostNear) s.near_score[at] = f, s.near_x[at] = x, s.near_token[at] = e;
+      });
+      __syncthreads();
+      const int n_near = s.n_near;
+      found = !s.unsure && n_near <= kMostNear;
       if (found) {
-        for (int i = 0; i < n_again; ++i)
-          again.segment(s.again[i], [&](float x, int e) {
-            if (scale.score(x, noise[e]) < near) return;
-            const int l = left(x, key_of(x, e));
-            if (l > 0) take(x, e);
-            if (l < 0) s.unsure = 1;
-          });
-        __syncthreads();
-        found = !s.unsure;
+        const float f = t < n_near ? s.near_score[t] : -INFINITY, least = near_score(block_max(f, s.room_n));
+        const bool is = t < n_near && f >= least;
+        const int many = __syncthreads_count(is);
+        if (is && many == 1) mine = 1, mine_at = (u64)(uint32_t)~s.near_token[t] << 32 | __float_as_uint(s.near_x[t]);
+        if (is && many > 1) take(s.near_x[t], s.near_token[t]);
       }
     }
     if (!found) {
@@ -767,17 +814,23 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
         const float far = -log_least * (kBinsPerUnit / 1.44269504f) + 3.f;
         reach = min(reach, far < (float)kBins ? max((int)far, 0) : kBins - 1);
       }
-      a.clear();
+      __syncthreads();
       if (t == reach) s.bin_count = by_k ? n_before + n : 0u;
       __syncthreads();
       bool listed = by_order && s.bin_count <= kList;
       if (listed) {
         // all that the filters can leave, if it fits the list
-        for (int c = 0; c < blocks; ++c)
-          if (s.away[c] <= reach)
-            again.stretch(c, [&](float x, int e) {
-              if (scale.bin(x) <= reach) a.enter(x, e);
-            });
+        const bool few = list_segments([&](int, int i) { return seg[i].top && scale.bin(x_of(seg[i].top)) <= reach; });
+        const int n_again = s.n_list;
+        a.clear();
+        auto enter = [&](float x, int e) {
+          if (scale.bin(x) <= reach) a.enter(x, e);
+        };
+        if (few)
+          again.segments(s.again, n_again, s.slot, nullptr, [&](float x, int e, float) { enter(x, e); });
+        else
+          for (int c = 0; c < blocks; ++c)
+            if (s.away[c] <= reach) again.stretch(c, enter);
         __syncthreads();
         listed = s.n_list <= kList;
       }
@@ -810,9 +863,19 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
           fast = fmaxf(fast, f[j]);
         }
         const float least = near_score(block_max(fast, s.room_n));
+        unsigned many = 0;
+#pragma unroll
+        for (int j = 0; j < kOf; ++j) many += f[j] > -INFINITY && f[j] >= least;
+        many = block_sum_int(many, s.room_n);
 #pragma unroll
         for (int j = 0; j < kOf; ++j)
-          if (f[j] > -INFINITY && f[j] >= least) take(x_of(s.list[t + j * kRowThreads]), token_of(s.list[t + j * kRowThreads]));
+          if (f[j] > -INFINITY && f[j] >= least) {
+            const u64 key = s.list[t + j * kRowThreads];
+            if (many == 1)
+              mine = 1, mine_at = key << 32 | __float_as_uint(x_of(key));
+            else
+              take(x_of(key), token_of(key));
+          }
       } else {
         u64 border = 0, of = total;
         auto start = [&](int bin) {  // what lies before a bin
