@@ -11,9 +11,9 @@
 //          the bins before the one in which a filter ends.  The best of the segments' winners that are left for sure is nearly the row's: only
 //          the few segments whose winner scores more, or as much but for rounding, can hold a better one, and are read again.
 //
-// Where the race turns on a token of the bin in which a filter ends, or no winner is left for sure, that bin is resolved: all tokens
-// down to it are sorted and cut exactly where the filters say, and raced; where they are too many for one list,
-// the bin is cut by its keys until what is left fits, and the race reads the row.
+// Where the race turns on a token of the bin in which a filter ends, that bin is resolved: its tokens are sorted and
+// cut exactly where the filter says (by the range of their keys before that, until they fit one list).  Where no
+// segment's winner is left, the race of what is left reads the row.
 //
 // Sums that decide where an order is cut are of whole numbers, so that no order of additions is of matter;
 // those of the log-probability are 32-bit sums in a fixed order, without the first token, whose
@@ -400,8 +400,8 @@ struct Shared {
   unsigned bin_n[kBins], bin_lo[kBins], bin_hi[kBins];
   uint32_t stretch_top[kMaxStretches];
   int away[kMaxStretches];  // bins from the row's first token to the stretch's, kBins: no token
-  int at, last, n_list, unsure;
-  unsigned base_count, bin_count;
+  int at, last, n_list, n_again, unsure;
+  unsigned base_count;
   int again[kMostAgain];    // segments
   uint8_t slot[kMaxStretches * kWarps];
   int n_near;
@@ -417,31 +417,43 @@ struct RowAgain {
   uint32_t* word;
   int blocks;
 
+  // Those that are at least `least`.
   template <class F>
-  __device__ void stretch(int c, F f) const {
-    constexpr int kVec = RowOf<T>::kVec;
-    const int p0 = c * kStretch;
-    if (kWords) rules.template count<kStretch>(p0, row.shift, row.n_vocab, word);
-    Pack<T, kVec> raw[kEach / kVec];
+  __device__ void each(float least, F f) const {
+    constexpr int kVec = RowOf<T>::kVec, kLoads = kEach / kVec;
+    Pack<T, kVec> raw[kLoads];
+    auto load = [&](int c) {
 #pragma unroll
-    for (int u = 0; u < kEach / kVec; ++u) raw[u] = row.load(p0 / kVec + u * kRowThreads + threadIdx.x);
+      for (int u = 0; u < kLoads; ++u) raw[u] = row.load(c * (kStretch / kVec) + u * kRowThreads + threadIdx.x);
+    };
+    load(0);
+    for (int c = 0; c < blocks; ++c) {
+      const int p0 = c * kStretch;
+      if (kWords) rules.template count<kStretch>(p0, row.shift, row.n_vocab, word);
+      uint32_t rest = 0;  // the places that may be
 #pragma unroll
-    for (int u = 0; u < kEach / kVec; ++u) {
-      const int i = u * kRowThreads + threadIdx.x, vec = p0 / kVec + i;
-      if (row.token(vec) >= row.n_vocab) continue;
-      const uint32_t worded = kWords ? RowOf<T>::worded(word + i * kVec) : 0u, bits = rules.mask ? row.allowed(rules.mask, vec) : ~0u;
+      for (int u = 0; u < kLoads; ++u) {
+        const int i = u * kRowThreads + threadIdx.x, vec = p0 / kVec + i;
+        uint32_t bits = 0;
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        float x = to_float(raw[u].v[j]);
-        if (worded >> j & 1) x = adjusted(rules, x, word[i * kVec + j]);
-        if (bits >> j & 1 && x > -INFINITY) f(clean(x), row.token(vec) + j);
+        for (int j = 0; j < kVec; ++j) bits |= to_float(raw[u].v[j]) >= least ? 1u << j : 0u;
+        if (row.token(vec) < row.n_vocab) {
+          if (kWords) bits |= RowOf<T>::worded(word + i * kVec);
+          if (bits && rules.mask) bits &= row.allowed(rules.mask, vec);
+          rest |= bits << u * kVec;
+        }
       }
+      if (c + 1 < blocks) load(c + 1);
+      // one after the other, so that f is here once
+      for (; rest; rest &= rest - 1) {
+        const int j = __ffs(rest) - 1, i = (j / kVec * kRowThreads + threadIdx.x) * kVec + j % kVec, e = p0 + i - row.shift;
+        if ((unsigned)e >= (unsigned)row.n_vocab) continue;
+        float x = to_float(row.first[e]);
+        if (kWords && word[i]) x = adjusted(rules, x, word[i]);
+        if (x >= least && x > -INFINITY) f(clean(x), e);
+      }
+      if (kWords) __syncthreads();  // the words are the next stretch's
     }
-    if (kWords) __syncthreads();  // the words are the next stretch's
-  }
-  template <class F>
-  __device__ void each(F f) const {
-    for (int c = 0; c < blocks; ++c) stretch(c, f);
   }
   // Segments list[0, n), a place of each for every thread and four segments at a time; f(x, token, noise), the noise read only if
   // there is one.  slot: room for a byte for each of the row's segments.
@@ -535,43 +547,37 @@ struct Picker {
       }
   }
 
-  // Enters a token in the list; at most kList are kept.
-  __device__ void enter(float x, int e) {
-    const int at = atomicAdd(&s.n_list, 1);
-    if (at < kList) s.list[at] = key_of(x, e);
-  }
-  __device__ void clear() {
-    __syncthreads();
-    if (threadIdx.x == 0) s.n_list = 0;
-    __syncthreads();
-  }
-
   // The key at which the sum over the order (of tokens, or of their mass) first reaches target, the tokens of bin `bin` being
-  // those in question, `base` what is before them.  Leaves the mass up to there in s.border_mass.
-  __device__ u64 border(bool by_mass, u64 target, int bin, u64 base, u64 base_mass) {
+  // those in question, `base` what is before them.  Leaves the mass up to there in s.border_mass.  read(f): f for all tokens that may
+  // be in the bin.
+  template <class Read>
+  __device__ u64 border(bool by_mass, u64 target, int bin, u64 base, u64 base_mass, Read read) {
     const int t = threadIdx.x;
     u64 lo = 0, hi = ~0ull;
     auto in = [&](float x, u64 key) { return key >= lo && key <= hi && scale.bin(x) == bin; };
     for (int turn = 0; turn < 16; ++turn) {
-      clear();
-      row.each([&](float x, int e) {
-        if (in(x, key_of(x, e))) enter(x, e);
+      // what is in question, into the list; and the largest of ~key and of key
+      u64 a = 0, b = 0;
+      __syncthreads();
+      if (t == 0) s.n_list = 0;
+      __syncthreads();
+      read([&](float x, int e) {
+        const u64 key = key_of(x, e);
+        if (!in(x, key)) return;
+        a = max(a, ~key), b = max(b, key);
+        const int at = atomicAdd(&s.n_list, 1);
+        if (at < kList) s.list[at] = key;
       });
       __syncthreads();
       if (s.n_list <= kList) break;
-      // narrow the keys to those of the tokens, and cut them in parts
-      u64 a = 0, b = 0;  // the largest of ~key and of key
-      row.each([&](float x, int e) {
-        const u64 key = key_of(x, e);
-        if (in(x, key)) a = max(a, ~key), b = max(b, key);
-      });
+      // too many: cut the range of their keys in parts
       lo = ~block_max(a, s.room), hi = block_max(b, s.room);
       int shift = 0;
       while (((hi - lo) >> shift) >= kBins) ++shift;
       __syncthreads();
       s.bin_n[t] = s.bin_lo[t] = s.bin_hi[t] = 0;
       __syncthreads();
-      row.each([&](float x, int e) {
+      read([&](float x, int e) {
         const u64 key = key_of(x, e);
         if (in(x, key)) count((int)((hi - key) >> shift), scale.share(x));
       });
@@ -595,7 +601,7 @@ struct Picker {
     return along(m, by_mass, target, base, base_mass);
   }
 
-  // The same over the sorted list alone.  s.last is the number of tokens up to there.
+  // The same over the sorted list alone.
   __device__ u64 along(int m, bool by_mass, u64 target, u64 base, u64 base_mass) {
     constexpr int kMine = kList / kRowThreads;
     const int t = threadIdx.x;
@@ -648,7 +654,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
   }
   top = block_max(top, s.room);
   Scale scale(x_of(top), pick.T);
-  float part = 0.f, best_mine = -INFINITY;  // of the others' weights
+  float part = 0.f;  // of the others' weights
 #pragma unroll
   for (int j = 0; j < kMine; ++j) {
     const int i = t + j * kRowThreads;
@@ -672,10 +678,18 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
     const float log_least = !(pick.m > 0.f) ? -INFINITY : pick.m < 1.f ? log2f(pick.m) : pick.m > 1.f ? INFINITY : 0.f;
     const bool by_order = pick.by_order();
     bool by_k = false, by_p = false;
-    int sure = kBins, out = kBins;  // tokens of bins before `sure` are left, of those behind `out` they are not
-    int bin_k = kBins - 1, bin_p = kBins - 1;
-    unsigned n_before = 0, n = 0;
     u64 mass = 0, mass_before = 0, total = 0;
+    auto bin_at = [&](u64 target) {  // where the sum of the bins' masses reaches it
+      __syncthreads();
+      if (t == 0) s.at = kBins - 1;
+      __syncthreads();
+      if (mass_before < target && mass_before + mass >= target) s.at = t;
+      __syncthreads();
+      return s.at;
+    };
+    int sure = kBins, out = kBins;  // tokens of bins before `sure` are left, of those behind `out` they are not
+    int bin_k = kBins - 1;
+    unsigned n_before = 0, n = 0;
     if (by_order) {
       all = (int)block_sum_int((unsigned)all, s.room_n);
       // bins of the whole row: of its stretches'; where the grid is too coarse for them (T is small), of its tokens', from
@@ -686,16 +700,24 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
       __syncthreads();
       u64 sum_w = 0;
       if (fine) {
-        const unsigned* bins = w.bins + (int64_t)row * blocks * 2 * kBins;
-        for (int c = 0; c < blocks; ++c) {
-          const int b = t - s.away[c];
-          if (b < 0 || t == kBins - 1) continue;
-          if (pick.k > 0) n += bins[c * 2 * kBins + b];
-          if (pick.p < 1.f) sum_w += bins[(c * 2 + 1) * kBins + b];
-        }
+        const unsigned* bins = w.bins + (int64_t)row * blocks * 2 * kBins + t;
+        auto add = [&](int which, auto& sum) {  // eight stretches' loads on their way at a time
+          for (int c0 = 0; c0 < blocks; c0 += 8) {
+            unsigned v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const int c = c0 + q, away = c < blocks ? s.away[c] : kBins;
+              v[q] = t >= away && t < kBins - 1 ? bins[(c * 2 + which) * kBins - away] : 0u;
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum += v[q];
+          }
+        };
+        if (pick.k > 0) add(0, n);
+        if (pick.p < 1.f) add(1, sum_w);
       } else {
         scale.begin_at_top();
-        again.each([&](float x, int) {
+        again.each(-INFINITY, [&](float x, int) {
           unsigned share;
           const int b = scale.bin(x, &share);
           a.count(b, share);
@@ -717,14 +739,6 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
       total = s.mass_total;
       by_k = pick.k > 0 && pick.k < all, by_p = pick.p < 1.f;
       u64 least = total, most = total;  // mass that p is of
-      auto bin_at = [&](u64 target) {  // where the sum reaches it
-        __syncthreads();
-        if (t == 0) s.at = kBins - 1;
-        __syncthreads();
-        if (mass_before < target && mass_before + mass >= target) s.at = t;
-        __syncthreads();
-        return s.at;
-      };
       if (by_k) {
         if (n_before < (unsigned)pick.k && n_before + n >= (unsigned)pick.k) s.at = t, s.base_mass = mass_before, s.border_mass = mass_before + mass;
         __syncthreads();
@@ -732,36 +746,21 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
         sure = out = bin_k;
       }
       if (by_p) {
-        bin_p = bin_at(min(part_of(pick.p, most), most));
+        const int bin_p = bin_at(min(part_of(pick.p, most), most));
         const int from = by_k ? bin_at(min(part_of(pick.p, least), max(least, (u64)1))) : bin_p;
         sure = min(sure, from), out = min(out, bin_p);
       }
     }
+    u64 border = 0;  // once they are resolved, the last token that the filters by order leave
+    bool resolved = !by_k && !by_p;
     // 1: the filters leave it, 0: they do not, -1: it is in a bin where they end
     auto left = [&](float x, u64 key) {
       if (key == top) return 1;
       if (scale.below(x) < log_least) return 0;
-      if (!by_order) return 1;
+      if (resolved) return key >= border ? 1 : 0;
       const int b = scale.bin(x);
       return b < sure ? 1 : b > out ? 0 : -1;
     };
-    float unsure = -INFINITY, score[kMine];
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int i = t + j * kRowThreads;
-      score[j] = -INFINITY;
-      if (i >= n_seg) continue;
-      const Segment g = seg[i];
-      if (g.token < 0 || (scale.top == INFINITY && g.token_x < INFINITY)) continue;
-      score[j] = g.score + scale.below(x_of(g.top));
-      const int l = left(g.token_x, key_of(g.token_x, g.token));
-      if (l > 0) best_mine = fmaxf(best_mine, score[j]);
-      if (l < 0) unsure = fmaxf(unsure, score[j]);
-    }
-    const float best = block_max(best_mine, s.room_n);
-    unsure = block_max(unsure, s.room_n);
-    const float near = near_score(best);
-    bool found = best > -INFINITY && unsure < near;
     u64 mine = 0, mine_at = 0;
     auto take = [&](float x, int e) {
       const u64 f = exact_score(scale.top, scale.T, x, noise[e]);
@@ -770,147 +769,101 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
     // lists the segments that f holds for; whether there is room for them
     auto list_segments = [&](auto f) {
       __syncthreads();
-      if (t == 0) s.n_list = 0, s.unsure = 0, s.n_near = 0;
+      if (t == 0) s.n_again = 0, s.unsure = 0, s.n_near = 0;
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < kMine; ++j) {
         const int i = t + j * kRowThreads;
-        if (i < n_seg && f(j, i)) {
-          const int at = atomicAdd(&s.n_list, 1);
+        if (i < n_seg && f(seg[i])) {
+          const int at = atomicAdd(&s.n_again, 1);
           if (at < kMostAgain) s.again[at] = i;
         }
       }
       __syncthreads();
-      return s.n_list <= kMostAgain;
+      return s.n_again <= kMostAgain;
     };
-    if (found) found = list_segments([&](int j, int) { return score[j] >= near; });
-    if (found) {
-      again.segments(s.again, s.n_list, s.slot, noise, [&](float x, int e, float z) {
-        const float f = scale.score(x, z);
-        if (f < near) return;
-        const int l = left(x, key_of(x, e));
-        if (l < 0) s.unsure = 1;
-        if (l <= 0) return;
-        const int at = atomicAdd(&s.n_near, 1);
-        if (at < kMostNear) s.near_score[at] = f, s.near_x[at] = x, s.near_token[at] = e;
-      });
-      __syncthreads();
-      const int n_near = s.n_near;
-      found = !s.unsure && n_near <= kMostNear;
-      if (found) {
-        const float f = t < n_near ? s.near_score[t] : -INFINITY, least = near_score(block_max(f, s.room_n));
-        const bool is = t < n_near && f >= least;
-        const int many = __syncthreads_count(is);
-        if (is && many == 1) mine = 1, mine_at = (u64)(uint32_t)~s.near_token[t] << 32 | __float_as_uint(s.near_x[t]);
-        if (is && many > 1) take(s.near_x[t], s.near_token[t]);
+    auto score_of = [&](const Segment& g) {
+      return g.token < 0 || (scale.top == INFINITY && g.token_x < INFINITY) ? -INFINITY : g.score + scale.below(x_of(g.top));
+    };
+    bool found = false;
+    while (true) {
+      float best = -INFINITY, unsure = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int i = t + j * kRowThreads;
+        if (i >= n_seg) continue;
+        const Segment g = seg[i];
+        const float f = score_of(g);
+        if (f == -INFINITY) continue;
+        const int l = left(g.token_x, key_of(g.token_x, g.token));
+        if (l > 0) best = fmaxf(best, f);
+        if (l < 0) unsure = fmaxf(unsure, f);
       }
+      best = block_max(best, s.room_n);
+      unsure = block_max(unsure, s.room_n);
+      const float near = near_score(best);
+      found = best > -INFINITY && unsure < near && list_segments([&](const Segment& g) { return score_of(g) >= near; });
+      if (found) {
+        again.segments(s.again, s.n_again, s.slot, noise, [&](float x, int e, float z) {
+          const float f = scale.score(x, z);
+          if (f < near) return;
+          const int l = left(x, key_of(x, e));
+          if (l < 0) s.unsure = 1;
+          if (l <= 0) return;
+          const int at = atomicAdd(&s.n_near, 1);
+          if (at < kMostNear) s.near_score[at] = f, s.near_x[at] = x, s.near_token[at] = e;
+        });
+        __syncthreads();
+        const int n_near = s.n_near;
+        found = !s.unsure && n_near <= kMostNear;
+        if (found) {
+          const float f = t < n_near ? s.near_score[t] : -INFINITY, least = near_score(block_max(f, s.room_n));
+          const bool is = t < n_near && f >= least;
+          const int many = __syncthreads_count(is);
+          if (is && many == 1) mine = 1, mine_at = (u64)(uint32_t)~s.near_token[t] << 32 | __float_as_uint(s.near_x[t]);
+          if (is && many > 1) take(s.near_x[t], s.near_token[t]);
+        }
+      }
+      if (found || resolved) break;
+      // resolve the filters
+      auto end = [&](bool by_mass, u64 target, int bin) {
+        __syncthreads();
+        if (t == bin) s.base_count = n_before, s.base_mass = mass_before;
+        __syncthreads();
+        const u64 m0 = s.base_mass, base = by_mass ? m0 : s.base_count;
+        // no token of the bin is below this: bin + 1 bins further down than the first token, but for roundings
+        const float down = (float)(bin + 2) / kBinsPerUnit * scale.T, least = scale.top < INFINITY ? scale.top - (down + fabsf(scale.top) * 0x1p-20f) : -INFINITY;
+        const bool few = list_segments([&](const Segment& g) { return g.top && scale.bin(x_of(g.top)) <= bin; });
+        return a.border(by_mass, target, bin, base, m0, [&](auto f) {
+          if (few)
+            again.segments(s.again, s.n_again, s.slot, nullptr, [&](float x, int e, float) { f(x, e); });
+          else
+            again.each(bin < kBins - 1 ? least : -INFINITY, f);
+        });
+      };
+      u64 of = total;
+      if (by_k) {
+        border = end(false, (u64)pick.k, bin_k);
+        of = s.border_mass;
+      }
+      if (by_p) {
+        const u64 target = min(part_of(pick.p, of), max(of, (u64)1));
+        border = max(border, end(true, target, bin_at(target)));
+      }
+      resolved = true;
     }
     if (!found) {
-      // resolve the filters
-      mine = 0, mine_at = 0;
-      int reach = by_k ? bin_k : by_p ? bin_p : kBins - 1;
-      if (by_order && pick.m > 0.f && !(by_k && by_p)) {
-        // what has at least m of the first token's weight is no further down than this
-        const float far = -log_least * (kBinsPerUnit / 1.44269504f) + 3.f;
-        reach = min(reach, far < (float)kBins ? max((int)far, 0) : kBins - 1);
-      }
-      __syncthreads();
-      if (t == reach) s.bin_count = by_k ? n_before + n : 0u;
-      __syncthreads();
-      bool listed = by_order && s.bin_count <= kList;
-      if (listed) {
-        // all that the filters can leave, if it fits the list
-        const bool few = list_segments([&](int, int i) { return seg[i].top && scale.bin(x_of(seg[i].top)) <= reach; });
-        const int n_again = s.n_list;
-        a.clear();
-        auto enter = [&](float x, int e) {
-          if (scale.bin(x) <= reach) a.enter(x, e);
-        };
-        if (few)
-          again.segments(s.again, n_again, s.slot, nullptr, [&](float x, int e, float) { enter(x, e); });
-        else
-          for (int c = 0; c < blocks; ++c)
-            if (s.away[c] <= reach) again.stretch(c, enter);
-        __syncthreads();
-        listed = s.n_list <= kList;
-      }
+      // no segment's winner is left: the race of all that are
       float fast = -INFINITY;
-      if (listed) {
-        const int m = s.n_list;
-        a.sort(m);
-        int n_left = m;
-        u64 of = total;
-        if (by_k && reach == bin_k) {
-          a.along(m, false, (u64)pick.k, 0, 0);
-          n_left = s.last, of = s.border_mass;
-          __syncthreads();
-        }
-        if (by_p) {
-          a.along(n_left, true, min(part_of(pick.p, of), of), 0, 0);
-          n_left = min(n_left, s.last);
-          __syncthreads();
-        }
-        constexpr int kOf = kList / kRowThreads;
-        float f[kOf];
-#pragma unroll
-        for (int j = 0; j < kOf; ++j) {
-          const int i = t + j * kRowThreads;
-          f[j] = -INFINITY;
-          if (i < n_left) {
-            const float x = x_of(s.list[i]);
-            if (i == 0 || !(scale.below(x) < log_least)) f[j] = scale.score(x, noise[token_of(s.list[i])]);
-          }
-          fast = fmaxf(fast, f[j]);
-        }
-        const float least = near_score(block_max(fast, s.room_n));
-        unsigned many = 0;
-#pragma unroll
-        for (int j = 0; j < kOf; ++j) many += f[j] > -INFINITY && f[j] >= least;
-        many = block_sum_int(many, s.room_n);
-#pragma unroll
-        for (int j = 0; j < kOf; ++j)
-          if (f[j] > -INFINITY && f[j] >= least) {
-            const u64 key = s.list[t + j * kRowThreads];
-            if (many == 1)
-              mine = 1, mine_at = key << 32 | __float_as_uint(x_of(key));
-            else
-              take(x_of(key), token_of(key));
-          }
-      } else {
-        u64 border = 0, of = total;
-        auto start = [&](int bin) {  // what lies before a bin
-          __syncthreads();
-          if (t == bin) s.base_count = n_before, s.base_mass = mass_before;
-          __syncthreads();
-        };
-        if (by_k) {
-          start(bin_k);
-          const u64 c0 = s.base_count, m0 = s.base_mass;
-          border = a.border(false, (u64)pick.k, bin_k, c0, m0);
-          of = s.border_mass;
-          __syncthreads();
-        }
-        if (by_p) {
-          const u64 target = min(part_of(pick.p, of), of);
-          if (t == 0) s.at = bin_k;
-          __syncthreads();
-          if (mass_before < target && mass_before + mass >= target) s.at = t;
-          __syncthreads();
-          const int bin = s.at;
-          start(bin);
-          const u64 m0 = s.base_mass;
-          border = max(border, a.border(true, target, bin, m0, m0));
-          __syncthreads();
-        }
-        auto kept = [&](float x, u64 key) { return key >= border && (key == top || !(scale.below(x) < log_least)); };
-        again.each([&](float x, int e) {
-          if (kept(x, key_of(x, e))) fast = fmaxf(fast, scale.score(x, noise[e]));
-        });
-        const float least = near_score(block_max(fast, s.room_n));
-        again.each([&](float x, int e) {
-          if (fast > -INFINITY && fast >= least && kept(x, key_of(x, e)) && scale.score(x, noise[e]) >= least) take(x, e);
-        });
-      }
+      const float least = border ? x_of(border) : -INFINITY;
+      again.each(least, [&](float x, int e) {
+        if (left(x, key_of(x, e)) > 0) fast = fmaxf(fast, scale.score(x, noise[e]));
+      });
+      const float near = near_score(block_max(fast, s.room_n));
+      const bool any = fast > -INFINITY && fast >= near;
+      again.each(least, [&](float x, int e) {
+        if (any && left(x, key_of(x, e)) > 0 && scale.score(x, noise[e]) >= near) take(x, e);
+      });
     }
     const u64 high = block_max(mine, s.room);
     const u64 low = block_max(mine && mine == high ? mine_at : 0, s.room);
