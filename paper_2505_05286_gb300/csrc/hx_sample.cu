@@ -53,8 +53,7 @@ struct alignas(16) Segment {
   float score;     // the race's best, in units of log 2, of the first token's weight
   int token;       // that has it
   float token_x;
-  unsigned count;  // tokens in the warp's 32nd part of its block's bins
-  int pad;
+  int pad[2];
 };
 
 struct Work {
@@ -119,13 +118,6 @@ __device__ float block_sum(float x, float* room) {
   const float y = threadIdx.x % 32 < kWarps ? room[threadIdx.x % kWarps] : 0.f;
   return warp_sum(y);
 }
-__device__ unsigned block_sum_int(unsigned x, uint32_t* room) {
-  x = __reduce_add_sync(~0u, x);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) room[threadIdx.x / 32] = x;
-  __syncthreads();
-  return __reduce_add_sync(~0u, threadIdx.x % 32 < kWarps ? room[threadIdx.x % kWarps] : 0u);
-}
 // The sum over the threads before this one.
 template <class N>
 __device__ N block_before(N x, N* room) {
@@ -149,7 +141,7 @@ __device__ N block_before(N x, N* room) {
 
 __device__ float clean(float x) { return __fadd_rn(x, 0.f); }  // -0 is 0
 
-// 2^x and log2(x) of the special function unit: 2^-22 relative, and 2^-22 relative or absolute near 1.
+// 2^x and log2(x) of the special function unit: 2^-22 relative, and 2^-22 relative or absolute near 1; numbers below 2^-126 are 0.
 __device__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -157,13 +149,14 @@ __device__ float exp2_fast(float x) {
 }
 __device__ float log2_fast(float x) {
   float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
 // Scores in 32 bits, in units of log 2.  Those near the largest are off by less than a third of this difference: four roundings of
-// a difference of logits over T, which is at most the score and the logarithm of a 32-bit number (150), and the logarithm's.
-__device__ float near_score(float best) { return best - (3e-4f + fabsf(best) * 0x1p-19f); }
+// a difference of logits over T, which is at most the score and the logarithm of a 32-bit number (128), the logarithm's,
+// and the five bits that a number takes the place of in the scan (2^-18).
+__device__ float near_score(float best) { return best - (3e-4f + fabsf(best) * 0x1p-16f); }
 
 // x / T below that of the row's (or segment's) first token.
 struct Scale {
@@ -197,15 +190,18 @@ struct Scale {
       if (share) *share = x == top ? 1u << kWeightBits : 0u;
       return x == top ? 0 : kBins - 1;
     }
-    const float z = __fsub_rn(x, zero), m = __fmaf_rn(z, inv_bin, kMagic);
-    const unsigned b = min((unsigned)first_bin - (unsigned)__float_as_int(m), (unsigned)(kBins - 1));
-    if (share) {
-      constexpr float k1 = (float)(1 << kWeightBits), k = 1.f / kBinsPerUnit;
-      const float d = __fmaf_rn(z, inv_bin, -__fsub_rn(m, kMagic));
-      const float f = __fmaf_rn(__fmaf_rn(__fmaf_rn(d, k1 * k * k * k / 6, k1 * k * k / 2), d, k1 * k), d, k1 + 8388608.f);
-      *share = b < kBins - 1 ? __float_as_uint(f) & 0x7fffffu : 0u;
-    }
+    unsigned s;
+    const unsigned b = min(bin_or_more(x, &s), (unsigned)(kBins - 1));
+    if (share) *share = b < kBins - 1 ? s : 0u;
     return (int)b;
+  }
+  // The same without what tells the last bin from those behind it, where the grid is not at the first token.
+  __device__ unsigned bin_or_more(float x, unsigned* share) const {
+    constexpr float k1 = (float)(1 << kWeightBits), k = 1.f / kBinsPerUnit;
+    const float z = __fsub_rn(x, zero), m = __fmaf_rn(z, inv_bin, kMagic), d = __fmaf_rn(z, inv_bin, -__fsub_rn(m, kMagic));
+    const float f = __fmaf_rn(__fmaf_rn(__fmaf_rn(d, k1 * k * k * k / 6, k1 * k * k / 2), d, k1 * k), d, k1 + 8388608.f);
+    *share = __float_as_uint(f) & 0x7fffffu;
+    return (unsigned)first_bin - (unsigned)__float_as_int(m);
   }
   __device__ unsigned share(float x) const {
     unsigned s;
@@ -215,12 +211,12 @@ struct Scale {
   // A score in 32 bits, in units of log 2; a number that is not fit never wins, nor what weighs nothing beside an infinite logit.
   __device__ float score(float x, float e) const {
     const float s = __fsub_rn(below(x), log2_fast(e));
-    return e > 0.f && e < INFINITY && (x == top || top < INFINITY) ? s : -INFINITY;
+    return e >= 0x1p-126f && e < INFINITY && (x == top || top < INFINITY) ? s : -INFINITY;
   }
 };
 
-__device__ void add_shared(uint32_t at, unsigned x, bool on) {
-  asm volatile("{.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.shared.add.u32 [%0], %1;}" ::"r"(at), "r"(x), "r"((unsigned)on) : "memory");
+__device__ void add_shared(uint32_t at, unsigned x, unsigned bin) {
+  asm volatile("{.reg .pred p;\n\tsetp.lt.u32 p, %2, %3;\n\t@p red.shared.add.u32 [%0], %1;}" ::"r"(at), "r"(x), "r"(bin), "n"(kBins - 1) : "memory");
 }
 
 // The score that decides, in 64 bits.  (Not inline: few calls, many registers.)
@@ -303,53 +299,55 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
       for (int i = 0; i < kEach; ++i)
         if (x[i] == x[i]) x[i] = x[i] == INFINITY ? 0.f : -INFINITY;
     }
-    float part = 0.f;
+    const bool race = pick.T > 0.f;
+    const float* noise = p.noise + row * p.noise_stride - from.shift + p0;  // by place
+    const int first_token = p0 + warp * kSegment - from.shift;
+    const bool plain = ((uintptr_t)noise & 15) == 0 && first_token >= 0 && first_token + kSegment <= in.n_vocab;
+    float part = 0.f, best = -INFINITY;
     uint32_t ties = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const float weight = exp2_fast(__fmul_rn(__fsub_rn(x[i], base), scale.unit));
-      const bool tie = x[i] == base;
-      part = __fadd_rn(part, tie ? 0.f : weight);
-      ties |= tie ? 1u << i : 0u;
+    for (int u = 0; u < kEach / 4; ++u) {
+      const int at = place(4 * u / kVec) + 4 * u % kVec;
+      float e[4] = {0.f, 0.f, 0.f, 0.f};
+      if (race) {
+        if (plain) {
+          const float4 v = *(const float4*)(noise + at);
+          e[0] = v.x, e[1] = v.y, e[2] = v.z, e[3] = v.w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if ((unsigned)(p0 + at - from.shift + j) < (unsigned)in.n_vocab) e[j] = noise[at + j];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * u + j;
+        const float below = __fmul_rn(__fsub_rn(x[i], base), scale.unit), weight = exp2_fast(below);
+        const bool tie = x[i] == base;
+        part = __fadd_rn(part, tie ? 0.f : weight);
+        ties |= tie ? 1u << i : 0u;
+        // a score with its logit's number from 1 in its last bits: infinite ones (noise 0 or infinite, logits of -infinity) become
+        // NaN by it, which loses, as does a negative noise's
+        const float f = __fsub_rn(below, log2_fast(e[j]));
+        best = fmaxf(best, __uint_as_float((__float_as_uint(f) & ~31u) | (unsigned)(i + 1)));
+      }
     }
     auto token = [&](int i) { return p0 - from.shift + place(i / kVec) + i % kVec; };  // of x[i]
     const uint32_t first = __reduce_min_sync(~0u, ties ? (uint32_t)token(__ffs(ties) - 1) : ~0u);
     s.top = key_of(top, (int)first);
     s.sum = warp_sum(part) + (float)((int)__reduce_add_sync(~0u, (unsigned)__popc(ties)) - 1);
     s.score = -INFINITY, s.token = -1;
-    if (pick.T > 0.f) {
-      const float* noise = p.noise + row * p.noise_stride - from.shift + p0;  // by place
-      const bool even = ((uintptr_t)noise & 15) == 0;
-      float best = -INFINITY, best_x = 0.f;
-      int best_i = 0;
+    const uint32_t most = __reduce_max_sync(~0u, order(best));
+    if (race && unorder(most) > -INFINITY) {
+      const int best_i = (int)(__float_as_uint(best) & 31u) - 1;
+      const uint32_t mine = order(best) == most ? (uint32_t)token(best_i) : ~0u, e = __reduce_min_sync(~0u, mine);
+      float best_x = x[0];
 #pragma unroll
-      for (int u = 0; u < kEach / 4; ++u) {
-        const int at = place(4 * u / kVec) + 4 * u % kVec;
-        float4 e = {0.f, 0.f, 0.f, 0.f};
-        const int first_token = p0 + at - from.shift;
-        if (even && first_token >= 0 && first_token + 4 <= in.n_vocab) {
-          e = *(const float4*)(noise + at);
-        } else {
-          if ((unsigned)first_token < (unsigned)in.n_vocab) e.x = noise[at];
-          if ((unsigned)(first_token + 1) < (unsigned)in.n_vocab) e.y = noise[at + 1];
-          if ((unsigned)(first_token + 2) < (unsigned)in.n_vocab) e.z = noise[at + 2];
-          if ((unsigned)(first_token + 3) < (unsigned)in.n_vocab) e.w = noise[at + 3];
-        }
-        const float es[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = 4 * u + j;
-          const float f = __fsub_rn(__fmul_rn(__fsub_rn(x[i], base), scale.unit), log2_fast(es[j]));
-          if (es[j] > 0.f && f > best) best = f, best_x = x[i], best_i = i;  // an infinite one's logarithm is infinite too
-        }
-      }
-      const uint32_t most = __reduce_max_sync(~0u, order(best));
-      if (unorder(most) > -INFINITY) {
-        const uint32_t mine = order(best) == most ? (uint32_t)token(best_i) : ~0u, e = __reduce_min_sync(~0u, mine);
-        const int src = __ffs(__ballot_sync(~0u, mine == e)) - 1;
-        s.score = unorder(most), s.token = (int)e, s.token_x = __shfl_sync(~0u, best_x, src);
-        if (top == INFINITY) s.token_x = top;
-      }
+      for (int i = 1; i < kEach; ++i)
+        if (i == best_i) best_x = x[i];
+      s.score = unorder(most), s.token = (int)e;
+      s.token_x = __shfl_sync(~0u, best_x, __ffs(__ballot_sync(~0u, mine == e)) - 1);
+      if (top == INFINITY) s.token_x = top;
     }
   } else {
     bool nan = false;
@@ -363,27 +361,22 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
     __syncthreads();
     const Scale scale(unorder(__reduce_max_sync(~0u, warp_top[lane % kWarps])), pick.T);
     const bool fine = scale.fine(), by_k = pick.k > 0, by_p = pick.p < 1.f;
-    if (fine) {
-      // without branches: of a warp's tokens hardly ever none is entered
+    if (fine && top < INFINITY) {
+      // without branches: of a warp's tokens hardly ever none is entered.  (Logits of -infinity are in the last bin, which nothing reads;
+      // so are all of a stretch whose grid is not the row's.)
       const uint32_t n0 = (uint32_t)__cvta_generic_to_shared(bin_n), w0 = (uint32_t)__cvta_generic_to_shared(bin_w);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         unsigned share;
-        const unsigned b = scale.bin(x[i], &share);
-        if (by_k) add_shared(n0 + 4 * b, 1u, x[i] > -INFINITY);
-        if (by_p) add_shared(w0 + 4 * b, share, share != 0);
+        const unsigned b = scale.bin_or_more(x[i], &share);
+        if (by_k) add_shared(n0 + 4 * b, 1u, b);
+        if (by_p) add_shared(w0 + 4 * b, share, b);
       }
-    } else if (by_k) {  // the row's grid begins elsewhere, or all is far below it
-      unsigned n = 0;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) n += x[i] > -INFINITY;
-      if (n) atomicAdd(&bin_n[kBins - 1], n);
     }
     __syncthreads();
     unsigned* bins = w.bins + ((int64_t)row * blocks + stretch) * 2 * kBins;
     if (by_k) bins[t] = bin_n[t];
     if (by_p) bins[kBins + t] = bin_w[t];
-    s.count = __reduce_add_sync(~0u, bin_n[t]);
   }
   if (lane == 0) w.segment[((int64_t)row * blocks + stretch) * kWarps + warp] = s;
 }
@@ -641,7 +634,6 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
   __syncthreads();
   // add up the segments
   u64 top = 0;
-  int all = 0;
 #pragma unroll
   for (int j = 0; j < kMine; ++j) {
     const int i = t + j * kRowThreads;
@@ -649,7 +641,6 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
       const u64 k = seg[i].top;
       top = max(top, k);
       if (k) atomicMax(&s.stretch_top[i / kWarps], (uint32_t)(k >> 32));
-      if (pick.by_order()) all += (int)seg[i].count;
     }
   }
   top = block_max(top, s.room);
@@ -691,7 +682,6 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
     int bin_k = kBins - 1;
     unsigned n_before = 0, n = 0;
     if (by_order) {
-      all = (int)block_sum_int((unsigned)all, s.room_n);
       // bins of the whole row: of its stretches'; where the grid is too coarse for them (T is small), of its tokens', from
       // the first token down
       const bool fine = scale.fine();
@@ -726,7 +716,6 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
         if (t < kBins - 1) n = s.bin_n[t], sum_w = (u64)s.bin_hi[t] << 32 | s.bin_lo[t];
       }
       n_before = block_before<unsigned>(n, s.room_n);
-      if (t == kBins - 1) n = (unsigned)all - n_before;  // all that is further down
       // as many bits for the sums as fit
       const float about = block_sum(exp2f((float)t * (-1.44269504f / kBinsPerUnit)) * (float)sum_w, s.room_f);
       const int bits = min(44, 60 - (int)(__float_as_uint(fmaxf(about, 1.f)) >> 23) + 127);
@@ -737,10 +726,12 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
       if (t == 0) s.at = kBins - 1;
       __syncthreads();
       total = s.mass_total;
-      by_k = pick.k > 0 && pick.k < all, by_p = pick.p < 1.f;
+      by_k = pick.k > 0, by_p = pick.p < 1.f;
       u64 least = total, most = total;  // mass that p is of
       if (by_k) {
-        if (n_before < (unsigned)pick.k && n_before + n >= (unsigned)pick.k) s.at = t, s.base_mass = mass_before, s.border_mass = mass_before + mass;
+        // the last bin if there are fewer tokens before it (or in all)
+        if (n_before < (unsigned)pick.k && (n_before + n >= (unsigned)pick.k || t == kBins - 1))
+          s.at = t, s.base_mass = mass_before, s.border_mass = mass_before + mass;
         __syncthreads();
         bin_k = s.at, least = s.base_mass, most = s.border_mass;
         sure = out = bin_k;

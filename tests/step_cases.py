@@ -108,7 +108,7 @@ def sample_plain(x, noise, temperature, top_k, top_p, min_p):
         if min_p > 0:
             kept = kept[:max(1, int((w[kept] >= min_p).sum()))]
         e = noise[kept].astype(np.float64)
-        fine = (e > 0) & (e < np.inf)
+        fine = (e >= 2.0 ** -126) & (e < np.inf)
         score = np.where(fine, z[kept] - np.log(np.where(fine, e, 1)), -np.inf)
         if (score > -np.inf).any():
             token = int(kept[score == score.max()].min())
