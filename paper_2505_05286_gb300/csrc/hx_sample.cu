@@ -196,11 +196,11 @@ struct Scale {
     return (int)b;
   }
   // The same without what tells the last bin from those behind it, where the grid is not at the first token.
-  __device__ unsigned bin_or_more(float x, unsigned* share) const {
+  __device__ unsigned bin_or_more(float x, unsigned* share = nullptr) const {
     constexpr float k1 = (float)(1 << kWeightBits), k = 1.f / kBinsPerUnit;
     const float z = __fsub_rn(x, zero), m = __fmaf_rn(z, inv_bin, kMagic), d = __fmaf_rn(z, inv_bin, -__fsub_rn(m, kMagic));
     const float f = __fmaf_rn(__fmaf_rn(__fmaf_rn(d, k1 * k * k * k / 6, k1 * k * k / 2), d, k1 * k), d, k1 + 8388608.f);
-    *share = __float_as_uint(f) & 0x7fffffu;
+    if (share) *share = __float_as_uint(f) & 0x7fffffu;
     return (unsigned)first_bin - (unsigned)__float_as_int(m);
   }
   __device__ unsigned share(float x) const {
@@ -303,33 +303,40 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
     const float* noise = p.noise + row * p.noise_stride - from.shift + p0;  // by place
     const int first_token = p0 + warp * kSegment - from.shift;
     const bool plain = ((uintptr_t)noise & 15) == 0 && first_token >= 0 && first_token + kSegment <= in.n_vocab;
-    float part = 0.f, best = -INFINITY;
+    float part = 0.f, best = -INFINITY, e[kEach];
     uint32_t ties = 0;
+    if (race) {
+      if (plain) {
 #pragma unroll
-    for (int u = 0; u < kEach / 4; ++u) {
-      const int at = place(4 * u / kVec) + 4 * u % kVec;
-      float e[4] = {0.f, 0.f, 0.f, 0.f};
-      if (race) {
-        if (plain) {
-          const float4 v = *(const float4*)(noise + at);
-          e[0] = v.x, e[1] = v.y, e[2] = v.z, e[3] = v.w;
-        } else {
+        for (int u = 0; u < kEach / 4; ++u) {
+          const float4 v = *(const float4*)(noise + place(4 * u / kVec) + 4 * u % kVec);
+          e[4 * u] = v.x, e[4 * u + 1] = v.y, e[4 * u + 2] = v.z, e[4 * u + 3] = v.w;
+        }
+      } else {
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if ((unsigned)(p0 + at - from.shift + j) < (unsigned)in.n_vocab) e[j] = noise[at + j];
+        for (int i = 0; i < kEach; ++i) {
+          const int at = place(i / kVec) + i % kVec;
+          e[i] = (unsigned)(p0 + at - from.shift) < (unsigned)in.n_vocab ? noise[at] : 0.f;
         }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 4 * u + j;
+      for (int i = 0; i < kEach; ++i) {
         const float below = __fmul_rn(__fsub_rn(x[i], base), scale.unit), weight = exp2_fast(below);
         const bool tie = x[i] == base;
         part = __fadd_rn(part, tie ? 0.f : weight);
         ties |= tie ? 1u << i : 0u;
         // a score with its logit's number from 1 in its last bits: infinite ones (noise 0 or infinite, logits of -infinity) become
         // NaN by it, which loses, as does a negative noise's
-        const float f = __fsub_rn(below, log2_fast(e[j]));
+        const float f = __fsub_rn(below, log2_fast(e[i]));
         best = fmaxf(best, __uint_as_float((__float_as_uint(f) & ~31u) | (unsigned)(i + 1)));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const float weight = exp2_fast(__fmul_rn(__fsub_rn(x[i], base), scale.unit));
+        const bool tie = x[i] == base;
+        part = __fadd_rn(part, tie ? 0.f : weight);
+        ties |= tie ? 1u << i : 0u;
       }
     }
     auto token = [&](int i) { return p0 - from.shift + place(i / kVec) + i % kVec; };  // of x[i]
@@ -365,12 +372,20 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
       // without branches: of a warp's tokens hardly ever none is entered.  (Logits of -infinity are in the last bin, which nothing reads;
       // so are all of a stretch whose grid is not the row's.)
       const uint32_t n0 = (uint32_t)__cvta_generic_to_shared(bin_n), w0 = (uint32_t)__cvta_generic_to_shared(bin_w);
+      if (by_k) {
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        unsigned share;
-        const unsigned b = scale.bin_or_more(x[i], &share);
-        if (by_k) add_shared(n0 + 4 * b, 1u, b);
-        if (by_p) add_shared(w0 + 4 * b, share, b);
+        for (int i = 0; i < kEach; ++i) {
+          const unsigned b = scale.bin_or_more(x[i]);
+          add_shared(n0 + 4 * b, 1u, b);
+        }
+      }
+      if (by_p) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          unsigned share;
+          const unsigned b = scale.bin_or_more(x[i], &share);
+          add_shared(w0 + 4 * b, share, b);
+        }
       }
     }
     __syncthreads();
