@@ -14,9 +14,14 @@ namespace {
 
 constexpr int kThreads = 256;
 
+constexpr int kTile = 16;      // tokens of a block at most
+// Loads of a thread on their way at a time: 16-byte ones one by one, as then more threads run (eight prompts of 5600, 32 and 8
+// heads of 128 in bf16: 147 us, four at a time 277), narrow ones four (12 and 12 heads of 90 in f32, 30 of them turned: 61 -> KKK us).
+__host__ __device__ constexpr int at_once(int bytes) { return bytes < 16 ? 4 : 1; }
+
 struct Plan {
-  int vec;         // values of a load
-  int units;       // loads of a head that one thread each takes: pairs of two, then values that are copied
+  int vec;         // values of a load that are turned
+  int wide;        // bytes of a load that are copied, 0: nothing is
   int tile;        // tokens of a block
   int smem;
 };
@@ -37,15 +42,57 @@ __device__ int row_of(const int32_t* row_start, int n_rows, int t, int lane) {
   return lo;
 }
 
+// All tokens and heads of a tile, `units` loads to a head, kAtOnce of a thread on their way at a time: load(q, token, head, unit) for q in
+// order, then store(q, ...).  (q indexes registers.)
+template <int kAtOnce, class Load, class Store>
+__device__ void walk(int n, int heads, int units, const int* on, Load load, Store store) {
+  const bool whole = units <= kThreads;  // a head by fewer threads than there are
+  const int lanes = whole ? kThreads / units : 1, first = whole ? threadIdx.x / units : 0;
+  if (first >= lanes) return;
+  const int step_tok = lanes / heads, step_h = lanes - step_tok * heads;
+  for (int u = whole ? threadIdx.x % units : threadIdx.x; u < units; u += whole ? units : kThreads) {
+    int tok = first / heads, h = first - tok * heads;
+    while (tok < n) {
+      int toks[kAtOnce], hs[kAtOnce];
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        toks[q] = tok < n && on[tok] ? tok : -1, hs[q] = h;
+        if (toks[q] >= 0) load(q, tok, h, u);
+        tok += step_tok, h += step_h;
+        if (h >= heads) h -= heads, ++tok;
+      }
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q)
+        if (toks[q] >= 0) store(q, toks[q], hs[q], u);
+    }
+  }
+}
+
+template <class W>
+__device__ void copy_rest(const hx_rotate_args& a, int64_t t0, int n, const int* on, int size) {
+  const int units = (a.head_dim - a.rotary_dim) * size / (int)sizeof(W);
+  constexpr int kAtOnce = at_once(sizeof(W));
+  W x[kAtOnce];
+  auto place = [&](int tok, int h, int u, bool out) {
+    const bool key = h >= a.n_heads;
+    const int64_t ts = key ? (out ? a.k_out_token_stride : a.k_token_stride) : out ? a.q_out_token_stride : a.q_token_stride;
+    const int64_t hs = key ? (out ? a.k_out_head_stride : a.k_head_stride) : out ? a.q_out_head_stride : a.q_head_stride;
+    const char* base = (const char*)(key ? (out ? a.k_out : a.k) : out ? a.q_out : a.q);
+    return (W*)(base + ((t0 + tok) * ts + (key ? h - a.n_heads : h) * hs + a.rotary_dim) * size) + u;
+  };
+  walk<kAtOnce>(n, a.n_heads + a.n_kv_heads, units, on, [&](int q, int tok, int h, int u) { x[q] = *place(tok, h, u, false); },
+       [&](int q, int tok, int h, int u) { *place(tok, h, u, true) = x[q]; });
+}
+
 template <class T, int V, bool kInterleaved>
-__global__ void __launch_bounds__(1024) hx_rotate_kernel(const hx_rotate_args a, int units, int tile) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) * V == 16 ? 8 : 4) hx_rotate_kernel(const hx_rotate_args a, int tile, int wide) {
   extern __shared__ float2 s_turn[];  // cos and sin, [tile][rotary_dim / 2]: two neighbours of every unit side by side
-  __shared__ int64_t s_pos[16];
-  __shared__ int s_on[16];
+  __shared__ int64_t s_pos[kTile];
+  __shared__ int s_on[kTile];
   const int half = a.rotary_dim / 2;
   const int64_t t0 = (int64_t)blockIdx.x * tile;
   const int n = (int)min((int64_t)tile, a.n_tokens - t0);
-  for (int i = threadIdx.x / 32; i < n; i += blockDim.x / 32) {
+  for (int i = threadIdx.x / 32; i < n; i += kThreads / 32) {
     const int t = (int)(t0 + i), lane = threadIdx.x & 31;
     int64_t pos = 0;
     int on = 1;
@@ -60,7 +107,7 @@ __global__ void __launch_bounds__(1024) hx_rotate_kernel(const hx_rotate_args a,
   }
   __syncthreads();
   constexpr int kSide = V > 1 ? 2 : 1;
-  for (int i = threadIdx.x; i < n * half; i += blockDim.x) {
+  for (int i = threadIdx.x; i < n * half; i += kThreads) {
     const int tok = i / half, j = i - tok * half;
     const uint32_t turn = (uint32_t)(((uint64_t)s_pos[tok] * a.turns[j]) >> 32);
     const uint32_t quarter = (turn + (1u << 29)) >> 30;
@@ -75,73 +122,96 @@ __global__ void __launch_bounds__(1024) hx_rotate_kernel(const hx_rotate_args a,
     s_turn[tok * half + ((w / kSide) * (half / V) + u) * kSide + w % kSide] = float2{c * a.scale, s * a.scale};
   }
   __syncthreads();
-  const int lanes = blockDim.x / units;  // heads at a time
-  const int u = threadIdx.x % units, first = threadIdx.x / units;
-  if (first >= lanes) return;
-  const int H = a.n_heads + a.n_kv_heads;
-  const bool turned = u < half / V;
-  // where the unit's values are in a head
-  const int at = !turned ? a.rotary_dim + (u - half / V) * V : kInterleaved ? 2 * u * V : u * V;
-  const int apart = kInterleaved ? V : half;
   using P = Pack<T, V>;
-  for (int r = first; r < n * H; r += lanes) {
-    const int tok = r / H, h = r - tok * H;
-    if (!s_on[tok]) continue;
-    const int64_t t = t0 + tok;
-    const bool key = h >= a.n_heads;
-    const int hh = key ? h - a.n_heads : h;
-    const T* from = (const T*)(key ? a.k : a.q) + t * (key ? a.k_token_stride : a.q_token_stride) +
-                    hh * (key ? a.k_head_stride : a.q_head_stride) + at;
-    T* to = (T*)(key ? a.k_out : a.q_out) + t * (key ? a.k_out_token_stride : a.q_out_token_stride) +
-            hh * (key ? a.k_out_head_stride : a.q_out_head_stride) + at;
-    if (!turned) {
-      *(P*)to = *(const P*)from;
-      continue;
-    }
-    P x = *(const P*)from, y = *(const P*)(from + apart);
+  const int apart = kInterleaved ? V : half, H = a.n_heads + a.n_kv_heads;
+  auto turn = [&](P& x, P& y, int tok, int u) {
     const float2* cs = s_turn + tok * half;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      T& p = kInterleaved ? (2 * i < V ? x.v[2 * i % V] : y.v[2 * i % V]) : x.v[i];
-      T& q = kInterleaved ? (2 * i + 1 < V ? x.v[(2 * i + 1) % V] : y.v[(2 * i + 1) % V]) : y.v[i];
+      T& c = kInterleaved ? (2 * i < V ? x.v[2 * i % V] : y.v[2 * i % V]) : x.v[i];
+      T& d = kInterleaved ? (2 * i + 1 < V ? x.v[(2 * i + 1) % V] : y.v[(2 * i + 1) % V]) : y.v[i];
       const float2 w = cs[((i / kSide) * (half / V) + u) * kSide + i % kSide];
-      const float f = to_float(p), g = to_float(q);
-      p = from_float<T>(f * w.x - g * w.y);
-      q = from_float<T>(f * w.y + g * w.x);
+      const float f = to_float(c), g = to_float(d);
+      c = from_float<T>(f * w.x - g * w.y);
+      d = from_float<T>(f * w.y + g * w.x);
     }
-    *(P*)to = x;
-    *(P*)(to + apart) = y;
+  };
+  if constexpr (at_once(sizeof(P)) == 1) {
+    const int units = half / V, lanes = kThreads / units, u = threadIdx.x % units, first = threadIdx.x / units;  // half / V <= 64
+    const int at = kInterleaved ? 2 * u * V : u * V;
+    for (int r = first < lanes ? first : n * H; r < n * H; r += lanes) {
+      const int tok = r / H, h = r - tok * H;
+      if (!s_on[tok]) continue;
+      const int64_t t = t0 + tok;
+      const bool key = h >= a.n_heads;
+      const int hh = key ? h - a.n_heads : h;
+      const T* from = (const T*)(key ? a.k : a.q) + t * (key ? a.k_token_stride : a.q_token_stride) +
+                      hh * (key ? a.k_head_stride : a.q_head_stride) + at;
+      T* to = (T*)(key ? a.k_out : a.q_out) + t * (key ? a.k_out_token_stride : a.q_out_token_stride) +
+              hh * (key ? a.k_out_head_stride : a.q_out_head_stride) + at;
+      P x = *(const P*)from, y = *(const P*)(from + apart);
+      turn(x, y, tok, u);
+      *(P*)to = x;
+      *(P*)(to + apart) = y;
+    }
+  } else {
+    constexpr int kAtOnce = at_once(sizeof(P));
+    P x[kAtOnce], y[kAtOnce];
+    auto place = [&](int tok, int h, int u, bool out) {
+      const bool key = h >= a.n_heads;
+      const int64_t ts = key ? (out ? a.k_out_token_stride : a.k_token_stride) : out ? a.q_out_token_stride : a.q_token_stride;
+      const int64_t hs = key ? (out ? a.k_out_head_stride : a.k_head_stride) : out ? a.q_out_head_stride : a.q_head_stride;
+      T* base = (T*)(key ? (out ? a.k_out : a.k) : out ? a.q_out : a.q);
+      return base + (t0 + tok) * ts + (key ? h - a.n_heads : h) * hs + (kInterleaved ? 2 * u * V : u * V);
+    };
+    walk<kAtOnce>(n, H, half / V, s_on,
+                  [&](int q, int tok, int h, int u) {
+                    const T* from = place(tok, h, u, false);
+                    x[q] = *(const P*)from, y[q] = *(const P*)(from + apart);
+                  },
+                  [&](int q, int tok, int h, int u) {
+                    turn(x[q], y[q], tok, u);
+                    T* to = place(tok, h, u, true);
+                    *(P*)to = x[q], *(P*)(to + apart) = y[q];
+                  });
   }
+  if (wide == 16) copy_rest<uint4>(a, t0, n, s_on, sizeof(T));
+  if (wide == 8) copy_rest<uint2>(a, t0, n, s_on, sizeof(T));
+  if (wide == 4) copy_rest<uint32_t>(a, t0, n, s_on, sizeof(T));
+  if (wide == 2) copy_rest<uint16_t>(a, t0, n, s_on, sizeof(T));
 }
 
-// The widest load whose places all arguments allow.
+// The widest loads whose places all arguments allow, and tiles of so many tokens that every thread has some items to load at a
+// time, but no fewer blocks than run at once.
 Plan plan(const hx_rotate_args& a, int size) {
   const int half = a.rotary_dim / 2;
   const bool in_place = a.q_out == a.q && (!a.k || a.k_out == a.k);
   const int rest = in_place ? 0 : a.head_dim - a.rotary_dim;
-  uint64_t all = half | rest;
-  if (a.n_tokens > 1)
-    all |= a.q_token_stride | a.q_out_token_stride | (a.k ? a.k_token_stride | a.k_out_token_stride : 0);
+  uint64_t all = 0;  // strides, in values
+  if (a.n_tokens > 1) all |= a.q_token_stride | a.q_out_token_stride | (a.k ? a.k_token_stride | a.k_out_token_stride : 0);
   if (a.n_heads > 1) all |= a.q_head_stride | a.q_out_head_stride;
   if (a.n_kv_heads > 1) all |= a.k_head_stride | a.k_out_head_stride;
-  const uint64_t base = (uint64_t)a.q | (uint64_t)a.q_out | (uint64_t)a.k | (uint64_t)(a.k ? a.k_out : nullptr);
-  Plan p;
+  all = all * size | (uint64_t)a.q | (uint64_t)a.q_out | (uint64_t)a.k | (uint64_t)(a.k ? a.k_out : nullptr);
+  Plan p = {};
   p.vec = 16 / size;
-  while (p.vec > 1 && (all % p.vec || base % (p.vec * size))) p.vec /= 2;
-  p.units = half / p.vec + rest / p.vec;
-  p.tile = 1;
+  while (p.vec > 1 && (all % (p.vec * size) || half % p.vec)) p.vec /= 2;
+  if (rest) {
+    p.wide = 16;
+    while ((all | a.rotary_dim * size | rest * size) % p.wide) p.wide /= 2;
+  }
+  const int heads = a.n_heads + a.n_kv_heads, lanes = std::max(1, kThreads / (half / p.vec));
+  p.tile = std::min({kTile, (at_once(p.vec * size) * lanes + heads - 1) / heads, std::max(1, 16384 / (8 * half)), std::max(1, a.n_tokens / (4 * 152))});
   p.smem = p.tile * half * (int)sizeof(float2);
   return p;
 }
 
 template <class T, int V>
 cudaError_t launch(const hx_rotate_args& a, const Plan& p, cudaStream_t s) {
-  const int threads = std::max(kThreads, (p.units + 31) / 32 * 32);
   const unsigned blocks = (unsigned)((a.n_tokens + p.tile - 1) / p.tile);
   if (a.interleaved)
-    hx_rotate_kernel<T, V, true><<<blocks, threads, p.smem, s>>>(a, p.units, p.tile);
+    hx_rotate_kernel<T, V, true><<<blocks, kThreads, p.smem, s>>>(a, p.tile, p.wide);
   else
-    hx_rotate_kernel<T, V, false><<<blocks, threads, p.smem, s>>>(a, p.units, p.tile);
+    hx_rotate_kernel<T, V, false><<<blocks, kThreads, p.smem, s>>>(a, p.tile, p.wide);
   return cudaGetLastError();
 }
 

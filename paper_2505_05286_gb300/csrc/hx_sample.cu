@@ -226,7 +226,7 @@ __device__ __noinline__ u64 exact_score(float top, float T, float x, float e) {
 }
 
 template <class T, bool kWords>
-__global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits in, const hx_rules r, const hx_pick p, const Work w, int blocks) {
+__global__ void __launch_bounds__(kRowThreads, kWords ? 2 : 3) hx_sample_scan(const hx_logits in, const hx_rules r, const hx_pick p, const Work w, int blocks) {
   __shared__ alignas(16) uint32_t word[kWords ? kStretch : 4];
   __shared__ unsigned bin_n[kBins], bin_w[kBins];
   __shared__ uint32_t warp_top[kWarps];
@@ -235,18 +235,18 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
   constexpr int kVec = R::kVec;
   const int row = blockIdx.x / blocks, stretch = blockIdx.x - row * blocks, p0 = stretch * kStretch;
   const int t = threadIdx.x, lane = t % 32, warp = t / 32;
+  Pick pick;
+  pick.k = p.top_k ? p.top_k[row] : p.all_top_k;
+  pick.T = !p.noise ? 0.f : p.temperature ? p.temperature[row] : p.all_temperature;
+  pick.p = p.top_p ? p.top_p[row] : p.all_top_p;
+  pick.m = p.min_p ? p.min_p[row] : p.all_min_p;
   if (t == 0) {
-    Pick a;
-    a.k = p.top_k ? p.top_k[row] : p.all_top_k;
-    a.T = !p.noise ? 0.f : p.temperature ? p.temperature[row] : p.all_temperature;
-    a.p = p.top_p ? p.top_p[row] : p.all_top_p;
-    a.m = p.min_p ? p.min_p[row] : p.all_min_p;
-    s_pick = a;
-    if (stretch == 0) w.pick[row] = a;
+    s_pick = pick;
+    if (stretch == 0) w.pick[row] = pick;
   }
   bin_n[t] = bin_w[t] = 0;
   const R from(in, row);
-  if (p.noise && (p.temperature ? p.temperature[row] : p.all_temperature) > 0.f) {
+  if (pick.T > 0.f) {
     // the noise is asked for now and read when the logits are done: a line for each of some threads
     const int e = p0 - from.shift + 32 * t;
     if (t < kStretch / 32 && (unsigned)e < (unsigned)in.n_vocab)
@@ -258,11 +258,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
 #pragma unroll
   for (int u = 0; u < kEach / kVec; ++u) raw[u] = from.load((p0 + place(u)) / kVec);
   const RowRules o(r, row);
-  if (kWords)
-    o.count<kStretch>(p0, from.shift, in.n_vocab, word);
-  else
-    __syncthreads();
-  const Pick pick = s_pick;
+  if (kWords) o.count<kStretch>(p0, from.shift, in.n_vocab, word);
   float x[kEach], top = -INFINITY;
 #pragma unroll
   for (int u = 0; u < kEach / kVec; ++u) {
@@ -363,9 +359,10 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_scan(const hx_logits
     s.sum = __any_sync(~0u, nan) ? NAN : 0.f;
     s.token = -1;
   }
+  if (lane == 0) warp_top[warp] = order(top);
+  __syncthreads();
+  pick = s_pick;  // for all threads the same, whatever becomes of the parameters meanwhile: there are barriers behind
   if (pick.by_order()) {
-    if (lane == 0) warp_top[warp] = order(top);
-    __syncthreads();
     const Scale scale(unorder(__reduce_max_sync(~0u, warp_top[lane % kWarps])), pick.T);
     const bool fine = scale.fine(), by_k = pick.k > 0, by_p = pick.p < 1.f;
     if (fine && top < INFINITY) {
@@ -644,8 +641,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
   const Segment* seg = w.segment + (int64_t)row * blocks * kWarps;
   const int n_seg = blocks * kWarps;
   constexpr int kMine = (kMaxStretches * kWarps + kRowThreads - 1) / kRowThreads;  // segments of a thread
-  const Pick pick = w.pick[row];
   if (t < kMaxStretches) s.stretch_top[t] = 0;
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched while the scan still runs
+  const Pick pick = w.pick[row];
   __syncthreads();
   // add up the segments
   u64 top = 0;
@@ -910,8 +908,17 @@ cudaError_t launch(const hx_logits& x, const hx_rules& r, const hx_pick& p, cuda
   const auto kernel = hx_sample_pick<T, kWords>;
   if (kWords)
     if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)) return e;
-  kernel<<<x.n_rows, kRowThreads, kSmem, s>>>(x, r, p, w, blocks);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(x.n_rows);
+  cfg.blockDim = kRowThreads;
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, x, r, p, w, blocks);
 }
 
 template <class T>
