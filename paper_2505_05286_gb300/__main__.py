@@ -10,6 +10,7 @@ operators on this GPU.
     python -m paper_2505_05286_gb300 --tune 5,20,5 --seconds 60,40,60 --window-s 20
     python -m paper_2505_05286_gb300 --recipe 4 --tune 20,30,20 --seconds 1500 --window-s 300 --time-sweeps
     python -m paper_2505_05286_gb300 --recipe 1 --traces 1 --queries 200 --replay 6
+    python -m paper_2505_05286_gb300 --recipe 1 --traces 1 --queries 200 --replay 6 --rope 10000 --vocab 32000
 """
 from __future__ import annotations
 
@@ -99,7 +100,9 @@ def replay(args) -> int:
         sim.run()
         records = sim.records(0)
     out = {"workload": wl.name, "point": point}
-    out.update(R.replay(wl.traces[0], records, wl.cluster, args.replay, chunk=args.chunk, max_steps=args.steps))
+    more = {"shape": R.Shape(theta=args.rope, vocab=args.vocab)} if args.rope or args.vocab else {}
+    out.update(R.replay(wl.traces[0], records, wl.cluster, args.replay, chunk=args.chunk, max_steps=args.steps, **more))
+    out.update({name: x for name, x in (("rope", args.rope), ("vocab", args.vocab)) if x})
     print(json.dumps(out))
     return 0
 
@@ -121,6 +124,8 @@ def main(argv=None) -> int:
     ap.add_argument("--replay", type=int, default=None, metavar="INSTANCE",
                     help="run this instance's calls of the best point's schedule as serving steps")
     ap.add_argument("--steps", type=int, default=1000, help="--replay: steps at most")
+    ap.add_argument("--rope", type=float, default=0.0, metavar="THETA", help="--replay: turn queries and keys by their positions")
+    ap.add_argument("--vocab", type=int, default=0, metavar="N", help="--replay: draw each row's token from N logits")
     ap.add_argument("--chunk", type=int, default=512, help="--replay: prompt tokens of a request in one step at most")
     args = ap.parse_args(argv)
     if args.tune is not None:

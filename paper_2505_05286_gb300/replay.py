@@ -16,7 +16,10 @@ work, and its launches are waiting when it begins.
     rep["us_per_step"], rep["us_per_1000_tokens"]     # of steps in which every request decodes
     rep["prompt_us_per_token"]
 
-Queries, keys and values are random; a real model's products are not part of it.
+With Shape.theta queries and keys are turned by their positions first, and with Shape.vocab each row's next token is drawn from
+logits at the end, with penalties for the tokens that its request holds.
+
+Queries, keys, values and logits are random; a real model's products are not part of it.
 """
 from __future__ import annotations
 
@@ -28,16 +31,20 @@ import torch
 
 from . import hxsim as H
 from . import kvcache as KV
+from . import logits as L
 
 
 @dataclass
 class Shape:
-    """The attention of one layer."""
+    """The attention of one layer; theta: the base of its rotary positions (0: none); vocab: the step ends with a
+    token for each row from so many logits (0: it does not)."""
     heads: int = 32
     kv_heads: int = 8
     head_dim: int = 128
     block_tokens: int = 64
     dtype: torch.dtype = torch.bfloat16
+    theta: float = 0.0
+    vocab: int = 0
 
 
 @dataclass
@@ -75,6 +82,20 @@ class Batch:
         self.qkv = None
         self.out = None
         self.step = None
+        self.q = self.k = None
+        self.token = self.logprob = None
+        if shape.theta:
+            self.rope = KV.Rope(KV.Rope.frequencies(shape.head_dim, shape.theta))
+        if shape.vocab:
+            V = shape.vocab
+            self.prompt = np.zeros(slots, np.int32)
+            self.logits = (3 * torch.randn((slots, V), generator=self.gen, device="cuda")).to(shape.dtype)
+            self.noise = torch.empty((slots, V), device="cuda").exponential_(generator=self.gen)
+            self.history = torch.randint(0, V, (slots, longest + 1), generator=self.gen, **i32)
+            self.lengths = torch.zeros((2, slots), **i32)  # held and the prompt's
+            full = lambda x: torch.full((slots,), x, device="cuda")
+            self.rules = L.Rules(history=self.history, length=self.lengths[0], prompt_len=self.lengths[1], repetition=full(1.1),
+                                 presence=full(0.1), frequency=full(0.05))
 
     def run(self, add: np.ndarray):
         """One step: row r gets add[r] tokens (0: none, -1: it has ended).  Returns the start and end events."""
@@ -85,15 +106,26 @@ class Batch:
             self.qkv = torch.randn((n, s.heads + 2 * s.kv_heads, s.head_dim), generator=self.gen, device="cuda").to(s.dtype)
         both = torch.from_numpy(np.stack([self.held, add]).astype(np.int32)).cuda()
         x = self.qkv[:n]
+        if s.vocab:
+            self.prompt = np.where((add < 0) | (self.held == 0), 0, self.prompt) + np.where((tok > 1) | (self.held == 0), tok, 0)
+            self.lengths.copy_(torch.from_numpy(np.stack([self.held + tok, self.prompt]).astype(np.int32)))
         begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         self.flush.zero_()
         begin.record()
         self.step = KV.map_step(both[0], both[1], self.table, self.ring, self.state, n, s.block_tokens)
         if n:
-            self.cache.append(x[:, s.heads:s.heads + s.kv_heads], x[:, s.heads + s.kv_heads:], self.step.runs)
-            self.out = self.cache.attend(x[:, :s.heads], self.table, self.step.row_start, self.step.kv_len,
+            self.q, self.k = x[:, :s.heads], x[:, s.heads:s.heads + s.kv_heads]
+            if s.theta:
+                self.q, self.k = self.rope.rotate(self.q, self.k, self.step.row_start, self.step.kv_len)
+            self.cache.append(self.k, x[:, s.heads + s.kv_heads:], self.step.runs)
+            self.out = self.cache.attend(self.q, self.table, self.step.row_start, self.step.kv_len,
                                          max_q=int(tok.max()))
+            if s.vocab:
+                self.token, self.logprob = L.sample(self.logits, self.noise, temperature=0.8, top_p=0.95, rules=self.rules)
         end.record()
+        if n and s.vocab:  # what each row will have said when its next token is drawn, and other random numbers for that
+            self.history.scatter_(1, self.lengths[:1].t().long().clamp(max=self.history.shape[1] - 1), self.token[:, None].clamp(min=0))
+            self.noise.exponential_(generator=self.gen)
         self.state = self.step.ring_state
         self.held = np.where(add < 0, 0, self.held + tok).astype(np.int32)
         return begin, end
