@@ -35,7 +35,7 @@ typedef struct hx_rotate_args {
   const void* k;              /* NULL: queries alone, n_kv_heads is 0 */
   void* q_out;                /* aligned to the type, as q and k */
   void* k_out;
-  int64_t q_token_stride, q_head_stride;          /* elements, 0..2^38 */
+  int64_t q_token_stride, q_head_stride;          /* elements, 0..2^38, and times their number at most 2^44 */
   int64_t k_token_stride, k_head_stride;
   int64_t q_out_token_stride, q_out_head_stride;  /* elements, 0..2^38; no two values at one place */
   int64_t k_out_token_stride, k_out_head_stride;

@@ -125,7 +125,7 @@ struct RowRules {
 
 // Few tokens have a word: 3 of 100 after 4000 tokens of 131072, but hardly a warp has none among its 256.  So every thread takes
 // its own words one after the other, and the warp as many turns as the lane that has the most, where adjusting
-// all places of a load with a word in it took 900 instructions a thread (256 rows, all rules: 75 us; so KKK).
+// all places of a load with a word in it took 900 instructions a thread (256 rows of 131072, all rules: 75 us; so 56).
 // Each operation is rounded by itself: the same logits give the same adjusted ones wherever they are adjusted.
 __device__ inline float adjusted(const RowRules& o, float x, uint32_t word) {
   if (word & (kTimes | kRead)) {

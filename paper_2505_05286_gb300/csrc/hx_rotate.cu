@@ -4,6 +4,10 @@
 // phi = 2 pi * position * turns.  Turns a position are 64-bit fractions, so position * turns
 // modulo 2^64 is the angle without loss, at any position; its upper 32 bits, less the nearest
 // quarter turn, convert to 32-bit floating point within 2^-25 of a radian.
+//
+// Bound by memory: every value is read once and written once.  A block has a tile of tokens; their angles' cosines and sines are formed
+// once for all heads, in shared memory.  Eight prompts of 5600 tokens, 32 and 8 heads of 128 in bf16: 149 us, 6.35 TB/s, 94 %
+// of a copy; 28 and 4 heads of 64, half of them turned: 66 us, 85 %; 16 single tokens: 3.1 us, a launch and two chains of loads.
 #include <algorithm>
 
 #include "hx_step.cuh"
@@ -16,7 +20,7 @@ constexpr int kThreads = 256;
 
 constexpr int kTile = 16;      // tokens of a block at most
 // Loads of a thread on their way at a time: 16-byte ones one by one, as then more threads run (eight prompts of 5600, 32 and 8
-// heads of 128 in bf16: 147 us, four at a time 277), narrow ones four (12 and 12 heads of 90 in f32, 30 of them turned: 61 -> KKK us).
+// heads of 128 in bf16: 147 us, four at a time 277), narrow ones four (12 and 12 heads of 90 in f32, 30 of them turned: 61 -> 37 us).
 __host__ __device__ constexpr int at_once(int bytes) { return bytes < 16 ? 4 : 1; }
 
 struct Plan {

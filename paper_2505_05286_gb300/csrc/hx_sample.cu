@@ -18,6 +18,10 @@
 // Sums that decide where an order is cut are of whole numbers, so that no order of additions is of matter;
 // those of the log-probability are 32-bit sums in a fixed order, without the first token, whose
 // weight is 1: the logarithm of a share near 1 keeps its bits.
+//
+// 256 rows of 131072 logits in bf16: the likeliest tokens 36 us (of them the scan 30; reading the logits takes 10), by temperature alone
+// 58 us (3.5 TB/s: the noise is twice the logits), by top-p 82 us: the scan 60, bound by instructions (56 for a logit, 19 of them
+// for its bin), the pick 22, a chain of barriers and, in one row of five, a resolved filter.  One row of 32000: 11.5 us.
 #include <algorithm>
 
 #include "hx_logits.cuh"
@@ -174,8 +178,9 @@ struct Scale {
     first = __fmul_rn(top, inv_bin);
     first_bin = __float_as_int(__fmaf_rn(top, inv_bin, kMagic));
   }
-  // Whether the grid has steps of 1 / 2 at least where the first token is, and numbers at all.
-  __device__ bool fine() const { return fabsf(first) < 4e6f; }
+  // Whether the grid has steps of 1 / 2 at least where the first token is, and numbers at all.  A row asks for less than its stretches
+  // do: one that has no bins because its grid is not fine lies far below a row whose grid is.
+  __device__ bool fine(float below = 4e6f) const { return fabsf(first) < below; }
   __device__ void begin_at_top() { zero = top, coarse = true, first = 0.f, first_bin = __float_as_int(kMagic); }
   // log2 of the weight
   __device__ float below(float x) const { return x == top ? 0.f : __fmul_rn(__fsub_rn(x, top), unit); }
@@ -697,7 +702,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
     if (by_order) {
       // bins of the whole row: of its stretches'; where the grid is too coarse for them (T is small), of its tokens', from
       // the first token down
-      const bool fine = scale.fine();
+      const bool fine = scale.fine(3.9e6f);
       if (t < blocks) s.away[t] = !s.stretch_top[t] ? kBins : fine ? scale.bin(clean(unorder(s.stretch_top[t]))) : 0;
       s.bin_n[t] = s.bin_lo[t] = s.bin_hi[t] = 0;
       __syncthreads();

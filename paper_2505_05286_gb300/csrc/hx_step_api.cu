@@ -150,6 +150,9 @@ int hx_rotate(const hx_rotate_args* a, void* stream) {
   for (int i = 0; i < (a->k ? 8 : 4); ++i)
     if (strides[i] < 0 || strides[i] >= (int64_t)1 << 38) return bad("rotate: strides must be 0..2^38");
   const int64_t T = a->n_tokens, D = a->head_dim;
+  for (int i = 0; i < (a->k ? 8 : 4); ++i)  // so that no place below overflows
+    if (strides[i] > ((int64_t)1 << 44) / (i % 2 == 0 ? T : i < 4 ? a->n_heads : a->n_kv_heads))
+      return bad("rotate: an array spans more than 2^44 values");
   const Places q = places(a->q, T, a->q_token_stride, a->n_heads, a->q_head_stride, D, size);
   const Places qo = places(a->q_out, T, a->q_out_token_stride, a->n_heads, a->q_out_head_stride, D, size);
   if (!qo.apart()) return bad("rotate: two values of q_out are at one place");

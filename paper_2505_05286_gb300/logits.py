@@ -222,7 +222,7 @@ def sample(logits, noise=None, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0
         else:
             if kind == torch.int32:
                 _count(x, "sample: " + name)
-            setattr(p, "all_" + name, x)
+            setattr(p, "all_" + name, int(x) if kind == torch.int32 else float(x))
     lib = load()
     with _on(dev, stream) as handle:
         if out is None:

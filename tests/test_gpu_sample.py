@@ -129,6 +129,17 @@ def test_sample_special_values():
     _check_sample(x, e, 1.0, 0, 1.0, 0.0)
 
 
+@pytest.mark.parametrize("at", [-3.9e6, -4e6, -4.1e6, 3.9e6, 4e6, -1e7, 1e20])
+def test_sample_far_from_zero(at):
+    """Logits so far from zero that the grid of bins ends between one part of the vocabulary and another: x / T * 16 about `at`."""
+    rng = np.random.default_rng(6)
+    V = 40000
+    x = torch.from_numpy((at / 16 + rng.standard_normal((3, V)) * max(3.0, abs(at) * 2e-8)).astype(np.float32)).cuda()
+    e = _noise(rng, 3, V)
+    for k, p in ((0, 0.9), (300, 1.0), (300, 0.7), (30000, 0.999)):
+        _check_sample(x, e, 1.0, k, p, 0.0)
+
+
 def test_sample_scores_next_to_each_other():
     """Scores that 32 bits cannot tell apart are told apart in 64, equal ones go to the lowest token."""
     rng = np.random.default_rng(5)

@@ -89,7 +89,7 @@ def test_rotate_refusals(lib):
                     (dict(turns=None), "NULL"), (dict(q=None), "NULL"), (dict(k_out=None), "NULL"), (dict(q=FAKE + 1), "aligned"),
                     (dict(k_out=FAKE + 3 * MB + 1), "aligned"), (dict(turns=FAKE + 4 * MB + 4), "aligned"),
                     (dict(row_start=FAKE + 5 * MB + 2), "aligned"), (dict(kv_len=FAKE + 6 * MB + 2), "aligned"),
-                    (dict(q_token_stride=-256), "strides"), (dict(k_head_stride=2 ** 38), "strides"),
+                    (dict(q_token_stride=-256), "strides"), (dict(n_tokens=2 ** 30, q_token_stride=2 ** 37), "2^44"), (dict(k_head_stride=2 ** 38), "strides"),
                     (dict(q_out_token_stride=255), "one place"), (dict(q_out_head_stride=63), "one place"),
                     (dict(k_out_token_stride=0), "one place"), (dict(q_out=FAKE + 2), "overlaps q"),
                     (dict(q_out=FAKE, q_out_head_stride=128, q_out_token_stride=512), "other strides"),
