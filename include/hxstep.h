@@ -127,8 +127,9 @@ int64_t hx_sample_workspace(const hx_logits* x, const hx_rules* r, const hx_pick
  * x / T - log(noise) is picked (the lowest of equals), which is one by their weights; logprob is the logarithm of its
  * share of all tokens' weights, before the filters (of exp(x) where T is not above 0).  Tokens with x = -infinity or NaN take no
  * part; a NaN makes the row's logprob NaN.  Where none is left, token is -1 and logprob -infinity.  A noise that is
- * not a finite number of at least 2^-126 never wins; if no token's does, the first of the order is picked.  Weights are in 32 bits
- * and are summed in 64-bit whole numbers, scores near the largest are compared in 64 bits: the same inputs give the same token. */
+ * not a finite number of at least 2^-126 never wins; if no token's does, the first of the order is picked.
+ * Weights are in 32 bits (their shares within a filter, in 2^-18 of a weight); what decides where the order ends is added up in whole
+ * numbers, and scores near the largest are compared in 64 bits: the same inputs give the same token and logprob. */
 int hx_sample(const hx_logits* x, const hx_rules* r, const hx_pick* p, void* stream);
 
 #ifdef __cplusplus

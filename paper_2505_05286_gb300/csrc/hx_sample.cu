@@ -11,17 +11,17 @@
 //          the bins before the one in which a filter ends.  The best of the segments' winners that are left for sure is nearly the row's: only
 //          the few segments whose winner scores more, or as much but for rounding, can hold a better one, and are read again.
 //
-// Where the race turns on a token of the bin in which a filter ends, that bin is resolved: its tokens are sorted and
-// cut exactly where the filter says (by the range of their keys before that, until they fit one list).  Where no
-// segment's winner is left, the race of what is left reads the row.
+// Where the race turns on a token of the bin in which a filter ends, that bin is resolved: the range of its tokens' keys
+// is cut in parts until few are left, which are sorted and cut exactly where the filter says.  Where no
+// segment's winner is left, all that are left race, in the segments whose first token is, or where there are too many in the row.
 //
 // Sums that decide where an order is cut are of whole numbers, so that no order of additions is of matter;
 // those of the log-probability are 32-bit sums in a fixed order, without the first token, whose
 // weight is 1: the logarithm of a share near 1 keeps its bits.
 //
 // 256 rows of 131072 logits in bf16: the likeliest tokens 36 us (of them the scan 30; reading the logits takes 10), by temperature alone
-// 58 us (3.5 TB/s: the noise is twice the logits), by top-p 82 us: the scan 60, bound by instructions (56 for a logit, 19 of them
-// for its bin), the pick 22, a chain of barriers and, in one row of five, a resolved filter.  One row of 32000: 11.5 us.
+// 58 us (3.5 TB/s: the noise is twice the logits), by top-p 82 to 152 us: the scan 60, bound by instructions (55 for a logit, 19 of them
+// for its bin), the pick 22, a chain of barriers, or up to 90 where a row has to be read again.  One row of 32000: 11.5 us.
 #include <algorithm>
 
 #include "hx_logits.cuh"
@@ -37,12 +37,16 @@ constexpr int kSegment = kStretch / kWarps;  // places of a warp
 constexpr int kBins = kRowThreads;           // a thread each
 constexpr float kBinsPerUnit = 16.f;
 constexpr int kWeightBits = 18;              // a weight within its bin: 8192 of them stay below 2^32
-constexpr int kList = 2048;                  // tokens of a row that are sorted at once
+constexpr int kList = 4096;                  // tokens of a bin that are kept at once
+constexpr int kShort = 128;                  // of them that are sorted
 constexpr int kMaxStretches = 64;
-constexpr int kMostAgain = 64;               // segments that are read again, where not the whole row is
-constexpr int kMostNear = 64;                // tokens in them whose scores are next to the best
+// Segments that are read again, where not the whole row is: four segments take as long as a stretch of sixteen (top-k of 256 rows: 90 us,
+// with up to 128 of them 111).
+constexpr int kMostAgain = 32;
+constexpr int kMostNear = 256;               // tokens in them whose scores are next to the best
 static_assert((HX_MAX_VOCAB + 8 + kStretch - 1) / kStretch <= kMaxStretches, "stretches of a row");
-static_assert(kList % kRowThreads == 0, "tokens of a list by threads");
+static_assert(kMostNear <= kRowThreads, "tokens next to the best by threads");
+static_assert(kShort <= kRowThreads, "tokens of a short list by threads");
 
 struct Pick {
   int k;
@@ -403,6 +407,7 @@ __global__ void __launch_bounds__(kRowThreads, kWords ? 2 : 3) hx_sample_scan(co
 struct Shared {
   u64 room[kWarps];
   u64 list[kList];          // keys
+  u64 sorted[kShort];
   u64 mass_total;
   u64 border_mass, base_mass;
   float room_f[kWarps];
@@ -427,9 +432,9 @@ struct RowAgain {
   uint32_t* word;
   int blocks;
 
-  // Those that are at least `least`.
+  // Those from `least` to `most`.
   template <class F>
-  __device__ void each(float least, F f) const {
+  __device__ void each(float least, float most, F f) const {
     constexpr int kVec = RowOf<T>::kVec, kLoads = kEach / kVec;
     Pack<T, kVec> raw[kLoads];
     auto load = [&](int c) {
@@ -446,7 +451,10 @@ struct RowAgain {
         const int i = u * kRowThreads + threadIdx.x, vec = p0 / kVec + i;
         uint32_t bits = 0;
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) bits |= to_float(raw[u].v[j]) >= least ? 1u << j : 0u;
+        for (int j = 0; j < kVec; ++j) {
+          const float x = to_float(raw[u].v[j]);
+          bits |= x >= least && x <= most ? 1u << j : 0u;
+        }
         if (row.token(vec) < row.n_vocab) {
           if (kWords) bits |= RowOf<T>::worded(word + i * kVec);
           if (bits && rules.mask) bits &= row.allowed(rules.mask, vec);
@@ -460,7 +468,7 @@ struct RowAgain {
         if ((unsigned)e >= (unsigned)row.n_vocab) continue;
         float x = to_float(row.first[e]);
         if (kWords && word[i]) x = adjusted(rules, x, word[i]);
-        if (x >= least && x > -INFINITY) f(clean(x), e);
+        if (x >= least && x <= most && x > -INFINITY) f(clean(x), e);
       }
       if (kWords) __syncthreads();  // the words are the next stretch's
     }
@@ -540,18 +548,18 @@ struct Picker {
     if (was + w < was) atomicAdd(&s.bin_hi[bin], 1u);
   }
 
-  // Sorts s.list[0, n), the largest first.
+  // Sorts s.sorted[0, n), the largest first.
   __device__ void sort(int n) {
     int size = 2;
     while (size < n) size *= 2;
-    for (int i = n + threadIdx.x; i < size; i += kRowThreads) s.list[i] = 0;
+    for (int i = n + threadIdx.x; i < size; i += kRowThreads) s.sorted[i] = 0;
     __syncthreads();
     for (int run = 2; run <= size; run *= 2)
       for (int d = run / 2; d; d /= 2) {
         for (int i = threadIdx.x; i < size / 2; i += kRowThreads) {
           const int a = (i & ~(d - 1)) * 2 + (i & (d - 1)), b = a + d;
-          const u64 x = s.list[a], y = s.list[b];
-          if ((x < y) == ((a & run) == 0)) s.list[a] = y, s.list[b] = x;
+          const u64 x = s.sorted[a], y = s.sorted[b];
+          if ((x < y) == ((a & run) == 0)) s.sorted[a] = y, s.sorted[b] = x;
         }
         __syncthreads();
       }
@@ -563,78 +571,101 @@ struct Picker {
   template <class Read>
   __device__ u64 border(bool by_mass, u64 target, int bin, u64 base, u64 base_mass, Read read) {
     const int t = threadIdx.x;
-    u64 lo = 0, hi = ~0ull;
-    auto in = [&](float x, u64 key) { return key >= lo && key <= hi && scale.bin(x) == bin; };
-    for (int turn = 0; turn < 16; ++turn) {
-      // what is in question, into the list; and the largest of ~key and of key
-      u64 a = 0, b = 0;
-      __syncthreads();
-      if (t == 0) s.n_list = 0;
-      __syncthreads();
-      read([&](float x, int e) {
-        const u64 key = key_of(x, e);
-        if (!in(x, key)) return;
-        a = max(a, ~key), b = max(b, key);
-        const int at = atomicAdd(&s.n_list, 1);
-        if (at < kList) s.list[at] = key;
-      });
-      __syncthreads();
-      if (s.n_list <= kList) break;
-      // too many: cut the range of their keys in parts
+    u64 lo = 0, hi = ~0ull;   // keys in question
+    unsigned left = 0;
+    // cuts their range in parts, of the tokens that `all` goes through, and keeps the one in which the sum reaches target
+    auto cut = [&](u64 a, u64 b, auto all) {  // the largest of ~key and of key among the thread's
       lo = ~block_max(a, s.room), hi = block_max(b, s.room);
       int shift = 0;
       while (((hi - lo) >> shift) >= kBins) ++shift;
       __syncthreads();
       s.bin_n[t] = s.bin_lo[t] = s.bin_hi[t] = 0;
       __syncthreads();
-      read([&](float x, int e) {
-        const u64 key = key_of(x, e);
-        if (in(x, key)) count((int)((hi - key) >> shift), scale.share(x));
+      all([&](u64 key) {
+        if (key >= lo && key <= hi) count((int)((hi - key) >> shift), scale.share(x_of(key)));
       });
       __syncthreads();
       const unsigned mine_n = s.bin_n[t];
       const u64 mine_w = ((u64)s.bin_hi[t] << 32 | s.bin_lo[t]) * mass_of_bin(bin);
       const u64 before_n = block_before<u64>(mine_n, s.room), before_w = block_before<u64>(mine_w, s.room);
-      if (t == 0) s.at = -1;
+      // the last part that has any if none reaches it: fewer tokens than asked for
+      if (t == 0) s.at = 0;
+      __syncthreads();
+      if (mine_n) atomicMax(&s.at, t);
+      __syncthreads();
+      const int last = s.at;
       __syncthreads();
       const u64 before = base + (by_mass ? before_w : before_n), mine = by_mass ? mine_w : mine_n;
-      if (before < target && before + mine >= target) s.at = t, s.base_mass = base_mass + before_w, s.base_count = (unsigned)before_n;
+      if (before < target && (before + mine >= target || t == last) && t <= last)
+        s.at = t, s.base_mass = base_mass + before_w, s.base_count = (unsigned)before_n, s.border_mass = mine_n;
       __syncthreads();
-      if (s.at < 0) break;  // no token reaches it: cannot be, as the sums are of the same whole numbers
       base = by_mass ? s.base_mass : base + s.base_count, base_mass = s.base_mass;
+      left = (unsigned)s.border_mass;
       hi -= (u64)s.at << shift;
       const u64 least = hi - ((1ull << shift) - 1);
       if (least > lo && least <= hi) lo = least;
+      __syncthreads();
+    };
+    for (int turn = 0; turn < 16; ++turn) {
+      // into the list
+      u64 a = 0, b = 0;
+      __syncthreads();
+      if (t == 0) s.n_list = 0;
+      __syncthreads();
+      read([&](float x, int e) {
+        const u64 key = key_of(x, e);
+        if (key < lo || key > hi || scale.bin(x) != bin) return;
+        a = max(a, ~key), b = max(b, key);
+        const int at = atomicAdd(&s.n_list, 1);
+        if (at < kList) s.list[at] = key;
+      });
+      __syncthreads();
+      left = (unsigned)s.n_list;
+      if (left <= kList) break;
+      cut(a, b, [&](auto f) {
+        read([&](float x, int e) {
+          if (scale.bin(x) == bin) f(key_of(x, e));
+        });
+      });
     }
-    const int m = min(s.n_list, kList);
+    // in the list
+    const int n = min(s.n_list, kList);
+    for (int turn = 0; left > kShort && turn < 16; ++turn) {
+      u64 a = 0, b = 0;
+      for (int i = t; i < n; i += kRowThreads) {
+        const u64 key = s.list[i];
+        if (key >= lo && key <= hi) a = max(a, ~key), b = max(b, key);
+      }
+      cut(a, b, [&](auto f) {
+        for (int i = t; i < n; i += kRowThreads) f(s.list[i]);
+      });
+    }
+    // in order
+    __syncthreads();
+    if (t == 0) s.n_list = 0;
+    __syncthreads();
+    for (int i = t; i < n; i += kRowThreads) {
+      const u64 key = s.list[i];
+      if (key < lo || key > hi) continue;
+      const int at = atomicAdd(&s.n_list, 1);
+      if (at < kShort) s.sorted[at] = key;
+    }
+    __syncthreads();
+    const int m = min(s.n_list, kShort);
     sort(m);
     return along(m, by_mass, target, base, base_mass);
   }
 
-  // The same over the sorted list alone.
+  // The same over the sorted tokens alone.
   __device__ u64 along(int m, bool by_mass, u64 target, u64 base, u64 base_mass) {
-    constexpr int kMine = kList / kRowThreads;
     const int t = threadIdx.x;
-    u64 part[kMine], sum = 0;
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int i = t * kMine + j;
-      part[j] = i < m ? mass(x_of(s.list[i])) : 0;
-      sum += part[j];
-    }
-    u64 w = base_mass + block_before<u64>(sum, s.room);
+    const u64 mine = t < m ? mass(x_of(s.sorted[t])) : 0, w = base_mass + block_before<u64>(mine, s.room);
     if (t == 0) s.last = m, s.border_mass = 0;
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int i = t * kMine + j;
-      const u64 before = by_mass ? w : base + i;
-      w += part[j];
-      const u64 after = by_mass ? w : base + i + 1;
-      if (i < m && ((before < target && after >= target) || (i == m - 1 && after < target))) s.last = i + 1, s.border_mass = w;
-    }
+    const u64 before = by_mass ? w : base + t, after = by_mass ? w + mine : base + t + 1;
+    if (t < m && before < target && (after >= target || t == m - 1)) s.last = t + 1, s.border_mass = w + mine;
     __syncthreads();
-    return s.last > 0 ? s.list[s.last - 1] : 0;
+    return s.last > 0 ? s.sorted[s.last - 1] : 0;
   }
 };
 
@@ -725,7 +756,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
         if (pick.p < 1.f) add(1, sum_w);
       } else {
         scale.begin_at_top();
-        again.each(-INFINITY, [&](float x, int) {
+        again.each(-INFINITY, INFINITY, [&](float x, int) {
           unsigned share;
           const int b = scale.bin(x, &share);
           a.count(b, share);
@@ -810,12 +841,15 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
       }
       best = block_max(best, s.room_n);
       unsure = block_max(unsure, s.room_n);
-      const float near = near_score(best);
-      found = best > -INFINITY && unsure < near && list_segments([&](const Segment& g) { return score_of(g) >= near; });
+      // where no winner is left, all that are left race: in the segments whose first token is
+      const bool none = resolved && best == -INFINITY;
+      const float near = none ? -INFINITY : near_score(best);
+      found = none ? list_segments([&](const Segment& g) { return g.top && left(x_of(g.top), g.top) > 0; })
+                   : best > -INFINITY && unsure < near && list_segments([&](const Segment& g) { return score_of(g) >= near; });
       if (found) {
         again.segments(s.again, s.n_again, s.slot, noise, [&](float x, int e, float z) {
           const float f = scale.score(x, z);
-          if (f < near) return;
+          if (f < near || f == -INFINITY) return;
           const int l = left(x, key_of(x, e));
           if (l < 0) s.unsure = 1;
           if (l <= 0) return;
@@ -840,14 +874,17 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
         if (t == bin) s.base_count = n_before, s.base_mass = mass_before;
         __syncthreads();
         const u64 m0 = s.base_mass, base = by_mass ? m0 : s.base_count;
-        // no token of the bin is below this: bin + 1 bins further down than the first token, but for roundings
-        const float down = (float)(bin + 2) / kBinsPerUnit * scale.T, least = scale.top < INFINITY ? scale.top - (down + fabsf(scale.top) * 0x1p-20f) : -INFINITY;
+        // the bin's tokens are between these: bin - 1 and bin + 1 bins further down than the first token, but for roundings
+        const float step = scale.T / kBinsPerUnit, slack = fabsf(scale.top) * 0x1p-20f;
+        const bool finite = scale.top < INFINITY;
+        const float least = finite && bin < kBins - 1 ? scale.top - ((float)(bin + 2) * step + slack) : -INFINITY;
+        const float most = finite && bin > 2 ? scale.top - ((float)(bin - 2) * step - slack) : INFINITY;
         const bool few = list_segments([&](const Segment& g) { return g.top && scale.bin(x_of(g.top)) <= bin; });
         return a.border(by_mass, target, bin, base, m0, [&](auto f) {
           if (few)
             again.segments(s.again, s.n_again, s.slot, nullptr, [&](float x, int e, float) { f(x, e); });
           else
-            again.each(bin < kBins - 1 ? least : -INFINITY, f);
+            again.each(least, most, f);
         });
       };
       u64 of = total;
@@ -862,15 +899,15 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
       resolved = true;
     }
     if (!found) {
-      // no segment's winner is left: the race of all that are
+      // more than there is room for: the race of all that are left
       float fast = -INFINITY;
       const float least = border ? x_of(border) : -INFINITY;
-      again.each(least, [&](float x, int e) {
+      again.each(least, INFINITY, [&](float x, int e) {
         if (left(x, key_of(x, e)) > 0) fast = fmaxf(fast, scale.score(x, noise[e]));
       });
       const float near = near_score(block_max(fast, s.room_n));
       const bool any = fast > -INFINITY && fast >= near;
-      again.each(least, [&](float x, int e) {
+      again.each(least, INFINITY, [&](float x, int e) {
         if (any && left(x, key_of(x, e)) > 0 && scale.score(x, noise[e]) >= near) take(x, e);
       });
     }
