@@ -69,7 +69,9 @@ def test_replay_with_everything(capsys):
     assert M.main(["--recipe", "1", "--traces", "1", "--queries", "30", "--replay", "6", "--steps", "60", "--rope", "10000",
                    "--vocab", "32000"]) == 0
     out = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
-    assert out["steps"] > 30 and out["rope"] == 10000 and out["vocab"] == 32000 and out["us_per_step"] > 0
+    assert out["steps"] > 30 and out["rope"] == 10000 and out["vocab"] == 32000
+    # (the fit's constant part alone may have either sign over so few contexts)
+    assert out["mean_decode_us"] > 0 and out["prompt_us_per_token"] > 0
 
 
 def test_the_command_hands_its_options_on(monkeypatch, capsys):
