@@ -656,11 +656,12 @@ struct Picker {
     return along(m, by_mass, target, base, base_mass);
   }
 
-  // The same over the sorted tokens alone.
+  // The same over the sorted tokens alone.  Without any (a row that has fewer tokens than asked for and none in its last bin), all before
+  // them are left, with their mass.
   __device__ u64 along(int m, bool by_mass, u64 target, u64 base, u64 base_mass) {
     const int t = threadIdx.x;
     const u64 mine = t < m ? mass(x_of(s.sorted[t])) : 0, w = base_mass + block_before<u64>(mine, s.room);
-    if (t == 0) s.last = m, s.border_mass = 0;
+    if (t == 0) s.last = m, s.border_mass = base_mass;
     __syncthreads();
     const u64 before = by_mass ? w : base + t, after = by_mass ? w + mine : base + t + 1;
     if (t < m && before < target && (after >= target || t == m - 1)) s.last = t + 1, s.border_mass = w + mine;

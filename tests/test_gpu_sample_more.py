@@ -1,0 +1,89 @@
+"""Sampling on the GPU where filters meet: calls whose rows leave fewer tokens than they ask for, against the plain
+64-bit implementation."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_05286_gb300 import build as B_
+from paper_2505_05286_gb300 import logits as L
+from tests import step_cases as P
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    B_.build()
+
+
+def _cuda(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+# A weight within its bin is rounded to 2^-18 of that of the bin's middle, so by 2^-19, and is at least exp(-1/32) of it: 2^-18.95 of the
+# weight; its series and its bin's factor are off by 2^-22 together.  The sum up to the border and the sum that top_p is of: twice that,
+# below 2^-17 of top_p.
+SHARE = 2.0 ** -17
+
+
+def _check(x, noise, T, k, p, allowed=None):
+    """Rows of x [n, V] with numbers T, k, p for each; allowed [n, V]: the mask's tokens."""
+    n, V = x.shape
+    rules, z = None, x
+    if allowed is not None:
+        words = (V + 31) // 32
+        bits = np.zeros((n, words * 32), bool)
+        bits[:, :V] = allowed
+        w = (bits.reshape(n, words, 32) * (1 << np.arange(32, dtype=np.int64))).sum(-1).astype(np.uint32).view(np.int32)
+        rules, z = L.Rules(mask=_cuda(w)), np.where(allowed, x, -np.inf)
+    token, logprob = L.sample(_cuda(x), _cuda(noise), temperature=_cuda(T), top_k=_cuda(k), top_p=_cuda(p), rules=rules)
+    token, logprob = token.cpu().numpy(), logprob.cpu().numpy()
+    wrong = []
+    for r in range(n):
+        args = z[r], noise[r], float(T[r]), int(k[r])
+        if P.sample_plain(*args, float(p[r]), 0.0)[0] == token[r]:
+            continue
+        if token[r] not in [P.sample_plain(*args, float(p[r]) * (1 + d), 0.0)[0] for d in (-SHARE, SHARE)]:
+            wrong.append(r)
+    assert not wrong, (len(wrong), n, wrong[:5], token[wrong[:5]], k[wrong[:5]], p[wrong[:5]])
+    for r in range(0, n, 7):
+        t, lp, tol = P.sample_plain(z[r], noise[r], float(T[r]), int(k[r]), float(p[r]), 0.0)
+        assert token[r] != t or abs(logprob[r] - lp) <= tol
+
+
+def _rows(rng, n, V, k):
+    x = (3 * rng.standard_normal((n, V))).astype(np.float32)
+    noise = rng.exponential(size=(n, V)).astype(np.float32)
+    return (x, noise, rng.choice([0.5, 1.0, 1.5], n).astype(np.float32), np.full(n, k, np.int32) if np.isscalar(k) else k,
+            rng.uniform(0.3, 0.95, n).astype(np.float32))
+
+
+@pytest.mark.parametrize("V", [3, 8, 12, 40, 100])
+@pytest.mark.parametrize("more", [0, 1, 38, 5000])
+def test_top_k_above_a_small_vocabulary_with_top_p(V, more):
+    """top_k of all tokens or more leaves them all, whatever top_p does then."""
+    rng = np.random.default_rng(V + more)
+    _check(*_rows(rng, 600, V, V + more))
+
+
+@pytest.mark.parametrize("V", [50, 5003, 40000])
+def test_top_k_above_what_a_mask_leaves_with_top_p(V):
+    """Grammar masks that allow 1 to 40 tokens, top_k below and above that."""
+    rng = np.random.default_rng(V)
+    n = 1500 if V < 10000 else 300
+    allowed = np.zeros((n, V), bool)
+    for r in range(n):
+        allowed[r, rng.choice(V, int(rng.integers(1, 41)), replace=False)] = True
+    k = rng.choice([1, 5, 20, 50, 50, 200, V + 9], n).astype(np.int32)
+    _check(*_rows(rng, n, V, k), allowed=allowed)
+
+
+def test_top_k_above_what_is_left_where_the_last_bin_is_not_empty():
+    """Some tokens so far down that a filter's bins hold them no more: with and without a token there, the sums are the same."""
+    rng = np.random.default_rng(1)
+    x, noise, T, k, p = _rows(rng, 900, 30, 64)
+    x[::2, ::5] -= 200
+    x[::3, 7] = -math.inf
+    _check(x, noise, T, k, p)
