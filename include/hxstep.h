@@ -105,7 +105,7 @@ int hx_adjust(const hx_logits* x, const hx_rules* r, void* out, int64_t out_stri
 /* How a row's token is picked from its adjusted logits x.  For each parameter an array by row, or NULL
  * and one value for all rows. */
 typedef struct hx_pick {
-  const float* noise;         /* [n_rows][noise_stride] random numbers > 0 of the exponential distribution; NULL: the likeliest token */
+  const float* noise;         /* [n_rows][noise_stride] random numbers > 0 of the exponential distribution; NULL: the likeliest token, T holds for its logprob */
   int64_t noise_stride;       /* >= n_vocab */
   const float* temperature;   /* T; not above 0: the likeliest token is picked */
   const int32_t* top_k;       /* above 0: only the k likeliest */

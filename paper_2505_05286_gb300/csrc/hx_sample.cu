@@ -51,7 +51,9 @@ static_assert(kShort <= kRowThreads, "tokens of a short list by threads");
 struct Pick {
   int k;
   float T, p, m;
-  __device__ bool by_order() const { return T > 0.f && (k > 0 || p < 1.f); }
+  // A race and its filters; T alone is also what the log-probability is at.
+  __device__ bool race(const hx_pick& from) const { return from.noise && T > 0.f; }
+  __device__ bool by_order() const { return k > 0 || p < 1.f; }
 };
 
 // What a warp leaves of its segment.
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(kRowThreads, kWords ? 2 : 3) hx_sample_scan(co
   const int t = threadIdx.x, lane = t % 32, warp = t / 32;
   Pick pick;
   pick.k = p.top_k ? p.top_k[row] : p.all_top_k;
-  pick.T = !p.noise ? 0.f : p.temperature ? p.temperature[row] : p.all_temperature;
+  pick.T = p.temperature ? p.temperature[row] : p.all_temperature;
   pick.p = p.top_p ? p.top_p[row] : p.all_top_p;
   pick.m = p.min_p ? p.min_p[row] : p.all_min_p;
   if (t == 0) {
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(kRowThreads, kWords ? 2 : 3) hx_sample_scan(co
   }
   bin_n[t] = bin_w[t] = 0;
   const R from(in, row);
-  if (pick.T > 0.f) {
+  if (pick.race(p)) {
     // the noise is asked for now and read when the logits are done: a line for each of some threads
     const int e = p0 - from.shift + 32 * t;
     if (t < kStretch / 32 && (unsigned)e < (unsigned)in.n_vocab)
@@ -304,7 +306,7 @@ __global__ void __launch_bounds__(kRowThreads, kWords ? 2 : 3) hx_sample_scan(co
       for (int i = 0; i < kEach; ++i)
         if (x[i] == x[i]) x[i] = x[i] == INFINITY ? 0.f : -INFINITY;
     }
-    const bool race = pick.T > 0.f;
+    const bool race = pick.race(p);
     const float* noise = p.noise + row * p.noise_stride - from.shift + p0;  // by place
     const int first_token = p0 + warp * kSegment - from.shift;
     const bool plain = ((uintptr_t)noise & 15) == 0 && first_token >= 0 && first_token + kSegment <= in.n_vocab;
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(kRowThreads, kWords ? 2 : 3) hx_sample_scan(co
   if (lane == 0) warp_top[warp] = order(top);
   __syncthreads();
   pick = s_pick;  // for all threads the same, whatever becomes of the parameters meanwhile: there are barriers behind
-  if (pick.by_order()) {
+  if (pick.race(p) && pick.by_order()) {
     const Scale scale(unorder(__reduce_max_sync(~0u, warp_top[lane % kWarps])), pick.T);
     const bool fine = scale.fine(), by_k = pick.k > 0, by_p = pick.p < 1.f;
     if (fine && top < INFINITY) {
@@ -713,7 +715,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
   int token = token_of(top);
   float token_x = scale.top;
   const float* noise = p.noise + row * p.noise_stride;
-  if (top && pick.T > 0.f) {
+  if (top && pick.race(p)) {
     RowAgain<T, kWords> again = {RowOf<T>(in, row), RowRules(r, row), word, blocks};
     Picker<RowAgain<T, kWords>> a{s, scale, again, 1.f};
     const float log_least = !(pick.m > 0.f) ? -INFINITY : pick.m < 1.f ? log2f(pick.m) : pick.m > 1.f ? INFINITY : 0.f;

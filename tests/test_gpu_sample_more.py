@@ -87,3 +87,31 @@ def test_top_k_above_what_is_left_where_the_last_bin_is_not_empty():
     x[::2, ::5] -= 200
     x[::3, 7] = -math.inf
     _check(x, noise, T, k, p)
+
+
+# ---------------------------------------------------------------- without a race
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("V", [1, 40, 9000, 50021])
+def test_without_noise_the_share_is_at_the_row_s_temperature(dtype, V):
+    """No noise picks the likeliest token; its log-probability is of exp(x / T) all the same, by number or by row, with filters
+    that it passes anyway, with rules and without."""
+    rng = np.random.default_rng(V)
+    n = 8
+    x = torch.from_numpy((3 * rng.standard_normal((n, V))).astype(np.float32)).to(dtype)
+    T = np.array([0.3, 2.0, 1.0, 0.0, -1.0, math.nan, 0.01, 50.0], np.float32)
+    rules = P.random_rules(rng, n, V, history=50, bias=4, mask=0.6)
+    for r in (None, rules):
+        z = x.float().numpy() if r is None else P.adjust_plain(x.float().numpy(), r, np.float32)[0]
+        on_gpu = None if r is None else P.rules_on_gpu(r)
+        for kw in ({}, dict(top_k=3), dict(top_p=0.5, min_p=0.1)):
+            results = [L.sample(x.cuda(), temperature=_cuda(T), rules=on_gpu, **kw)]
+            if r is None:
+                for t in T:
+                    token, logprob = L.sample(x.cuda(), temperature=float(t), **kw)
+                    results.append((token, logprob, float(t)))
+            for token, logprob, *t in results:
+                for i in range(n):
+                    want, lp, tol = P.sample_plain(z[i], None, t[0] if t else float(T[i]), 0, 1.0, 0.0)
+                    got = float(logprob[i])
+                    assert int(token[i]) == want and (got == lp or abs(got - lp) <= tol), (i, got, lp, tol)
