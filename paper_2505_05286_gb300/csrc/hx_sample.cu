@@ -163,10 +163,11 @@ __device__ float log2_fast(float x) {
   return y;
 }
 
-// Scores in 32 bits, in units of log 2.  Those near the largest are off by less than a third of this difference: four roundings of
-// a difference of logits over T, which is at most the score and the logarithm of a 32-bit number (128), the logarithm's,
-// and the five bits that a number takes the place of in the scan (2^-18).
-__device__ float near_score(float best) { return best - (3e-4f + fabsf(best) * 0x1p-16f); }
+// Scores in 32 bits, in units of log 2.  One near the largest, s, is off by less than half of this difference: a difference of logits over T, which
+// is at most |s| and the logarithm of a number of 2^-126 (126), is rounded four times (2^-22 of it, 6e-5 with |s| up to 128), the logarithm is
+// off by 2^-22 of 126 (3e-5), their sum is rounded (8e-6), and the scan puts a number in the place of five bits of a segment's
+// score, which is up to 126 however small s is: 31 * 2^-17 = 2.4e-4, or 2^-18 of a larger one.
+__device__ float near_score(float best) { return best - (1e-3f + fabsf(best) * 0x1p-16f); }
 
 // x / T below that of the row's (or segment's) first token.
 struct Scale {

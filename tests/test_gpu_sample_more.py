@@ -115,3 +115,44 @@ def test_without_noise_the_share_is_at_the_row_s_temperature(dtype, V):
                     want, lp, tol = P.sample_plain(z[i], None, t[0] if t else float(T[i]), 0, 1.0, 0.0)
                     got = float(logprob[i])
                     assert int(token[i]) == want and (got == lp or abs(got - lp) <= tol), (i, got, lp, tol)
+
+
+# ---------------------------------------------------------------- far scores
+
+def _scored(rng, n):
+    """Rows of two segments far below the first token, whose tokens' noise makes up for it: token A wins by 1e-6 to 4e-5 of log 2.
+    (rows, noise, A's place, B's place)"""
+    V, log2 = 4 * 512, math.log(2)
+    x = np.full((n, V), -400.0, np.float32)
+    e = np.ones((n, V), np.float32)
+    x[:, 0], e[:, 0] = 0.0, 2.0 ** 20
+    a, b = 512 + 4 * rng.integers(0, 32, n), 1024 + 384 + 4 * rng.integers(0, 32, n) + 3  # the first and last of a thread's logits
+    i, ulp = np.arange(n), 2.0 ** -17  # of numbers from 64 to 128
+    for r in range(n):
+        far = rng.uniform(70, 120)
+        x[r, a[r]] = -far * log2
+        # the scores within their segments, which are -log2 of the noise: A's last five bits about 31, B's about 0
+        fa = (np.floor(rng.uniform(far - 1, far + 1) / ulp / 32) * 32 + rng.choice([28, 29, 30, 31])) * ulp
+        e[r, a[r]] = 2.0 ** -fa
+        want = float(x[r, a[r]]) / log2 - math.log2(float(e[r, a[r]])) - rng.uniform(1e-6, 4e-5)  # B's score
+        fb = (np.floor(fa / ulp / 32) * 32 + 32 * rng.integers(-3, 4) + rng.choice([0, 1, 2])) * ulp
+        x[r, b[r]] = (want - fb) * log2
+        e[r, b[r]] = 2.0 ** -(want - float(x[r, b[r]]) / log2)
+    return x, e, a, b
+
+
+def test_scores_of_far_segments_with_tiny_noise():
+    """Noise down to 2^-121: what a segment's winner scores is large beside what is left of it below the first token, and so
+    are its roundings."""
+    n = 4000
+    x, e, a, b = _scored(np.random.default_rng(12), n)
+    i = np.arange(n)
+    score = lambda at: x[i, at].astype(np.float64) - np.log(e[i, at].astype(np.float64))
+    assert (np.abs(score(a) - score(b)) < 1e-4).all() and (np.maximum(score(a), score(b)) > -2).all()
+    want = np.where(score(a) > score(b), a, b)  # (equal ones would go to the lower, which is a)
+    want = np.where(score(a) == score(b), a, want)
+    one = np.float32(1)
+    for T in (1.0, 0.5):
+        token, _ = L.sample(_cuda(x * one * np.float32(T)), _cuda(e), temperature=T)
+        wrong = np.flatnonzero(token.cpu().numpy() != want)
+        assert not len(wrong), (len(wrong), T)
