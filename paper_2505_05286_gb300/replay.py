@@ -97,8 +97,10 @@ class Batch:
             self.rules = L.Rules(history=self.history, length=self.lengths[0], prompt_len=self.lengths[1], repetition=full(1.1),
                                  presence=full(0.1), frequency=full(0.05))
 
-    def run(self, add: np.ndarray):
-        """One step: row r gets add[r] tokens (0: none, -1: it has ended).  Returns the start and end events."""
+    def run(self, add: np.ndarray, read: Optional[np.ndarray] = None):
+        """One step: row r gets add[r] tokens (0: none, -1: it has ended), of which the first read[r] are of its prompt, the others were
+        written.  Without read: more than one token, and a request's first ones, are its prompt's.  Returns the start
+        and end events."""
         s = self.shape
         tok = np.maximum(add, 0)
         n = int(tok.sum())
@@ -107,7 +109,9 @@ class Batch:
         both = torch.from_numpy(np.stack([self.held, add]).astype(np.int32)).cuda()
         x = self.qkv[:n]
         if s.vocab:
-            self.prompt = np.where((add < 0) | (self.held == 0), 0, self.prompt) + np.where((tok > 1) | (self.held == 0), tok, 0)
+            if read is None:
+                read = np.where((tok > 1) | (self.held == 0), tok, 0)
+            self.prompt = np.where((add < 0) | (self.held == 0), 0, self.prompt) + np.minimum(read, tok)
             self.lengths.copy_(torch.from_numpy(np.stack([self.held + tok, self.prompt]).astype(np.int32)))
         begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         self.flush.zero_()
@@ -166,7 +170,7 @@ def replay(trace, records: dict, cluster, instance: int, shape: Optional[Shape] 
     steps: List[_Step] = []
     waiting.reverse()
     while len(steps) < max_steps + warmup:
-        add = np.zeros(slots, np.int32)
+        add, read = np.zeros(slots, np.int32), np.zeros(slots, np.int32)
         for r in range(slots):
             if rows[r] is None and waiting:
                 rows[r] = waiting.pop()
@@ -174,7 +178,7 @@ def replay(trace, records: dict, cluster, instance: int, shape: Optional[Shape] 
             if c is None:
                 continue
             if c.read < c.prompt:
-                add[r] = min(chunk, c.prompt - c.read)
+                add[r] = read[r] = min(chunk, c.prompt - c.read)
                 c.read += int(add[r])
             elif c.written < c.out:
                 add[r] = 1
@@ -185,7 +189,7 @@ def replay(trace, records: dict, cluster, instance: int, shape: Optional[Shape] 
         if not add.any():
             break
         context = int(np.maximum(batch.held, 0).sum() + np.maximum(add, 0).sum())
-        events = batch.run(add)
+        events = batch.run(add, read)
         steps.append(_Step(int(np.maximum(add, 0).sum()), context, bool((add <= 1).all()) and bool((add == 1).any()), events))
     torch.cuda.synchronize()
     steps = steps[warmup if len(steps) > 2 * warmup else 0:][-max_steps:]
