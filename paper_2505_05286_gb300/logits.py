@@ -17,7 +17,7 @@ import torch
 
 from . import hxsim as H
 from . import kvcache as KV
-from .kvcache import _count, _dense, _fail, _on, _want
+from .kvcache import _dense, _fail, _on, _want
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
@@ -195,7 +195,7 @@ def sample(logits, noise=None, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0
                  strided; None: the likeliest token of every row
     temperature, top_p, min_p   float32 [rows] or a number
     top_k        int32 [rows] or a number
-                 (temperature 0: the likeliest token; top_k 0, top_p 1, min_p 0: no tokens left out)
+                 (temperature 0 or below: the likeliest token; top_k 0 or below, top_p 1, min_p 0: no tokens left out)
     rules        how the logits are adjusted before
     out          (token int32 [rows], logprob float32 [rows]) to write to
 
@@ -220,8 +220,8 @@ def sample(logits, noise=None, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0
                 _fail(f"sample: {name} must have one entry per row")
             setattr(p, name, x.data_ptr())
         else:
-            if kind == torch.int32:
-                _count(x, "sample: " + name)
+            if kind == torch.int32 and (not -1 << 31 <= x < 1 << 31 or x != int(x)):
+                _fail(f"sample: {name} must be a whole number of 32 bits")
             setattr(p, "all_" + name, int(x) if kind == torch.int32 else float(x))
     lib = load()
     with _on(dev, stream) as handle:

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2505_05286_gb300 import build as B_
+from paper_2505_05286_gb300 import hxsim as H
 from paper_2505_05286_gb300 import logits as L
 from tests import step_cases as P
 
@@ -156,3 +157,18 @@ def test_scores_of_far_segments_with_tiny_noise():
         token, _ = L.sample(_cuda(x * one * np.float32(T)), _cuda(e), temperature=T)
         wrong = np.flatnonzero(token.cpu().numpy() != want)
         assert not len(wrong), (len(wrong), T)
+
+
+def test_top_k_as_a_number_means_what_it_means_by_row():
+    """Numbers below 0 leave none out, those that are not whole or do not fit are refused."""
+    rng = np.random.default_rng(4)
+    n, V = 64, 300
+    x, e = _cuda((3 * rng.standard_normal((n, V))).astype(np.float32)), _cuda(rng.exponential(size=(n, V)).astype(np.float32))
+    for k in (-1, -2 ** 31, 0, 7, 7.0, np.int64(7), 2 ** 31 - 1):
+        a = L.sample(x, e, top_k=k, top_p=0.9)
+        b = L.sample(x, e, top_k=torch.full((n,), int(k), dtype=torch.int32, device="cuda"), top_p=0.9)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    for k in (2.7, 0.5, -1.5, math.nan, math.inf, 2 ** 31, -2 ** 31 - 1):
+        with pytest.raises(H.HxError) as err:
+            L.sample(x, e, top_k=k)
+        assert err.value.code == H.HX_ERR_INVALID and "top_k" in str(err.value)
