@@ -118,6 +118,8 @@ class Rules:
             _want(mask, "mask", i32, 2, self.device)
             if mask.shape[1] > 1 and mask.stride(1) != 1:
                 _fail("rules: a mask's words must be contiguous")
+            if mask.shape[0] and not mask.shape[1]:  # its address would say that there is none
+                _fail("rules: a mask has no words")
             if mask_row is None:
                 self._rows(mask.shape[0], "mask")
         p = lambda x: None if x is None else x.data_ptr()
