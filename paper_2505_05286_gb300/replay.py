@@ -189,7 +189,8 @@ def replay(trace, records: dict, cluster, instance: int, shape: Optional[Shape] 
         if not add.any():
             break
         context = int(np.maximum(batch.held, 0).sum() + np.maximum(add, 0).sum())
-        events = batch.run(add, read)
+        # which tokens are prompts' is of matter to those that are drawn
+        events = batch.run(add, read) if shape.vocab else batch.run(add)
         steps.append(_Step(int(np.maximum(add, 0).sum()), context, bool((add <= 1).all()) and bool((add == 1).any()), events))
     torch.cuda.synchronize()
     steps = steps[warmup if len(steps) > 2 * warmup else 0:][-max_steps:]

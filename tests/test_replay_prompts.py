@@ -36,7 +36,7 @@ def test_a_step_s_tokens_are_told_apart(monkeypatch, chunk):
 
     monkeypatch.setattr(R, "Batch", Fake)
     monkeypatch.setattr(torch.cuda, "synchronize", lambda: None)
-    R.replay(*_calls(), instance=0, chunk=chunk, max_steps=10000, warmup=0)
+    R.replay(*_calls(), instance=0, shape=R.Shape(vocab=300), chunk=chunk, max_steps=10000, warmup=0)
     totals, now = [], [[0, 0] for _ in range(3)]
     for add, read in seen:
         for r in range(3):
