@@ -46,7 +46,8 @@ typedef struct hx_rotate_args {
   int32_t rotary_dim;         /* even, 2..head_dim */
   int32_t dtype;              /* HX_BF16, HX_F16 or HX_F32 */
   int32_t interleaved;        /* 0 or 1 */
-  int32_t inverse;            /* 1: turned back (with scale 1 also the gradient's way) */
+  int32_t inverse;            /* 1: turned the other way and multiplied by scale all the same: the gradient's way, and the way back
+                                 where scale is 1 or -1 */
   float scale;                /* finite */
   int32_t n_rows;             /* 1..HX_KV_MAX_ROWS; 0 with positions */
   const uint64_t* turns;      /* [rotary_dim / 2] turns a position, in units of 2^-64 */

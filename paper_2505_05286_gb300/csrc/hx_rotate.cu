@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) * V == 16 ? 8 : 4) hx_rota
     }
   };
   if constexpr (at_once(sizeof(P)) == 1) {
-    const int units = half / V, lanes = kThreads / units, u = threadIdx.x % units, first = threadIdx.x / units;  // half / V <= 64
+    const int units = half / V, lanes = kThreads / units, u = threadIdx.x % units, first = threadIdx.x / units;  // half / V <= 128
     const int at = kInterleaved ? 2 * u * V : u * V;
     for (int r = first < lanes ? first : n * H; r < n * H; r += lanes) {
       const int tok = r / H, h = r - tok * H;

@@ -301,10 +301,10 @@ class Rope:
                    new outputs too, where they are then undefined
         positions  int32 [tokens] in their place
         out        (q's, k's) tensors to write to; (q, k) itself: in place
-        inverse    turn back
+        inverse    turn the other way, times the same scale: the way back where that is 1 (with scale s, s * s times what was turned)
 
-        Returns q's and k's, or q's alone where there is no k.  The gradient of what is turned is the gradient of the result,
-        turned back: no other backward pass is recorded.
+        Returns q's and k's, or q's alone where there is no k.  No backward pass is recorded: the gradient of what is turned is
+        rotate(the gradient of the result, inverse=True), at every scale.
         """
         dev = self.device
         kinds = (torch.bfloat16, torch.float16, torch.float32)
