@@ -157,11 +157,6 @@ struct RowOf {
     for (int j = 0; j < kVec; ++j) v.v[j] = (unsigned)(e + j) < (unsigned)n_vocab ? first[e + j] : from_float<T>(-INFINITY);
     return v;
   }
-  __device__ void load(int vec, float* x) const {
-    const Pack<T, kVec> v = load(vec);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) x[j] = to_float(v.v[j]);
-  }
   // Which of a load's places the row's mask allows, one bit each.
   __device__ uint32_t allowed(const uint32_t* mask, int vec) const {
     const int e = token(vec);

@@ -530,11 +530,9 @@ __device__ u64 part_of(float p, u64 all) {
   return max(up, (u64)1);
 }
 
-template <class Again>
 struct Picker {
   Shared& s;
   Scale& scale;
-  const Again& row;
   float one;               // 2^shift: weights of 1 / 2^kWeightBits of the first token's bin in whole numbers
 
   __device__ u64 mass_of_bin(int b) const { return __float2ull_rn(exp2f((float)b * (-1.44269504f / kBinsPerUnit)) * one); }
@@ -682,7 +680,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
   const int n_seg = blocks * kWarps;
   constexpr int kMine = (kMaxStretches * kWarps + kRowThreads - 1) / kRowThreads;  // segments of a thread
   if (t < kMaxStretches) s.stretch_top[t] = 0;
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched while the scan still runs
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as the scan's last blocks end
   const Pick pick = w.pick[row];
   __syncthreads();
   // add up the segments
@@ -718,7 +716,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) hx_sample_pick(const hx_logits
   const float* noise = p.noise + row * p.noise_stride;
   if (top && p.noise && pick.T > 0.f) {
     RowAgain<T, kWords> again = {RowOf<T>(in, row), RowRules(r, row), word, blocks};
-    Picker<RowAgain<T, kWords>> a{s, scale, again, 1.f};
+    Picker a{s, scale, 1.f};
     const float log_least = !(pick.m > 0.f) ? -INFINITY : pick.m < 1.f ? log2f(pick.m) : pick.m > 1.f ? INFINITY : 0.f;
     const bool by_order = pick.by_order();
     bool by_k = false, by_p = false;
