@@ -129,6 +129,7 @@ int64_t hx_sample_workspace(const hx_logits* x, const hx_rules* r, const hx_pick
  * share of all tokens' weights, before the filters (of exp(x) where T is not above 0).  Tokens with x = -infinity or NaN take no
  * part; a NaN makes the row's logprob NaN.  Where none is left, token is -1 and logprob -infinity.  A noise that is
  * not a finite number of at least 2^-126 never wins; if no token's does, the first of the order is picked.
+ * Differences of logits are formed in 32 bits and may become infinite, and T below 1.5e-30 weighs as that.
  * Weights are in 32 bits (their shares within a filter, in 2^-18 of a weight); what decides where the order ends is added up in whole
  * numbers, and scores near the largest are compared in 64 bits: the same inputs give the same token and logprob. */
 int hx_sample(const hx_logits* x, const hx_rules* r, const hx_pick* p, void* stream);

@@ -19,9 +19,10 @@
 // those of the log-probability are 32-bit sums in a fixed order, without the first token, whose
 // weight is 1: the logarithm of a share near 1 keeps its bits.
 //
-// 256 rows of 131072 logits in bf16: the likeliest tokens 36 us (of them the scan 30; reading the logits takes 10), by temperature alone
-// 58 us (3.5 TB/s: the noise is twice the logits), by top-p 82 to 152 us: the scan 60, bound by instructions (55 for a logit, 19 of them
-// for its bin), the pick 22, a chain of barriers, or up to 90 where a row has to be read again.  One row of 32000: 11.5 us.
+// 256 rows of 131072 logits in bf16: the likeliest tokens 35 us (reading the logits takes 10), by temperature alone
+// 58 us (3.5 TB/s: the noise is twice the logits), by min-p 68 us, by top-k 76 to 112 us, by top-p 82 to 153 us (median of ten inputs 128): the
+// scan 60, bound by instructions (60 for a logit, 19 of them for its bin), the pick 22, a chain of barriers, or up to 90 where
+// a row has to be read again.  One row of 32000: 11.4 us.
 #include <algorithm>
 
 #include "hx_logits.cuh"

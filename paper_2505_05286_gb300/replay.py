@@ -17,7 +17,8 @@ work, and its launches are waiting when it begins.
     rep["prompt_us_per_token"]
 
 With Shape.theta queries and keys are turned by their positions first, and with Shape.vocab each row's next token is drawn from
-logits at the end, with penalties for the tokens that its request holds.
+logits at the end, with penalties for the tokens that its request holds; the random numbers for that are written between the steps, outside
+of their time.
 
 Queries, keys, values and logits are random; a real model's products are not part of it.
 """
